@@ -404,6 +404,97 @@ int b2_model_predict_variant(int dtype, int variant, double* fraction, char* jso
  */
 int b2_model_enumerate(int dtype, int top, char* json_out, size_t cap);
 
+/*
+ * Linear layers in 8 bits.  No counterpart in the paper: its GEMM is the same sum of rank-k updates over staged
+ * panels, here with operands held as 8-bit floating-point numbers (e4m3: 4 exponent bits, 3 mantissa bits, largest
+ * finite value 448) and one scale for each block of 128 consecutive elements along the summed index.
+ *
+ * Storage is column-major with leading dimensions in ELEMENTS, as everywhere in this file.  An activation matrix is
+ * d x t: a token is one column of d contiguous features.
+ *
+ * Types of activations and results: B2_TYPE_BF16 or B2_TYPE_F32.  Types of scales: B2_SCALE_E8M0 (one byte b, the value
+ * 2^(b-127), 255 = NaN) or B2_SCALE_F32.
+ *
+ * The quantisation rule of b2_rmsnorm_f8 and b2_quant_f8, per block of values v: with a = max|v|,
+ *     s = the smallest power of two with a/s <= 448   (1 when a == 0, at least 2^-127),   q = v/s rounded to nearest even e4m3.
+ * Nothing saturates.  A block that holds a NaN or an infinity is stored as NaN throughout (scale byte 255, every q 0x7f).
+ * Division by a power of two is exact, so q*s differs from v by the one rounding to e4m3; q*s is representable in bf16.
+ */
+#define B2_TYPE_F32 1
+#define B2_TYPE_BF16 2
+#define B2_SCALE_E8M0 0
+#define B2_SCALE_F32 1
+
+/*
+ * Root-mean-square norm with the residual's addition and an 8-bit result.  For every token (column) of X, d x t:
+ *     h = x + r,   rstd = 1 / sqrt(sum_i h_i^2 / d + eps),   y_i = h_i * rstd * w_i,   (q, s) = quantised y
+ * with one scale for each 128 features of the token (the last block of a token may be shorter).  All arithmetic in fp32,
+ * from the unrounded sum x + r; h is rounded once when it is stored.
+ *   type   of X, R, w and H.
+ *   R      the residual, or NULL (then h = x and ldr is ignored).   H  where h is stored, or NULL (ldh ignored); H may be X or R.
+ *   Q, S   e4m3 numbers d x t (ldq >= d) and scale bytes ceil(d/128) x t (lds >= ceil(d/128)).   rstd  t floats, or NULL.
+ * Arguments: d 1, t 2, type 3, X 4, ldx 5, R 6, ldr 7, w 8, eps 9 (>= 0), H 10, ldh 11, Q 12, ldq 13, S 14, lds 15.
+ */
+int b2_rmsnorm_f8(int64_t d, int64_t t, int type, const void* X, int64_t ldx, const void* R, int64_t ldr, const void* w,
+                  float eps, void* H, int64_t ldh, void* Q, int64_t ldq, void* S, int64_t lds, float* rstd,
+                  void* cuda_stream);
+
+/*
+ * Its backward pass; the quantisation is passed straight through.  With xh = h * rstd and g_i = dy_i * w_i:
+ *     dx_i = rstd * (g_i - xh_i * sum_j g_j xh_j / d) + dh_i,    dw_i = sum over tokens of dy_i * xh_i
+ * dx is the gradient of x and of r alike.  DH (the gradient that reaches h from the residual stream) may be NULL.
+ * DX may be DY, DH or H.  dw is d floats, summed in an order that depends on d, t and the device only: the same bits
+ * on every call.  The workspace (device, 256-byte aligned) holds the partial sums of dw.
+ * Arguments: d 1, t 2, type 3, DY 4, lddy 5, H 6, ldh 7, rstd 8, w 9, DH 10, lddh 11, DX 12, lddx 13, dw 14.
+ */
+size_t b2_rmsnorm_backward_workspace_bytes(int64_t d, int64_t t);
+int b2_rmsnorm_backward(int64_t d, int64_t t, int type, const void* DY, int64_t lddy, const void* H, int64_t ldh,
+                        const float* rstd, const void* w, const void* DH, int64_t lddh, void* DX, int64_t lddx, float* dw,
+                        void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Quantise X (d x t) to e4m3: blocks of 128 features by `block` tokens, block 1 (activations: what b2_gemm_f8 takes as an
+ * operand with one scale per column, and what b2_wgrad_f8 reads) or 128 (weights).  S is ceil(d/128) x ceil(t/block).
+ * Arguments: d 1, t 2, block 3, type 4, X 5, ldx 6, Q 7, ldq 8, S 9, lds 10.
+ */
+int b2_quant_f8(int64_t d, int64_t t, int block, int type, const void* X, int64_t ldx, void* Q, int64_t ldq, void* S,
+                int64_t lds, void* cuda_stream);
+
+/*
+ * Matrix product of two block-scaled e4m3 matrices:
+ *     C := alpha * sum_p op(A)_ip sA(i/block_a, p/128) * op(B)_pj sB(j/block_b, p/128) + beta * C
+ * op(A) is m x k, op(B) k x n; block_a, block_b in {1, 128}; C in bf16 or fp32.  The scales are stored the way their
+ * operand is: for transa 'T' (A stored k x m) SA is ceil(k/128) x ceil(m/block_a), for 'N' ceil(m/block_a) x ceil(k/128);
+ * for transb 'N' SB is ceil(k/128) x ceil(n/block_b), for 'T' ceil(n/block_b) x ceil(k/128).  Accumulation in fp32.
+ * A linear layer y = W x with W stored row by row (k contiguous) is ('T','N'), its input gradient W^T dy is ('N','N') on
+ * the same weight and the same scales.
+ * An operand whose base is not 16-byte aligned or whose leading dimension is not a multiple of 16 is first copied to
+ * the workspace (device, 256-byte aligned); for others the workspace size is 0 and workspace may be NULL.
+ * m, n, k < 2^31 - 512, else B2_ERR_VARIANT.
+ * Arguments: transa 1, transb 2, m 3, n 4, k 5, alpha 6, A 7, lda 8, SA 9, ldsa 10, block_a 11, scale_type_a 12, B 13,
+ * ldb 14, SB 15, ldsb 16, block_b 17, scale_type_b 18, beta 19, C 20, ldc 21, type_c 22.
+ */
+size_t b2_gemm_f8_workspace_bytes(char transa, char transb, int64_t m, int64_t n, int64_t k, const void* A, int64_t lda,
+                                  const void* B, int64_t ldb);
+int b2_gemm_f8(char transa, char transb, int64_t m, int64_t n, int64_t k, float alpha, const void* A, int64_t lda,
+               const void* SA, int64_t ldsa, int block_a, int scale_type_a, const void* B, int64_t ldb, const void* SB,
+               int64_t ldsb, int block_b, int scale_type_b, float beta, void* C, int64_t ldc, int type_c, void* workspace,
+               size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The weight gradient from an activation that was kept in 8 bits (Q and S as b2_rmsnorm_f8 or b2_quant_f8 with block 1
+ * wrote them, m x k: k tokens of m features) and the gradient Y of the layer's result (bf16, n x k):
+ *     C(i,j) := alpha * sum_p Q(i,p) * S(i/128, p) * Y(j,p) + beta * C(i,j)          (C m x n, bf16 or fp32)
+ * Q*S enters the product as bf16 numbers, which hold it exactly (scales below 2^-124 excepted, whose smallest
+ * numbers are subnormal in bf16), with fp32 accumulation.
+ * An operand that is not 16-byte aligned (base and column) is first copied to the workspace, as in b2_gemm_f8.
+ * Arguments: m 1, n 2, k 3, alpha 4, Q 5, ldq 6, S 7, lds 8, Y 9, ldy 10, beta 11, C 12, ldc 13, type_c 14.
+ */
+size_t b2_wgrad_f8_workspace_bytes(int64_t m, int64_t n, int64_t k, const void* Q, int64_t ldq, const void* Y, int64_t ldy);
+int b2_wgrad_f8(int64_t m, int64_t n, int64_t k, float alpha, const void* Q, int64_t ldq, const void* S, int64_t lds,
+                const void* Y, int64_t ldy, float beta, void* C, int64_t ldc, int type_c, void* workspace,
+                size_t workspace_bytes, void* cuda_stream);
+
 /* Static, NUL-terminated text for a return value of any call above. */
 const char* b2_strerror(int status);
 /* Static, NUL-terminated library version. */

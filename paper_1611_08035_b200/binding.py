@@ -72,6 +72,21 @@ _SIGNATURES = {
     "b2_gemm_host_workspace_bytes": (c_size_t, [c_int, c_char, c_char, c_int64, c_int64, c_int64]),
     "b2_dgemm_host": (c_int, _GEMM_TAIL_D + [c_void_p, c_size_t, c_void_p]),
     "b2_sgemm_host": (c_int, _GEMM_TAIL_S + [c_void_p, c_size_t, c_void_p]),
+    "b2_rmsnorm_f8": (c_int, [c_int64, c_int64, c_int, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_float, c_void_p,
+                              c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]),
+    "b2_rmsnorm_backward_workspace_bytes": (c_size_t, [c_int64, c_int64]),
+    "b2_rmsnorm_backward": (c_int, [c_int64, c_int64, c_int, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p,
+                                    c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "b2_quant_f8": (c_int, [c_int64, c_int64, c_int, c_int, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64,
+                            c_void_p]),
+    "b2_gemm_f8_workspace_bytes": (c_size_t, [c_char, c_char, c_int64, c_int64, c_int64, c_void_p, c_int64, c_void_p,
+                                              c_int64]),
+    "b2_gemm_f8": (c_int, [c_char, c_char, c_int64, c_int64, c_int64, c_float, c_void_p, c_int64, c_void_p, c_int64, c_int,
+                           c_int, c_void_p, c_int64, c_void_p, c_int64, c_int, c_int, c_float, c_void_p, c_int64, c_int,
+                           c_void_p, c_size_t, c_void_p]),
+    "b2_wgrad_f8_workspace_bytes": (c_size_t, [c_int64, c_int64, c_int64, c_void_p, c_int64, c_void_p, c_int64]),
+    "b2_wgrad_f8": (c_int, [c_int64, c_int64, c_int64, c_float, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64,
+                            c_float, c_void_p, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
     "b2_pipe_probe": (c_int, [c_int, c_int, c_int, c_int64, c_void_p, c_size_t, ctypes.POINTER(c_double), c_void_p]),
     "b2_model_throughput": (c_double, [c_int, ctypes.POINTER(c_double), ctypes.POINTER(c_double)]),
     "b2_model_stalled_throughput": (c_double, [c_double, c_int, c_double]),
@@ -437,4 +452,107 @@ def b2_gemm_strided_batched(transa, transb, m, n, k, alpha, A, lda, stride_a, B,
             stride_c, batch, _stream())
     if check:
         _check(name, rc)
+    return rc
+
+
+# ---- linear layers in 8 bits --------------------------------------------------------------------------------
+_TYPES = {torch.float32: 1, torch.bfloat16: 2}  # B2_TYPE_*
+_SCALES = {torch.float8_e8m0fnu: 0, torch.float32: 1}  # B2_SCALE_*
+
+
+def _typed(fn: str, table: dict, t, what: str) -> int:
+    """Code of a tensor's type, which the library takes as an argument."""
+    code = table.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{fn}: {what} is {t.dtype}, not one of {', '.join(str(k) for k in table)}")
+    return code
+
+
+def _want(fn: str, *pairs) -> None:
+    for t, dtype in pairs:
+        if t is not None and (t.dtype != dtype or not t.is_cuda):
+            raise TypeError(f"{fn} takes a {dtype} CUDA tensor where it was given {t.dtype} on {t.device}")
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def b2_rmsnorm_f8(d, t, x, ldx, residual, ldr, w, eps, h, ldh, q, ldq, s, lds, rstd, check=True) -> int:
+    """h = x + residual; y = h / sqrt(mean(h^2) + eps) * w per token (column of d); y leaves as e4m3 numbers q with e8m0
+    scales s, one for 128 features.  x, residual, w, h: bfloat16 or float32 alike; residual, h and rstd (float32) may be None."""
+    fn = "b2_rmsnorm_f8"
+    code = _typed(fn, _TYPES, x, "x")
+    dt = x.dtype
+    _want(fn, (x, dt), (residual, dt), (w, dt), (h, dt), (q, torch.float8_e4m3fn), (s, torch.float8_e8m0fnu),
+          (rstd, torch.float32))
+    rc = lib().b2_rmsnorm_f8(d, t, code, x.data_ptr(), ldx, _ptr(residual), ldr, w.data_ptr(), eps, _ptr(h), ldh,
+                             q.data_ptr(), ldq, s.data_ptr(), lds, _ptr(rstd), _stream())
+    if check:
+        _check(fn, rc)
+    return rc
+
+
+def b2_rmsnorm_backward_workspace_bytes(d: int, t: int) -> int:
+    return lib().b2_rmsnorm_backward_workspace_bytes(d, t)
+
+
+def b2_rmsnorm_backward(d, t, dy, lddy, h, ldh, rstd, w, dh, lddh, dx, lddx, dw, workspace, check=True) -> int:
+    """Gradients of the norm: dx (of x and residual alike; dh, the gradient that reaches h directly, is added, or None)
+    and dw (float32, d).  dy, h, w, dh, dx: bfloat16 or float32 alike."""
+    fn = "b2_rmsnorm_backward"
+    code = _typed(fn, _TYPES, dy, "dy")
+    dt = dy.dtype
+    _want(fn, (dy, dt), (h, dt), (w, dt), (dh, dt), (dx, dt), (rstd, torch.float32), (dw, torch.float32))
+    rc = lib().b2_rmsnorm_backward(d, t, code, dy.data_ptr(), lddy, h.data_ptr(), ldh, rstd.data_ptr(), w.data_ptr(),
+                                   _ptr(dh), lddh, dx.data_ptr(), lddx, dw.data_ptr(), _ptr(workspace),
+                                   _nbytes(workspace), _stream())
+    if check:
+        _check(fn, rc)
+    return rc
+
+
+def b2_quant_f8(d, t, block, x, ldx, q, ldq, s, lds, check=True) -> int:
+    """x (d x t, bfloat16 or float32) as e4m3 numbers q with e8m0 scales s for blocks of 128 features by 1 or 128 tokens."""
+    fn = "b2_quant_f8"
+    code = _typed(fn, _TYPES, x, "x")
+    _want(fn, (x, x.dtype), (q, torch.float8_e4m3fn), (s, torch.float8_e8m0fnu))
+    rc = lib().b2_quant_f8(d, t, block, code, x.data_ptr(), ldx, q.data_ptr(), ldq, s.data_ptr(), lds, _stream())
+    if check:
+        _check(fn, rc)
+    return rc
+
+
+def b2_gemm_f8_workspace_bytes(transa, transb, m, n, k, A, lda, B, ldb) -> int:
+    return lib().b2_gemm_f8_workspace_bytes(_tr(transa), _tr(transb), m, n, k, _ptr(A), lda, _ptr(B), ldb)
+
+
+def b2_gemm_f8(transa, transb, m, n, k, alpha, A, lda, SA, ldsa, block_a, B, ldb, SB, ldsb, block_b, beta, C, ldc,
+               workspace=None, check=True) -> int:
+    """C := alpha*op(A)*op(B) + beta*C of block-scaled e4m3 matrices; scales float8_e8m0fnu or float32, C bfloat16 or float32."""
+    fn = "b2_gemm_f8"
+    code = _typed(fn, _TYPES, C, "C")
+    ca, cb = _typed(fn, _SCALES, SA, "SA"), _typed(fn, _SCALES, SB, "SB")
+    _want(fn, (A, torch.float8_e4m3fn), (B, torch.float8_e4m3fn), (SA, SA.dtype), (SB, SB.dtype), (C, C.dtype))
+    rc = lib().b2_gemm_f8(_tr(transa), _tr(transb), m, n, k, alpha, A.data_ptr(), lda, SA.data_ptr(), ldsa, block_a, ca,
+                          B.data_ptr(), ldb, SB.data_ptr(), ldsb, block_b, cb, beta, C.data_ptr(), ldc, code,
+                          _ptr(workspace), _nbytes(workspace), _stream())
+    if check:
+        _check(fn, rc)
+    return rc
+
+
+def b2_wgrad_f8_workspace_bytes(m, n, k, Q, ldq, Y, ldy) -> int:
+    return lib().b2_wgrad_f8_workspace_bytes(m, n, k, _ptr(Q), ldq, _ptr(Y), ldy)
+
+
+def b2_wgrad_f8(m, n, k, alpha, Q, ldq, S, lds, Y, ldy, beta, C, ldc, workspace=None, check=True) -> int:
+    """C (m x n) := alpha * X Y^T + beta*C over k tokens, X = Q*S an activation kept in 8 bits, Y bfloat16 gradients."""
+    fn = "b2_wgrad_f8"
+    code = _typed(fn, _TYPES, C, "C")
+    _want(fn, (Q, torch.float8_e4m3fn), (S, torch.float8_e8m0fnu), (Y, torch.bfloat16), (C, C.dtype))
+    rc = lib().b2_wgrad_f8(m, n, k, alpha, Q.data_ptr(), ldq, S.data_ptr(), lds, Y.data_ptr(), ldy, beta, C.data_ptr(),
+                           ldc, code, _ptr(workspace), _nbytes(workspace), _stream())
+    if check:
+        _check(fn, rc)
     return rc

@@ -448,6 +448,14 @@ extern "C" const char* b2_strerror(int status) {
     case -12: return "argument 12 is illegal";
     case -13: return "argument 13 is illegal";
     case -14: return "argument 14 is illegal";
+    case -15: return "argument 15 is illegal";
+    case -16: return "argument 16 is illegal";
+    case -17: return "argument 17 is illegal";
+    case -18: return "argument 18 is illegal";
+    case -19: return "argument 19 is illegal";
+    case -20: return "argument 20 is illegal";
+    case -21: return "argument 21 is illegal";
+    case -22: return "argument 22 is illegal";
     default: return status < 0 ? "illegal argument" : "unknown status";
   }
 }

@@ -1,0 +1,453 @@
+// Product of two block-scaled e4m3 matrices on the 5th-generation tensor cores.
+//
+//   C_ij = alpha * sum_b sA(i, b) sB(j, b) * ( sum_{p in block b} a_ip b_pj ) + beta * C_ij,   blocks of 128 along p
+//
+// The inner sums are exact products accumulated in fp32 in tensor memory; a stage of the shared-memory ring holds
+// exactly one block (128 bytes of e4m3), so that the factor of a stage is a number per row times a number per column.
+//
+// Roles of a CTA: warp 0 streams both operands with TMA (128-byte swizzle) into the ring, warp 1 issues tcgen05.mma,
+// the other warps read a block's sums from tensor memory (two buffers in turn) and add them, times the scales, to
+// fp32 accumulators in registers.
+//
+// The matrix whose index is contiguous in C (A, index i) is the MMA's column operand when C is large: a thread then owns
+// one j and consecutive i, and writes them with 16-byte stores; the scale of a 128 x 128 block of A is then one number
+// for all of a thread's accumulators.  For few columns (decoding: n <= 64) A gives the 128 rows and the
+// tile is as narrow as n; k is split over a cluster, whose CTAs add their shares through distributed shared memory.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+
+#include "b2gemm.h"
+#include "entry.h"
+#include "f8.cuh"
+#include "f8_out.cuh"
+#include "tcgen05.cuh"
+
+namespace b2 {
+namespace {
+
+constexpr int kRows = 128;                       // MMA rows of a tile
+constexpr uint32_t kRowStage = kRows * kF8Block;  // bytes of the row operand in a stage
+constexpr int kMaxSplit = 8;
+
+struct F8Scale {  // value for index i and block b: p[(i >> shift) * si + b * sb]
+  const void* p;
+  int64_t si, sb;
+  int shift, f32;
+};
+struct F8Args {
+  F8Out out;
+  int kb;              // blocks of 128 along the summed index
+  int splits;          // CTAs of a cluster that share a tile's blocks
+  int r_mn, c_mn;      // the operand's own index is contiguous (else the summed one)
+  int tiles_r, tiles_c, group;
+  F8Scale sr, sc;
+  int* status;
+};
+
+template <int TBN>
+struct F8Cfg {
+  static constexpr int EW = TBN >= 128 ? 8 : 4;             // warps that scale and add
+  static constexpr int COLS = TBN / (EW / 4);               // accumulators of a thread
+  static constexpr int NT = 64 + 32 * EW;
+  static constexpr uint32_t STAGE = kRowStage + TBN * kF8Block;
+  static constexpr int STAGES = TBN == 256 ? 4 : TBN == 128 ? 6 : 5;
+  static constexpr uint32_t RING = STAGE * STAGES;
+  static constexpr uint32_t TMEM = 2 * TBN < 32 ? 32 : 2 * TBN;
+  static constexpr size_t SMEM = 1024 + RING + 512 + EW * COLS * sizeof(float);
+  static_assert(kRows * TBN * 4 <= RING, "the split's shares pass through the ring");
+};
+
+__device__ __forceinline__ float f8_scale_at(const F8Scale& s, int64_t i, int b) {
+  const int64_t at = (i >> s.shift) * s.si + (int64_t)b * s.sb;
+  return s.f32 ? static_cast<const float*>(s.p)[at] : e8m0_value(static_cast<const uint8_t*>(s.p)[at]);
+}
+
+__device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Instruction descriptor: fp32 accumulator, e4m3 operands (format 0), which of them have their own index contiguous, N, M.
+__device__ __forceinline__ uint32_t umma_idesc_f8(int m, int n, int a_mn, int b_mn) {
+  return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+template <int TBN, typename TC, bool COLS_CONTIG>
+__global__ void __launch_bounds__(F8Cfg<TBN>::NT, 1)
+    f8_gemm_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
+  using Cfg = F8Cfg<TBN>;
+  constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES;
+  extern __shared__ unsigned char f8_smem_raw[];
+  const uint32_t raw = smem_u32(f8_smem_raw);
+  unsigned char* ring = f8_smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + Cfg::RING);
+  uint64_t* empty = full + STAGES;
+  uint64_t* tfull = empty + STAGES;
+  uint64_t* tempty = tfull + 2;
+  uint64_t* drained = tempty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+  float* sc_smem = reinterpret_cast<float*>(ring + Cfg::RING + 512);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], EW);
+    }
+    mbar_init(drained, 1);
+    mbar_fence_init();
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, Cfg::TMEM);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  // split: the cluster's CTAs (blockIdx.y) share one tile; otherwise the grid walks over the tiles
+  const int tiles = p.tiles_r * p.tiles_c, share = blockIdx.y;
+  const int kb0 = (int)((int64_t)p.kb * share / p.splits), kb1 = (int)((int64_t)p.kb * (share + 1) / p.splits);
+  bool ok = true;
+  float acc[COLS];
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int it = 0;
+      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+        int tr, tc;
+        tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+          const int s = it % STAGES, r = it / STAGES;
+          if (r > 0 && !mbar_wait_bounded(&empty[s], (uint32_t)((r - 1) & 1))) {
+            ok = false;
+            break;
+          }
+          unsigned char* st = ring + (size_t)s * Cfg::STAGE;
+          mbar_arrive_expect_tx(&full[s], Cfg::STAGE);
+          tma_load_2d(st, &map_r, p.r_mn ? tr * kRows : kb * kF8Block, p.r_mn ? kb * kF8Block : tr * kRows, &full[s]);
+          if (p.c_mn) {
+#pragma unroll
+            for (int j = 0; j < (TBN >= 128 ? TBN / 128 : 1); ++j)
+              tma_load_2d(st + kRowStage + j * kRowStage, &map_c, tc * TBN + j * 128, kb * kF8Block, &full[s]);
+          } else {
+            tma_load_2d(st + kRowStage, &map_c, kb * kF8Block, tc * TBN, &full[s]);
+          }
+        }
+      }
+      if (!ok) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+      // nothing of this CTA's copies may still be in flight when it leaves: the latest fill of every slot
+      if (!ok)
+        for (int s = 0; s < STAGES; ++s)
+          if (it > s) (void)mbar_wait_bounded(&full[s], (uint32_t)(((it - 1 - s) / STAGES) & 1), kDrainLimitNs);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = umma_idesc_f8(kRows, TBN, p.r_mn, p.c_mn);
+      int it = 0;
+      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+          const int s = it % STAGES, b = it & 1;
+          if ((it >= 2 && !mbar_wait_bounded(&tempty[b], (uint32_t)(((it >> 1) - 1) & 1))) ||
+              !mbar_wait_bounded(&full[s], (uint32_t)((it / STAGES) & 1))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t a0 = smem_u32(ring + (size_t)s * Cfg::STAGE), b0 = a0 + kRowStage;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {  // 32 of the summed index an instruction
+            const uint64_t da = p.r_mn ? umma_desc_mn_major_sw128(a0 + j * 4096, kRowStage) : umma_desc_k_major_sw128(a0 + j * 32);
+            const uint64_t db = p.c_mn ? umma_desc_mn_major_sw128(b0 + j * 4096, kRowStage) : umma_desc_k_major_sw128(b0 + j * 32);
+            umma_f8(tmem + b * TBN, da, db, idesc, j != 0 ? 1u : 0u);
+          }
+          umma_commit(&empty[s]);
+          umma_commit(&tfull[b]);
+        }
+      }
+      if (!ok) {  // multiply-adds in flight write tensor memory: let them end before it is freed
+        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+        umma_commit(drained);
+        (void)mbar_wait_bounded(drained, 0, kDrainLimitNs);
+      }
+    }
+  } else {
+    const int ew = warp - 2, quad = warp & 3, half = ew >> 2;  // tensor-memory lanes go by the warp's number modulo 4
+    float* scw = sc_smem + ew * COLS;
+    const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * COLS);
+    constexpr int SPL = (COLS + 31) / 32;
+    int it = 0;
+    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+      int tr, tc;
+      tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+      const int64_t row = (int64_t)tr * kRows + quad * 32 + lane, col0 = (int64_t)tc * TBN + half * COLS;
+      const int64_t srow = row < p.out.rows ? row : p.out.rows - 1;
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) acc[j] = 0.0f;
+      float fr = 0.0f, fc[SPL];
+      auto fetch = [&](int kb) {
+        fr = f8_scale_at(p.sr, srow, kb);
+#pragma unroll
+        for (int i = 0; i < SPL; ++i) {
+          int64_t c = col0 + i * 32 + (lane % COLS);
+          fc[i] = f8_scale_at(p.sc, c < p.out.cols ? c : p.out.cols - 1, kb);
+        }
+      };
+      if (kb0 < kb1) fetch(kb0);
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        const int b = it & 1;
+        const float f = fr;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < SPL; ++i)
+          if (COLS >= 32 || lane < COLS) scw[i * 32 + lane] = fc[i];
+        __syncwarp();
+        if (kb + 1 < kb1) fetch(kb + 1);
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&tfull[b], (uint32_t)((it >> 1) & 1)) ? 1 : 0)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int c0 = 0; c0 < COLS; c0 += 16) {
+          uint32_t v[16];
+          tmem_ld16_issue(taddr + (uint32_t)(b * TBN + c0), v);
+          tmem_ld_wait16(v);
+          if (c0 + 16 >= COLS) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tempty[b]);
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) acc[c0 + j] += __uint_as_float(v[j]) * (f * scw[c0 + j]);
+        }
+      }
+      if (!ok) {
+        if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+      } else if (p.splits == 1) {
+        f8_emit<TC, COLS_CONTIG, COLS>(p.out, row, col0, acc);
+      } else {
+        // this CTA's share of the tile, [column][row]; the ring is idle once the last block's sums have been read
+        float* mine = reinterpret_cast<float*>(ring) + (size_t)half * COLS * kRows + quad * 32 + lane;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) mine[(size_t)j * kRows] = acc[j];
+      }
+    }
+  }
+  __syncwarp();
+
+  if (p.splits > 1) {
+    int tr, tc;
+    tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
+    f8_split_join<TC, COLS_CONTIG, TBN, EW>(p.out, ring, p.splits, share, warp >= 2 && ok ? warp - 2 : -1, warp & 3,
+                                            (int64_t)tr * kRows, (int64_t)tc * TBN);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem, Cfg::TMEM);
+}
+
+// ---- operands whose columns are not 16-byte aligned are copied into columns that are --------------------
+__global__ void __launch_bounds__(256) f8_repitch_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, uint8_t* dst, int64_t ldd) {
+  const int64_t per = ldd / 16;
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < per * cols; i += (int64_t)gridDim.x * 256) {
+    const int64_t c = i / per, r = (i - c * per) * 16;
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (r + j < rows) w[j >> 2] |= (uint32_t)src[c * ld + r + j] << (8 * (j & 3));
+    *reinterpret_cast<uint4*>(dst + c * ldd + r) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+template <typename TC>
+__global__ void __launch_bounds__(256) f8_scale_c_kernel(int64_t m, int64_t n, float beta, TC* C, int64_t ldc) {
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < m * n; i += (int64_t)gridDim.x * 256) {
+    TC* c = C + i % m + i / m * ldc;
+    f8_store1(c, beta == 0.0f ? 0.0f : beta * f8_load1(c));
+  }
+}
+
+unsigned grid_for(int64_t threads) {
+  const int64_t b = blocks_of(threads, 256), cap = (int64_t)sm_count_cached() * 16;
+  return (unsigned)(b < 1 ? 1 : b < cap ? b : cap);
+}
+
+// Matrix of bytes, `inner` contiguous; boxes of 128 bytes by box_outer, 128-byte swizzle.
+bool f8_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int box_outer) {
+  EncodeFn enc = tensor_map_encode_fn();
+  if (!enc) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_outer};
+  const cuuint32_t estr[2] = {1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct F8Operand {
+  const void* p;
+  int64_t n, ld;  // extent of its own index, leading dimension
+  bool mn;        // its own index is contiguous
+  F8Scale s;
+};
+
+template <int TBN, typename TC, bool COLS_CONTIG>
+int f8_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, int splits, cudaStream_t st) {
+  using Cfg = F8Cfg<TBN>;
+  static std::atomic<bool> configured[64];
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return B2_ERR_LAUNCH;
+  auto kfn = f8_gemm_kernel<TBN, TC, COLS_CONTIG>;
+  if (!configured[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(kfn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM) != cudaSuccess) return B2_ERR_LAUNCH;
+    configured[dev].store(true, std::memory_order_release);
+  }
+  CUtensorMap mr, mc;
+  if (!f8_map(&mr, r.p, r.mn ? r.n : k, r.mn ? k : r.n, r.ld, 128) ||
+      !f8_map(&mc, c.p, c.mn ? c.n : k, c.mn ? k : c.n, c.ld, c.mn ? 128 : TBN))
+    return B2_ERR_LAUNCH;
+  const int64_t tr = blocks_of(r.n, kRows), tc = blocks_of(c.n, TBN);
+  if (tr * tc > 0x7fffffffLL) return B2_ERR_VARIANT;
+  a.out.rows = r.n, a.out.cols = c.n, a.r_mn = r.mn, a.c_mn = c.mn, a.sr = r.s, a.sc = c.s;
+  a.tiles_r = (int)tr, a.tiles_c = (int)tc, a.splits = splits;
+  a.group = 8;
+  const int tiles = a.tiles_r * a.tiles_c, sms = sm_count_cached();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = splits > 1 ? dim3((unsigned)tiles, (unsigned)splits) : dim3((unsigned)(tiles < sms ? tiles : sms));
+  cfg.blockDim = dim3(Cfg::NT);
+  cfg.dynamicSmemBytes = Cfg::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim = {1, (unsigned)splits, 1};
+  cfg.attrs = at, cfg.numAttrs = splits > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kfn, a, mr, mc) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+}
+
+template <typename TC>
+int f8_choose(const F8Args& a, const F8Operand& A, const F8Operand& B, int64_t k, cudaStream_t st) {
+  const int sms = sm_count_cached();
+  // CTAs that share a tile: as many as leave every one of them a few blocks and no SM without a CTA
+  auto splits_for = [&](int64_t tiles, int resident) {
+    int s = 1;
+    while (s < kMaxSplit && tiles * s * 2 <= (int64_t)sms * resident && a.kb / (s * 2) >= 2) s *= 2;
+    return s;
+  };
+  if (B.n <= 64 && !B.mn) {  // decoding
+    const int s = splits_for(blocks_of(A.n, kRows), 2);
+    if (B.n <= 16) return f8_launch<16, TC, false>(a, A, B, k, s, st);
+    if (B.n <= 32) return f8_launch<32, TC, false>(a, A, B, k, s, st);
+    return f8_launch<64, TC, false>(a, A, B, k, s, st);
+  }
+  const int64_t wide = blocks_of(B.n, kRows) * blocks_of(A.n, 256);
+  if (wide >= sms) return f8_launch<256, TC, true>(a, B, A, k, 1, st);
+  const int s = splits_for(blocks_of(B.n, kRows) * blocks_of(A.n, 128), 1);
+  return f8_launch<128, TC, true>(a, B, A, k, s, st);
+}
+
+bool f8_is_n(char c) { return c == 'N' || c == 'n'; }
+bool f8_is_t(char c) { return c == 'T' || c == 't' || c == 'C' || c == 'c'; }
+
+// Copies of operands that TMA cannot read.
+struct F8Pack {
+  bool a, b;
+  int64_t lda, ldb;
+  size_t off_b, total;
+};
+F8Pack f8_pack_plan(bool an, bool bn, int64_t m, int64_t n, int64_t k, const void* A, int64_t lda, const void* B, int64_t ldb) {
+  F8Pack p{};
+  p.a = !columns_aligned(A, lda, 1, 16), p.b = !columns_aligned(B, ldb, 1, 16);
+  const int64_t ra = an ? m : k, ca = an ? k : m, rb = bn ? k : n, cb = bn ? n : k;
+  p.lda = (int64_t)round_up((size_t)ra, 16), p.ldb = (int64_t)round_up((size_t)rb, 16);
+  p.off_b = p.a ? round_up((size_t)p.lda * ca, 256) : 0;
+  p.total = p.off_b + (p.b ? round_up((size_t)p.ldb * cb, 256) : 0);
+  return p;
+}
+
+}  // namespace
+
+int f8_repitch(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd, cudaStream_t st) {
+  f8_repitch_kernel<<<grid_for(ldd / 16 * cols), 256, 0, st>>>(static_cast<const uint8_t*>(src), ld, rows, cols, static_cast<uint8_t*>(dst), ldd);
+  return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+}
+int f8_scale_c(int64_t m, int64_t n, float beta, void* C, int64_t ldc, int type_c, cudaStream_t st) {
+  if (beta == 1.0f) return B2_OK;
+  if (type_c == B2_TYPE_BF16) f8_scale_c_kernel<<<grid_for(m * n), 256, 0, st>>>(m, n, beta, static_cast<__nv_bfloat16*>(C), ldc);
+  else f8_scale_c_kernel<<<grid_for(m * n), 256, 0, st>>>(m, n, beta, static_cast<float*>(C), ldc);
+  return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+}
+
+}  // namespace b2
+
+extern "C" size_t b2_gemm_f8_workspace_bytes(char transa, char transb, int64_t m, int64_t n, int64_t k, const void* A,
+                                             int64_t lda, const void* B, int64_t ldb) {
+  using namespace b2;
+  if ((!f8_is_n(transa) && !f8_is_t(transa)) || (!f8_is_n(transb) && !f8_is_t(transb)) || m <= 0 || n <= 0 || k <= 0) return 0;
+  return f8_pack_plan(f8_is_n(transa), f8_is_n(transb), m, n, k, A, lda, B, ldb).total;
+}
+
+extern "C" int b2_gemm_f8(char transa, char transb, int64_t m, int64_t n, int64_t k, float alpha, const void* A, int64_t lda,
+                          const void* SA, int64_t ldsa, int block_a, int scale_type_a, const void* B, int64_t ldb,
+                          const void* SB, int64_t ldsb, int block_b, int scale_type_b, float beta, void* C, int64_t ldc,
+                          int type_c, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  using namespace b2;
+  const bool an = f8_is_n(transa), bn = f8_is_n(transb);
+  if (!an && !f8_is_t(transa)) return -1;
+  if (!bn && !f8_is_t(transb)) return -2;
+  if (m < 0) return -3;
+  if (n < 0) return -4;
+  if (k < 0) return -5;
+  const bool nonempty = m > 0 && n > 0, reads = nonempty && k > 0 && alpha != 0.0f;
+  auto least = [](int64_t v) { return v > 1 ? v : 1; };
+  if (reads && !A) return -7;
+  if (lda < least(an ? m : k)) return -8;
+  if (reads && !SA) return -9;
+  if (block_a != 1 && block_a != kF8Block) return -11;
+  if (ldsa < least(an ? blocks_of(m, block_a) : blocks_of(k, kF8Block))) return -10;
+  if (scale_type_a != B2_SCALE_E8M0 && scale_type_a != B2_SCALE_F32) return -12;
+  if (reads && !B) return -13;
+  if (ldb < least(bn ? k : n)) return -14;
+  if (reads && !SB) return -15;
+  if (block_b != 1 && block_b != kF8Block) return -17;
+  if (ldsb < least(bn ? blocks_of(k, kF8Block) : blocks_of(n, block_b))) return -16;
+  if (scale_type_b != B2_SCALE_E8M0 && scale_type_b != B2_SCALE_F32) return -18;
+  if (nonempty && !C) return -20;
+  if (ldc < least(m)) return -21;
+  if (type_c != B2_TYPE_F32 && type_c != B2_TYPE_BF16) return -22;
+  if (!nonempty) return B2_OK;
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (!reads) return f8_scale_c(m, n, beta, C, ldc, type_c, st);
+  constexpr int64_t kMost = 0x7fffffffLL - 512;
+  if (m > kMost || n > kMost || k > kMost) return B2_ERR_VARIANT;
+  const F8Pack pk = f8_pack_plan(an, bn, m, n, k, A, lda, B, ldb);
+  if (pk.total && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < pk.total)) return B2_ERR_WORKSPACE;
+  if (pk.a) {
+    const int rc = f8_repitch(A, lda, an ? m : k, an ? k : m, workspace, pk.lda, st);
+    if (rc) return rc;
+    A = workspace, lda = pk.lda;
+  }
+  if (pk.b) {
+    void* to = static_cast<char*>(workspace) + pk.off_b;
+    const int rc = f8_repitch(B, ldb, bn ? k : n, bn ? n : k, to, pk.ldb, st);
+    if (rc) return rc;
+    B = to, ldb = pk.ldb;
+  }
+  F8Args a = {};
+  a.kb = (int)blocks_of(k, kF8Block);
+  a.out.alpha = alpha, a.out.beta = beta, a.out.C = C, a.out.ldc = ldc;
+  a.out.vec = columns_aligned(C, ldc, type_c == B2_TYPE_BF16 ? 2 : 4, 16);
+  a.status = status_pointer();
+  if (!a.status) return B2_ERR_LAUNCH;
+  const F8Operand oa{A, m, lda, an, {SA, an ? 1 : ldsa, an ? ldsa : 1, block_a == 1 ? 0 : 7, scale_type_a == B2_SCALE_F32}};
+  const F8Operand ob{B, n, ldb, !bn, {SB, bn ? ldsb : 1, bn ? 1 : ldsb, block_b == 1 ? 0 : 7, scale_type_b == B2_SCALE_F32}};
+  return type_c == B2_TYPE_BF16 ? f8_choose<__nv_bfloat16>(a, oa, ob, k, st) : f8_choose<float>(a, oa, ob, k, st);
+}

@@ -24,6 +24,7 @@
 #include "b2gemm.h"
 #include "entry.h"
 #include "gemm_tma.cuh"
+#include "tcgen05.cuh"
 
 namespace b2 {
 namespace {
@@ -113,18 +114,7 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// ---- tcgen05 helpers ---------------------------------------------------------------------------
-__device__ __forceinline__ void tmem_alloc(uint32_t* smem_result, uint32_t ncols) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem_result)),
-               "r"(ncols)
-               : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// ---- tcgen05: the TF32 multiply-add -------------------------------------------------------------
 // D[tmem] (+)= A[smem] * B[smem], TF32 inputs, fp32 accumulate; accumulate == 0 overwrites D.
 __device__ __forceinline__ void umma_tf32(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc,
                                           uint32_t accumulate) {
@@ -134,44 +124,6 @@ __device__ __forceinline__ void umma_tf32(uint32_t tmem_d, uint64_t desc_a, uint
       "tcgen05.mma.cta_group::1.kind::tf32 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
       : "memory");
-}
-// The mbarrier gets one arrival when all tcgen05.mma issued so far by this thread have completed.
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-               : "memory");
-}
-// 16 consecutive accumulator columns of this lane's row (32 lanes x 32 bits, 16 repetitions); the values are
-// defined only after tmem_ld_wait().
-__device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-}
-// The registers pass through the wait as read-write operands, so that no use of them is scheduled before it.
-__device__ __forceinline__ void tmem_ld_wait(uint32_t (&a)[16], uint32_t (&b)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(a[0]), "+r"(a[1]), "+r"(a[2]), "+r"(a[3]), "+r"(a[4]), "+r"(a[5]), "+r"(a[6]), "+r"(a[7]),
-                 "+r"(a[8]), "+r"(a[9]), "+r"(a[10]), "+r"(a[11]), "+r"(a[12]), "+r"(a[13]), "+r"(a[14]), "+r"(a[15]),
-                 "+r"(b[0]), "+r"(b[1]), "+r"(b[2]), "+r"(b[3]), "+r"(b[4]), "+r"(b[5]), "+r"(b[6]), "+r"(b[7]),
-                 "+r"(b[8]), "+r"(b[9]), "+r"(b[10]), "+r"(b[11]), "+r"(b[12]), "+r"(b[13]), "+r"(b[14]), "+r"(b[15])
-               :
-               : "memory");
-}
-
-// Shared-memory matrix descriptor of a K-major operand tile stored as rows of 128 bytes (32 floats) with the
-// 128-byte swizzle: 8-row groups are 1024 bytes apart (stride byte offset), the leading byte offset is not
-// used by swizzled K-major layouts, descriptor version 1, layout type 2 (128-byte swizzle).
-__device__ __forceinline__ uint64_t umma_desc_k_major_sw128(uint32_t smem_addr) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr >> 4) & 0x3FFF);
-  d |= (uint64_t)1 << 16;            // leading byte offset (16 bytes, ignored)
-  d |= (uint64_t)(1024 >> 4) << 32;  // stride byte offset
-  d |= (uint64_t)1 << 46;            // version
-  d |= (uint64_t)2 << 61;            // 128-byte swizzle
-  return d;
 }
 // Instruction descriptor: fp32 accumulator, TF32 A and B, both K-major, N and M of the instruction.
 __host__ __device__ constexpr uint32_t umma_idesc_tf32(int m, int n) {
@@ -331,25 +283,9 @@ __global__ void __launch_bounds__(128, MINB)
   if (warp == 1) tmem_dealloc(tmem_d, TBN);
 }
 
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                              const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeFn tf32_lookup_encode_fn() {
-  void* ptr = nullptr;
-  cudaDriverEntryPointQueryResult q;
-  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess &&
-      q == cudaDriverEntryPointSuccess)
-    return reinterpret_cast<EncodeFn>(ptr);
-  return nullptr;
-}
-EncodeFn tf32_encode_fn() {
-  static const EncodeFn fn = tf32_lookup_encode_fn();  // initialised once, thread-safe
-  return fn;
-}
-
 // Panel P[rows][pitch] (pitch floats, k contiguous): boxes of 32 k by box_rows rows, 128-byte swizzle.
 bool panel_map(CUtensorMap* map, const float* P, int64_t rows, int64_t pitch, int box_rows) {
-  EncodeFn enc = tf32_encode_fn();
+  EncodeFn enc = tensor_map_encode_fn();
   if (!enc) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)pitch * sizeof(float)};
