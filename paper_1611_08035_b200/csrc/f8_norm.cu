@@ -57,26 +57,29 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_kernel(const NormA
   const T* R = p.R ? static_cast<const T*>(p.R) + row * p.ldr : nullptr;
   T* H = p.H ? static_cast<T*>(p.H) + row * p.ldh : nullptr;
   const T* W = static_cast<const T*>(p.w);
-  float v[VPT][8], w[VPT][8], ss = 0.0f;
+  Raw8<T> rx[VPT], rr[VPT], rw[VPT];  // all loads first
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
-    load8(X + e, nv, p.vx, v[i]);
+    load8(X + e, nv, p.vx, rx[i]);
+    if (R) load8(R + e, nv, p.vr, rr[i]);
   }
-  if (R) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
+  for (int i = 0; i < VPT; ++i) {
+    const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
+    load8(W + e, nv, p.vw, rw[i]);
+  }
+  float v[VPT][8], ss = 0.0f;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
+    unpack8(rx[i], v[i]);
+    if (R) {
       float r[8];
-      load8(R + e, nv, p.vr, r);
+      unpack8(rr[i], r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] += r[j];
     }
-  }
-#pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
-    load8(W + e, nv, p.vw, w[i]);
     if (H) store8(H + e, nv, p.vh, v[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) ss += v[i][j] * v[i][j];
@@ -86,11 +89,12 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_kernel(const NormA
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
-    float y[8];
+    float y[8], w[8];
     uint32_t m = 0;
+    unpack8(rw[i], w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      y[j] = j < nv ? v[i][j] * rstd * w[i][j] : 0.0f;  // beyond the row: no 0 * inf
+      y[j] = j < nv ? v[i][j] * rstd * w[j] : 0.0f;  // beyond the row: no 0 * inf
       m = max(m, mag_bits(y[j]));
     }
     const uint32_t byte = f8_scale_byte(block_max(m));
@@ -187,43 +191,53 @@ template <typename T, int NT, int VPT>
 __global__ void __launch_bounds__(NT) norm_bwd_kernel(const NormBwdArgs p) {
   __shared__ float part[2][NT / 32];
   const int l = threadIdx.x;
-  float dw[VPT][8], w[VPT][8];
+  float dw[VPT][8];
+  Raw8<T> rw[VPT], ry[VPT], rh[VPT], rg[VPT];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int64_t e = (int64_t)(l + i * NT) * 8, nv = row < p.t ? p.d - e : 0;
+      load8(static_cast<const T*>(p.DY) + row * p.lddy + e, nv, p.vy, ry[i]);
+      load8(static_cast<const T*>(p.H) + row * p.ldh + e, nv, p.vh, rh[i]);
+      if (p.DH) load8(static_cast<const T*>(p.DH) + row * p.lddh + e, nv, p.vr, rg[i]);
+    }
+  };
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int64_t e = (int64_t)(l + i * NT) * 8;
-    load8(static_cast<const T*>(p.w) + e, p.d - e, p.vw, w[i]);
+    load8(static_cast<const T*>(p.w) + e, p.d - e, p.vw, rw[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
   }
   int parity = 0;
+  fetch(blockIdx.x);
   for (int64_t row = blockIdx.x; row < p.t; row += gridDim.x, parity ^= 1) {
-    const T* DY = static_cast<const T*>(p.DY) + row * p.lddy;
-    const T* H = static_cast<const T*>(p.H) + row * p.ldh;
     const float rstd = p.rstd[row];
-    float dy[VPT][8], xh[VPT][8], dot = 0.0f;
+    Raw8<T> cy[VPT], ch[VPT], cg[VPT];
+    float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t e = (int64_t)(l + i * NT) * 8;
-      load8(DY + e, p.d - e, p.vy, dy[i]);
-      load8(H + e, p.d - e, p.vh, xh[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
+      cy[i] = ry[i], ch[i] = rh[i], cg[i] = rg[i];
+      float dy[8], xh[8], w[8];
+      unpack8(cy[i], dy), unpack8(ch[i], xh), unpack8(rw[i], w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        xh[i][j] *= rstd;
-        dot += dy[i][j] * w[i][j] * xh[i][j];
-        dw[i][j] += dy[i][j] * xh[i][j];
+        xh[j] *= rstd;
+        dot += dy[j] * w[j] * xh[j];
+        dw[i][j] += dy[j] * xh[j];
       }
+    }
+    fetch(row + gridDim.x);  // on its way while this token's sum is taken
     const float mean = row_sum<NT>(dot, part[parity]) / (float)p.d;  // two arrays in turn: one barrier a token
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int64_t e = (int64_t)(l + i * NT) * 8, nv = p.d - e;
-      float dx[8], dh[8];
-      if (p.DH) load8(static_cast<const T*>(p.DH) + row * p.lddh + e, nv, p.vr, dh);
+      float dx[8], dy[8], xh[8], w[8], dh[8];
+      unpack8(cy[i], dy), unpack8(ch[i], xh), unpack8(rw[i], w);
+      if (p.DH) unpack8(cg[i], dh);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        dx[j] = rstd * (dy[i][j] * w[i][j] - xh[i][j] * mean);
+        dx[j] = rstd * (dy[j] * w[j] - xh[j] * rstd * mean);
         if (p.DH) dx[j] += dh[j];
       }
       store8(static_cast<T*>(p.DX) + row * p.lddx + e, nv, p.vx, dx);

@@ -14,33 +14,34 @@ struct QuantArgs {
   bool vx, vq;
 };
 
-// One block of 128 features of one token per sixteen lanes, eight features a thread; `rowlen` blocks a token.
+// One block of 128 features of one token per sixteen lanes, eight features a thread.  U blocks are in flight per group of
+// lanes, one CTA's 16 U blocks following each other in memory.
 template <typename T, int U>
-__global__ void __launch_bounds__(256) quant_rows_kernel(const QuantArgs p, int64_t rowlen) {
-  const int64_t total = rowlen * p.t;
-  const int64_t first = ((int64_t)blockIdx.x * 256 + threadIdx.x) / 16, step = (int64_t)gridDim.x * 16;
+__global__ void __launch_bounds__(256) quant_rows_kernel(const QuantArgs p, const FastDiv per_token, uint32_t total) {
   const int l = threadIdx.x & 15;
-  float v[U][8];
+  const uint32_t first = blockIdx.x * (16 * U) + (threadIdx.x >> 4);
+  Raw8<T> raw[U];
+  int64_t row[U], e[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t b = first + u * step;
-    const int64_t row = b / rowlen, e = (b - row * rowlen) * kF8Block + l * 8;
-    load8(static_cast<const T*>(p.X) + row * p.ldx + e, b < total ? p.d - e : 0, p.vx, v[u]);
+    const uint32_t b = first + u * 16, r = div_by(b, per_token);
+    row[u] = r, e[u] = (int64_t)(b - r * per_token.d) * kF8Block + l * 8;
+    load8(static_cast<const T*>(p.X) + row[u] * p.ldx + e[u], b < total ? p.d - e[u] : 0, p.vx, raw[u]);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t b = first + u * step;
-    const int64_t row = b / rowlen, blk = b - row * rowlen, e = blk * kF8Block + l * 8;
-    const int64_t nv = b < total ? p.d - e : 0;
+    const int64_t nv = first + u * 16 < total ? p.d - e[u] : 0;
+    float v[8];
+    unpack8(raw[u], v);
     uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, mag_bits(v[u][j]));
+    for (int j = 0; j < 8; ++j) m = max(m, mag_bits(v[j]));
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
     const uint32_t byte = f8_scale_byte(m);
     if (nv > 0) {
-      store8_f8(static_cast<uint8_t*>(p.Q) + row * p.ldq + e, nv, p.vq, f8_quant8(v[u], byte));
-      if (l == 0) static_cast<uint8_t*>(p.S)[row * p.lds + blk] = (uint8_t)byte;
+      store8_f8(static_cast<uint8_t*>(p.Q) + row[u] * p.ldq + e[u], nv, p.vq, f8_quant8(v, byte));
+      if (l == 0) static_cast<uint8_t*>(p.S)[row[u] * p.lds + e[u] / kF8Block] = (uint8_t)byte;
     }
   }
 }
@@ -52,17 +53,20 @@ __global__ void __launch_bounds__(256) quant_tiles_kernel(const QuantArgs p, int
   const int64_t bt = blockIdx.x / blocks_d, bd = blockIdx.x - bt * blocks_d;
   const int l = threadIdx.x & 15, r = threadIdx.x >> 4;
   const int64_t e = bd * kF8Block + l * 8;
-  float v[8][8];
+  Raw8<T> raw[8];
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = bt * kF8Block + r + 16 * i;
-    load8(static_cast<const T*>(p.X) + row * p.ldx + e, row < p.t ? p.d - e : 0, p.vx, v[i]);
+    load8(static_cast<const T*>(p.X) + row * p.ldx + e, row < p.t ? p.d - e : 0, p.vx, raw[i]);
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 8; ++i) {
+    float v[8];
+    unpack8(raw[i], v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, mag_bits(v[i][j]));
+    for (int j = 0; j < 8; ++j) m = max(m, mag_bits(v[j]));
+  }
   m = __reduce_max_sync(0xffffffffu, m);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
   __syncthreads();
@@ -72,7 +76,9 @@ __global__ void __launch_bounds__(256) quant_tiles_kernel(const QuantArgs p, int
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = bt * kF8Block + r + 16 * i, nv = row < p.t ? p.d - e : 0;
-    if (nv > 0) store8_f8(static_cast<uint8_t*>(p.Q) + row * p.ldq + e, nv, p.vq, f8_quant8(v[i], byte));
+    float v[8];
+    unpack8(raw[i], v);
+    if (nv > 0) store8_f8(static_cast<uint8_t*>(p.Q) + row * p.ldq + e, nv, p.vq, f8_quant8(v, byte));
   }
   if (threadIdx.x == 0) static_cast<uint8_t*>(p.S)[bt * p.lds + bd] = (uint8_t)byte;
 }
@@ -82,9 +88,9 @@ int quant_launch(const QuantArgs& a, int block, cudaStream_t st) {
   const int64_t nb = blocks_of(a.d, kF8Block);
   if (block == 1) {
     constexpr int U = 4;
-    const int64_t ctas = blocks_of(nb * a.t, 16 * U);
-    if (ctas > 0x7fffffffLL) return B2_ERR_VARIANT;
-    quant_rows_kernel<T, U><<<(unsigned)ctas, 256, 0, st>>>(a, nb);
+    const int64_t total = nb * a.t;
+    if (a.t > 0x7fffffffLL || total > 0x7fffffffLL - 16 * U) return B2_ERR_VARIANT;  // 2^38 numbers
+    quant_rows_kernel<T, U><<<(unsigned)blocks_of(total, 16 * U), 256, 0, st>>>(a, fast_div((uint32_t)nb), (uint32_t)total);
   } else {
     const int64_t ctas = nb * blocks_of(a.t, kF8Block);
     if (ctas > 0x7fffffffLL) return B2_ERR_VARIANT;
