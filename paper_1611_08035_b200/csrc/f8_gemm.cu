@@ -18,33 +18,10 @@
 
 #include <atomic>
 
-#include "b2gemm.h"
-#include "entry.h"
-#include "f8.cuh"
-#include "f8_out.cuh"
-#include "tcgen05.cuh"
+#include "f8_gemm.cuh"
 
 namespace b2 {
 namespace {
-
-constexpr int kRows = 128;                       // MMA rows of a tile
-constexpr uint32_t kRowStage = kRows * kF8Block;  // bytes of the row operand in a stage
-constexpr int kMaxSplit = 8;
-
-struct F8Scale {  // value for index i and block b: p[(i >> shift) * si + b * sb]
-  const void* p;
-  int64_t si, sb;
-  int shift, f32;
-};
-struct F8Args {
-  F8Out out;
-  int kb;              // blocks of 128 along the summed index
-  int splits;          // CTAs of a cluster that share a tile's blocks
-  int r_mn, c_mn;      // the operand's own index is contiguous (else the summed one)
-  int tiles_r, tiles_c, group;
-  F8Scale sr, sc;
-  int* status;
-};
 
 template <int TBN>
 struct F8Cfg {
@@ -58,11 +35,6 @@ struct F8Cfg {
   static constexpr size_t SMEM = 1024 + RING + 512 + EW * COLS * sizeof(float);
   static_assert(kRows * TBN * 4 <= RING, "the split's shares pass through the ring");
 };
-
-__device__ __forceinline__ float f8_scale_at(const F8Scale& s, int64_t i, int b) {
-  const int64_t at = (i >> s.shift) * s.si + (int64_t)b * s.sb;
-  return s.f32 ? static_cast<const float*>(s.p)[at] : e8m0_value(static_cast<const uint8_t*>(s.p)[at]);
-}
 
 __device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -280,26 +252,6 @@ unsigned grid_for(int64_t threads) {
   return (unsigned)(b < 1 ? 1 : b < cap ? b : cap);
 }
 
-// Matrix of bytes, `inner` contiguous; boxes of 128 bytes by box_outer, 128-byte swizzle.
-bool f8_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int box_outer) {
-  EncodeFn enc = tensor_map_encode_fn();
-  if (!enc) return false;
-  const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
-  const cuuint64_t strides[1] = {(cuuint64_t)ld};
-  const cuuint32_t box[2] = {128, (cuuint32_t)box_outer};
-  const cuuint32_t estr[2] = {1, 1};
-  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-struct F8Operand {
-  const void* p;
-  int64_t n, ld;  // extent of its own index, leading dimension
-  bool mn;        // its own index is contiguous
-  F8Scale s;
-};
-
 template <int TBN, typename TC, bool COLS_CONTIG>
 int f8_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, int splits, cudaStream_t st) {
   using Cfg = F8Cfg<TBN>;
@@ -349,6 +301,7 @@ int f8_choose(const F8Args& a, const F8Operand& A, const F8Operand& B, int64_t k
     return f8_launch<64, TC, false>(a, A, B, k, s, st);
   }
   const int64_t wide = blocks_of(B.n, kRows) * blocks_of(A.n, 256);
+  if (!A.s.f32 && !B.s.f32 && blocks_of(B.n, 256) * blocks_of(A.n, 256) * 2 >= sms) return f8_mx_launch<TC>(a, B, A, k, st);
   if (wide >= sms) return f8_launch<256, TC, true>(a, B, A, k, 1, st);
   const int s = splits_for(blocks_of(B.n, kRows) * blocks_of(A.n, 128), 1);
   return f8_launch<128, TC, true>(a, B, A, k, s, st);

@@ -1,0 +1,277 @@
+// The block-scaled e4m3 product with power-of-two scales applied by the tensor core itself
+// (tcgen05.mma kind::mxf8f6f4, one e8m0 factor per row or column and 32 elements of the summed index: the four
+// instructions of a block of 128 take the same one), on pairs of CTAs.
+//
+// A pair owns a 256 x 256 tile of C: each CTA fetches its 128 rows of the row operand and its 128 columns of the
+// column operand, so that shared memory is written and read 32 KB per block and SM where a CTA alone would need 48 for the same
+// multiply-adds; the leader's tensor core instruction reads both halves.  The sums stay in tensor memory (256 columns) for the
+// whole tile; 48 more columns hold the scales of sixteen blocks.
+//
+// Warps of a CTA: 0 streams the operands (TMA), 1 issues the multiply-adds (leader only), 4-7 put the scales
+// into tensor memory, four blocks at a time (byte = block, lane and column = row), 8-15 write C.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+
+#include "f8_gemm.cuh"
+
+namespace b2 {
+namespace {
+
+constexpr int kBN = 256;                       // columns of the pair's tile
+constexpr int kStages = 6, kSlots = 4;         // operand ring, scale ring
+constexpr uint32_t kStageBytes = 2 * kRowStage;  // a CTA's halves of both operands
+constexpr uint32_t kRing = kStageBytes * kStages;
+constexpr size_t kSmem = 1024 + kRing + 512;
+constexpr int kThreads = 512, kEW = 8, kCols = kBN / 2;
+constexpr uint32_t kTmem = 512, kSfCols = 12;  // scales of four blocks: 128 rows in 4 columns, 256 columns in 8
+
+__device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+      : "memory");
+}
+// Instruction descriptor: byte of the scale words (both operands), e4m3, which operands have their own index contiguous,
+// N, e8m0 scales, M.
+__device__ __forceinline__ uint32_t umma_idesc_mx(int m, int n, int a_mn, int b_mn, int byte) {
+  return ((uint32_t)byte << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
+         ((uint32_t)(m >> 7) << 27) | ((uint32_t)byte << 29);
+}
+
+// Scale bytes of index i (clamped to the last one) for blocks b .. b+3, the first in the lowest byte; blocks beyond the
+// last are never multiplied with.
+__device__ __forceinline__ uint32_t scale_word(const F8Scale& s, int64_t i, int64_t extent, int b, int kb) {
+  const uint8_t* p = static_cast<const uint8_t*>(s.p) + ((i < extent ? i : extent - 1) >> s.shift) * s.si + (int64_t)b * s.sb;
+  if (s.sb == 1 && b + 4 <= kb && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return *reinterpret_cast<const uint32_t*>(p);
+  uint32_t w = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (b + j < kb) w |= (uint32_t)p[j * s.sb] << (8 * j);
+  return w;
+}
+
+// CHUNK: blocks whose products are summed in tensor memory, whose additions truncate, before they are added to fp32
+// registers; 0: all of them.  A bf16 result does not see the difference.
+template <typename TC, int CHUNK>
+__global__ void __launch_bounds__(kThreads, 1)
+    f8_mx_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
+  extern __shared__ unsigned char mx_smem_raw[];
+  const uint32_t raw = smem_u32(mx_smem_raw);
+  unsigned char* ring = mx_smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + kRing);
+  uint64_t* empty = full + kStages;
+  uint64_t* sf_full = empty + kStages;
+  uint64_t* sf_empty = sf_full + kSlots;
+  uint64_t* tfull = sf_empty + kSlots;
+  uint64_t* tempty = tfull + 1;
+  uint64_t* drained = tempty + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_rank();
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&sf_full[s], 8);  // four warps of each CTA
+      mbar_init(&sf_empty[s], 1);
+    }
+    mbar_init(tfull, 1);
+    mbar_init(tempty, 2 * kEW);
+    mbar_init(drained, 1);
+    mbar_fence_init();
+  }
+  if (warp == 1) tmem_alloc_pair(tmem_slot, kTmem);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // the other CTA's barriers exist before anything arrives on them
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int tiles = p.tiles_r * p.tiles_c, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  bool ok = true;
+
+  if (warp < 4) {
+    // registers: 4 x 128 at launch; 64 + 80 + 2 x 184 = 512 after the moves
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 0 && lane == 0) {
+      int it = 0;
+      for (int tile = pair; tile < tiles && ok; tile += pairs) {
+        int tr, tc;
+        tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+        const int r0 = tr * 2 * kRows + (int)rank * kRows, c0 = tc * kBN + (int)rank * (kBN / 2);
+        for (int kb = 0; kb < p.kb; ++kb, ++it) {
+          const int s = it % kStages, r = it / kStages;
+          if (r > 0 && !mbar_wait_cluster(&empty[s], (uint32_t)((r - 1) & 1))) {
+            ok = false;
+            break;
+          }
+          unsigned char* st = ring + (size_t)s * kStageBytes;
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kStageBytes);
+          const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
+          const int k0 = kb * kF8Block;
+          tma_load_2d_pair(st, &map_r, p.r_mn ? r0 : k0, p.r_mn ? k0 : r0, bar);
+          tma_load_2d_pair(st + kRowStage, &map_c, p.c_mn ? c0 : k0, p.c_mn ? k0 : c0, bar);
+        }
+      }
+      if (!ok) {
+        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+        if (rank == 0)  // both CTAs' copies are counted here; no CTA leaves before the barrier at the end
+          for (int s = 0; s < kStages; ++s)
+            if (it > s) (void)mbar_wait_cluster(&full[s], (uint32_t)(((it - 1 - s) / kStages) & 1), kDrainLimitNs);
+      }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+      int it = 0, grp = 0, ch = 0;
+      for (int tile = pair; tile < tiles && ok; tile += pairs) {
+        for (int kb = 0; kb < p.kb; ++kb, ++it) {
+          const int s = it % kStages, in = CHUNK ? kb % CHUNK : kb, slot = grp % kSlots;
+          if ((in == 0 && ch > 0 && !mbar_wait_cluster(tempty, (uint32_t)((ch - 1) & 1))) ||
+              ((kb & 3) == 0 && !mbar_wait_cluster(&sf_full[slot], (uint32_t)((grp / kSlots) & 1))) ||
+              !mbar_wait_cluster(&full[s], (uint32_t)((it / kStages) & 1))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t a0 = smem_u32(ring + (size_t)s * kStageBytes), b0 = a0 + kRowStage;
+          const uint32_t sfa = tmem + kBN + slot * kSfCols, sfb = sfa + 4;
+          const uint32_t idesc = umma_idesc_mx(2 * kRows, kBN, p.r_mn, p.c_mn, kb & 3);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint64_t da = p.r_mn ? umma_desc_mn_major_sw128(a0 + j * 4096, kRowStage) : umma_desc_k_major_sw128(a0 + j * 32);
+            const uint64_t db = p.c_mn ? umma_desc_mn_major_sw128(b0 + j * 4096, kRowStage) : umma_desc_k_major_sw128(b0 + j * 32);
+            umma_mx(tmem, da, db, idesc, sfa, sfb, (in | j) != 0 ? 1u : 0u);
+          }
+          umma_commit_pair(&empty[s]);
+          if ((kb & 3) == 3 || kb == p.kb - 1) {
+            umma_commit_pair(&sf_empty[slot]);
+            ++grp;
+          }
+          if ((CHUNK && in == CHUNK - 1) || kb == p.kb - 1) {
+            umma_commit_pair(tfull);
+            ++ch;
+          }
+        }
+      }
+      if (!ok) {
+        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+        umma_commit_pair(drained);
+        (void)mbar_wait_cluster(drained, 0, kDrainLimitNs);
+      }
+    }
+  } else if (warp < 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    const int quad = warp & 3;
+    const uint32_t sf = tmem + kBN + ((uint32_t)(quad * 32) << 16);
+    int grp = 0;
+    for (int tile = pair; tile < tiles && ok; tile += pairs) {
+      int tr, tc;
+      tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+      const int64_t r0 = (int64_t)tr * 2 * kRows + rank * kRows + lane, c0 = (int64_t)tc * kBN + lane;
+      for (int kb = 0; kb < p.kb; kb += 4, ++grp) {
+        const int slot = grp % kSlots, r = grp / kSlots;
+        uint32_t w[kSfCols];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = scale_word(p.sr, r0 + 32 * i, p.out.rows, kb, p.kb);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[4 + i] = scale_word(p.sc, c0 + 32 * i, p.out.cols, kb, p.kb);
+        if (r > 0 && !__all_sync(0xffffffffu, mbar_wait_cluster(&sf_empty[slot], (uint32_t)((r - 1) & 1)) ? 1 : 0)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int i = 0; i < 3; ++i) tmem_st4(sf + slot * kSfCols + 4 * i, w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(cluster_map_shared(smem_u32(&sf_full[slot]), 0));
+      }
+    }
+    if (!ok && lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    const int quad = warp & 3, half = (warp - 8) >> 2;
+    const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
+    const uint32_t leader_tempty = cluster_map_shared(smem_u32(tempty), 0);
+    const uint64_t limit = kWaitLimitNs + (uint64_t)p.kb * 8192ull;  // outlasts the k loop that it waits for
+    float acc[kCols];
+    int ch = 0;
+    for (int tile = pair; tile < tiles && ok; tile += pairs) {
+      int tr, tc;
+      tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+      if constexpr (CHUNK > 0) {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) acc[j] = 0.0f;
+      }
+      for (int kb = 0; kb < p.kb; kb += CHUNK ? CHUNK : p.kb, ++ch) {
+        if (!__all_sync(0xffffffffu, mbar_wait_cluster(tfull, (uint32_t)(ch & 1), limit) ? 1 : 0)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int c0 = 0; c0 < kCols; c0 += 32) {
+          uint32_t v[32];
+          tmem_ld32_issue(taddr + c0, v);
+          tmem_ld_wait32(v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) acc[c0 + j] = CHUNK ? acc[c0 + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(leader_tempty);
+      }
+      if (ok)
+        f8_emit<TC, true, kCols>(p.out, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32 + lane, (int64_t)tc * kBN + half * kCols, acc);
+      else if (lane == 0)
+        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // the pair's instructions read both CTAs' memory: neither leaves first
+  if (warp == 1) tmem_dealloc_pair(tmem, kTmem);
+}
+
+}  // namespace
+
+template <typename TC>
+int f8_mx_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
+  static std::atomic<bool> configured[64];
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return B2_ERR_LAUNCH;
+  auto kfn = f8_mx_kernel<TC, sizeof(TC) == 4 ? 16 : 0>;
+  if (!configured[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(kfn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) return B2_ERR_LAUNCH;
+    configured[dev].store(true, std::memory_order_release);
+  }
+  CUtensorMap mr, mc;
+  if (!f8_map(&mr, r.p, r.mn ? r.n : k, r.mn ? k : r.n, r.ld, 128) || !f8_map(&mc, c.p, c.mn ? c.n : k, c.mn ? k : c.n, c.ld, 128))
+    return B2_ERR_LAUNCH;
+  const int64_t tr = blocks_of(r.n, 2 * kRows), tc = blocks_of(c.n, kBN);
+  if (tr * tc > 0x3fffffffLL) return B2_ERR_VARIANT;
+  a.out.rows = r.n, a.out.cols = c.n, a.r_mn = r.mn, a.c_mn = c.mn, a.sr = r.s, a.sc = c.s;
+  a.tiles_r = (int)tr, a.tiles_c = (int)tc, a.splits = 1, a.group = 8;
+  const int tiles = a.tiles_r * a.tiles_c, pairs = sm_count_cached() / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim = {2, 1, 1};
+  cfg.attrs = at, cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kfn, a, mr, mc) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+}
+template int f8_mx_launch<float>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_mx_launch<__nv_bfloat16>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+
+}  // namespace b2
