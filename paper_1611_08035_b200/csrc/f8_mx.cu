@@ -20,12 +20,15 @@ namespace b2 {
 namespace {
 
 constexpr int kBN = 256;                       // columns of the pair's tile
-constexpr int kStages = 6, kSlots = 4;         // operand ring, scale ring
-constexpr uint32_t kStageBytes = 2 * kRowStage;  // a CTA's halves of both operands
+constexpr int kStages = 3, kSlots = 4;         // operand ring, scale ring
+constexpr int kPerStage = 2;                   // blocks of a stage
+constexpr uint32_t kBlockBytes = 2 * kRowStage;  // a CTA's halves of both operands, a block
+constexpr uint32_t kStageBytes = kPerStage * kBlockBytes;
 constexpr uint32_t kRing = kStageBytes * kStages;
-constexpr size_t kSmem = 1024 + kRing + 512;
 constexpr int kThreads = 512, kEW = 8, kCols = kBN / 2;
 constexpr uint32_t kTmem = 512, kSfCols = 12;  // scales of four blocks: 128 rows in 4 columns, 256 columns in 8
+constexpr uint32_t kSfBytes = 2 * kSfCols * 32 * 4;
+constexpr size_t kSmem = 1024 + kRing + 512 + kSfBytes + kEW * kEmitBytes;
 
 __device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                         uint32_t accumulate) {
@@ -71,6 +74,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* tempty = tfull + 1;
   uint64_t* drained = tempty + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+  uint32_t* sf_words = reinterpret_cast<uint32_t*>(ring + kRing + 512);  // [2][kSfCols][32]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank();
@@ -101,67 +105,89 @@ __global__ void __launch_bounds__(kThreads, 1)
     // registers: 4 x 128 at launch; 64 + 80 + 2 x 184 = 512 after the moves
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0 && lane == 0) {
-      int it = 0;
+      RingPos<kStages> pos;
+      int filled = 0;  // stages that have been filled at least once
+      const uint32_t leader_full = cluster_map_shared(smem_u32(full), 0);
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
         int tr, tc;
         tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
         const int r0 = tr * 2 * kRows + (int)rank * kRows, c0 = tc * kBN + (int)rank * (kBN / 2);
-        for (int kb = 0; kb < p.kb; ++kb, ++it) {
-          const int s = it % kStages, r = it / kStages;
-          if (r > 0 && !mbar_wait_cluster(&empty[s], (uint32_t)((r - 1) & 1))) {
+        for (int kb = 0; kb < p.kb; kb += kPerStage, pos.next()) {
+          const int s = pos.s, here = min(kPerStage, p.kb - kb);
+          if (filled < kStages) {
+            ++filled;
+          } else if (!mbar_wait_bounded(&empty[s], pos.phase ^ 1u)) {
             ok = false;
             break;
           }
-          unsigned char* st = ring + (size_t)s * kStageBytes;
-          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kStageBytes);
-          const uint32_t bar = cluster_map_shared(smem_u32(&full[s]), 0);
-          const int k0 = kb * kF8Block;
-          tma_load_2d_pair(st, &map_r, p.r_mn ? r0 : k0, p.r_mn ? k0 : r0, bar);
-          tma_load_2d_pair(st + kRowStage, &map_c, p.c_mn ? c0 : k0, p.c_mn ? k0 : c0, bar);
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kBlockBytes * here);
+          for (int h = 0; h < here; ++h) {
+            unsigned char* st = ring + (size_t)s * kStageBytes + (size_t)h * kBlockBytes;
+            const int k0 = (kb + h) * kF8Block;
+            tma_load_2d_pair(st, &map_r, p.r_mn ? r0 : k0, p.r_mn ? k0 : r0, leader_full + 8u * s);
+            tma_load_2d_pair(st + kRowStage, &map_c, p.c_mn ? c0 : k0, p.c_mn ? k0 : c0, leader_full + 8u * s);
+          }
         }
       }
       if (!ok) {
         atomicExch(p.status, (int)B2_ERR_TIMEOUT);
         if (rank == 0)  // both CTAs' copies are counted here; no CTA leaves before the barrier at the end
-          for (int s = 0; s < kStages; ++s)
-            if (it > s) (void)mbar_wait_cluster(&full[s], (uint32_t)(((it - 1 - s) / kStages) & 1), kDrainLimitNs);
+          for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_bounded(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
       }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
-      int it = 0, grp = 0, ch = 0;
+    } else if (warp == 1 && rank == 0) {
+      RingPos<kStages> pos;
+      RingPos<kSlots> slot;
+      const uint32_t a0 = smem_u32(ring), b0 = a0 + kRowStage;
+      const uint64_t da0 = p.r_mn ? umma_desc_mn_major_sw128(a0, kRowStage) : umma_desc_k_major_sw128(a0);
+      const uint64_t db0 = p.c_mn ? umma_desc_mn_major_sw128(b0, kRowStage) : umma_desc_k_major_sw128(b0);
+      const uint32_t step_a = p.r_mn ? 4096 : 32, step_b = p.c_mn ? 4096 : 32;  // bytes between instructions of a block
+      const uint32_t idesc0 = umma_idesc_mx(2 * kRows, kBN, p.r_mn, p.c_mn, 0);
+      // The instructions of a stage go out as fast as the tensor core takes them, one or two ahead of the one it works on; what
+      // this warp does between two stages is free only as far as those cover it.  Hence two blocks to a stage, and a look
+      // at the next stage's barrier, which is usually complete, right after.
+      int ch = 0, in = 0;
+      bool ready = false;
       for (int tile = pair; tile < tiles && ok; tile += pairs) {
-        for (int kb = 0; kb < p.kb; ++kb, ++it) {
-          const int s = it % kStages, in = CHUNK ? kb % CHUNK : kb, slot = grp % kSlots;
-          if ((in == 0 && ch > 0 && !mbar_wait_cluster(tempty, (uint32_t)((ch - 1) & 1))) ||
-              ((kb & 3) == 0 && !mbar_wait_cluster(&sf_full[slot], (uint32_t)((grp / kSlots) & 1))) ||
-              !mbar_wait_cluster(&full[s], (uint32_t)((it / kStages) & 1))) {
+        for (int kb = 0; kb < p.kb; kb += kPerStage) {
+          const int s = pos.s, byte = kb & 3;
+          if ((!ready && !mbar_wait_warp(&full[s], pos.phase)) || (byte == 0 && !mbar_wait_warp(&sf_full[slot.s], slot.phase)) ||
+              (in == 0 && ch > 0 && !mbar_wait_warp(tempty, (uint32_t)((ch - 1) & 1)))) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t a0 = smem_u32(ring + (size_t)s * kStageBytes), b0 = a0 + kRowStage;
-          const uint32_t sfa = tmem + kBN + slot * kSfCols, sfb = sfa + 4;
-          const uint32_t idesc = umma_idesc_mx(2 * kRows, kBN, p.r_mn, p.c_mn, kb & 3);
+          const bool two = kb + 1 < p.kb, last = kb + 2 >= p.kb, end = last || (CHUNK && in + kPerStage == CHUNK);
+          const uint64_t da = umma_desc_advance(da0, (uint32_t)s * kStageBytes), db = umma_desc_advance(db0, (uint32_t)s * kStageBytes);
+          const uint32_t sfa = tmem + kBN + slot.s * kSfCols, idesc = idesc0 | ((uint32_t)byte << 4) | ((uint32_t)byte << 29);
+          if (elect_one()) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint64_t da = p.r_mn ? umma_desc_mn_major_sw128(a0 + j * 4096, kRowStage) : umma_desc_k_major_sw128(a0 + j * 32);
-            const uint64_t db = p.c_mn ? umma_desc_mn_major_sw128(b0 + j * 4096, kRowStage) : umma_desc_k_major_sw128(b0 + j * 32);
-            umma_mx(tmem, da, db, idesc, sfa, sfb, (in | j) != 0 ? 1u : 0u);
+            for (int j = 0; j < 4; ++j)
+              umma_mx(tmem, umma_desc_advance(da, j * step_a), umma_desc_advance(db, j * step_b), idesc, sfa, sfa + 4, (in | j) != 0 ? 1u : 0u);
+            if (two) {
+              constexpr uint32_t next_byte = (1u << 4) | (1u << 29);  // byte is even
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                umma_mx(tmem, umma_desc_advance(da, kBlockBytes + j * step_a), umma_desc_advance(db, kBlockBytes + j * step_b), idesc | next_byte, sfa,
+                        sfa + 4, 1u);
+            }
+            umma_commit_pair(&empty[s]);
+            if (byte == 2 || last) umma_commit_pair(&sf_empty[slot.s]);
+            if (end) umma_commit_pair(tfull);
           }
-          umma_commit_pair(&empty[s]);
-          if ((kb & 3) == 3 || kb == p.kb - 1) {
-            umma_commit_pair(&sf_empty[slot]);
-            ++grp;
-          }
-          if ((CHUNK && in == CHUNK - 1) || kb == p.kb - 1) {
-            umma_commit_pair(tfull);
-            ++ch;
-          }
+          __syncwarp();
+          if (byte == 2 || last) slot.next();
+          in += kPerStage;
+          if (end) ++ch, in = 0;
+          pos.next();
+          ready = mbar_test_warp(&full[pos.s], pos.phase);
         }
       }
       if (!ok) {
-        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-        umma_commit_pair(drained);
-        (void)mbar_wait_cluster(drained, 0, kDrainLimitNs);
+        if (elect_one()) {
+          atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+          umma_commit_pair(drained);
+        }
+        (void)mbar_wait_warp(drained, 0, kDrainLimitNs);
       }
     }
   } else if (warp < 8) {
@@ -173,14 +199,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
       const int64_t r0 = (int64_t)tr * 2 * kRows + rank * kRows + lane, c0 = (int64_t)tc * kBN + lane;
+      // Tensor memory wants every word four times, once for each quarter of its lanes.  Each warp fetches a quarter of the
+      // words, one group ahead, and the four swap them through shared memory: rows of scales lie far apart, so fetching is what
+      // these warps spend their time on (all of them fetching all: 8192^3 514 us).
+      uint32_t next[3];
+      auto fetch = [&](int kb) {
+        next[0] = scale_word(p.sr, r0 + 32 * quad, p.out.rows, kb, p.kb);
+        next[1] = scale_word(p.sc, c0 + 64 * quad, p.out.cols, kb, p.kb);
+        next[2] = scale_word(p.sc, c0 + 64 * quad + 32, p.out.cols, kb, p.kb);
+      };
+      fetch(0);
       for (int kb = 0; kb < p.kb; kb += 4, ++grp) {
         const int slot = grp % kSlots, r = grp / kSlots;
+        uint32_t* words = sf_words + (grp & 1) * kSfCols * 32 + lane;
+        words[quad * 32] = next[0], words[(4 + 2 * quad) * 32] = next[1], words[(5 + 2 * quad) * 32] = next[2];
+        asm volatile("bar.sync 1, 128;" ::: "memory");  // also: everyone has read the buffer of two groups ago
+        if (kb + 4 < p.kb) fetch(kb + 4);
         uint32_t w[kSfCols];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = scale_word(p.sr, r0 + 32 * i, p.out.rows, kb, p.kb);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[4 + i] = scale_word(p.sc, c0 + 32 * i, p.out.cols, kb, p.kb);
-        if (r > 0 && !__all_sync(0xffffffffu, mbar_wait_cluster(&sf_empty[slot], (uint32_t)((r - 1) & 1)) ? 1 : 0)) {
+        for (int i = 0; i < (int)kSfCols; ++i) w[i] = words[i * 32];
+        if (r > 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(&sf_empty[slot], (uint32_t)((r - 1) & 1)) ? 1 : 0)) {
           ok = false;
           break;
         }
@@ -200,6 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
     const uint32_t leader_tempty = cluster_map_shared(smem_u32(tempty), 0);
     const uint64_t limit = kWaitLimitNs + (uint64_t)p.kb * 8192ull;  // outlasts the k loop that it waits for
+    unsigned char* stage = ring + kRing + 512 + kSfBytes + (warp - 8) * kEmitBytes;
     float acc[kCols];
     int ch = 0;
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
@@ -210,27 +249,43 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int j = 0; j < kCols; ++j) acc[j] = 0.0f;
       }
       for (int kb = 0; kb < p.kb; kb += CHUNK ? CHUNK : p.kb, ++ch) {
-        if (!__all_sync(0xffffffffu, mbar_wait_cluster(tfull, (uint32_t)(ch & 1), limit) ? 1 : 0)) {
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded(tfull, (uint32_t)(ch & 1), limit) ? 1 : 0)) {
           ok = false;
           break;
         }
         tc_fence_after();
+        if constexpr (CHUNK == 0) {
+          uint32_t v[kCols / 32][32];
 #pragma unroll
-        for (int c0 = 0; c0 < kCols; c0 += 32) {
-          uint32_t v[32];
-          tmem_ld32_issue(taddr + c0, v);
-          tmem_ld_wait32(v);
+          for (int i = 0; i < kCols / 32; ++i) tmem_ld32_issue(taddr + 32 * i, v[i]);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) acc[c0 + j] = CHUNK ? acc[c0 + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+          for (int i = 0; i < kCols / 32; ++i) {
+            tmem_ld_wait32(v[i]);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) acc[32 * i + j] = __uint_as_float(v[i][j]);
+          }
+        } else {
+#pragma unroll
+          for (int c0 = 0; c0 < kCols; c0 += 32) {
+            uint32_t v[32];
+            tmem_ld32_issue(taddr + c0, v);
+            tmem_ld_wait32(v);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) acc[c0 + j] += __uint_as_float(v[j]);
+          }
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(leader_tempty);
       }
-      if (ok)
-        f8_emit<TC, true, kCols>(p.out, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32 + lane, (int64_t)tc * kBN + half * kCols, acc);
-      else if (lane == 0)
-        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+      const int64_t row0 = (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, col0 = (int64_t)tc * kBN + half * kCols;
+      if (!ok) {
+        if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+      } else if (p.out.vec) {
+        f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
+      } else {
+        f8_emit<TC, true, kCols>(p.out, row0 + lane, col0, acc);
+      }
     }
   }
   __syncwarp();

@@ -59,6 +59,81 @@ __device__ __forceinline__ void f8_emit(const F8Out& p, int64_t row, int64_t col
   }
 }
 
+// The same for a warp whose lanes own 32 consecutive rows (row0 + lane) and N consecutive columns each, columns
+// contiguous and aligned in C.  64 bytes of every row pass through shared memory at a time and leave as whole 64-byte pieces
+// of eight rows an instruction: a lane that stores its own row directly touches 32 lines with every instruction (a 256 x 256
+// bf16 tile: 8000 clocks of storing, as long as the multiply-adds of 2000 summed elements).
+constexpr int kEmitPitch = 80;  // bytes between staged rows: 16-byte pieces of eight rows in different banks
+constexpr int kEmitBytes = 32 * kEmitPitch;
+template <typename TC, int N>
+__device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int64_t col0, const float* acc, unsigned char* stage) {
+  const int lane = threadIdx.x & 31, piece = lane & 3;
+  TC* C = static_cast<TC*>(p.C);
+  unsigned char* own = stage + lane * kEmitPitch;
+  const unsigned char* swap = stage + (lane >> 2) * kEmitPitch + piece * 16;
+  if (sizeof(TC) == 2 && p.beta == 0.0f) {
+#pragma unroll
+    for (int j = 0; j < N; j += 32) {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float* a = acc + j + 8 * i;
+        *reinterpret_cast<uint4*>(own + 16 * i) = make_uint4(pack_bf16(p.alpha * a[0], p.alpha * a[1]), pack_bf16(p.alpha * a[2], p.alpha * a[3]),
+                                                             pack_bf16(p.alpha * a[4], p.alpha * a[5]), pack_bf16(p.alpha * a[6], p.alpha * a[7]));
+      }
+      __syncwarp();
+      const int64_t col = col0 + j + piece * 8, nv = p.cols - col;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + 8 * i + (lane >> 2);
+        const uint4 q = *reinterpret_cast<const uint4*>(swap + 8 * i * kEmitPitch);
+        if (row < p.rows) {
+          if (nv >= 8) {
+            *reinterpret_cast<uint4*>(C + row * p.ldc + col) = q;
+          } else {
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            uint16_t* c = reinterpret_cast<uint16_t*>(C + row * p.ldc + col);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e < nv) c[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+          }
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; j += 16) {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(own + 16 * i) = make_float4(p.alpha * acc[j + 4 * i], p.alpha * acc[j + 4 * i + 1], p.alpha * acc[j + 4 * i + 2], p.alpha * acc[j + 4 * i + 3]);
+      __syncwarp();
+      const int64_t col = col0 + j + piece * 4, nv = p.cols - col;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + 8 * i + (lane >> 2);
+        const float4 q = *reinterpret_cast<const float4*>(swap + 8 * i * kEmitPitch);
+        float v[4] = {q.x, q.y, q.z, q.w};
+        if (row < p.rows) {
+          TC* c = C + row * p.ldc + col;
+          if (p.beta != 0.0f) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e < nv) v[e] += p.beta * f8_load1(c + e);
+          }
+          if (sizeof(TC) == 4 && nv >= 4) {
+            *reinterpret_cast<float4*>(c) = make_float4(v[0], v[1], v[2], v[3]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e < nv) f8_store1(c + e, v[e]);
+          }
+        }
+      }
+    }
+  }
+}
+
 // Joining the shares of a k split: the CTAs of a cluster (rank = share) have each put their part of the 128 x TBN tile
 // into their shared memory as floats [column][row]; each adds all parts, in the order of the ranks, for its columns.  All
 // threads of all CTAs of the cluster call this; warps with writer >= 0 (0 .. EW-1, covering the tensor-memory lanes 32 *

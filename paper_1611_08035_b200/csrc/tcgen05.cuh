@@ -97,33 +97,12 @@ __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorM
       ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(c_inner), "r"(c_outer), "r"(bar)
       : "memory");
 }
-// arrival on a barrier of another CTA of the cluster (cluster_map_shared), releasing at cluster scope
+// Arrival on a barrier of another CTA of the cluster (cluster_map_shared).  The waiting side acquires at its own CTA's
+// scope: what these barriers hand over is tensor memory and shared memory that only the tensor core and TMA touch, ordered by
+// their own fences.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// bounded wait for a phase that arrivals from the other CTA complete
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, uint64_t limit_ns = kWaitLimitNs) {
-  auto poll = [&]() {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return done != 0;
-  };
-  if (poll()) return true;
-  const uint64_t t0 = global_timer_ns();
-  do {
-#pragma unroll 1
-    for (int i = 0; i < 32; ++i)
-      if (poll()) return true;
-  } while (global_timer_ns() - t0 < limit_ns);
-  return false;
-}
-
 // Shared-memory matrix descriptor of a K-major operand tile stored as rows of 128 bytes (32 floats) with the
 // 128-byte swizzle: 8-row groups are 1024 bytes apart (stride byte offset), the leading byte offset is not
 // used by swizzled K-major layouts, descriptor version 1, layout type 2 (128-byte swizzle).
@@ -149,6 +128,40 @@ __device__ __forceinline__ uint64_t umma_desc_mn_major_sw128(uint32_t smem_addr,
   d |= (uint64_t)2 << 61;
   return d;
 }
+
+// The descriptor of a tile `bytes` further in shared memory (the address field holds 16-byte units below 2^14, so that
+// the addition never leaves it).
+__device__ __forceinline__ uint64_t umma_desc_advance(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
+
+// One lane of a converged warp.  The warp that feeds the tensor core runs its loop as a whole and only the instructions
+// themselves are under this predicate: their descriptors and addresses are uniform registers, which the compiler computes
+// in place in convergent code and moves over one by one in a branch that a single lane takes.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(e));
+  return e != 0;
+}
+// the same answer in all lanes
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, uint64_t limit_ns = kWaitLimitNs) {
+  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, limit_ns) ? 1 : 0) != 0;
+}
+__device__ __forceinline__ bool mbar_test_warp(uint64_t* bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, mbar_test_wait(bar, parity) ? 1 : 0) != 0;
+}
+
+// Position in a ring of N stages and the parity of its current round.
+template <int N>
+struct RingPos {
+  int s = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++s == N) s = 0, phase ^= 1u;
+  }
+};
 
 // ---- host: the driver's tensor-map encoder, looked up once ------------------------------------------
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
