@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN>::NT, 1)
     int tr, tc;
     tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
     f8_split_join<TC, COLS_CONTIG, TBN, EW>(p.out, ring, p.splits, share, warp >= 2 && ok ? warp - 2 : -1, warp & 3,
-                                            (int64_t)tr * kRows, (int64_t)tc * TBN);
+                                            (int64_t)tr * kRows + (warp & 3) * 32 + lane, (int64_t)tc * TBN);
   }
   tc_fence_before();
   __syncthreads();

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int s = pos.s, here = min(kPerStage, p.kb - kb);
           if (filled < kStages) {
             ++filled;
-          } else if (!mbar_wait_bounded(&empty[s], pos.phase ^ 1u)) {
+          } else if (!mbar_wait_lane(&empty[s], pos.phase ^ 1u)) {
             ok = false;
             break;
           }
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) {
         atomicExch(p.status, (int)B2_ERR_TIMEOUT);
         if (rank == 0)  // both CTAs' copies are counted here; no CTA leaves before the barrier at the end
-          for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_bounded(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
+          for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_lane(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
       }
     } else if (warp == 1 && rank == 0) {
       RingPos<kStages> pos;
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t w[kSfCols];
 #pragma unroll
         for (int i = 0; i < (int)kSfCols; ++i) w[i] = words[i * 32];
-        if (r > 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(&sf_empty[slot], (uint32_t)((r - 1) & 1)) ? 1 : 0)) {
+        if (r > 0 && !mbar_wait_warp(&sf_empty[slot], (uint32_t)((r - 1) & 1))) {
           ok = false;
           break;
         }
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int j = 0; j < kCols; ++j) acc[j] = 0.0f;
       }
       for (int kb = 0; kb < p.kb; kb += CHUNK ? CHUNK : p.kb, ++ch) {
-        if (!__all_sync(0xffffffffu, mbar_wait_bounded(tfull, (uint32_t)(ch & 1), limit) ? 1 : 0)) {
+        if (!mbar_wait_warp(tfull, (uint32_t)(ch & 1), limit)) {
           ok = false;
           break;
         }

@@ -137,10 +137,10 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
 // Joining the shares of a k split: the CTAs of a cluster (rank = share) have each put their part of the 128 x TBN tile
 // into their shared memory as floats [column][row]; each adds all parts, in the order of the ranks, for its columns.  All
 // threads of all CTAs of the cluster call this; warps with writer >= 0 (0 .. EW-1, covering the tensor-memory lanes 32 *
-// quad .. + 31) add and write.
+// quad .. + 31) add and write; `row` is the row of C that this lane's accumulators belong to.
 template <typename TC, bool COLS_CONTIG, int TBN, int EW>
 __device__ __forceinline__ void f8_split_join(const F8Out& p, const void* tile, int splits, int share, int writer, int quad,
-                                              int64_t row0, int64_t col0) {
+                                              int64_t row, int64_t col0) {
   cluster_sync_all();
   if (writer >= 0) {
     const int lane = threadIdx.x & 31;
@@ -159,7 +159,7 @@ __device__ __forceinline__ void f8_split_join(const F8Out& p, const void* tile, 
           v[g] += x;
         }
       }
-      f8_emit<TC, COLS_CONTIG, G>(p, row0 + quad * 32 + lane, col0 + c, v);
+      f8_emit<TC, COLS_CONTIG, G>(p, row, col0 + c, v);
     }
   }
   __syncwarp();

@@ -6,9 +6,16 @@
 // b2_gemm_f8.  It is a power of two, though, so q*s IS a bf16 number, and the product is a bf16 one on exact operands:
 // 8-bit numbers are fetched, and turned into bf16 on their way to the tensor core.
 //
-// Roles of a CTA: warp 0 streams 64 tokens at a time of both operands with TMA, warp 1 issues tcgen05.mma, four warps
-// turn the 8-bit tile into the bf16 tile the multiply reads (128-byte swizzle), eight warps add the sums of kChunk
-// tokens to fp32 accumulators in registers (two tensor-memory buffers in turn) and write C.
+// Large gradients go to pairs of CTAs (256 features by 256 columns of Y, cta_group::2), small ones to single CTAs (128 x 128)
+// whose k range may be shared by a cluster.  Either way a CTA fetches and converts 128 features by 64 tokens a stage and
+// fetches 128 columns of Y.
+//
+// Roles of a CTA: warp 0 streams 64 tokens at a time of both operands with TMA, warp 1 issues tcgen05.mma (of a pair:
+// the leader's), warps 4-11 turn the 8-bit tile into the bf16 tile the multiply reads (128-byte swizzle), warps 12-19 add
+// the sums of kChunk stages to fp32 accumulators in registers (two tensor-memory buffers in turn) and write C.
+//
+// What bounds it: shared memory.  A stage's 512 clocks of tensor pipe come with 24 KB written by TMA, 8 KB read and 16 KB
+// written by the conversion and 32 KB read by the multiply: 640 clocks at 128 bytes each.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -40,25 +47,41 @@ struct WgArgs {
   int* status;
 };
 
-template <int TBN>
+template <int CTAS>
 struct WgCfg {
-  static constexpr int EW = 8, CW = 4;
+  static constexpr int TBN = CTAS * 128;  // columns of the tile
+  static constexpr int EW = 8, CW = 4;    // warps that accumulate, warps that convert a stage (two groups of them in turn)
   static constexpr int COLS = TBN / 2;
-  static constexpr int NT = 512;  // four warpgroups: roles, converters, two that accumulate
-  static constexpr uint32_t STAGE = kRaw + kAct + TBN * kTok * 2;
-  static constexpr int STAGES = TBN == 256 ? 4 : 5;
-  static constexpr uint32_t RING = STAGE * STAGES;
+  static constexpr int NT = 640;  // five warpgroups: roles, two that convert, two that accumulate
+  static constexpr uint32_t YTILE = 128 * kTok * 2, STAGE = kRaw + kAct + YTILE;
+  static constexpr int STAGES = 5;
+  static constexpr uint32_t RING = STAGE * STAGES, TMEM = 2 * TBN;
   static constexpr size_t SMEM = 1024 + RING + 512;
-  static_assert(kRows * TBN * 4 <= RING, "the split's shares pass through the ring");
+  static_assert(kRows * 128 * 4 <= RING, "the split's shares pass through the ring");
 };
 
+template <int CTAS>
 __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
-      : "memory");
+  if constexpr (CTAS == 2) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  }
+}
+template <int CTAS>
+__device__ __forceinline__ void wg_commit(uint64_t* bar) {
+  if constexpr (CTAS == 2) umma_commit_pair(bar);
+  else umma_commit(bar);
 }
 // fp32 accumulator, both operands bf16 with their own index contiguous
 __host__ __device__ constexpr uint32_t umma_idesc_bf16_mn(int m, int n) {
@@ -70,19 +93,38 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
-// Two e4m3 numbers (the upper bytes of the halves of x) times 2^(byte-127) as bf16.  With the four exponent and three
-// mantissa bits moved to the top of bf16's, the number reads as its value times 2^(7-127), subnormal e4m3
-// numbers as subnormal bf16 ones; f1 * f2 = 2^120 * scale puts the exponent right, exactly.
-__device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t x, uint32_t f1, uint32_t f2) {
-  const uint32_t r = (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u);
-  return mul_bf16x2(mul_bf16x2(r, f1), f2);
+// Four e4m3 numbers b0..b3 of a word as bf16 pairs (b0, b2) and (b1, b3) times 2^-120: with the four exponent and three
+// mantissa bits at the top of bf16's, subnormal numbers become subnormal ones and nothing is rounded.  Splitting the word
+// into even and odd bytes saves the permutations that the order b0..b3 would take; the product's rows are in the same order, and
+// are put back where they are written (kept_row).
+__device__ __forceinline__ uint32_t e4m3_even(uint32_t w) { return ((w << 8) & 0x80008000u) | ((w << 4) & 0x07f007f0u); }
+__device__ __forceinline__ uint32_t e4m3_odd(uint32_t w) { return (w & 0x80008000u) | ((w >> 4) & 0x07f007f0u); }
+__device__ __forceinline__ int kept_row(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
+
+// Eight e4m3 numbers to bf16, times 2^120 * scale.
+__device__ __forceinline__ uint4 e4m3x8_to_bf16(uint2 w, uint32_t f1) {
+  return make_uint4(mul_bf16x2(e4m3_even(w.x), f1), mul_bf16x2(e4m3_odd(w.x), f1), mul_bf16x2(e4m3_even(w.y), f1),
+                    mul_bf16x2(e4m3_odd(w.y), f1));
+}
+// bit 7 of a byte of the result is set where the number (or its carry's neighbour) may be e4m3's NaN, 0x7f
+__device__ __forceinline__ uint32_t e4m3_nan_bits(uint2 w) {
+  return (((w.x & 0x7f7f7f7fu) + 0x01010101u) | ((w.y & 0x7f7f7f7fu) + 0x01010101u)) & 0x80808080u;
+}
+// The arithmetic above reads a NaN as 480: put NaNs where the numbers are NaN.
+__device__ __forceinline__ uint4 e4m3x8_nans(uint2 w, uint4 o) {
+  auto fix = [](uint32_t word, int lo, int hi, uint32_t r) {
+    if (((word >> (8 * lo)) & 0x7fu) == 0x7fu) r |= 0x7fc0u;
+    if (((word >> (8 * hi)) & 0x7fu) == 0x7fu) r |= 0x7fc00000u;
+    return r;
+  };
+  return make_uint4(fix(w.x, 0, 2, o.x), fix(w.x, 1, 3, o.y), fix(w.y, 0, 2, o.z), fix(w.y, 1, 3, o.w));
 }
 
-template <int TBN, typename TC>
-__global__ void __launch_bounds__(WgCfg<TBN>::NT, 1)
+template <int CTAS, typename TC>
+__global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
     wgrad_kernel(const WgArgs p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_y) {
-  using Cfg = WgCfg<TBN>;
-  constexpr int EW = Cfg::EW, CW = Cfg::CW, COLS = Cfg::COLS, STAGES = Cfg::STAGES;
+  using Cfg = WgCfg<CTAS>;
+  constexpr int EW = Cfg::EW, CW = Cfg::CW, COLS = Cfg::COLS, STAGES = Cfg::STAGES, TBN = Cfg::TBN;
   extern __shared__ unsigned char wg_smem_raw[];
   const uint32_t raw = smem_u32(wg_smem_raw);
   unsigned char* ring = wg_smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -95,152 +137,192 @@ __global__ void __launch_bounds__(WgCfg<TBN>::NT, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = CTAS == 2 ? cluster_rank() : 0;
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 1);
-      mbar_init(&conv[s], CW);
+      mbar_init(&full[s], 3);
+      mbar_init(&conv[s], CTAS * CW);
       mbar_init(&empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&tfull[b], 1);
-      mbar_init(&tempty[b], EW);
+      mbar_init(&tempty[b], CTAS * EW);
     }
     mbar_init(drained, 1);
     mbar_fence_init();
   }
-  if (warp == 1) tmem_alloc(tmem_slot, 2 * TBN);
+  if (warp == 1) {
+    if (CTAS == 2) tmem_alloc_pair(tmem_slot, Cfg::TMEM);
+    else tmem_alloc(tmem_slot, Cfg::TMEM);
+  }
   tc_fence_before();
   __syncthreads();
+  if (CTAS == 2) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  const int tiles = p.tiles_r * p.tiles_c, share = blockIdx.y;
+  const int tiles = p.tiles_r * p.tiles_c, share = CTAS == 2 ? 0 : blockIdx.y;
+  const int first = blockIdx.x / CTAS, stride = gridDim.x / CTAS;
   const int kb0 = (int)((int64_t)p.kb * share / p.splits), kb1 = (int)((int64_t)p.kb * (share + 1) / p.splits);
+  // address of a barrier of the CTA that issues the multiply-adds
+  auto leader = [&](uint64_t* bar) { return CTAS == 2 ? cluster_map_shared(smem_u32(bar), 0) : smem_u32(bar); };
+  auto arrive_leader = [&](uint32_t addr) {
+    if (CTAS == 2) mbar_arrive_cluster(addr);
+    else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr) : "memory");
+  };
   bool ok = true;
 
+  // registers: 5 x 96 at launch; 40 + 2 x 64 + 2 x 152 = 472 after the moves
   if (warp < 4) {
-    // registers: 4 x 128 at launch; 64 + 96 + 2 x 176 = 512 after the moves
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    if (warp == 0 && lane == 0) {
-      int it = 0;
-      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp != 1) {
+      // warp 0 fetches the activation, warps 2 and 3 half of Y's columns each: one thread issuing all three boxes of a stage
+      // needs about 1000 clocks for them
+      RingPos<STAGES> pos;
+      int filled = 0;
+      const CUtensorMap* map = warp == 0 ? &map_q : &map_y;
+      const uint32_t bytes = warp == 0 ? kRaw : Cfg::YTILE / 2, at = warp == 0 ? kAct : kAct + kRaw + (warp - 2) * (Cfg::YTILE / 2);
+      for (int tile = first; tile < tiles && ok; tile += stride) {
         int tr, tc;
         tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-          const int s = it % STAGES, r = it / STAGES;
-          if (r > 0 && !mbar_wait_bounded(&empty[s], (uint32_t)((r - 1) & 1))) {
+        const int x = warp == 0 ? (tr * CTAS + (int)rank) * kRows : tc * TBN + (int)rank * 128 + (warp - 2) * 64;
+        for (int kb = kb0; kb < kb1; ++kb, pos.next()) {
+          const int s = pos.s;
+          if (filled < STAGES) {
+            ++filled;
+          } else if (!mbar_wait_warp(&empty[s], pos.phase ^ 1u)) {
             ok = false;
             break;
           }
-          unsigned char* st = ring + (size_t)s * Cfg::STAGE;
-          mbar_arrive_expect_tx(&full[s], Cfg::STAGE - kAct);
-          tma_load_2d(st + kAct, &map_q, tr * kRows, kb * kTok, &full[s]);
-#pragma unroll
-          for (int j = 0; j < TBN / 64; ++j)
-            tma_load_2d(st + kAct + kRaw + j * 8192, &map_y, tc * TBN + j * 64, kb * kTok, &full[s]);
+          if (elect_one()) {
+            mbar_arrive_expect_tx(&full[s], bytes);
+            tma_load_2d(ring + (size_t)s * Cfg::STAGE + at, map, x, kb * kTok, &full[s]);
+          }
+          __syncwarp();
         }
       }
       if (!ok) {
-        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-        for (int s = 0; s < STAGES; ++s)
-          if (it > s) (void)mbar_wait_bounded(&full[s], (uint32_t)(((it - 1 - s) / STAGES) & 1), kDrainLimitNs);
+        if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+        for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_warp(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
       }
-    } else if (warp == 1 && lane == 0) {
-      constexpr uint32_t idesc = umma_idesc_bf16_mn(kRows, TBN);
-      int it = 0, ch = 0;
-      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-          const int s = it % STAGES, in = (kb - kb0) % kChunk, b = ch & 1;
-          const uint32_t phase = (uint32_t)((it / STAGES) & 1);
-          if ((in == 0 && ch >= 2 && !mbar_wait_bounded(&tempty[b], (uint32_t)(((ch >> 1) - 1) & 1))) ||
-              !mbar_wait_bounded(&full[s], phase) || !mbar_wait_bounded(&conv[s], phase)) {
+    } else if (warp == 1 && rank == 0) {
+      constexpr uint32_t idesc = umma_idesc_bf16_mn(CTAS * kRows, TBN);
+      const uint32_t base = smem_u32(ring);
+      const uint64_t da0 = umma_desc_mn_major_sw128(base, 8192), db0 = umma_desc_mn_major_sw128(base + kAct + kRaw, 8192);
+      RingPos<STAGES> pos;
+      int ch = 0, in = 0;
+      for (int tile = first; tile < tiles && ok; tile += stride) {
+        for (int kb = kb0; kb < kb1; ++kb) {
+          const int s = pos.s, b = ch & 1;
+          // a converted stage has also been fetched: whoever converted it had waited for both operands
+          if (!mbar_wait_warp(&conv[s], pos.phase) ||
+              (in == 0 && ch >= 2 && !mbar_wait_warp(&tempty[b], (uint32_t)(((ch >> 1) - 1) & 1)))) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t a0 = smem_u32(ring + (size_t)s * Cfg::STAGE), b0 = a0 + kAct + kRaw;
+          const uint64_t da = umma_desc_advance(da0, (uint32_t)s * Cfg::STAGE), db = umma_desc_advance(db0, (uint32_t)s * Cfg::STAGE);
+          const bool end = in == kChunk - 1 || kb == kb1 - 1;
+          if (elect_one()) {
 #pragma unroll
-          for (int j = 0; j < kTok / 16; ++j)  // 16 tokens an instruction: two groups of eight 128-byte rows
-            umma_bf16(tmem + b * TBN, umma_desc_mn_major_sw128(a0 + j * 2048, 8192), umma_desc_mn_major_sw128(b0 + j * 2048, 8192),
-                      idesc, (in | j) != 0 ? 1u : 0u);
-          umma_commit(&empty[s]);
-          if (in == kChunk - 1 || kb == kb1 - 1) {
-            umma_commit(&tfull[b]);
-            ++ch;
+            for (int j = 0; j < kTok / 16; ++j)  // 16 tokens an instruction: two groups of eight 128-byte rows
+              umma_bf16<CTAS>(tmem + b * TBN, umma_desc_advance(da, j * 2048), umma_desc_advance(db, j * 2048), idesc, (in | j) != 0 ? 1u : 0u);
+            wg_commit<CTAS>(&empty[s]);
+            if (end) wg_commit<CTAS>(&tfull[b]);
           }
+          __syncwarp();
+          ++in;
+          if (end) ++ch, in = 0;
+          pos.next();
         }
       }
       if (!ok) {
-        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-        umma_commit(drained);
-        (void)mbar_wait_bounded(drained, 0, kDrainLimitNs);
+        if (elect_one()) {
+          atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+          wg_commit<CTAS>(drained);
+        }
+        (void)mbar_wait_warp(drained, 0, kDrainLimitNs);
       }
     }
-  } else if (warp < 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    const int cw = warp - 4, f = lane & 15, th = lane >> 4;  // eight features of every other token
-    int it = 0;
-    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    // The two warpgroups convert every other stage each, a warp 16 tokens of it: what a stage costs besides the conversion (the
+    // wait, the proxy fence, the arrival) then has the time of two stages to hide in.
+    const int group = (warp - 4) >> 2, t0 = (warp & 3) * 16, f = lane & 15, th = lane >> 4;  // eight features of every other token
+    const uint32_t dst0 = (uint32_t)((f >> 3) * 8192 + t0 * 128), src0 = kAct + t0 * 128 + f * 8;
+    RingPos<STAGES> pos;
+    for (int tile = first; tile < tiles && ok; tile += stride) {
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
-      auto scale_of = [&](int kb) -> uint32_t {  // lanes 0-15: the warp's tokens of stage kb
-        const int64_t tok = (int64_t)kb * kTok + cw * 16 + f;
-        return tok < p.k ? p.S[tok * p.lds + tr] : 127u;
+      const int64_t blk = min((int64_t)tr * CTAS + rank, (p.out.rows - 1) / kF8Block);  // the tile may begin beyond the last feature
+      // Scales of two of this group's stages at a time, one token a lane, fetched while the two before are converted.
+      auto scales_of = [&](int kb) -> uint32_t {
+        const int64_t tok = (int64_t)(kb + 2 * th) * kTok + t0 + f;
+        return tok < p.k ? p.S[tok * p.lds + blk] : 127u;
       };
-      uint32_t next = kb0 < kb1 ? scale_of(kb0) : 127u;
-      for (int kb = kb0; kb < kb1; ++kb, ++it) {
-        const int s = it % STAGES;
-        const uint32_t mine = next;
-        if (kb + 1 < kb1) next = scale_of(kb + 1);
-        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (uint32_t)((it / STAGES) & 1)) ? 1 : 0)) {
+      uint32_t next = scales_of(kb0 + group), h = 0;
+      bool large = false;
+      for (int kb = kb0, own = 0; kb < kb1; ++kb, pos.next()) {
+        if (((kb - kb0) & 1) != group) continue;
+        if ((own & 1) == 0) {
+          // 2^120 * 2^(byte-127) = 2^e1 * 2^e2, both factors in range; a NaN scale makes everything NaN
+          const int e = (int)next - 7, e1 = min(e, 127), e2 = e - e1;
+          h = next == kScaleNan ? 0x7fc07fc0u : (uint32_t)(e1 + 127) << 7 | (uint32_t)(e2 + 127) << 23;
+          large = e2 > 0;
+          next = scales_of(kb + 4);
+        }
+        const int s = pos.s;
+        if (!mbar_wait_warp(&full[s], pos.phase)) {
           ok = false;
           break;
         }
-        unsigned char* act = ring + (size_t)s * Cfg::STAGE;
-        const unsigned char* src = act + kAct;
+        unsigned char* st = ring + (size_t)s * Cfg::STAGE;
+        uint2 w[8];
+        uint32_t nans = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const uint2*>(st + src0 + (2 * i + th) * 128);
+        const int src_lane = (own & 1) * 16 + th;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int t = cw * 16 + 2 * i + th;
-          const uint32_t byte = __shfl_sync(0xffffffffu, mine, 2 * i + th);
-          // 2^120 * 2^(byte-127) = 2^e1 * 2^e2 with both factors in range; a NaN scale makes everything NaN
-          const int e = (int)byte - 7, e1 = min(e, 120), e2 = e - e1;
-          const uint32_t h1 = byte == kScaleNan ? 0x7fc0u : (uint32_t)(e1 + 127) << 7, h2 = byte == kScaleNan ? 0x7fc0u : (uint32_t)(e2 + 127) << 7;
-          const uint32_t f1 = h1 * 0x10001u, f2 = h2 * 0x10001u;
-          const uint2 w = *reinterpret_cast<const uint2*>(src + t * 128 + f * 8);
-          uint4 o;
-          o.x = e4m3x2_to_bf16x2(__byte_perm(w.x, 0, 0x1404), f1, f2);
-          o.y = e4m3x2_to_bf16x2(__byte_perm(w.x, 0, 0x3424), f1, f2);
-          o.z = e4m3x2_to_bf16x2(__byte_perm(w.y, 0, 0x1404), f1, f2);
-          o.w = e4m3x2_to_bf16x2(__byte_perm(w.y, 0, 0x3424), f1, f2);
-          // the pattern of e4m3's NaN is 480 to the arithmetic above
-          if ((((w.x & 0x7f7f7f7fu) + 0x01010101u) | ((w.y & 0x7f7f7f7fu) + 0x01010101u)) & 0x80808080u) {
-            uint32_t* po = reinterpret_cast<uint32_t*>(&o);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if ((((j < 4 ? w.x : w.y) >> (8 * (j & 3))) & 0x7fu) == 0x7fu) po[j >> 1] |= 0x7fc0u << (16 * (j & 1));
-          }
-          *reinterpret_cast<uint4*>(act + (f >> 3) * 8192 + t * 128 + (((f & 7) ^ (t & 7)) << 4)) = o;
+          const int t = 2 * i + th;
+          const uint32_t hh = __shfl_sync(0xffffffffu, h, src_lane + 2 * i);
+          nans |= e4m3_nan_bits(w[i]);
+          *reinterpret_cast<uint4*>(st + dst0 + t * 128 + (((f ^ t) & 7) << 4)) =
+              e4m3x8_to_bf16(w[i], __byte_perm(hh, 0, 0x1010));
         }
+        // Rare, and therefore apart: branches among the eight conversions above would keep the compiler from overlapping them.
+        if (__any_sync(0xffffffffu, large || nans != 0)) {
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) {
+            const int t = 2 * i + th;
+            const uint32_t f2 = __byte_perm(__shfl_sync(0xffffffffu, h, src_lane + 2 * i), 0, 0x3232);
+            uint4* o = reinterpret_cast<uint4*>(st + dst0 + t * 128 + (((f ^ t) & 7) << 4));
+            const uint4 v = make_uint4(mul_bf16x2(o->x, f2), mul_bf16x2(o->y, f2), mul_bf16x2(o->z, f2), mul_bf16x2(o->w, f2));
+            *o = e4m3x8_nans(*reinterpret_cast<const uint2*>(st + src0 + t * 128), v);
+          }
+        }
+        __syncwarp();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the tensor core reads through the async proxy
         __syncwarp();
-        if (lane == 0) mbar_arrive(&conv[s]);
+        if (lane == 0) arrive_leader(leader(&conv[s]));
+        ++own;
       }
     }
     if (!ok && lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-    const int quad = warp & 3, half = (warp - 8) >> 2;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+    const int quad = warp & 3, half = (warp - 12) >> 2;
     const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * COLS);
     float acc[COLS];
     int ch = 0;
-    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+    for (int tile = first; tile < tiles && ok; tile += stride) {
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
 #pragma unroll
       for (int j = 0; j < COLS; ++j) acc[j] = 0.0f;
       for (int kb = kb0; kb < kb1; kb += kChunk, ++ch) {
         const int b = ch & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&tfull[b], (uint32_t)((ch >> 1) & 1)) ? 1 : 0)) {
+        if (!mbar_wait_warp(&tfull[b], (uint32_t)((ch >> 1) & 1))) {
           ok = false;
           break;
         }
@@ -250,19 +332,17 @@ __global__ void __launch_bounds__(WgCfg<TBN>::NT, 1)
           uint32_t v[16];
           tmem_ld16_issue(taddr + (uint32_t)(b * TBN + c0), v);
           tmem_ld_wait16(v);
-          if (c0 + 16 >= COLS) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&tempty[b]);
-          }
 #pragma unroll
           for (int j = 0; j < 16; ++j) acc[c0 + j] += __uint_as_float(v[j]);
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_leader(leader(&tempty[b]));
       }
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
       } else if (p.splits == 1) {
-        f8_emit<TC, false, COLS>(p.out, (int64_t)tr * kRows + quad * 32 + lane, (int64_t)tc * TBN + half * COLS, acc);
+        f8_emit<TC, false, COLS>(p.out, (int64_t)(tr * CTAS + (int)rank) * kRows + quad * 32 + kept_row(lane), (int64_t)tc * TBN + half * COLS, acc);
       } else {
         float* mine = reinterpret_cast<float*>(ring) + (size_t)half * COLS * kRows + quad * 32 + lane;
 #pragma unroll
@@ -271,15 +351,21 @@ __global__ void __launch_bounds__(WgCfg<TBN>::NT, 1)
     }
   }
   __syncwarp();
-  if (p.splits > 1) {
-    int tr, tc;
-    tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
-    f8_split_join<TC, false, TBN, EW>(p.out, ring, p.splits, share, warp >= 8 && ok ? warp - 8 : -1, warp & 3,
-                                      (int64_t)tr * kRows, (int64_t)tc * TBN);
+  if constexpr (CTAS == 1) {
+    if (p.splits > 1) {
+      int tr, tc;
+      tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
+      f8_split_join<TC, false, TBN, EW>(p.out, ring, p.splits, share, warp >= 12 && ok ? warp - 12 : -1, warp & 3,
+                                        (int64_t)tr * kRows + (warp & 3) * 32 + kept_row(lane), (int64_t)tc * TBN);
+    }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) tmem_dealloc(tmem, 2 * TBN);
+  if (CTAS == 2) cluster_sync_all();  // the pair's instructions read both CTAs' memory: neither leaves first
+  if (warp == 1) {
+    if (CTAS == 2) tmem_dealloc_pair(tmem, Cfg::TMEM);
+    else tmem_dealloc(tmem, Cfg::TMEM);
+  }
 }
 
 bool wg_map(CUtensorMap* map, CUtensorMapDataType type, int elem, const void* base, int64_t inner, int64_t outer, int64_t ld,
@@ -294,14 +380,14 @@ bool wg_map(CUtensorMap* map, CUtensorMapDataType type, int elem, const void* ba
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int TBN, typename TC>
+template <int CTAS, typename TC>
 int wg_launch(WgArgs a, int64_t m, int64_t n, int64_t k, const void* Q, int64_t ldq, const void* Y, int64_t ldy, int splits,
               cudaStream_t st) {
-  using Cfg = WgCfg<TBN>;
+  using Cfg = WgCfg<CTAS>;
   static std::atomic<bool> configured[64];
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return B2_ERR_LAUNCH;
-  auto kfn = wgrad_kernel<TBN, TC>;
+  auto kfn = wgrad_kernel<CTAS, TC>;
   if (!configured[dev].load(std::memory_order_acquire)) {
     if (cudaFuncSetAttribute(kfn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM) != cudaSuccess) return B2_ERR_LAUNCH;
     configured[dev].store(true, std::memory_order_release);
@@ -310,30 +396,30 @@ int wg_launch(WgArgs a, int64_t m, int64_t n, int64_t k, const void* Q, int64_t 
   if (!wg_map(&mq, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Q, m, k, ldq, kRows, CU_TENSOR_MAP_SWIZZLE_NONE) ||
       !wg_map(&my, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, Y, n, k, ldy, 64, CU_TENSOR_MAP_SWIZZLE_128B))
     return B2_ERR_LAUNCH;
-  const int64_t tr = blocks_of(m, kRows), tc = blocks_of(n, TBN);
-  if (tr * tc > 0x7fffffffLL) return B2_ERR_VARIANT;
+  const int64_t tr = blocks_of(m, CTAS * kRows), tc = blocks_of(n, Cfg::TBN);
+  if (tr * tc > 0x3fffffffLL) return B2_ERR_VARIANT;
   a.tiles_r = (int)tr, a.tiles_c = (int)tc, a.splits = splits, a.group = 8;
-  const int tiles = a.tiles_r * a.tiles_c, sms = sm_count_cached();
+  const int tiles = a.tiles_r * a.tiles_c, resident = sm_count_cached() / CTAS;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = splits > 1 ? dim3((unsigned)tiles, (unsigned)splits) : dim3((unsigned)(tiles < sms ? tiles : sms));
+  cfg.gridDim = splits > 1 ? dim3((unsigned)tiles, (unsigned)splits) : dim3((unsigned)((tiles < resident ? tiles : resident) * CTAS));
   cfg.blockDim = dim3(Cfg::NT);
   cfg.dynamicSmemBytes = Cfg::SMEM;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {1, (unsigned)splits, 1};
-  cfg.attrs = at, cfg.numAttrs = splits > 1 ? 1 : 0;
+  at[0].val.clusterDim = {(unsigned)CTAS, (unsigned)splits, 1};
+  cfg.attrs = at, cfg.numAttrs = CTAS * splits > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kfn, a, mq, my) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
 }
 
 template <typename TC>
 int wg_choose(const WgArgs& a, int64_t m, int64_t n, int64_t k, const void* Q, int64_t ldq, const void* Y, int64_t ldy, cudaStream_t st) {
   const int sms = sm_count_cached();
-  if (blocks_of(m, kRows) * blocks_of(n, 256) >= sms) return wg_launch<256, TC>(a, m, n, k, Q, ldq, Y, ldy, 1, st);
+  if (blocks_of(m, 256) * blocks_of(n, 256) * 2 >= sms) return wg_launch<2, TC>(a, m, n, k, Q, ldq, Y, ldy, 1, st);
   const int64_t tiles = blocks_of(m, kRows) * blocks_of(n, 128);
   int s = 1;
   while (s < 8 && tiles * s * 2 <= sms && a.kb / (s * 2) >= 2) s *= 2;
-  return wg_launch<128, TC>(a, m, n, k, Q, ldq, Y, ldy, s, st);
+  return wg_launch<1, TC>(a, m, n, k, Q, ldq, Y, ldy, s, st);
 }
 
 struct WgPack {

@@ -97,12 +97,14 @@ __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorM
       ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(c_inner), "r"(c_outer), "r"(bar)
       : "memory");
 }
-// Arrival on a barrier of another CTA of the cluster (cluster_map_shared).  The waiting side acquires at its own CTA's
-// scope: what these barriers hand over is tensor memory and shared memory that only the tensor core and TMA touch, ordered by
-// their own fences.
+// Arrival on a barrier of another CTA of the cluster (an address from cluster_map_shared).  What these barriers hand over
+// is tensor memory, or shared memory that this CTA's threads wrote, pushed to the async proxy with fence.proxy.async before,
+// and that the tensor core of the same SM reads: nothing the other CTA's threads load.  So neither side asks for cluster
+// scope; a release at that scope waits for everything this thread has in flight, 1000 clocks and more.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+
 // Shared-memory matrix descriptor of a K-major operand tile stored as rows of 128 bytes (32 floats) with the
 // 128-byte swizzle: 8-row groups are 1024 bytes apart (stride byte offset), the leading byte offset is not
 // used by swizzled K-major layouts, descriptor version 1, layout type 2 (128-byte swizzle).
@@ -145,9 +147,31 @@ __device__ __forceinline__ bool elect_one() {
       : "=r"(e));
   return e != 0;
 }
+// Bounded wait of a warp with nothing else to do.  The hint lets the hardware suspend it for up to a millisecond at a time
+// instead of having it poll, which takes issue slots and shared-memory cycles from the warps that work.
+constexpr uint32_t kSuspendNs = 1000 * 1000;
+__device__ __forceinline__ bool mbar_suspend(uint64_t* bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs)
+      : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ bool mbar_wait_lane(uint64_t* bar, uint32_t parity, uint64_t limit_ns = kWaitLimitNs) {
+  if (mbar_suspend(bar, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+  do {
+    if (mbar_suspend(bar, parity)) return true;
+  } while (global_timer_ns() - t0 < limit_ns);
+  return false;
+}
 // the same answer in all lanes
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, uint64_t limit_ns = kWaitLimitNs) {
-  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, limit_ns) ? 1 : 0) != 0;
+  return __all_sync(0xffffffffu, mbar_wait_lane(bar, parity, limit_ns) ? 1 : 0) != 0;
 }
 __device__ __forceinline__ bool mbar_test_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, mbar_test_wait(bar, parity) ? 1 : 0) != 0;
