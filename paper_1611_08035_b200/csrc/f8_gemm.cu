@@ -44,11 +44,6 @@ __device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t desc_a, uint64
       ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Instruction descriptor: fp32 accumulator, e4m3 operands (format 0), which of them have their own index contiguous, N, M.
-__device__ __forceinline__ uint32_t umma_idesc_f8(int m, int n, int a_mn, int b_mn) {
-  return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
-}
-
 template <int TBN, typename TC, bool COLS_CONTIG>
 __global__ void __launch_bounds__(F8Cfg<TBN>::NT, 1)
     f8_gemm_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
@@ -300,9 +295,8 @@ int f8_choose(const F8Args& a, const F8Operand& A, const F8Operand& B, int64_t k
     if (B.n <= 32) return f8_launch<32, TC, false>(a, A, B, k, s, st);
     return f8_launch<64, TC, false>(a, A, B, k, s, st);
   }
-  const int64_t wide = blocks_of(B.n, kRows) * blocks_of(A.n, 256);
-  if (!A.s.f32 && !B.s.f32 && blocks_of(B.n, 256) * blocks_of(A.n, 256) * 2 >= sms) return f8_mx_launch<TC>(a, B, A, k, st);
-  if (wide >= sms) return f8_launch<256, TC, true>(a, B, A, k, 1, st);
+  if (blocks_of(B.n, 256) * blocks_of(A.n, 256) * 2 >= sms)
+    return !A.s.f32 && !B.s.f32 ? f8_mx_launch<TC>(a, B, A, k, st) : f8_fs_launch<TC>(a, B, A, k, st);
   const int s = splits_for(blocks_of(B.n, kRows) * blocks_of(A.n, 128), 1);
   return f8_launch<128, TC, true>(a, B, A, k, s, st);
 }

@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <atomic>
+
 #include "b2gemm.h"
 #include "entry.h"
 #include "f8.cuh"
@@ -55,8 +57,46 @@ inline bool f8_map(CUtensorMap* map, const void* base, int64_t inner, int64_t ou
 }
 
 
+// Instruction descriptor: fp32 accumulator, e4m3 operands (format 0), which of them have their own index contiguous, N, M.
+__device__ __forceinline__ uint32_t umma_idesc_f8(int m, int n, int a_mn, int b_mn) {
+  return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// Launch of a persistent kernel on pairs of CTAs with 256 x 256 tiles.
+template <typename Kernel>
+int f8_pair_launch(Kernel kfn, std::atomic<bool>* configured, int threads, size_t smem, F8Args a, const F8Operand& r, const F8Operand& c,
+                   int64_t k, cudaStream_t st) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return B2_ERR_LAUNCH;
+  if (!configured[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(kfn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return B2_ERR_LAUNCH;
+    configured[dev].store(true, std::memory_order_release);
+  }
+  CUtensorMap mr, mc;
+  if (!f8_map(&mr, r.p, r.mn ? r.n : k, r.mn ? k : r.n, r.ld, 128) || !f8_map(&mc, c.p, c.mn ? c.n : k, c.mn ? k : c.n, c.ld, 128))
+    return B2_ERR_LAUNCH;
+  const int64_t tr = blocks_of(r.n, 256), tc = blocks_of(c.n, 256);
+  if (tr * tc > 0x3fffffffLL) return B2_ERR_VARIANT;
+  a.out.rows = r.n, a.out.cols = c.n, a.r_mn = r.mn, a.c_mn = c.mn, a.sr = r.s, a.sc = c.s;
+  a.tiles_r = (int)tr, a.tiles_c = (int)tc, a.splits = 1, a.group = 8;
+  const int tiles = a.tiles_r * a.tiles_c, pairs = sm_count_cached() / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs));
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim = {2, 1, 1};
+  cfg.attrs = at, cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kfn, a, mr, mc) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+}
+
 // f8_mx.cu: products whose scales are both e8m0, 256 x 256 tiles; TC = float or __nv_bfloat16
 template <typename TC>
 int f8_mx_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st);
+// f8_fs.cu: the same with scales of either type
+template <typename TC>
+int f8_fs_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st);
 
 }  // namespace b2

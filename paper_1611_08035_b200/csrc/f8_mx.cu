@@ -300,31 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <typename TC>
 int f8_mx_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
   static std::atomic<bool> configured[64];
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return B2_ERR_LAUNCH;
-  auto kfn = f8_mx_kernel<TC, sizeof(TC) == 4 ? 16 : 0>;
-  if (!configured[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(kfn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) return B2_ERR_LAUNCH;
-    configured[dev].store(true, std::memory_order_release);
-  }
-  CUtensorMap mr, mc;
-  if (!f8_map(&mr, r.p, r.mn ? r.n : k, r.mn ? k : r.n, r.ld, 128) || !f8_map(&mc, c.p, c.mn ? c.n : k, c.mn ? k : c.n, c.ld, 128))
-    return B2_ERR_LAUNCH;
-  const int64_t tr = blocks_of(r.n, 2 * kRows), tc = blocks_of(c.n, kBN);
-  if (tr * tc > 0x3fffffffLL) return B2_ERR_VARIANT;
-  a.out.rows = r.n, a.out.cols = c.n, a.r_mn = r.mn, a.c_mn = c.mn, a.sr = r.s, a.sc = c.s;
-  a.tiles_r = (int)tr, a.tiles_c = (int)tc, a.splits = 1, a.group = 8;
-  const int tiles = a.tiles_r * a.tiles_c, pairs = sm_count_cached() / 2;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {2, 1, 1};
-  cfg.attrs = at, cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kfn, a, mr, mc) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  return f8_pair_launch(f8_mx_kernel<TC, sizeof(TC) == 4 ? 16 : 0>, configured, kThreads, kSmem, a, r, c, k, st);
 }
 template int f8_mx_launch<float>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
 template int f8_mx_launch<__nv_bfloat16>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
