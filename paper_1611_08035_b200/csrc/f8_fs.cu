@@ -319,10 +319,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-      } else if (p.out.vec) {
-        f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
       } else {
-        f8_emit<TC, true, kCols>(p.out, row0 + lane, col0, acc);
+        f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
       }
     }
   }

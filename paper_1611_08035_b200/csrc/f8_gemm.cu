@@ -23,17 +23,21 @@
 namespace b2 {
 namespace {
 
-template <int TBN>
+// MX: both scales are e8m0 and the tensor core applies them (f8_mx.cu describes how): the sums of a tile stay in tensor
+// memory, behind them the scales of sixteen blocks.  Otherwise every block's sums are scaled and added in registers.
+template <int TBN, bool MX>
 struct F8Cfg {
-  static constexpr int EW = TBN >= 128 ? 8 : 4;             // warps that scale and add
+  static constexpr int EW = TBN >= 128 ? 8 : 4;             // warps that read the sums
   static constexpr int COLS = TBN / (EW / 4);               // accumulators of a thread
   static constexpr int NT = 64 + 32 * EW;
   static constexpr uint32_t STAGE = kRowStage + TBN * kF8Block;
-  static constexpr int STAGES = TBN == 256 ? 4 : TBN == 128 ? 6 : 5;
+  static constexpr int STAGES = TBN == 128 ? 6 : 5;
   static constexpr uint32_t RING = STAGE * STAGES;
-  static constexpr uint32_t TMEM = 2 * TBN < 32 ? 32 : 2 * TBN;
-  static constexpr size_t SMEM = 1024 + RING + 512 + EW * COLS * sizeof(float);
-  static_assert(kRows * TBN * 4 <= RING, "the split's shares pass through the ring");
+  static constexpr int SLOTS = 4, SF_COLS = 8;              // scale ring in tensor memory: 4 columns for 128 rows, 4 for 128 columns
+  static constexpr uint32_t TMEM = MX ? (TBN <= 32 ? 64 : TBN == 64 ? 128 : 256) : (TBN == 16 ? 32 : 2 * TBN);
+  static_assert(!MX || TBN + SLOTS * SF_COLS <= (int)TMEM, "sums and scales");
+  static constexpr size_t SMEM = 1024 + RING + 512 + EW * (TBN >= 128 ? kEmitBytes : COLS * (int)sizeof(float));
+  static_assert(share_bytes(TBN) <= RING, "the split's shares pass through the ring");
 };
 
 __device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
@@ -44,10 +48,20 @@ __device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t desc_a, uint64
       ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-template <int TBN, typename TC, bool COLS_CONTIG>
-__global__ void __launch_bounds__(F8Cfg<TBN>::NT, 1)
+__device__ __forceinline__ void umma_mx1(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                         uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+      : "memory");
+}
+
+template <int TBN, typename TC, bool COLS_CONTIG, bool MX>
+__global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
     f8_gemm_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
-  using Cfg = F8Cfg<TBN>;
+  using Cfg = F8Cfg<TBN, MX>;
   constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES;
   extern __shared__ unsigned char f8_smem_raw[];
   const uint32_t raw = smem_u32(f8_smem_raw);
@@ -56,9 +70,11 @@ __global__ void __launch_bounds__(F8Cfg<TBN>::NT, 1)
   uint64_t* empty = full + STAGES;
   uint64_t* tfull = empty + STAGES;
   uint64_t* tempty = tfull + 2;
-  uint64_t* drained = tempty + 2;
+  uint64_t* sf_full = tempty + 2;
+  uint64_t* sf_empty = sf_full + Cfg::SLOTS;
+  uint64_t* drained = sf_empty + Cfg::SLOTS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
-  float* sc_smem = reinterpret_cast<float*>(ring + Cfg::RING + 512);
+  unsigned char* scratch = ring + Cfg::RING + 512;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -69,6 +85,10 @@ __global__ void __launch_bounds__(F8Cfg<TBN>::NT, 1)
     for (int b = 0; b < 2; ++b) {
       mbar_init(&tfull[b], 1);
       mbar_init(&tempty[b], EW);
+    }
+    for (int s = 0; s < Cfg::SLOTS; ++s) {
+      mbar_init(&sf_full[s], 4);
+      mbar_init(&sf_empty[s], 1);
     }
     mbar_init(drained, 1);
     mbar_fence_init();
@@ -87,124 +107,200 @@ __global__ void __launch_bounds__(F8Cfg<TBN>::NT, 1)
 
   if (warp == 0) {
     if (lane == 0) {
-      int it = 0;
+      RingPos<STAGES> pos;
+      int filled = 0;
       for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
         int tr, tc;
         tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-          const int s = it % STAGES, r = it / STAGES;
-          if (r > 0 && !mbar_wait_bounded(&empty[s], (uint32_t)((r - 1) & 1))) {
+        for (int kb = kb0; kb < kb1; ++kb, pos.next()) {
+          const int s = pos.s;
+          if (filled < STAGES) {
+            ++filled;
+          } else if (!mbar_wait_bounded(&empty[s], pos.phase ^ 1u)) {
             ok = false;
             break;
           }
           unsigned char* st = ring + (size_t)s * Cfg::STAGE;
           mbar_arrive_expect_tx(&full[s], Cfg::STAGE);
           tma_load_2d(st, &map_r, p.r_mn ? tr * kRows : kb * kF8Block, p.r_mn ? kb * kF8Block : tr * kRows, &full[s]);
-          if (p.c_mn) {
-#pragma unroll
-            for (int j = 0; j < (TBN >= 128 ? TBN / 128 : 1); ++j)
-              tma_load_2d(st + kRowStage + j * kRowStage, &map_c, tc * TBN + j * 128, kb * kF8Block, &full[s]);
-          } else {
-            tma_load_2d(st + kRowStage, &map_c, kb * kF8Block, tc * TBN, &full[s]);
-          }
+          tma_load_2d(st + kRowStage, &map_c, p.c_mn ? tc * TBN : kb * kF8Block, p.c_mn ? kb * kF8Block : tc * TBN, &full[s]);
         }
       }
-      if (!ok) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-      // nothing of this CTA's copies may still be in flight when it leaves: the latest fill of every slot
-      if (!ok)
-        for (int s = 0; s < STAGES; ++s)
-          if (it > s) (void)mbar_wait_bounded(&full[s], (uint32_t)(((it - 1 - s) / STAGES) & 1), kDrainLimitNs);
+      if (!ok) {  // nothing of this CTA's copies may still be in flight when it leaves: the latest fill of every slot
+        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+        for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_bounded(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
+      }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t idesc = umma_idesc_f8(kRows, TBN, p.r_mn, p.c_mn);
-      int it = 0;
-      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-          const int s = it % STAGES, b = it & 1;
-          if ((it >= 2 && !mbar_wait_bounded(&tempty[b], (uint32_t)(((it >> 1) - 1) & 1))) ||
-              !mbar_wait_bounded(&full[s], (uint32_t)((it / STAGES) & 1))) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint32_t a0 = smem_u32(ring + (size_t)s * Cfg::STAGE), b0 = a0 + kRowStage;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {  // 32 of the summed index an instruction
-            const uint64_t da = p.r_mn ? umma_desc_mn_major_sw128(a0 + j * 4096, kRowStage) : umma_desc_k_major_sw128(a0 + j * 32);
-            const uint64_t db = p.c_mn ? umma_desc_mn_major_sw128(b0 + j * 4096, kRowStage) : umma_desc_k_major_sw128(b0 + j * 32);
-            umma_f8(tmem + b * TBN, da, db, idesc, j != 0 ? 1u : 0u);
-          }
-          umma_commit(&empty[s]);
-          umma_commit(&tfull[b]);
-        }
-      }
-      if (!ok) {  // multiply-adds in flight write tensor memory: let them end before it is freed
-        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-        umma_commit(drained);
-        (void)mbar_wait_bounded(drained, 0, kDrainLimitNs);
-      }
-    }
-  } else {
-    const int ew = warp - 2, quad = warp & 3, half = ew >> 2;  // tensor-memory lanes go by the warp's number modulo 4
-    float* scw = sc_smem + ew * COLS;
-    const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * COLS);
-    constexpr int SPL = (COLS + 31) / 32;
-    int it = 0;
+    const uint32_t a0 = smem_u32(ring), b0 = a0 + kRowStage;
+    const uint64_t da0 = p.r_mn ? umma_desc_mn_major_sw128(a0, kRowStage) : umma_desc_k_major_sw128(a0);
+    const uint64_t db0 = p.c_mn ? umma_desc_mn_major_sw128(b0, kRowStage) : umma_desc_k_major_sw128(b0);
+    const uint32_t step_a = p.r_mn ? 4096 : 32, step_b = p.c_mn ? 4096 : 32;  // bytes between instructions of a block
+    const uint32_t idesc = MX ? umma_idesc_mx(kRows, TBN, p.r_mn, p.c_mn, 0) : umma_idesc_f8(kRows, TBN, p.r_mn, p.c_mn);
+    RingPos<STAGES> pos;
+    RingPos<Cfg::SLOTS> slot;
+    int ch = 0;  // sums handed over so far: buffer and round (MX: one buffer)
     for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-      int tr, tc;
-      tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
-      const int64_t row = (int64_t)tr * kRows + quad * 32 + lane, col0 = (int64_t)tc * TBN + half * COLS;
-      const int64_t srow = row < p.out.rows ? row : p.out.rows - 1;
-#pragma unroll
-      for (int j = 0; j < COLS; ++j) acc[j] = 0.0f;
-      float fr = 0.0f, fc[SPL];
-      auto fetch = [&](int kb) {
-        fr = f8_scale_at(p.sr, srow, kb);
-#pragma unroll
-        for (int i = 0; i < SPL; ++i) {
-          int64_t c = col0 + i * 32 + (lane % COLS);
-          fc[i] = f8_scale_at(p.sc, c < p.out.cols ? c : p.out.cols - 1, kb);
-        }
-      };
-      if (kb0 < kb1) fetch(kb0);
-      for (int kb = kb0; kb < kb1; ++kb, ++it) {
-        const int b = it & 1;
-        const float f = fr;
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < SPL; ++i)
-          if (COLS >= 32 || lane < COLS) scw[i * 32 + lane] = fc[i];
-        __syncwarp();
-        if (kb + 1 < kb1) fetch(kb + 1);
-        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&tfull[b], (uint32_t)((it >> 1) & 1)) ? 1 : 0)) {
+      for (int kb = kb0; kb < kb1; ++kb, pos.next()) {
+        const int s = pos.s, b = MX ? 0 : ch & 1, byte = kb & 3;
+        const bool first = !MX || kb == kb0, end = !MX || kb == kb1 - 1;
+        const uint32_t behind = MX ? 1 : 2, round = (uint32_t)(MX ? ch : ch >> 1);
+        if ((first && ch >= (int)behind && !__all_sync(0xffffffffu, mbar_wait_bounded(&tempty[b], (round - 1) & 1) ? 1 : 0)) ||
+            (MX && (byte == 0 || kb == kb0) && !__all_sync(0xffffffffu, mbar_wait_bounded(&sf_full[slot.s], slot.phase) ? 1 : 0)) ||
+            !__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], pos.phase) ? 1 : 0)) {
           ok = false;
           break;
         }
         tc_fence_after();
+        const uint64_t da = umma_desc_advance(da0, (uint32_t)s * Cfg::STAGE), db = umma_desc_advance(db0, (uint32_t)s * Cfg::STAGE);
+        const bool group_end = MX && (byte == 3 || end);
+        if (elect_one()) {
+          if constexpr (MX) {
+            const uint32_t sfa = tmem + TBN + slot.s * Cfg::SF_COLS, id = idesc | ((uint32_t)byte << 4) | ((uint32_t)byte << 29);
 #pragma unroll
-        for (int c0 = 0; c0 < COLS; c0 += 16) {
-          uint32_t v[16];
-          tmem_ld16_issue(taddr + (uint32_t)(b * TBN + c0), v);
-          tmem_ld_wait16(v);
-          if (c0 + 16 >= COLS) {
+            for (int j = 0; j < 4; ++j)  // 32 of the summed index an instruction
+              umma_mx1(tmem, umma_desc_advance(da, j * step_a), umma_desc_advance(db, j * step_b), id, sfa, sfa + 4, (!first || j != 0) ? 1u : 0u);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              umma_f8(tmem + b * TBN, umma_desc_advance(da, j * step_a), umma_desc_advance(db, j * step_b), idesc, j != 0 ? 1u : 0u);
+          }
+          umma_commit(&empty[s]);
+          if (group_end) umma_commit(&sf_empty[slot.s]);
+          if (end) umma_commit(&tfull[b]);
+        }
+        __syncwarp();
+        if (group_end) slot.next();
+        if (end) ++ch;
+      }
+    }
+    if (!ok) {  // multiply-adds in flight write tensor memory: let them end before it is freed
+      if (elect_one()) {
+        atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+        umma_commit(drained);
+      }
+      (void)mbar_wait_warp(drained, 0, kDrainLimitNs);
+    }
+  } else {
+    const int ew = warp - 2, quad = warp & 3, half = ew >> 2;  // tensor-memory lanes go by the warp's number modulo 4
+    const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * COLS);
+    constexpr int SPL = (COLS + 31) / 32;
+    RingPos<Cfg::SLOTS> slot;
+    int ch = 0, groups = 0;
+    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+      int tr, tc;
+      tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+      const int64_t row = (int64_t)tr * kRows + quad * 32 + lane, col0 = (int64_t)tc * TBN + half * COLS;
+      if constexpr (MX) {
+        if (half == 0) {  // four warps, one for each quarter of the lanes, bring the scales
+          const int64_t r0 = (int64_t)tr * kRows + lane, c0 = (int64_t)tc * TBN + lane;
+          constexpr int CW = TBN >= 32 ? TBN / 32 : 1;
+          uint32_t next[4 + CW];
+          auto fetch = [&](int kb) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) next[i] = scale_word(p.sr, r0 + 32 * i, p.out.rows, kb, p.kb);
+#pragma unroll
+            for (int i = 0; i < CW; ++i) next[4 + i] = scale_word(p.sc, c0 + 32 * i, p.out.cols, kb, p.kb);
+          };
+          fetch(kb0 & ~3);
+          for (int kb = kb0 & ~3; kb < kb1; kb += 4, slot.next()) {
+            uint32_t w[8] = {};
+#pragma unroll
+            for (int i = 0; i < 4 + CW; ++i) w[i] = next[i];
+            if (kb + 4 < kb1) fetch(kb + 4);
+            if (groups < Cfg::SLOTS) {
+              ++groups;
+            } else if (!mbar_wait_warp(&sf_empty[slot.s], slot.phase ^ 1u)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t sf = tmem + ((uint32_t)(quad * 32) << 16) + TBN + slot.s * Cfg::SF_COLS;
+            tmem_st4(sf, w[0], w[1], w[2], w[3]);
+            tmem_st4(sf + 4, w[4], w[5], w[6], w[7]);
+            tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&tempty[b]);
+            if (lane == 0) mbar_arrive(&sf_full[slot.s]);
           }
-#pragma unroll
-          for (int j = 0; j < 16; ++j) acc[c0 + j] += __uint_as_float(v[j]) * (f * scw[c0 + j]);
         }
+        if (ok && !mbar_wait_warp(&tfull[0], (uint32_t)(ch & 1), kWaitLimitNs + (uint64_t)p.kb * 8192ull)) ok = false;
+        ++ch;
+        tc_fence_after();
+        if (ok) {
+#pragma unroll
+          for (int c0 = 0; c0 < COLS; c0 += 16) {
+            uint32_t v[16];
+            tmem_ld16_issue(taddr + (uint32_t)c0, v);
+            tmem_ld_wait16(v);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[c0 + j] = __uint_as_float(v[j]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&tempty[0]);
+        }
+      } else {
+        float* scw = reinterpret_cast<float*>(scratch) + ew * COLS;
+        const int64_t srow = row < p.out.rows ? row : p.out.rows - 1;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) acc[j] = 0.0f;
+        float fr = 0.0f, fc[SPL];
+        auto fetch = [&](int kb) {
+          fr = f8_scale_at(p.sr, srow, kb);
+#pragma unroll
+          for (int i = 0; i < SPL; ++i) {
+            int64_t c = col0 + i * 32 + (lane % COLS);
+            fc[i] = f8_scale_at(p.sc, c < p.out.cols ? c : p.out.cols - 1, kb);
+          }
+        };
+        if (kb0 < kb1) fetch(kb0);
+        for (int kb = kb0; kb < kb1; ++kb, ++ch) {
+          const int b = ch & 1;
+          const float f = fr;
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < SPL; ++i)
+            if (COLS >= 32 || lane < COLS) scw[i * 32 + lane] = fc[i];
+          __syncwarp();
+          if (kb + 1 < kb1) fetch(kb + 1);
+          if (!__all_sync(0xffffffffu, mbar_wait_bounded(&tfull[b], (uint32_t)((ch >> 1) & 1)) ? 1 : 0)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          constexpr int W = COLS >= 32 ? 32 : 16;
+#pragma unroll
+          for (int c0 = 0; c0 < COLS; c0 += W) {
+            uint32_t v[32];
+            if constexpr (W == 32) {
+              tmem_ld32_issue(taddr + (uint32_t)(b * TBN + c0), v);
+              tmem_ld_wait32(v);
+            } else {
+              uint32_t(&v16)[16] = *reinterpret_cast<uint32_t(*)[16]>(v);
+              tmem_ld16_issue(taddr + (uint32_t)(b * TBN + c0), v16);
+              tmem_ld_wait16(v16);
+            }
+            if (c0 + W >= COLS) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&tempty[b]);
+            }
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[c0 + j] += __uint_as_float(v[j]) * (f * scw[c0 + j]);
+          }
+        }
+        __syncwarp();
       }
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-      } else if (p.splits == 1) {
-        f8_emit<TC, COLS_CONTIG, COLS>(p.out, row, col0, acc);
+      } else if (p.splits > 1) {
+        // this CTA's share of the tile; the ring is idle once the last block's sums have been read
+        f8_put_share<COLS_CONTIG, TBN, COLS>(ring, quad * 32 + lane, half * COLS, acc);
+      } else if constexpr (COLS_CONTIG) {
+        f8_emit_staged<TC, COLS>(p.out, row - lane, col0, acc, scratch + ew * kEmitBytes);
       } else {
-        // this CTA's share of the tile, [column][row]; the ring is idle once the last block's sums have been read
-        float* mine = reinterpret_cast<float*>(ring) + (size_t)half * COLS * kRows + quad * 32 + lane;
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) mine[(size_t)j * kRows] = acc[j];
+        f8_emit_rows<TC, COLS>(p.out, row, col0, acc);
       }
     }
   }
@@ -213,8 +309,8 @@ __global__ void __launch_bounds__(F8Cfg<TBN>::NT, 1)
   if (p.splits > 1) {
     int tr, tc;
     tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
-    f8_split_join<TC, COLS_CONTIG, TBN, EW>(p.out, ring, p.splits, share, warp >= 2 && ok ? warp - 2 : -1, warp & 3,
-                                            (int64_t)tr * kRows + (warp & 3) * 32 + lane, (int64_t)tc * TBN);
+    f8_split_join<TC, COLS_CONTIG, TBN, EW, false>(p.out, ring, p.splits, share, warp >= 2 && ok ? tid - 64 : -1, (int64_t)tr * kRows,
+                                                   (int64_t)tc * TBN);
   }
   tc_fence_before();
   __syncthreads();
@@ -247,13 +343,13 @@ unsigned grid_for(int64_t threads) {
   return (unsigned)(b < 1 ? 1 : b < cap ? b : cap);
 }
 
-template <int TBN, typename TC, bool COLS_CONTIG>
+template <int TBN, typename TC, bool COLS_CONTIG, bool MX>
 int f8_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, int splits, cudaStream_t st) {
-  using Cfg = F8Cfg<TBN>;
+  using Cfg = F8Cfg<TBN, MX>;
   static std::atomic<bool> configured[64];
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return B2_ERR_LAUNCH;
-  auto kfn = f8_gemm_kernel<TBN, TC, COLS_CONTIG>;
+  auto kfn = f8_gemm_kernel<TBN, TC, COLS_CONTIG, MX>;
   if (!configured[dev].load(std::memory_order_acquire)) {
     if (cudaFuncSetAttribute(kfn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM) != cudaSuccess) return B2_ERR_LAUNCH;
     configured[dev].store(true, std::memory_order_release);
@@ -280,7 +376,7 @@ int f8_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, int s
   return cudaLaunchKernelEx(&cfg, kfn, a, mr, mc) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
 }
 
-template <typename TC>
+template <typename TC, bool MX>
 int f8_choose(const F8Args& a, const F8Operand& A, const F8Operand& B, int64_t k, cudaStream_t st) {
   const int sms = sm_count_cached();
   // CTAs that share a tile: as many as leave every one of them a few blocks and no SM without a CTA
@@ -291,14 +387,14 @@ int f8_choose(const F8Args& a, const F8Operand& A, const F8Operand& B, int64_t k
   };
   if (B.n <= 64 && !B.mn) {  // decoding
     const int s = splits_for(blocks_of(A.n, kRows), 2);
-    if (B.n <= 16) return f8_launch<16, TC, false>(a, A, B, k, s, st);
-    if (B.n <= 32) return f8_launch<32, TC, false>(a, A, B, k, s, st);
-    return f8_launch<64, TC, false>(a, A, B, k, s, st);
+    if (B.n <= 16) return f8_launch<16, TC, false, MX>(a, A, B, k, s, st);
+    if (B.n <= 32) return f8_launch<32, TC, false, MX>(a, A, B, k, s, st);
+    return f8_launch<64, TC, false, MX>(a, A, B, k, s, st);
   }
-  if (blocks_of(B.n, 256) * blocks_of(A.n, 256) * 2 >= sms)
-    return !A.s.f32 && !B.s.f32 ? f8_mx_launch<TC>(a, B, A, k, st) : f8_fs_launch<TC>(a, B, A, k, st);
+  // pairs of CTAs as soon as single ones, with tiles a quarter of the size, would take more than one turn
+  if (blocks_of(B.n, 256) * blocks_of(A.n, 256) * 4 > sms) return MX ? f8_mx_launch<TC>(a, B, A, k, st) : f8_fs_launch<TC>(a, B, A, k, st);
   const int s = splits_for(blocks_of(B.n, kRows) * blocks_of(A.n, 128), 1);
-  return f8_launch<128, TC, true>(a, B, A, k, s, st);
+  return f8_launch<128, TC, true, MX>(a, B, A, k, s, st);
 }
 
 bool f8_is_n(char c) { return c == 'N' || c == 'n'; }
@@ -396,5 +492,7 @@ extern "C" int b2_gemm_f8(char transa, char transb, int64_t m, int64_t n, int64_
   if (!a.status) return B2_ERR_LAUNCH;
   const F8Operand oa{A, m, lda, an, {SA, an ? 1 : ldsa, an ? ldsa : 1, block_a == 1 ? 0 : 7, scale_type_a == B2_SCALE_F32}};
   const F8Operand ob{B, n, ldb, !bn, {SB, bn ? ldsb : 1, bn ? 1 : ldsb, block_b == 1 ? 0 : 7, scale_type_b == B2_SCALE_F32}};
-  return type_c == B2_TYPE_BF16 ? f8_choose<__nv_bfloat16>(a, oa, ob, k, st) : f8_choose<float>(a, oa, ob, k, st);
+  const bool mx = scale_type_a == B2_SCALE_E8M0 && scale_type_b == B2_SCALE_E8M0;
+  if (type_c == B2_TYPE_BF16) return mx ? f8_choose<__nv_bfloat16, true>(a, oa, ob, k, st) : f8_choose<__nv_bfloat16, false>(a, oa, ob, k, st);
+  return mx ? f8_choose<float, true>(a, oa, ob, k, st) : f8_choose<float, false>(a, oa, ob, k, st);
 }

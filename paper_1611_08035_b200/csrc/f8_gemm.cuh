@@ -14,7 +14,6 @@ namespace b2 {
 
 constexpr int kRows = 128;                       // MMA rows of a CTA's tile
 constexpr uint32_t kRowStage = kRows * kF8Block;  // bytes of the row operand in a stage
-constexpr int kMaxSplit = 8;
 
 struct F8Scale {  // value for index i and block b: p[(i >> shift) * si + b * sb]
   const void* p;
@@ -60,6 +59,25 @@ inline bool f8_map(CUtensorMap* map, const void* base, int64_t inner, int64_t ou
 // Instruction descriptor: fp32 accumulator, e4m3 operands (format 0), which of them have their own index contiguous, N, M.
 __device__ __forceinline__ uint32_t umma_idesc_f8(int m, int n, int a_mn, int b_mn) {
   return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// Instruction descriptor: byte of the scale words (both operands), e4m3, which operands have their own index contiguous,
+// N, e8m0 scales, M.
+__device__ __forceinline__ uint32_t umma_idesc_mx(int m, int n, int a_mn, int b_mn, int byte) {
+  return ((uint32_t)byte << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
+         ((uint32_t)(m >> 7) << 27) | ((uint32_t)byte << 29);
+}
+
+// Scale bytes of index i (clamped to the last one) for blocks b .. b+3, the first in the lowest byte; blocks beyond the
+// last are never multiplied with.
+__device__ __forceinline__ uint32_t scale_word(const F8Scale& s, int64_t i, int64_t extent, int b, int kb) {
+  const uint8_t* p = static_cast<const uint8_t*>(s.p) + ((i < extent ? i : extent - 1) >> s.shift) * s.si + (int64_t)b * s.sb;
+  if (s.sb == 1 && b + 4 <= kb && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return *reinterpret_cast<const uint32_t*>(p);
+  uint32_t w = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (b + j < kb) w |= (uint32_t)p[j * s.sb] << (8 * j);
+  return w;
 }
 
 // Launch of a persistent kernel on pairs of CTAs with 256 x 256 tiles.

@@ -39,25 +39,6 @@ __device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64
       ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
       : "memory");
 }
-// Instruction descriptor: byte of the scale words (both operands), e4m3, which operands have their own index contiguous,
-// N, e8m0 scales, M.
-__device__ __forceinline__ uint32_t umma_idesc_mx(int m, int n, int a_mn, int b_mn, int byte) {
-  return ((uint32_t)byte << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
-         ((uint32_t)(m >> 7) << 27) | ((uint32_t)byte << 29);
-}
-
-// Scale bytes of index i (clamped to the last one) for blocks b .. b+3, the first in the lowest byte; blocks beyond the
-// last are never multiplied with.
-__device__ __forceinline__ uint32_t scale_word(const F8Scale& s, int64_t i, int64_t extent, int b, int kb) {
-  const uint8_t* p = static_cast<const uint8_t*>(s.p) + ((i < extent ? i : extent - 1) >> s.shift) * s.si + (int64_t)b * s.sb;
-  if (s.sb == 1 && b + 4 <= kb && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return *reinterpret_cast<const uint32_t*>(p);
-  uint32_t w = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (b + j < kb) w |= (uint32_t)p[j * s.sb] << (8 * j);
-  return w;
-}
-
 // CHUNK: blocks whose products are summed in tensor memory, whose additions truncate, before they are added to fp32
 // registers; 0: all of them.  A bf16 result does not see the difference.
 template <typename TC, int CHUNK>
@@ -281,10 +262,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int64_t row0 = (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, col0 = (int64_t)tc * kBN + half * kCols;
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-      } else if (p.out.vec) {
-        f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
       } else {
-        f8_emit<TC, true, kCols>(p.out, row0 + lane, col0, acc);
+        f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
       }
     }
   }

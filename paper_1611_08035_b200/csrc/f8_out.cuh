@@ -14,53 +14,29 @@ struct F8Out {
   int vec;  // columns of C are 16-byte aligned
 };
 
-// alpha * v + beta * old for 8 (or fewer) consecutive elements
-template <typename TC>
-__device__ __forceinline__ void f8_emit8(TC* c, int64_t nv, bool vec, float alpha, float beta, float (&v)[8]) {
-  if (beta != 0.0f) {
-    float old[8];
-    load8(c, nv, vec, old);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = alpha * v[j] + beta * old[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= alpha;
-  }
-  store8(c, nv, vec, v);
-}
 __device__ __forceinline__ float f8_load1(const float* p) { return *p; }
 __device__ __forceinline__ float f8_load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void f8_store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void f8_store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// N (a multiple of 8, or any count with rows contiguous) accumulators of one row.  COLS_CONTIG: C[row * ldc + col].
-template <typename TC, bool COLS_CONTIG, int N>
-__device__ __forceinline__ void f8_emit(const F8Out& p, int64_t row, int64_t col, const float* acc) {
-  if (row >= p.rows) return;
-  TC* C = static_cast<TC*>(p.C);
-  if constexpr (COLS_CONTIG) {
-#pragma unroll
-    for (int j = 0; j < N; j += 8) {
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = acc[j + i];
-      f8_emit8(C + row * p.ldc + col + j, p.cols - col - j, p.vec != 0, p.alpha, p.beta, v);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      if (col + j < p.cols) {
-        TC* c = C + (col + j) * p.ldc + row;
-        float v = p.alpha * acc[j];
-        if (p.beta != 0.0f) v += p.beta * f8_load1(c);
-        f8_store1(c, v);
-      }
-    }
-  }
+template <typename TC>
+__device__ __forceinline__ void f8_put(const F8Out& p, TC* c, float v) {
+  v *= p.alpha;
+  if (p.beta != 0.0f) v += p.beta * f8_load1(c);
+  f8_store1(c, v);
 }
 
-// The same for a warp whose lanes own 32 consecutive rows (row0 + lane) and N consecutive columns each, columns
-// contiguous and aligned in C.  64 bytes of every row pass through shared memory at a time and leave as whole 64-byte pieces
+// N accumulators of one row of a tile whose rows are contiguous in C (C[col * ldc + row]): neighbouring lanes, neighbouring rows.
+template <typename TC, int N>
+__device__ __forceinline__ void f8_emit_rows(const F8Out& p, int64_t row, int64_t col, const float* acc) {
+  if (row >= p.rows) return;
+  TC* C = static_cast<TC*>(p.C) + row;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (col + j < p.cols) f8_put(p, C + (col + j) * p.ldc, acc[j]);
+}
+
+// N consecutive accumulators each of 32 consecutive rows (row0 + lane), columns contiguous in C.  64 bytes of every row pass through shared memory at a time and leave as whole 64-byte pieces
 // of eight rows an instruction: a lane that stores its own row directly touches 32 lines with every instruction (a 256 x 256
 // bf16 tile: 8000 clocks of storing, as long as the multiply-adds of 2000 summed elements).
 constexpr int kEmitPitch = 80;  // bytes between staged rows: 16-byte pieces of eight rows in different banks
@@ -71,7 +47,7 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
   TC* C = static_cast<TC*>(p.C);
   unsigned char* own = stage + lane * kEmitPitch;
   const unsigned char* swap = stage + (lane >> 2) * kEmitPitch + piece * 16;
-  if (sizeof(TC) == 2 && p.beta == 0.0f) {
+  if (sizeof(TC) == 2 && p.beta == 0.0f && p.vec) {
 #pragma unroll
     for (int j = 0; j < N; j += 32) {
       __syncwarp();
@@ -108,6 +84,17 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<float4*>(own + 16 * i) = make_float4(p.alpha * acc[j + 4 * i], p.alpha * acc[j + 4 * i + 1], p.alpha * acc[j + 4 * i + 2], p.alpha * acc[j + 4 * i + 3]);
       __syncwarp();
+      if (!p.vec) {  // columns of C that start anywhere: element by element, sixteen lanes to a row
+        const int64_t col = col0 + j + (lane & 15);
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+          const int r = 2 * i + (lane >> 4);
+          float v = *reinterpret_cast<const float*>(stage + r * kEmitPitch + (lane & 15) * 4);
+          TC* c = C + (row0 + r) * p.ldc + col;
+          if (row0 + r < p.rows && col < p.cols) f8_store1(c, p.beta != 0.0f ? v + p.beta * f8_load1(c) : v);
+        }
+        continue;
+      }
       const int64_t col = col0 + j + piece * 4, nv = p.cols - col;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -134,32 +121,73 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
   }
 }
 
-// Joining the shares of a k split: the CTAs of a cluster (rank = share) have each put their part of the 128 x TBN tile
-// into their shared memory as floats [column][row]; each adds all parts, in the order of the ranks, for its columns.  All
-// threads of all CTAs of the cluster call this; warps with writer >= 0 (0 .. EW-1, covering the tensor-memory lanes 32 *
-// quad .. + 31) add and write; `row` is the row of C that this lane's accumulators belong to.
-template <typename TC, bool COLS_CONTIG, int TBN, int EW>
-__device__ __forceinline__ void f8_split_join(const F8Out& p, const void* tile, int splits, int share, int writer, int quad,
-                                              int64_t row, int64_t col0) {
+// Joining the shares of a k split: the CTAs of a cluster (rank = share) have each put their sums of the same 128 x TBN tile
+// into their shared memory (f8_put_share), the index that is contiguous in C contiguous there too; each CTA adds all shares, in the
+// order of their rank, for its part of the other index, four numbers at a time and all ranks' numbers on their way at once
+// (one after the other, their latency made up most of a 1024^3 product: 21 us).  All threads of all CTAs of the cluster call this; the
+// 32 EW threads with worker >= 0 (numbered) add and write.  PERMUTE: row r of the tile is row kept_row(r) of C.
+constexpr int kMaxSplit = 8;
+__host__ __device__ constexpr int share_pitch(int inner) { return inner + 4; }  // 16-byte pieces of consecutive lines in different banks
+__host__ __device__ constexpr int share_bytes(int tbn) { return 4 * (tbn * share_pitch(128) > 128 * share_pitch(tbn) ? tbn * share_pitch(128) : 128 * share_pitch(tbn)); }
+__device__ __forceinline__ int kept_row(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
+
+// N consecutive columns from `col` of row `row` of the tile
+template <bool COLS_CONTIG, int TBN, int N>
+__device__ __forceinline__ void f8_put_share(void* tile, int row, int col, const float* acc) {
+  float* t = static_cast<float*>(tile);
+  if constexpr (COLS_CONTIG) {
+#pragma unroll
+    for (int j = 0; j < N; j += 4)
+      *reinterpret_cast<float4*>(t + row * share_pitch(TBN) + col + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) t[(col + j) * share_pitch(128) + row] = acc[j];
+  }
+}
+
+template <typename TC, bool COLS_CONTIG, int TBN, int EW, bool PERMUTE>
+__device__ __forceinline__ void f8_split_join(const F8Out& p, const void* tile, int splits, int share, int worker, int64_t row0,
+                                              int64_t col0) {
   cluster_sync_all();
-  if (writer >= 0) {
-    const int lane = threadIdx.x & 31;
-    const int per = TBN / splits / (EW / 4), c_first = share * (TBN / splits) + (writer >> 2) * per;
-    constexpr int G = COLS_CONTIG ? 8 : 2;
-    for (int c = c_first; c < c_first + per; c += G) {
-      float v[G];
+  if (worker >= 0) {
+    constexpr int INNER = COLS_CONTIG ? TBN : 128, OUTER = COLS_CONTIG ? 128 : TBN;
+    const int per = OUTER / splits;
+    for (int i = worker; i < per * (INNER / 4); i += 32 * EW) {
+      const int o = share * per + i / (INNER / 4), in = i % (INNER / 4) * 4;
+      const uint32_t at = smem_u32(tile) + (uint32_t)(o * share_pitch(INNER) + in) * 4;
+      float x[kMaxSplit][4];
 #pragma unroll
-      for (int g = 0; g < G; ++g) v[g] = 0.0f;
-      for (int q = 0; q < splits; ++q) {
-        const uint32_t base = cluster_map_shared(smem_u32(tile), (uint32_t)q);
+      for (int q = 0; q < kMaxSplit; ++q)
+        if (q < splits)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(x[q][0]), "=f"(x[q][1]), "=f"(x[q][2]), "=f"(x[q][3])
+                       : "r"(cluster_map_shared(at, (uint32_t)q)));
+      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          float x;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(base + (uint32_t)(((c + g) * 128 + quad * 32 + lane) * 4)) : "memory");
-          v[g] += x;
+      for (int q = 0; q < kMaxSplit; ++q)
+        if (q < splits) v[0] += x[q][0], v[1] += x[q][1], v[2] += x[q][2], v[3] += x[q][3];
+      if (PERMUTE) {
+        const float t = v[1];
+        v[1] = v[2], v[2] = t;
+      }
+      const int64_t row = row0 + (COLS_CONTIG ? o : in), col = col0 + (COLS_CONTIG ? in : o);
+      const int64_t nv = COLS_CONTIG ? p.cols - col : p.rows - row;
+      if (COLS_CONTIG ? row < p.rows : col < p.cols) {
+        TC* c = static_cast<TC*>(p.C) + (COLS_CONTIG ? row * p.ldc + col : col * p.ldc + row);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] *= p.alpha;
+          if (p.beta != 0.0f && e < nv) v[e] += p.beta * f8_load1(c + e);
+        }
+        if (p.vec && nv >= 4) {
+          if constexpr (sizeof(TC) == 4) *reinterpret_cast<float4*>(c) = make_float4(v[0], v[1], v[2], v[3]);
+          else *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < nv) f8_store1(c + e, v[e]);
         }
       }
-      f8_emit<TC, COLS_CONTIG, G>(p, row, col0 + c, v);
     }
   }
   __syncwarp();

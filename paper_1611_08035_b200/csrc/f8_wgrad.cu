@@ -57,7 +57,7 @@ struct WgCfg {
   static constexpr int STAGES = 5;
   static constexpr uint32_t RING = STAGE * STAGES, TMEM = 2 * TBN;
   static constexpr size_t SMEM = 1024 + RING + 512;
-  static_assert(kRows * 128 * 4 <= RING, "the split's shares pass through the ring");
+  static_assert(share_bytes(128) <= RING, "the split's shares pass through the ring");
 };
 
 template <int CTAS>
@@ -99,7 +99,6 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 // are put back where they are written (kept_row).
 __device__ __forceinline__ uint32_t e4m3_even(uint32_t w) { return ((w << 8) & 0x80008000u) | ((w << 4) & 0x07f007f0u); }
 __device__ __forceinline__ uint32_t e4m3_odd(uint32_t w) { return (w & 0x80008000u) | ((w >> 4) & 0x07f007f0u); }
-__device__ __forceinline__ int kept_row(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
 
 // Eight e4m3 numbers to bf16, times 2^120 * scale.
 __device__ __forceinline__ uint4 e4m3x8_to_bf16(uint2 w, uint32_t f1) {
@@ -342,11 +341,9 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
       } else if (p.splits == 1) {
-        f8_emit<TC, false, COLS>(p.out, (int64_t)(tr * CTAS + (int)rank) * kRows + quad * 32 + kept_row(lane), (int64_t)tc * TBN + half * COLS, acc);
+        f8_emit_rows<TC, COLS>(p.out, (int64_t)(tr * CTAS + (int)rank) * kRows + quad * 32 + kept_row(lane), (int64_t)tc * TBN + half * COLS, acc);
       } else {
-        float* mine = reinterpret_cast<float*>(ring) + (size_t)half * COLS * kRows + quad * 32 + lane;
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) mine[(size_t)j * kRows] = acc[j];
+        if constexpr (CTAS == 1) f8_put_share<false, TBN, COLS>(ring, quad * 32 + lane, half * COLS, acc);
       }
     }
   }
@@ -355,8 +352,8 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
     if (p.splits > 1) {
       int tr, tc;
       tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
-      f8_split_join<TC, false, TBN, EW>(p.out, ring, p.splits, share, warp >= 12 && ok ? warp - 12 : -1, warp & 3,
-                                        (int64_t)tr * kRows + (warp & 3) * 32 + kept_row(lane), (int64_t)tc * TBN);
+      f8_split_join<TC, false, TBN, EW, true>(p.out, ring, p.splits, share, warp >= 12 && ok ? tid - 384 : -1, (int64_t)tr * kRows,
+                                              (int64_t)tc * TBN);
     }
   }
   tc_fence_before();
@@ -415,10 +412,10 @@ int wg_launch(WgArgs a, int64_t m, int64_t n, int64_t k, const void* Q, int64_t 
 template <typename TC>
 int wg_choose(const WgArgs& a, int64_t m, int64_t n, int64_t k, const void* Q, int64_t ldq, const void* Y, int64_t ldy, cudaStream_t st) {
   const int sms = sm_count_cached();
-  if (blocks_of(m, 256) * blocks_of(n, 256) * 2 >= sms) return wg_launch<2, TC>(a, m, n, k, Q, ldq, Y, ldy, 1, st);
+  if (blocks_of(m, 256) * blocks_of(n, 256) * 4 > sms) return wg_launch<2, TC>(a, m, n, k, Q, ldq, Y, ldy, 1, st);
   const int64_t tiles = blocks_of(m, kRows) * blocks_of(n, 128);
   int s = 1;
-  while (s < 8 && tiles * s * 2 <= sms && a.kb / (s * 2) >= 2) s *= 2;
+  while (s < kMaxSplit && tiles * s * 2 <= sms && a.kb / (s * 2) >= 2) s *= 2;
   return wg_launch<1, TC>(a, m, n, k, Q, ldq, Y, ldy, s, st);
 }
 
