@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int s = pos.s, here = min(kPerStage, p.kb - kb);
           if (filled < kStages) {
             ++filled;
-          } else if (!mbar_wait_lane(&empty[s], pos.phase ^ 1u)) {
+          } else if (!mbar_wait_bounded(&empty[s], pos.phase ^ 1u)) {
             ok = false;
             break;
           }
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) {
         atomicExch(p.status, (int)B2_ERR_TIMEOUT);
         if (rank == 0)  // both CTAs' copies are counted here; no CTA leaves before the barrier at the end
-          for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_lane(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
+          for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_bounded(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
       }
     } else if (warp == 1 && rank == 0) {
       RingPos<kStages> pos;
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           for (int h = 0; h < here; ++h, ++ch) {
             const int b = ch & 1;
-            if (ch >= 2 && !__all_sync(0xffffffffu, mbar_wait_bounded(&tempty[b], (uint32_t)(((ch >> 1) - 1) & 1)) ? 1 : 0)) {
+            if (ch >= 2 && !mbar_wait_warp(&tempty[b], (uint32_t)(((ch >> 1) - 1) & 1))) {
               ok = false;
               break;
             }
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = 0; j < kCols / 2; ++j) acc2[j] = 0;
       for (int kb = 0; kb < p.kb; ++kb, ++ch) {
         const int b = ch & 1, g = kb % kGroup;
-        if (g == 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(&sf_full[slot.s], slot.phase) ? 1 : 0)) {
+        if (g == 0 && !mbar_wait_warp(&sf_full[slot.s], slot.phase)) {
           ok = false;
           break;
         }
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         };
-        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&tfull[b], (uint32_t)((ch >> 1) & 1)) ? 1 : 0)) {
+        if (!mbar_wait_warp(&tfull[b], (uint32_t)((ch >> 1) & 1))) {
           ok = false;
           break;
         }

@@ -31,7 +31,7 @@ struct F8Cfg {
   static constexpr int COLS = TBN / (EW / 4);               // accumulators of a thread
   static constexpr int NT = 64 + 32 * EW;
   static constexpr uint32_t STAGE = kRowStage + TBN * kF8Block;
-  static constexpr int STAGES = TBN == 128 ? 6 : 5;
+  static constexpr int STAGES = TBN == 128 ? 6 : TBN == 64 ? 4 : 5;  // of the narrow tiles, two CTAs share an SM
   static constexpr uint32_t RING = STAGE * STAGES;
   static constexpr int SLOTS = 4, SF_COLS = 8;              // scale ring in tensor memory: 4 columns for 128 rows, 4 for 128 columns
   static constexpr uint32_t TMEM = MX ? (TBN <= 32 ? 64 : TBN == 64 ? 128 : 256) : (TBN == 16 ? 32 : 2 * TBN);
@@ -145,9 +145,9 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
         const int s = pos.s, b = MX ? 0 : ch & 1, byte = kb & 3;
         const bool first = !MX || kb == kb0, end = !MX || kb == kb1 - 1;
         const uint32_t behind = MX ? 1 : 2, round = (uint32_t)(MX ? ch : ch >> 1);
-        if ((first && ch >= (int)behind && !__all_sync(0xffffffffu, mbar_wait_bounded(&tempty[b], (round - 1) & 1) ? 1 : 0)) ||
-            (MX && (byte == 0 || kb == kb0) && !__all_sync(0xffffffffu, mbar_wait_bounded(&sf_full[slot.s], slot.phase) ? 1 : 0)) ||
-            !__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], pos.phase) ? 1 : 0)) {
+        if ((first && ch >= (int)behind && !mbar_wait_warp(&tempty[b], (round - 1) & 1)) ||
+            (MX && (byte == 0 || kb == kb0) && !mbar_wait_warp(&sf_full[slot.s], slot.phase)) ||
+            !mbar_wait_warp(&full[s], pos.phase)) {
           ok = false;
           break;
         }
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
             if (COLS >= 32 || lane < COLS) scw[i * 32 + lane] = fc[i];
           __syncwarp();
           if (kb + 1 < kb1) fetch(kb + 1);
-          if (!__all_sync(0xffffffffu, mbar_wait_bounded(&tfull[b], (uint32_t)((ch >> 1) & 1)) ? 1 : 0)) {
+          if (!mbar_wait_warp(&tfull[b], (uint32_t)((ch >> 1) & 1))) {
             ok = false;
             break;
           }

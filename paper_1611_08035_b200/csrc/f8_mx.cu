@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int s = pos.s, here = min(kPerStage, p.kb - kb);
           if (filled < kStages) {
             ++filled;
-          } else if (!mbar_wait_lane(&empty[s], pos.phase ^ 1u)) {
+          } else if (!mbar_wait_bounded(&empty[s], pos.phase ^ 1u)) {
             ok = false;
             break;
           }
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) {
         atomicExch(p.status, (int)B2_ERR_TIMEOUT);
         if (rank == 0)  // both CTAs' copies are counted here; no CTA leaves before the barrier at the end
-          for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_lane(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
+          for (int i = 0; i < filled; ++i, pos.next()) (void)mbar_wait_bounded(&full[pos.s], pos.phase ^ 1u, kDrainLimitNs);
       }
     } else if (warp == 1 && rank == 0) {
       RingPos<kStages> pos;

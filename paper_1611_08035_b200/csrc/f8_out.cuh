@@ -179,7 +179,9 @@ __device__ __forceinline__ void f8_split_join(const F8Out& p, const void* tile, 
           v[e] *= p.alpha;
           if (p.beta != 0.0f && e < nv) v[e] += p.beta * f8_load1(c + e);
         }
-        if (p.vec && nv >= 4) {
+        if (!p.vec) {
+          *reinterpret_cast<float4*>(const_cast<float*>(static_cast<const float*>(tile)) + o * share_pitch(INNER) + in) = make_float4(v[0], v[1], v[2], v[3]);
+        } else if (nv >= 4) {
           if constexpr (sizeof(TC) == 4) *reinterpret_cast<float4*>(c) = make_float4(v[0], v[1], v[2], v[3]);
           else *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
         } else {
@@ -187,6 +189,15 @@ __device__ __forceinline__ void f8_split_join(const F8Out& p, const void* tile, 
           for (int e = 0; e < 4; ++e)
             if (e < nv) f8_store1(c + e, v[e]);
         }
+      }
+    }
+    if (!p.vec) {  // columns of C that start anywhere: from this CTA's own part of its own share, which no other CTA reads, lane by lane
+      asm volatile("bar.sync 2, %0;" ::"n"(32 * EW) : "memory");
+      for (int i = worker; i < per * INNER; i += 32 * EW) {
+        const int o = share * per + i / INNER, in = i % INNER;
+        const int64_t row = row0 + (COLS_CONTIG ? o : in), col = col0 + (COLS_CONTIG ? in : o);
+        if (row < p.rows && col < p.cols)
+          f8_store1(static_cast<TC*>(p.C) + (COLS_CONTIG ? row * p.ldc + col : col * p.ldc + row), static_cast<const float*>(tile)[o * share_pitch(INNER) + in]);
       }
     }
   }

@@ -147,31 +147,9 @@ __device__ __forceinline__ bool elect_one() {
       : "=r"(e));
   return e != 0;
 }
-// Bounded wait of a warp with nothing else to do.  The hint lets the hardware suspend it for up to a millisecond at a time
-// instead of having it poll, which takes issue slots and shared-memory cycles from the warps that work.
-constexpr uint32_t kSuspendNs = 1000 * 1000;
-__device__ __forceinline__ bool mbar_suspend(uint64_t* bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(done)
-      : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs)
-      : "memory");
-  return done != 0;
-}
-__device__ __forceinline__ bool mbar_wait_lane(uint64_t* bar, uint32_t parity, uint64_t limit_ns = kWaitLimitNs) {
-  if (mbar_suspend(bar, parity)) return true;
-  const uint64_t t0 = global_timer_ns();
-  do {
-    if (mbar_suspend(bar, parity)) return true;
-  } while (global_timer_ns() - t0 < limit_ns);
-  return false;
-}
-// the same answer in all lanes
+// Bounded wait of a converged warp, with the same answer in all lanes.
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, uint64_t limit_ns = kWaitLimitNs) {
-  return __all_sync(0xffffffffu, mbar_wait_lane(bar, parity, limit_ns) ? 1 : 0) != 0;
+  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, limit_ns) ? 1 : 0) != 0;
 }
 __device__ __forceinline__ bool mbar_test_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, mbar_test_wait(bar, parity) ? 1 : 0) != 0;
