@@ -456,40 +456,35 @@ def b2_gemm_strided_batched(transa, transb, m, n, k, alpha, A, lda, stride_a, B,
 
 
 # ---- linear layers in 8 bits --------------------------------------------------------------------------------
+# A decoding step makes these calls on a few tokens, where the GPU needs two or three microseconds: the checks are written
+# out, without loops or helper calls, because they cost as much.
 _TYPES = {torch.float32: 1, torch.bfloat16: 2}  # B2_TYPE_*
 _SCALES = {torch.float8_e8m0fnu: 0, torch.float32: 1}  # B2_SCALE_*
+_E4M3, _E8M0, _F32, _BF16 = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float32, torch.bfloat16
 
 
-def _typed(fn: str, table: dict, t, what: str) -> int:
-    """Code of a tensor's type, which the library takes as an argument."""
-    code = table.get(t.dtype)
-    if code is None:
-        raise TypeError(f"{fn}: {what} is {t.dtype}, not one of {', '.join(str(k) for k in table)}")
-    return code
-
-
-def _want(fn: str, *pairs) -> None:
-    for t, dtype in pairs:
-        if t is not None and (t.dtype != dtype or not t.is_cuda):
-            raise TypeError(f"{fn} takes a {dtype} CUDA tensor where it was given {t.dtype} on {t.device}")
-
-
-def _nbytes(t) -> int:
-    return 0 if t is None else t.numel() * t.element_size()
+def _refuse(fn: str, *args) -> None:
+    """args: (name, tensor or None, allowed dtypes).  Raises for the first one that is not a CUDA tensor of such a type."""
+    for name, t, allowed in args:
+        if t is not None and (t.dtype not in allowed or not t.is_cuda):
+            raise TypeError(f"{fn}: {name} is {t.dtype} on {t.device}; it takes a CUDA tensor of {' or '.join(map(str, allowed))}")
+    raise TypeError(f"{fn}: tensors of different types")
 
 
 def b2_rmsnorm_f8(d, t, x, ldx, residual, ldr, w, eps, h, ldh, q, ldq, s, lds, rstd, check=True) -> int:
     """h = x + residual; y = h / sqrt(mean(h^2) + eps) * w per token (column of d); y leaves as e4m3 numbers q with e8m0
     scales s, one for 128 features.  x, residual, w, h: bfloat16 or float32 alike; residual, h and rstd (float32) may be None."""
-    fn = "b2_rmsnorm_f8"
-    code = _typed(fn, _TYPES, x, "x")
     dt = x.dtype
-    _want(fn, (x, dt), (residual, dt), (w, dt), (h, dt), (q, torch.float8_e4m3fn), (s, torch.float8_e8m0fnu),
-          (rstd, torch.float32))
-    rc = lib().b2_rmsnorm_f8(d, t, code, x.data_ptr(), ldx, _ptr(residual), ldr, w.data_ptr(), eps, _ptr(h), ldh,
-                             q.data_ptr(), ldq, s.data_ptr(), lds, _ptr(rstd), _stream())
-    if check:
-        _check(fn, rc)
+    if not (dt in _TYPES and w.dtype is dt and q.dtype is _E4M3 and s.dtype is _E8M0 and x.is_cuda and w.is_cuda and q.is_cuda and s.is_cuda
+            and (residual is None or (residual.dtype is dt and residual.is_cuda)) and (h is None or (h.dtype is dt and h.is_cuda))
+            and (rstd is None or (rstd.dtype is _F32 and rstd.is_cuda))):
+        _refuse("b2_rmsnorm_f8", ("x", x, tuple(_TYPES)), ("residual", residual, (dt,)), ("w", w, (dt,)), ("h", h, (dt,)), ("q", q, (_E4M3,)),
+                ("s", s, (_E8M0,)), ("rstd", rstd, (_F32,)))
+    rc = (_lib or lib()).b2_rmsnorm_f8(d, t, _TYPES[dt], x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, w.data_ptr(),
+                                       eps, None if h is None else h.data_ptr(), ldh, q.data_ptr(), ldq, s.data_ptr(), lds,
+                                       None if rstd is None else rstd.data_ptr(), _stream())
+    if rc and check:
+        raise B2Error("b2_rmsnorm_f8", rc)
     return rc
 
 
@@ -500,26 +495,29 @@ def b2_rmsnorm_backward_workspace_bytes(d: int, t: int) -> int:
 def b2_rmsnorm_backward(d, t, dy, lddy, h, ldh, rstd, w, dh, lddh, dx, lddx, dw, workspace, check=True) -> int:
     """Gradients of the norm: dx (of x and residual alike; dh, the gradient that reaches h directly, is added, or None)
     and dw (float32, d).  dy, h, w, dh, dx: bfloat16 or float32 alike."""
-    fn = "b2_rmsnorm_backward"
-    code = _typed(fn, _TYPES, dy, "dy")
     dt = dy.dtype
-    _want(fn, (dy, dt), (h, dt), (w, dt), (dh, dt), (dx, dt), (rstd, torch.float32), (dw, torch.float32))
-    rc = lib().b2_rmsnorm_backward(d, t, code, dy.data_ptr(), lddy, h.data_ptr(), ldh, rstd.data_ptr(), w.data_ptr(),
-                                   _ptr(dh), lddh, dx.data_ptr(), lddx, dw.data_ptr(), _ptr(workspace),
-                                   _nbytes(workspace), _stream())
-    if check:
-        _check(fn, rc)
+    if not (dt in _TYPES and h.dtype is dt and w.dtype is dt and dx.dtype is dt and rstd.dtype is _F32 and dw.dtype is _F32 and dy.is_cuda
+            and h.is_cuda and w.is_cuda and dx.is_cuda and rstd.is_cuda and dw.is_cuda and (dh is None or (dh.dtype is dt and dh.is_cuda))
+            and (workspace is None or workspace.is_cuda)):
+        _refuse("b2_rmsnorm_backward", ("dy", dy, tuple(_TYPES)), ("h", h, (dt,)), ("w", w, (dt,)), ("dh", dh, (dt,)), ("dx", dx, (dt,)),
+                ("rstd", rstd, (_F32,)), ("dw", dw, (_F32,)), ("workspace", workspace, (torch.uint8,)))
+    rc = (_lib or lib()).b2_rmsnorm_backward(d, t, _TYPES[dt], dy.data_ptr(), lddy, h.data_ptr(), ldh, rstd.data_ptr(), w.data_ptr(),
+                                             None if dh is None else dh.data_ptr(), lddh, dx.data_ptr(), lddx, dw.data_ptr(),
+                                             None if workspace is None else workspace.data_ptr(),
+                                             0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    if rc and check:
+        raise B2Error("b2_rmsnorm_backward", rc)
     return rc
 
 
 def b2_quant_f8(d, t, block, x, ldx, q, ldq, s, lds, check=True) -> int:
     """x (d x t, bfloat16 or float32) as e4m3 numbers q with e8m0 scales s for blocks of 128 features by 1 or 128 tokens."""
-    fn = "b2_quant_f8"
-    code = _typed(fn, _TYPES, x, "x")
-    _want(fn, (x, x.dtype), (q, torch.float8_e4m3fn), (s, torch.float8_e8m0fnu))
-    rc = lib().b2_quant_f8(d, t, block, code, x.data_ptr(), ldx, q.data_ptr(), ldq, s.data_ptr(), lds, _stream())
-    if check:
-        _check(fn, rc)
+    code = _TYPES.get(x.dtype)
+    if not (code and q.dtype is _E4M3 and s.dtype is _E8M0 and x.is_cuda and q.is_cuda and s.is_cuda):
+        _refuse("b2_quant_f8", ("x", x, tuple(_TYPES)), ("q", q, (_E4M3,)), ("s", s, (_E8M0,)))
+    rc = (_lib or lib()).b2_quant_f8(d, t, block, code, x.data_ptr(), ldx, q.data_ptr(), ldq, s.data_ptr(), lds, _stream())
+    if rc and check:
+        raise B2Error("b2_quant_f8", rc)
     return rc
 
 
@@ -530,15 +528,17 @@ def b2_gemm_f8_workspace_bytes(transa, transb, m, n, k, A, lda, B, ldb) -> int:
 def b2_gemm_f8(transa, transb, m, n, k, alpha, A, lda, SA, ldsa, block_a, B, ldb, SB, ldsb, block_b, beta, C, ldc,
                workspace=None, check=True) -> int:
     """C := alpha*op(A)*op(B) + beta*C of block-scaled e4m3 matrices; scales float8_e8m0fnu or float32, C bfloat16 or float32."""
-    fn = "b2_gemm_f8"
-    code = _typed(fn, _TYPES, C, "C")
-    ca, cb = _typed(fn, _SCALES, SA, "SA"), _typed(fn, _SCALES, SB, "SB")
-    _want(fn, (A, torch.float8_e4m3fn), (B, torch.float8_e4m3fn), (SA, SA.dtype), (SB, SB.dtype), (C, C.dtype))
-    rc = lib().b2_gemm_f8(_tr(transa), _tr(transb), m, n, k, alpha, A.data_ptr(), lda, SA.data_ptr(), ldsa, block_a, ca,
-                          B.data_ptr(), ldb, SB.data_ptr(), ldsb, block_b, cb, beta, C.data_ptr(), ldc, code,
-                          _ptr(workspace), _nbytes(workspace), _stream())
-    if check:
-        _check(fn, rc)
+    code, ca, cb = _TYPES.get(C.dtype), _SCALES.get(SA.dtype), _SCALES.get(SB.dtype)
+    if not (code and ca is not None and cb is not None and A.dtype is _E4M3 and B.dtype is _E4M3 and A.is_cuda and B.is_cuda and C.is_cuda
+            and SA.is_cuda and SB.is_cuda and (workspace is None or workspace.is_cuda)):
+        _refuse("b2_gemm_f8", ("A", A, (_E4M3,)), ("SA", SA, tuple(_SCALES)), ("B", B, (_E4M3,)), ("SB", SB, tuple(_SCALES)),
+                ("C", C, tuple(_TYPES)), ("workspace", workspace, (torch.uint8,)))
+    rc = (_lib or lib()).b2_gemm_f8(_tr(transa), _tr(transb), m, n, k, alpha, A.data_ptr(), lda, SA.data_ptr(), ldsa, block_a, ca, B.data_ptr(), ldb,
+                                    SB.data_ptr(), ldsb, block_b, cb, beta, C.data_ptr(), ldc, code,
+                                    None if workspace is None else workspace.data_ptr(),
+                                    0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    if rc and check:
+        raise B2Error("b2_gemm_f8", rc)
     return rc
 
 
@@ -548,11 +548,14 @@ def b2_wgrad_f8_workspace_bytes(m, n, k, Q, ldq, Y, ldy) -> int:
 
 def b2_wgrad_f8(m, n, k, alpha, Q, ldq, S, lds, Y, ldy, beta, C, ldc, workspace=None, check=True) -> int:
     """C (m x n) := alpha * X Y^T + beta*C over k tokens, X = Q*S an activation kept in 8 bits, Y bfloat16 gradients."""
-    fn = "b2_wgrad_f8"
-    code = _typed(fn, _TYPES, C, "C")
-    _want(fn, (Q, torch.float8_e4m3fn), (S, torch.float8_e8m0fnu), (Y, torch.bfloat16), (C, C.dtype))
-    rc = lib().b2_wgrad_f8(m, n, k, alpha, Q.data_ptr(), ldq, S.data_ptr(), lds, Y.data_ptr(), ldy, beta, C.data_ptr(),
-                           ldc, code, _ptr(workspace), _nbytes(workspace), _stream())
-    if check:
-        _check(fn, rc)
+    code = _TYPES.get(C.dtype)
+    if not (code and Q.dtype is _E4M3 and S.dtype is _E8M0 and Y.dtype is _BF16 and Q.is_cuda and S.is_cuda and Y.is_cuda and C.is_cuda
+            and (workspace is None or workspace.is_cuda)):
+        _refuse("b2_wgrad_f8", ("Q", Q, (_E4M3,)), ("S", S, (_E8M0,)), ("Y", Y, (_BF16,)), ("C", C, tuple(_TYPES)),
+                ("workspace", workspace, (torch.uint8,)))
+    rc = (_lib or lib()).b2_wgrad_f8(m, n, k, alpha, Q.data_ptr(), ldq, S.data_ptr(), lds, Y.data_ptr(), ldy, beta, C.data_ptr(), ldc, code,
+                                     None if workspace is None else workspace.data_ptr(),
+                                     0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    if rc and check:
+        raise B2Error("b2_wgrad_f8", rc)
     return rc

@@ -36,7 +36,8 @@ struct F8Cfg {
   static constexpr int SLOTS = 4, SF_COLS = 8;              // scale ring in tensor memory: 4 columns for 128 rows, 4 for 128 columns
   static constexpr uint32_t TMEM = MX ? (TBN <= 32 ? 64 : TBN == 64 ? 128 : 256) : (TBN == 16 ? 32 : 2 * TBN);
   static_assert(!MX || TBN + SLOTS * SF_COLS <= (int)TMEM, "sums and scales");
-  static constexpr size_t SMEM = 1024 + RING + 512 + EW * (TBN >= 128 ? kEmitBytes : COLS * (int)sizeof(float));
+  static constexpr int SCRATCH = kEmitBytes > COLS * 4 ? kEmitBytes : COLS * 4;  // of a warp: staged rows of C, or a block's column scales
+  static constexpr size_t SMEM = 1024 + RING + 512 + EW * SCRATCH;
   static_assert(share_bytes(TBN) <= RING, "the split's shares pass through the ring");
 };
 
@@ -78,6 +79,8 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
+    tma_prefetch_map(&map_r);
+    tma_prefetch_map(&map_c);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
@@ -134,8 +137,8 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
   } else if (warp == 1) {
     const uint32_t a0 = smem_u32(ring), b0 = a0 + kRowStage;
     const uint64_t da0 = p.r_mn ? umma_desc_mn_major_sw128(a0, kRowStage) : umma_desc_k_major_sw128(a0);
-    const uint64_t db0 = p.c_mn ? umma_desc_mn_major_sw128(b0, kRowStage) : umma_desc_k_major_sw128(b0);
-    const uint32_t step_a = p.r_mn ? 4096 : 32, step_b = p.c_mn ? 4096 : 32;  // bytes between instructions of a block
+    const uint64_t db0 = !p.c_mn ? umma_desc_k_major_sw128(b0) : TBN == 64 ? umma_desc_mn_major_sw64(b0) : umma_desc_mn_major_sw128(b0, kRowStage);
+    const uint32_t step_a = p.r_mn ? 4096 : 32, step_b = p.c_mn ? 32 * TBN : 32;  // bytes between instructions of a block
     const uint32_t idesc = MX ? umma_idesc_mx(kRows, TBN, p.r_mn, p.c_mn, 0) : umma_idesc_f8(kRows, TBN, p.r_mn, p.c_mn);
     RingPos<STAGES> pos;
     RingPos<Cfg::SLOTS> slot;
@@ -241,7 +244,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
           if (lane == 0) mbar_arrive(&tempty[0]);
         }
       } else {
-        float* scw = reinterpret_cast<float*>(scratch) + ew * COLS;
+        float* scw = reinterpret_cast<float*>(scratch + ew * Cfg::SCRATCH);
         const int64_t srow = row < p.out.rows ? row : p.out.rows - 1;
 #pragma unroll
         for (int j = 0; j < COLS; ++j) acc[j] = 0.0f;
@@ -298,7 +301,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
         // this CTA's share of the tile; the ring is idle once the last block's sums have been read
         f8_put_share<COLS_CONTIG, TBN, COLS>(ring, quad * 32 + lane, half * COLS, acc);
       } else if constexpr (COLS_CONTIG) {
-        f8_emit_staged<TC, COLS>(p.out, row - lane, col0, acc, scratch + ew * kEmitBytes);
+        f8_emit_staged<TC, COLS>(p.out, row - lane, col0, acc, scratch + ew * Cfg::SCRATCH);
       } else {
         f8_emit_rows<TC, COLS>(p.out, row, col0, acc);
       }
@@ -356,7 +359,7 @@ int f8_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, int s
   }
   CUtensorMap mr, mc;
   if (!f8_map(&mr, r.p, r.mn ? r.n : k, r.mn ? k : r.n, r.ld, 128) ||
-      !f8_map(&mc, c.p, c.mn ? c.n : k, c.mn ? k : c.n, c.ld, c.mn ? 128 : TBN))
+      !f8_map(&mc, c.p, c.mn ? c.n : k, c.mn ? k : c.n, c.ld, c.mn ? 128 : TBN, c.mn ? TBN : 128))
     return B2_ERR_LAUNCH;
   const int64_t tr = blocks_of(r.n, kRows), tc = blocks_of(c.n, TBN);
   if (tr * tc > 0x7fffffffLL) return B2_ERR_VARIANT;
@@ -376,25 +379,42 @@ int f8_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, int s
   return cudaLaunchKernelEx(&cfg, kfn, a, mr, mc) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
 }
 
+// CTAs that share a tile's k range, and what the product then takes, in clocks: turns of CTAs over the SMs, a turn being its
+// share of the blocks at 50 bytes of operands a clock, the rate at which one SM's copies arrived when measured, and adding the
+// shares, about 30 clocks a column of the tile when measured.  Clusters of eight do not fill every group of SMs.
+struct F8Split {
+  int s;
+  double clocks;
+};
+F8Split f8_split_for(int64_t tiles, int kb, int tbn, int resident) {
+  const double stage = (kRowStage + tbn * kF8Block) / 50.0, join = 30.0 * tbn;
+  F8Split best{1, 0.0};
+  for (int s = 1, log = 0; s <= kMaxSplit && (s == 1 || kb / s >= 2); s *= 2, ++log) {
+    const int64_t slots = (int64_t)sm_count_cached() * resident * (s == 8 ? 3 : 4) / 4;
+    const double clocks = (double)blocks_of(tiles * s, slots) * resident * (double)blocks_of(kb, s) * stage + (s > 1 ? join * (0.7 + 0.3 * log) : 0.0);
+    if (s == 1 || clocks < best.clocks) best = {s, clocks};
+  }
+  return best;
+}
+
 template <typename TC, bool MX>
 int f8_choose(const F8Args& a, const F8Operand& A, const F8Operand& B, int64_t k, cudaStream_t st) {
   const int sms = sm_count_cached();
-  // CTAs that share a tile: as many as leave every one of them a few blocks and no SM without a CTA
-  auto splits_for = [&](int64_t tiles, int resident) {
-    int s = 1;
-    while (s < kMaxSplit && tiles * s * 2 <= (int64_t)sms * resident && a.kb / (s * 2) >= 2) s *= 2;
-    return s;
-  };
-  if (B.n <= 64 && !B.mn) {  // decoding
-    const int s = splits_for(blocks_of(A.n, kRows), 2);
-    if (B.n <= 16) return f8_launch<16, TC, false, MX>(a, A, B, k, s, st);
-    if (B.n <= 32) return f8_launch<32, TC, false, MX>(a, A, B, k, s, st);
+  if (B.n <= 64 && !B.mn) {  // decoding: A's rows, tiles as narrow as n, two CTAs an SM
+    const int tbn = B.n <= 16 ? 16 : B.n <= 32 ? 32 : 64;
+    const int64_t tiles = blocks_of(A.n, kRows);
+    const int s = f8_split_for(tiles, a.kb, tbn, tiles >= sms ? 2 : 1).s;
+    if (tbn == 16) return f8_launch<16, TC, false, MX>(a, A, B, k, s, st);
+    if (tbn == 32) return f8_launch<32, TC, false, MX>(a, A, B, k, s, st);
     return f8_launch<64, TC, false, MX>(a, A, B, k, s, st);
   }
   // pairs of CTAs as soon as single ones, with tiles a quarter of the size, would take more than one turn
   if (blocks_of(B.n, 256) * blocks_of(A.n, 256) * 4 > sms) return MX ? f8_mx_launch<TC>(a, B, A, k, st) : f8_fs_launch<TC>(a, B, A, k, st);
-  const int s = splits_for(blocks_of(B.n, kRows) * blocks_of(A.n, 128), 1);
-  return f8_launch<128, TC, true, MX>(a, B, A, k, s, st);
+  const F8Split wide = f8_split_for(blocks_of(B.n, kRows) * blocks_of(A.n, 128), a.kb, 128, 1);
+  const F8Split narrow = f8_split_for(blocks_of(B.n, kRows) * blocks_of(A.n, 64), a.kb, 64, 1);
+  // half as many columns a tile fetch more than half as much, but spare the join when they fill the SMs without a split
+  if (narrow.clocks < wide.clocks) return f8_launch<64, TC, true, MX>(a, B, A, k, narrow.s, st);
+  return f8_launch<128, TC, true, MX>(a, B, A, k, wide.s, st);
 }
 
 bool f8_is_n(char c) { return c == 'N' || c == 'n'; }

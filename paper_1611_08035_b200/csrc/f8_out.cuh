@@ -85,14 +85,20 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
         *reinterpret_cast<float4*>(own + 16 * i) = make_float4(p.alpha * acc[j + 4 * i], p.alpha * acc[j + 4 * i + 1], p.alpha * acc[j + 4 * i + 2], p.alpha * acc[j + 4 * i + 3]);
       __syncwarp();
       if (!p.vec) {  // columns of C that start anywhere: element by element, sixteen lanes to a row
-        const int64_t col = col0 + j + (lane & 15);
-#pragma unroll 4
-        for (int i = 0; i < 16; ++i) {
-          const int r = 2 * i + (lane >> 4);
-          float v = *reinterpret_cast<const float*>(stage + r * kEmitPitch + (lane & 15) * 4);
-          TC* c = C + (row0 + r) * p.ldc + col;
-          if (row0 + r < p.rows && col < p.cols) f8_store1(c, p.beta != 0.0f ? v + p.beta * f8_load1(c) : v);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const float*>(stage + (2 * i + (lane >> 4)) * kEmitPitch + (lane & 15) * 4);
+        const int64_t col = col0 + j + (lane & 15), row = row0 + (lane >> 4);
+        const int64_t rows = col < p.cols ? p.rows - row : 0;
+        TC* c = C + row * p.ldc + col;
+        if (p.beta != 0.0f) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (2 * i < rows) v[i] += p.beta * f8_load1(c + 2 * i * p.ldc);
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (2 * i < rows) f8_store1(c + 2 * i * p.ldc, v[i]);
         continue;
       }
       const int64_t col = col0 + j + piece * 4, nv = p.cols - col;
@@ -126,7 +132,7 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
 // order of their rank, for its part of the other index, four numbers at a time and all ranks' numbers on their way at once
 // (one after the other, their latency made up most of a 1024^3 product: 21 us).  All threads of all CTAs of the cluster call this; the
 // 32 EW threads with worker >= 0 (numbered) add and write.  PERMUTE: row r of the tile is row kept_row(r) of C.
-constexpr int kMaxSplit = 8;
+constexpr int kMaxSplit = 8;  // 2, 4 or 8 CTAs
 __host__ __device__ constexpr int share_pitch(int inner) { return inner + 4; }  // 16-byte pieces of consecutive lines in different banks
 __host__ __device__ constexpr int share_bytes(int tbn) { return 4 * (tbn * share_pitch(128) > 128 * share_pitch(tbn) ? tbn * share_pitch(128) : 128 * share_pitch(tbn)); }
 __device__ __forceinline__ int kept_row(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
@@ -145,64 +151,79 @@ __device__ __forceinline__ void f8_put_share(void* tile, int row, int col, const
   }
 }
 
-template <typename TC, bool COLS_CONTIG, int TBN, int EW, bool PERMUTE>
-__device__ __forceinline__ void f8_split_join(const F8Out& p, const void* tile, int splits, int share, int worker, int64_t row0,
-                                              int64_t col0) {
-  cluster_sync_all();
-  if (worker >= 0) {
-    constexpr int INNER = COLS_CONTIG ? TBN : 128, OUTER = COLS_CONTIG ? 128 : TBN;
-    const int per = OUTER / splits;
-    for (int i = worker; i < per * (INNER / 4); i += 32 * EW) {
-      const int o = share * per + i / (INNER / 4), in = i % (INNER / 4) * 4;
-      const uint32_t at = smem_u32(tile) + (uint32_t)(o * share_pitch(INNER) + in) * 4;
-      float x[kMaxSplit][4];
+template <typename TC, bool COLS_CONTIG, int TBN, int EW, bool PERMUTE, int S>
+__device__ __forceinline__ void f8_add_shares(const F8Out& p, void* tile, int share, int worker, int64_t row0, int64_t col0) {
+  constexpr int INNER = COLS_CONTIG ? TBN : 128, OUTER = COLS_CONTIG ? 128 : TBN, PER = OUTER / S;
+  constexpr int PIECES = PER * (INNER / 4), WORKERS = 32 * EW, U = (PIECES + WORKERS - 1) / WORKERS;
+  uint32_t base[S];
 #pragma unroll
-      for (int q = 0; q < kMaxSplit; ++q)
-        if (q < splits)
-          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                       : "=f"(x[q][0]), "=f"(x[q][1]), "=f"(x[q][2]), "=f"(x[q][3])
-                       : "r"(cluster_map_shared(at, (uint32_t)q)));
-      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int q = 0; q < S; ++q) base[q] = cluster_map_shared(smem_u32(tile), (uint32_t)q);
+  float x[U][S][4];
 #pragma unroll
-      for (int q = 0; q < kMaxSplit; ++q)
-        if (q < splits) v[0] += x[q][0], v[1] += x[q][1], v[2] += x[q][2], v[3] += x[q][3];
-      if (PERMUTE) {
-        const float t = v[1];
-        v[1] = v[2], v[2] = t;
-      }
-      const int64_t row = row0 + (COLS_CONTIG ? o : in), col = col0 + (COLS_CONTIG ? in : o);
-      const int64_t nv = COLS_CONTIG ? p.cols - col : p.rows - row;
-      if (COLS_CONTIG ? row < p.rows : col < p.cols) {
-        TC* c = static_cast<TC*>(p.C) + (COLS_CONTIG ? row * p.ldc + col : col * p.ldc + row);
+  for (int u = 0; u < U; ++u) {
+    const int i = worker + u * WORKERS;
+    const uint32_t at = (uint32_t)((share * PER + i / (INNER / 4)) * share_pitch(INNER) + i % (INNER / 4) * 4) * 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] *= p.alpha;
-          if (p.beta != 0.0f && e < nv) v[e] += p.beta * f8_load1(c + e);
-        }
-        if (!p.vec) {
-          *reinterpret_cast<float4*>(const_cast<float*>(static_cast<const float*>(tile)) + o * share_pitch(INNER) + in) = make_float4(v[0], v[1], v[2], v[3]);
-        } else if (nv >= 4) {
-          if constexpr (sizeof(TC) == 4) *reinterpret_cast<float4*>(c) = make_float4(v[0], v[1], v[2], v[3]);
-          else *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-        } else {
+    for (int q = 0; q < S; ++q)
+      if (PIECES % WORKERS == 0 || i < PIECES)
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(x[u][q][0]), "=f"(x[u][q][1]), "=f"(x[u][q][2]), "=f"(x[u][q][3])
+                     : "r"(base[q] + at));
+  }
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e < nv) f8_store1(c + e, v[e]);
-        }
-      }
+  for (int u = 0; u < U; ++u) {
+    const int i = worker + u * WORKERS, o = share * PER + i / (INNER / 4), in = i % (INNER / 4) * 4;
+    if (PIECES % WORKERS != 0 && i >= PIECES) break;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int q = 0; q < S; ++q) v[0] += x[u][q][0], v[1] += x[u][q][1], v[2] += x[u][q][2], v[3] += x[u][q][3];
+    if (PERMUTE) {
+      const float t = v[1];
+      v[1] = v[2], v[2] = t;
     }
-    if (!p.vec) {  // columns of C that start anywhere: from this CTA's own part of its own share, which no other CTA reads, lane by lane
-      asm volatile("bar.sync 2, %0;" ::"n"(32 * EW) : "memory");
-      for (int i = worker; i < per * INNER; i += 32 * EW) {
-        const int o = share * per + i / INNER, in = i % INNER;
-        const int64_t row = row0 + (COLS_CONTIG ? o : in), col = col0 + (COLS_CONTIG ? in : o);
-        if (row < p.rows && col < p.cols)
-          f8_store1(static_cast<TC*>(p.C) + (COLS_CONTIG ? row * p.ldc + col : col * p.ldc + row), static_cast<const float*>(tile)[o * share_pitch(INNER) + in]);
+    const int64_t row = row0 + (COLS_CONTIG ? o : in), col = col0 + (COLS_CONTIG ? in : o);
+    const int64_t nv = COLS_CONTIG ? p.cols - col : p.rows - row;
+    if (COLS_CONTIG ? row < p.rows : col < p.cols) {
+      TC* c = static_cast<TC*>(p.C) + (COLS_CONTIG ? row * p.ldc + col : col * p.ldc + row);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] *= p.alpha;
+        if (p.beta != 0.0f && e < nv) v[e] += p.beta * f8_load1(c + e);
+      }
+      if (!p.vec) {
+        *reinterpret_cast<float4*>(static_cast<float*>(tile) + o * share_pitch(INNER) + in) = make_float4(v[0], v[1], v[2], v[3]);
+      } else if (nv >= 4) {
+        if constexpr (sizeof(TC) == 4) *reinterpret_cast<float4*>(c) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < nv) f8_store1(c + e, v[e]);
       }
     }
   }
+  if (!p.vec) {  // columns of C that start anywhere: from this CTA's own part of its own share, which no other CTA reads, lane by lane
+    asm volatile("bar.sync 2, %0;" ::"n"(WORKERS) : "memory");
+    for (int i = worker; i < PER * INNER; i += WORKERS) {
+      const int o = share * PER + i / INNER, in = i % INNER;
+      const int64_t row = row0 + (COLS_CONTIG ? o : in), col = col0 + (COLS_CONTIG ? in : o);
+      if (row < p.rows && col < p.cols)
+        f8_store1(static_cast<TC*>(p.C) + (COLS_CONTIG ? row * p.ldc + col : col * p.ldc + row), static_cast<const float*>(tile)[o * share_pitch(INNER) + in]);
+    }
+  }
+}
+
+template <typename TC, bool COLS_CONTIG, int TBN, int EW, bool PERMUTE>
+__device__ __forceinline__ void f8_split_join(const F8Out& p, void* tile, int splits, int share, int worker, int64_t row0, int64_t col0) {
+  cluster_sync_all();
+  if (worker >= 0) {
+    if (splits == 2) f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 2>(p, tile, share, worker, row0, col0);
+    else if (splits == 4) f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 4>(p, tile, share, worker, row0, col0);
+    else f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 8>(p, tile, share, worker, row0, col0);
+  }
   __syncwarp();
-  cluster_sync_all();  // no CTA leaves while another one reads its share
+  // no CTA leaves while another one reads its share; what was read has arrived, so there is nothing to release
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
 // C := beta * C, and copies of operands into 16-byte aligned columns (ldd a multiple of 16 bytes); defined in f8_gemm.cu.

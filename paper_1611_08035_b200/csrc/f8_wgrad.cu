@@ -138,6 +138,8 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CTAS == 2 ? cluster_rank() : 0;
   if (tid == 0) {
+    tma_prefetch_map(&map_q);
+    tma_prefetch_map(&map_y);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&full[s], 3);
       mbar_init(&conv[s], CTAS * CW);

@@ -131,9 +131,25 @@ __device__ __forceinline__ uint64_t umma_desc_mn_major_sw128(uint32_t smem_addr,
   return d;
 }
 
+// A tile 64 bytes wide along its own index: 64-byte rows under the 64-byte swizzle, groups of eight 512 bytes apart.
+__device__ __forceinline__ uint64_t umma_desc_mn_major_sw64(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr >> 4) & 0x3FFF);
+  d |= (uint64_t)1 << 16;
+  d |= (uint64_t)(512 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)4 << 61;
+  return d;
+}
+
 // The descriptor of a tile `bytes` further in shared memory (the address field holds 16-byte units below 2^14, so that
 // the addition never leaves it).
 __device__ __forceinline__ uint64_t umma_desc_advance(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
+
+// A tensor map is fetched before its first copy needs it.
+__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
 
 // One lane of a converged warp.  The warp that feeds the tensor core runs its loop as a whole and only the instructions
 // themselves are under this predicate: their descriptors and addresses are uniform registers, which the compiler computes
