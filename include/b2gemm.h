@@ -417,6 +417,7 @@ int b2_model_enumerate(int dtype, int top, char* json_out, size_t cap);
  *
  * The quantisation rule of b2_rmsnorm_f8 and b2_quant_f8, per block of values v: with a = max|v|,
  *     s = the smallest power of two with a/s <= 448   (1 when a == 0, at least 2^-127),   q = v/s rounded to nearest even e4m3.
+ * Fewer than 2^31 - 8192 features and 2^31 tokens, else B2_ERR_VARIANT.
  * Nothing saturates.  A block that holds a NaN or an infinity is stored as NaN throughout (scale byte 255, every q 0x7f).
  * Division by a power of two is exact, so q*s differs from v by the one rounding to e4m3; q*s is representable in bf16.
  */

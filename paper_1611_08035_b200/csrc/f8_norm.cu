@@ -14,13 +14,13 @@ namespace b2 {
 namespace {
 
 struct NormArgs {
-  int64_t d, t;
+  int d;
+  int64_t t;
   const void *X, *R, *w;
   void *H, *Q, *S;
   int64_t ldx, ldr, ldh, ldq, lds;
   float* rstd;
   float eps;
-  bool vx, vr, vh, vq, vw;  // 16-byte (Q: 8-byte) alignment of every column
 };
 
 // Sum over the TPR threads of a row; the same value in each of them.
@@ -38,15 +38,10 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
-// largest bit pattern over sixteen neighbouring lanes
-__device__ __forceinline__ uint32_t block_max(uint32_t b) {
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
-  return b;
-}
-
-template <typename T, int TPR, int VPT>
-__global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_kernel(const NormArgs p) {
+// TPR threads to a token, each VPT groups of eight features (Warp256: which eight).
+template <typename T, int TPR, int VPT, bool VEC>
+__global__ void __launch_bounds__(TPR > 128 ? TPR : 128, TPR == 512 && VPT == 4 && sizeof(T) == 2 ? 2 : 1) norm_kernel(const NormArgs p) {
+  using Piece = Warp256<T, VEC>;
   constexpr int NT = TPR > 128 ? TPR : 128, RPC = NT / TPR;
   static_assert(RPC == 1 || TPR == 32, "rows that share a CTA meet at no barrier");
   __shared__ float part[TPR > 32 ? TPR / 32 : 1];
@@ -56,23 +51,18 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_kernel(const NormA
   const T* X = static_cast<const T*>(p.X) + row * p.ldx;
   const T* R = p.R ? static_cast<const T*>(p.R) + row * p.ldr : nullptr;
   T* H = p.H ? static_cast<T*>(p.H) + row * p.ldh : nullptr;
-  const T* W = static_cast<const T*>(p.w);
+  auto first = [&](int i) { return ((l & ~31) + i * TPR) * 8; };
   Raw8<T> rx[VPT], rr[VPT], rw[VPT];  // all loads first
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
-    load8(X + e, nv, p.vx, rx[i]);
-    if (R) load8(R + e, nv, p.vr, rr[i]);
+    Piece::load(X, first(i), p.d, rx[i]);
+    if (R) Piece::load(R, first(i), p.d, rr[i]);
   }
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
-    load8(W + e, nv, p.vw, rw[i]);
-  }
+  for (int i = 0; i < VPT; ++i) Piece::load(static_cast<const T*>(p.w), first(i), p.d, rw[i]);
   float v[VPT][8], ss = 0.0f;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
     unpack8(rx[i], v[i]);
     if (R) {
       float r[8];
@@ -80,7 +70,7 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_kernel(const NormA
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] += r[j];
     }
-    if (H) store8(H + e, nv, p.vh, v[i]);
+    if (H) Piece::store(H, first(i), p.d, v[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) ss += v[i][j] * v[i][j];
   }
@@ -88,130 +78,124 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_kernel(const NormA
   if (p.rstd && l == 0) p.rstd[row] = rstd;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int64_t e = (int64_t)(l + i * TPR) * 8, nv = p.d - e;
     float y[8], w[8];
-    uint32_t m = 0;
     unpack8(rw[i], w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      y[j] = j < nv ? v[i][j] * rstd * w[j] : 0.0f;  // beyond the row: no 0 * inf
-      m = max(m, mag_bits(y[j]));
-    }
-    const uint32_t byte = f8_scale_byte(block_max(m));
-    if (nv > 0) {
-      store8_f8(static_cast<uint8_t*>(p.Q) + row * p.ldq + e, nv, p.vq, f8_quant8(y, byte));
-      if ((l & 15) == 0) static_cast<uint8_t*>(p.S)[row * p.lds + e / kF8Block] = (uint8_t)byte;
-    }
+    for (int j = 0; j < 8; ++j) y[j] = Piece::index(first(i), j) < p.d ? v[i][j] * rstd * w[j] : 0.0f;  // beyond the row: no 0 * inf
+    Piece::quantise(y, static_cast<uint8_t*>(p.Q) + row * p.ldq, static_cast<uint8_t*>(p.S) + row * p.lds, first(i), p.d);
   }
 }
 
 // Tokens too long for registers: the sum first, then everything else from a second reading (of L2).  h is stored in
 // the second pass only, because H may be X or R.
-template <typename T>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs p) {
+  using Piece = Warp256<T, VEC>;
   __shared__ float part[32];
   const int64_t row = blockIdx.x;
   const T* X = static_cast<const T*>(p.X) + row * p.ldx;
   const T* R = p.R ? static_cast<const T*>(p.R) + row * p.ldr : nullptr;
   T* H = p.H ? static_cast<T*>(p.H) + row * p.ldh : nullptr;
-  auto load = [&](int64_t e, float (&v)[8]) {
-    load8(X + e, p.d - e, p.vx, v);
+  auto load = [&](int first, float (&v)[8]) {
+    Raw8<T> a, b;
+    Piece::load(X, first, p.d, a);
+    if (R) Piece::load(R, first, p.d, b);
+    unpack8(a, v);
     if (R) {
       float r[8];
-      load8(R + e, p.d - e, p.vr, r);
+      unpack8(b, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += r[j];
     }
   };
   float ss = 0.0f;
-  for (int64_t e = (int64_t)threadIdx.x * 8; e < p.d; e += 8192) {
+  for (int first = (int)(threadIdx.x & ~31u) * 8; first < p.d; first += 8192) {
     float v[8];
-    load(e, v);
+    load(first, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) ss += v[j] * v[j];
   }
   const float rstd = 1.0f / sqrtf(row_sum<1024>(ss, part) / (float)p.d + p.eps);
   if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
-  for (int64_t base = 0; base < p.d; base += 8192) {  // the same trips for every lane: block_max is warp-wide
-    const int64_t e = base + (int64_t)threadIdx.x * 8, nv = p.d - e;
+  for (int first = (int)(threadIdx.x & ~31u) * 8; first < p.d; first += 8192) {  // the same for the lanes of a warp
     float y[8], w[8];
-    uint32_t m = 0;
-    load(e, y);
-    load8(static_cast<const T*>(p.w) + e, nv, p.vw, w);
-    if (H) store8(H + e, nv, p.vh, y);
+    Raw8<T> rw;
+    Piece::load(static_cast<const T*>(p.w), first, p.d, rw);
+    load(first, y);
+    unpack8(rw, w);
+    if (H) Piece::store(H, first, p.d, y);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      y[j] = j < nv ? y[j] * rstd * w[j] : 0.0f;
-      m = max(m, mag_bits(y[j]));
-    }
-    const uint32_t byte = f8_scale_byte(block_max(m));
-    if (nv > 0) {
-      store8_f8(static_cast<uint8_t*>(p.Q) + row * p.ldq + e, nv, p.vq, f8_quant8(y, byte));
-      if ((threadIdx.x & 15) == 0) static_cast<uint8_t*>(p.S)[row * p.lds + e / kF8Block] = (uint8_t)byte;
-    }
+    for (int j = 0; j < 8; ++j) y[j] = Piece::index(first, j) < p.d ? y[j] * rstd * w[j] : 0.0f;
+    Piece::quantise(y, static_cast<uint8_t*>(p.Q) + row * p.ldq, static_cast<uint8_t*>(p.S) + row * p.lds, first, p.d);
   }
 }
 
-template <typename T>
+template <typename T, bool VEC>
 int norm_launch(const NormArgs& a, cudaStream_t st) {
   const int64_t chunks = blocks_of(a.d, 8);
   if (a.t > 0x7fffffffLL) return B2_ERR_VARIANT;
   const unsigned t = (unsigned)a.t, t4 = (unsigned)blocks_of(a.t, 4);
   if (a.t <= 2 * sm_count_cached() && chunks > 32 && chunks <= 1024) {
     // few tokens: one group of eight per thread, the shortest chain from the load to the store
-    if (chunks <= 128) norm_kernel<T, 128, 1><<<t, 128, 0, st>>>(a);
-    else if (chunks <= 256) norm_kernel<T, 256, 1><<<t, 256, 0, st>>>(a);
-    else if (chunks <= 512) norm_kernel<T, 512, 1><<<t, 512, 0, st>>>(a);
-    else norm_kernel<T, 1024, 1><<<t, 1024, 0, st>>>(a);
-  } else if (chunks <= 32) norm_kernel<T, 32, 1><<<t4, 128, 0, st>>>(a);
-  else if (chunks <= 64) norm_kernel<T, 32, 2><<<t4, 128, 0, st>>>(a);
-  else if (chunks <= 128) norm_kernel<T, 32, 4><<<t4, 128, 0, st>>>(a);
-  else if (chunks <= 256) norm_kernel<T, 128, 2><<<t, 128, 0, st>>>(a);
-  else if (chunks <= 512) norm_kernel<T, 128, 4><<<t, 128, 0, st>>>(a);
-  else if (chunks <= 1024) norm_kernel<T, 256, 4><<<t, 256, 0, st>>>(a);
-  else if (chunks <= 2048) norm_kernel<T, 512, 4><<<t, 512, 0, st>>>(a);
-  else norm_long_kernel<T><<<t, 1024, 0, st>>>(a);
+    if (chunks <= 128) norm_kernel<T, 128, 1, VEC><<<t, 128, 0, st>>>(a);
+    else if (chunks <= 256) norm_kernel<T, 256, 1, VEC><<<t, 256, 0, st>>>(a);
+    else if (chunks <= 512) norm_kernel<T, 512, 1, VEC><<<t, 512, 0, st>>>(a);
+    else norm_kernel<T, 1024, 1, VEC><<<t, 1024, 0, st>>>(a);
+  } else if (chunks <= 32) norm_kernel<T, 32, 1, VEC><<<t4, 128, 0, st>>>(a);
+  else if (chunks <= 64) norm_kernel<T, 32, 2, VEC><<<t4, 128, 0, st>>>(a);
+  else if (chunks <= 128) norm_kernel<T, 32, 4, VEC><<<t4, 128, 0, st>>>(a);
+  else if (chunks <= 256) norm_kernel<T, 128, 2, VEC><<<t, 128, 0, st>>>(a);
+  else if (chunks <= 512) norm_kernel<T, 128, 4, VEC><<<t, 128, 0, st>>>(a);
+  else if (chunks <= 768) norm_kernel<T, 192, 4, VEC><<<t, 192, 0, st>>>(a);
+  else if (chunks <= 1024) norm_kernel<T, 256, 4, VEC><<<t, 256, 0, st>>>(a);
+  else if (chunks <= 2048) norm_kernel<T, 512, 4, VEC><<<t, 512, 0, st>>>(a);
+  else norm_long_kernel<T, VEC><<<t, 1024, 0, st>>>(a);
   return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
 }
 
 // ---- backward -------------------------------------------------------------------------------------------
 struct NormBwdArgs {
-  int64_t d, t;
+  int d;
+  int64_t t;
   const void *DY, *H, *w, *DH;
   void* DX;
   int64_t lddy, ldh, lddh, lddx;
   const float* rstd;
   float* partial;  // [gridDim.x][d]
-  bool vy, vh, vr, vx, vw;
 };
 
-// A CTA walks over the tokens cta, cta + grid, ...; a thread owns the same features of each of them, so that its share of
-// dw stays in registers until the end and leaves as one row of partial sums.
-template <typename T, int NT, int VPT>
+// A CTA walks over the tokens; a thread owns the same features of each of them, so that its share of dw stays in registers until the
+// end and leaves as one row of partial sums.  TPR threads to a token, NT / TPR tokens at a time (one, or one to a warp).
+template <typename T, int TPR, int NT, int VPT, bool VEC>
 __global__ void __launch_bounds__(NT) norm_bwd_kernel(const NormBwdArgs p) {
-  __shared__ float part[2][NT / 32];
-  const int l = threadIdx.x;
+  using Piece = Warp256<T, VEC>;
+  constexpr int RPC = NT / TPR;
+  static_assert(RPC == 1 || TPR == 32, "tokens that share a CTA meet at no barrier");
+  __shared__ float part[2][TPR / 32];
+  const int l = RPC > 1 ? threadIdx.x % TPR : threadIdx.x, sub = RPC > 1 ? threadIdx.x / TPR : 0;
+  const int64_t step = (int64_t)gridDim.x * RPC;
+  auto first = [&](int i) { return ((l & ~31) + i * TPR) * 8; };
   float dw[VPT][8];
   Raw8<T> rw[VPT], ry[VPT], rh[VPT], rg[VPT];
   auto fetch = [&](int64_t row) {
+    const int n = row < p.t ? p.d : 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t e = (int64_t)(l + i * NT) * 8, nv = row < p.t ? p.d - e : 0;
-      load8(static_cast<const T*>(p.DY) + row * p.lddy + e, nv, p.vy, ry[i]);
-      load8(static_cast<const T*>(p.H) + row * p.ldh + e, nv, p.vh, rh[i]);
-      if (p.DH) load8(static_cast<const T*>(p.DH) + row * p.lddh + e, nv, p.vr, rg[i]);
+      Piece::load(static_cast<const T*>(p.DY) + row * p.lddy, first(i), n, ry[i]);
+      Piece::load(static_cast<const T*>(p.H) + row * p.ldh, first(i), n, rh[i]);
+      if (p.DH) Piece::load(static_cast<const T*>(p.DH) + row * p.lddh, first(i), n, rg[i]);
     }
   };
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int64_t e = (int64_t)(l + i * NT) * 8;
-    load8(static_cast<const T*>(p.w) + e, p.d - e, p.vw, rw[i]);
+    Piece::load(static_cast<const T*>(p.w), first(i), p.d, rw[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
   }
   int parity = 0;
-  fetch(blockIdx.x);
-  for (int64_t row = blockIdx.x; row < p.t; row += gridDim.x, parity ^= 1) {
+  const int64_t begin = (int64_t)blockIdx.x * RPC + sub;
+  fetch(begin);
+  for (int64_t row = begin; row < p.t; row += step, parity ^= 1) {
     const float rstd = p.rstd[row];
     Raw8<T> cy[VPT], ch[VPT], cg[VPT];
     float dot = 0.0f;
@@ -227,11 +211,10 @@ __global__ void __launch_bounds__(NT) norm_bwd_kernel(const NormBwdArgs p) {
         dw[i][j] += dy[j] * xh[j];
       }
     }
-    fetch(row + gridDim.x);  // on its way while this token's sum is taken
-    const float mean = row_sum<NT>(dot, part[parity]) / (float)p.d;  // two arrays in turn: one barrier a token
+    fetch(row + step);  // on its way while this token's sum is taken
+    const float mean = row_sum<TPR>(dot, part[parity]) / (float)p.d;  // two arrays in turn: one barrier a token
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t e = (int64_t)(l + i * NT) * 8, nv = p.d - e;
       float dx[8], dy[8], xh[8], w[8], dh[8];
       unpack8(cy[i], dy), unpack8(ch[i], xh), unpack8(rw[i], w);
       if (p.DH) unpack8(cg[i], dh);
@@ -240,54 +223,122 @@ __global__ void __launch_bounds__(NT) norm_bwd_kernel(const NormBwdArgs p) {
         dx[j] = rstd * (dy[j] * w[j] - xh[j] * rstd * mean);
         if (p.DH) dx[j] += dh[j];
       }
-      store8(static_cast<T*>(p.DX) + row * p.lddx + e, nv, p.vx, dx);
+      Piece::store(static_cast<T*>(p.DX) + row * p.lddx, first(i), p.d, dx);
     }
   }
+  if constexpr (RPC > 1) {  // the warps' shares, added in their order
+    __shared__ float sums[NT / 32][VPT * 8 * 32];
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int64_t e = (int64_t)(l + i * NT) * 8;
-    store8(p.partial + (int64_t)blockIdx.x * p.d + e, p.d - e, (p.d & 3) == 0, dw[i]);
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sums[sub][(i * 8 + j) * 32 + l] = dw[i][j];
+    __syncthreads();
+    for (int k = threadIdx.x; k < VPT * 256; k += NT) {
+      float s = 0.0f;
+#pragma unroll
+      for (int r = 0; r < RPC; ++r) s += sums[r][k];
+      const int i = k / 256, j = k / 32 % 8, lane = k % 32;
+      const int e = i * 256 + (VEC ? lane * 8 + j : j * 32 + lane);
+      if (e < p.d) p.partial[(int64_t)blockIdx.x * p.d + e] = s;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int e = Piece::index(first(i), j);
+        if (e < p.d) p.partial[(int64_t)blockIdx.x * p.d + e] = dw[i][j];
+      }
   }
 }
 
-// Tokens too long for registers: dx from two readings of a token ...
-template <typename T>
-__global__ void __launch_bounds__(1024) norm_bwd_long_kernel(const NormBwdArgs p) {
-  __shared__ float part[32];
-  const int64_t row = blockIdx.x;
+// dx of one token by 256 threads, for tokens of any length, in two readings of it.
+template <typename T, bool VEC>
+__device__ __forceinline__ void norm_bwd_token(const NormBwdArgs& p, int64_t row, float* part) {
+  using Piece = Warp256<T, VEC>;
   const T* DY = static_cast<const T*>(p.DY) + row * p.lddy;
   const T* H = static_cast<const T*>(p.H) + row * p.ldh;
   const T* W = static_cast<const T*>(p.w);
   const float rstd = p.rstd[row];
   float dot = 0.0f;
-  for (int64_t e = (int64_t)threadIdx.x * 8; e < p.d; e += 8192) {
+  for (int first = (int)(threadIdx.x & ~31u) * 8; first < p.d; first += 2048) {
+    Raw8<T> a, b, c;
+    Piece::load(DY, first, p.d, a), Piece::load(H, first, p.d, b), Piece::load(W, first, p.d, c);
     float dy[8], h[8], w[8];
-    load8(DY + e, p.d - e, p.vy, dy);
-    load8(H + e, p.d - e, p.vh, h);
-    load8(W + e, p.d - e, p.vw, w);
+    unpack8(a, dy), unpack8(b, h), unpack8(c, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dot += dy[j] * w[j] * (h[j] * rstd);
   }
-  const float mean = row_sum<1024>(dot, part) / (float)p.d;
-  for (int64_t e = (int64_t)threadIdx.x * 8; e < p.d; e += 8192) {
-    const int64_t nv = p.d - e;
-    float dy[8], h[8], w[8], dh[8];
-    load8(DY + e, nv, p.vy, dy);
-    load8(H + e, nv, p.vh, h);
-    load8(W + e, nv, p.vw, w);
-    if (p.DH) load8(static_cast<const T*>(p.DH) + row * p.lddh + e, nv, p.vr, dh);
+  const float mean = row_sum<256>(dot, part) / (float)p.d;
+  for (int first = (int)(threadIdx.x & ~31u) * 8; first < p.d; first += 2048) {
+    Raw8<T> a, b, c, g;
+    Piece::load(DY, first, p.d, a), Piece::load(H, first, p.d, b), Piece::load(W, first, p.d, c);
+    if (p.DH) Piece::load(static_cast<const T*>(p.DH) + row * p.lddh, first, p.d, g);
+    float dx[8], h[8], w[8], dh[8];
+    unpack8(a, dx), unpack8(b, h), unpack8(c, w);
+    if (p.DH) unpack8(g, dh);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      dy[j] = rstd * (dy[j] * w[j] - (h[j] * rstd) * mean);
-      if (p.DH) dy[j] += dh[j];
+      dx[j] = rstd * (dx[j] * w[j] - (h[j] * rstd) * mean);
+      if (p.DH) dx[j] += dh[j];
     }
-    store8(static_cast<T*>(p.DX) + row * p.lddx + e, nv, p.vx, dy);
+    Piece::store(static_cast<T*>(p.DX) + row * p.lddx, first, p.d, dx);
   }
+}
+
+// Few tokens, in one launch: the first `tokens` CTAs write dx of a token each, the others dw of 64 features each, reading dy and h
+// once more (from L2) instead of meeting the first ones' partial sums.  tokens is t, or 0 where dx is written over dy or h
+// and a second launch has to follow (norm_bwd_token_kernel, the same arithmetic).
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) norm_bwd_few_kernel(const NormBwdArgs p, float* dw, int tokens) {
+  __shared__ float sums[32][65];
+  if ((int)blockIdx.x < tokens) {
+    norm_bwd_token<T, VEC>(p, blockIdx.x, &sums[0][0]);
+    return;
+  }
+  const int x = threadIdx.x & 7, y = threadIdx.x >> 3;  // eight features a thread, every 32nd token
+  const int e0 = ((int)blockIdx.x - tokens) * 64;
+  float s[8] = {};
+  auto at = [&](int j) { return e0 + (VEC ? x * 8 + j : j * 8 + x); };
+#pragma unroll 4
+  for (int64_t row = y; row < p.t; row += 32) {
+    const T* DY = static_cast<const T*>(p.DY) + row * p.lddy;
+    const T* H = static_cast<const T*>(p.H) + row * p.ldh;
+    const float rstd = p.rstd[row];
+    float dy[8], h[8];
+    if constexpr (VEC) {
+      load8(DY + at(0), p.d - at(0), true, dy), load8(H + at(0), p.d - at(0), true, h);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dy[j] = at(j) < p.d ? (float)DY[at(j)] : 0.0f;
+        h[j] = at(j) < p.d ? (float)H[at(j)] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] += dy[j] * (h[j] * rstd);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sums[y][VEC ? x * 8 + j : j * 8 + x] = s[j];
+  __syncthreads();
+  if (threadIdx.x < 64 && e0 + threadIdx.x < p.d) {
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v += sums[i][threadIdx.x];
+    dw[e0 + threadIdx.x] = v;
+  }
+}
+
+// Tokens too long for registers: dx from two readings of a token ...
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) norm_bwd_token_kernel(const NormBwdArgs p) {
+  __shared__ float part[8];
+  norm_bwd_token<T, VEC>(p, blockIdx.x, part);
 }
 // ... and dw, before dx may overwrite dy or h, with a thread for every feature.
 template <typename T>
 __global__ void __launch_bounds__(256) norm_bwd_long_dw_kernel(const NormBwdArgs p) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int e = (int)(blockIdx.x * 256 + threadIdx.x);
   if (e >= p.d) return;
   float s = 0.0f;
   for (int64_t row = blockIdx.y; row < p.t; row += gridDim.y)
@@ -320,25 +371,39 @@ int64_t bwd_rows(int64_t d, int64_t t) {
   const int64_t chunks = blocks_of(d, 8), sms = sm_count_cached();
   int64_t rows;
   if (chunks > kBwdLongest) rows = 16;
-  else rows = sms * (chunks <= 256 ? 4 : chunks <= 1024 ? 2 : 1);
-  const int64_t most = blocks_of(t, 4);
+  else rows = sms * (chunks <= 128 && chunks > 64 ? 6 : chunks <= 256 ? 4 : chunks <= 1024 ? 2 : 1);
+  const int64_t most = blocks_of(t, chunks <= 64 ? 32 : 4);
   return rows < most ? rows : most;
 }
 
-template <typename T>
+// One launch where launches are what takes the time (bf16: 4096 x 8 3.0 us, 7.6 with two; 4096 x 300 6.1 and 8.7), two where the walk over
+// the tokens does (4096 x 1024: 21 us, 14 with two; fp32 1003 x 1001: 23 us and 11).
+bool bwd_few(int64_t d, int64_t t) { return t <= 384 && t * d <= (int64_t)3 << 19; }
+
+template <typename T, bool VEC>
 int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
   const int64_t chunks = blocks_of(a.d, 8), rows = bwd_rows(a.d, a.t);
-  if (a.t > 0x7fffffffLL || a.d > 0x7fffffffLL) return B2_ERR_VARIANT;
+  if (a.t > 0x7fffffffLL) return B2_ERR_VARIANT;
+  if (a.t > 0 && bwd_few(a.d, a.t)) {
+    const bool over = a.DX == a.DY || a.DX == a.H;
+    const int tokens = over ? 0 : (int)a.t;
+    norm_bwd_few_kernel<T, VEC><<<(unsigned)(tokens + blocks_of(a.d, 64)), 256, 0, st>>>(a, dw, tokens);
+    if (over) norm_bwd_token_kernel<T, VEC><<<(unsigned)a.t, 256, 0, st>>>(a);
+    return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  }
   const unsigned g = (unsigned)rows;
   if (rows > 0) {
-    if (chunks <= 128) norm_bwd_kernel<T, 128, 1><<<g, 128, 0, st>>>(a);
-    else if (chunks <= 256) norm_bwd_kernel<T, 128, 2><<<g, 128, 0, st>>>(a);
-    else if (chunks <= 512) norm_bwd_kernel<T, 256, 2><<<g, 256, 0, st>>>(a);
-    else if (chunks <= 1024) norm_bwd_kernel<T, 512, 2><<<g, 512, 0, st>>>(a);
-    else if (chunks <= kBwdLongest) norm_bwd_kernel<T, 512, 4><<<g, 512, 0, st>>>(a);
+    if (chunks <= 32) norm_bwd_kernel<T, 32, 256, 1, VEC><<<g, 256, 0, st>>>(a);
+    else if (chunks <= 64) norm_bwd_kernel<T, 32, 256, 2, VEC><<<g, 256, 0, st>>>(a);
+    else if (chunks <= 128) norm_bwd_kernel<T, 128, 128, 1, VEC><<<g, 128, 0, st>>>(a);
+    else if (chunks <= 256) norm_bwd_kernel<T, 128, 128, 2, VEC><<<g, 128, 0, st>>>(a);
+    else if (chunks <= 512) norm_bwd_kernel<T, 256, 256, 2, VEC><<<g, 256, 0, st>>>(a);
+    else if (chunks <= 768) norm_bwd_kernel<T, 384, 384, 2, VEC><<<g, 384, 0, st>>>(a);
+    else if (chunks <= 1024) norm_bwd_kernel<T, 512, 512, 2, VEC><<<g, 512, 0, st>>>(a);
+    else if (chunks <= kBwdLongest) norm_bwd_kernel<T, 512, 512, 4, VEC><<<g, 512, 0, st>>>(a);
     else {
       norm_bwd_long_dw_kernel<T><<<dim3((unsigned)blocks_of(a.d, 256), g), 256, 0, st>>>(a);
-      norm_bwd_long_kernel<T><<<(unsigned)a.t, 1024, 0, st>>>(a);
+      norm_bwd_token_kernel<T, VEC><<<(unsigned)a.t, 256, 0, st>>>(a);
     }
   }
   norm_bwd_sum_kernel<<<(unsigned)blocks_of(a.d, 32), 512, 0, st>>>(a.partial, rows, a.d, dw);
@@ -371,11 +436,13 @@ extern "C" int b2_rmsnorm_f8(int64_t d, int64_t t, int type, const void* X, int6
   if (lds < nb) return -15;
   if (!work) return B2_OK;
   const int es = type == B2_TYPE_BF16 ? 2 : 4;
-  const NormArgs a{d, t, X, R, w, H, Q, S, ldx, ldr, ldh, ldq, lds, rstd, eps, columns_aligned(X, ldx, es, 16),
-                   columns_aligned(R, ldr, es, 16), columns_aligned(H, ldh, es, 16), columns_aligned(Q, ldq, 1, 8),
-                   columns_aligned(w, 0, es, 16)};
+  if (d > kMostFeatures) return B2_ERR_VARIANT;
+  const NormArgs a{(int)d, t, X, R, w, H, Q, S, ldx, ldr, ldh, ldq, lds, rstd, eps};
+  const bool vec = columns_aligned(X, ldx, es, 16) && (!R || columns_aligned(R, ldr, es, 16)) && (!H || columns_aligned(H, ldh, es, 16)) &&
+                   columns_aligned(Q, ldq, 1, 8) && columns_aligned(w, 0, es, 16);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  return type == B2_TYPE_BF16 ? norm_launch<__nv_bfloat16>(a, st) : norm_launch<float>(a, st);
+  if (type == B2_TYPE_BF16) return vec ? norm_launch<__nv_bfloat16, true>(a, st) : norm_launch<__nv_bfloat16, false>(a, st);
+  return vec ? norm_launch<float, true>(a, st) : norm_launch<float, false>(a, st);
 }
 
 extern "C" size_t b2_rmsnorm_backward_workspace_bytes(int64_t d, int64_t t) {
@@ -406,9 +473,11 @@ extern "C" int b2_rmsnorm_backward(int64_t d, int64_t t, int type, const void* D
   const size_t need = b2_rmsnorm_backward_workspace_bytes(d, t);
   if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need)) return B2_ERR_WORKSPACE;
   const int es = type == B2_TYPE_BF16 ? 2 : 4;
-  const NormBwdArgs a{d, t, DY, H, w, DH, DX, lddy, ldh, lddh, lddx, rstd, static_cast<float*>(workspace),
-                      columns_aligned(DY, lddy, es, 16), columns_aligned(H, ldh, es, 16), columns_aligned(DH, lddh, es, 16),
-                      columns_aligned(DX, lddx, es, 16), columns_aligned(w, 0, es, 16)};
+  if (d > kMostFeatures) return B2_ERR_VARIANT;
+  const NormBwdArgs a{(int)d, t, DY, H, w, DH, DX, lddy, ldh, lddh, lddx, rstd, static_cast<float*>(workspace)};
+  const bool vec = columns_aligned(DY, lddy, es, 16) && columns_aligned(H, ldh, es, 16) && (!DH || columns_aligned(DH, lddh, es, 16)) &&
+                   columns_aligned(DX, lddx, es, 16) && columns_aligned(w, 0, es, 16);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  return type == B2_TYPE_BF16 ? norm_bwd_launch<__nv_bfloat16>(a, dw, st) : norm_bwd_launch<float>(a, dw, st);
+  if (type == B2_TYPE_BF16) return vec ? norm_bwd_launch<__nv_bfloat16, true>(a, dw, st) : norm_bwd_launch<__nv_bfloat16, false>(a, dw, st);
+  return vec ? norm_bwd_launch<float, true>(a, dw, st) : norm_bwd_launch<float, false>(a, dw, st);
 }
