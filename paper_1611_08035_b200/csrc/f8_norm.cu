@@ -242,13 +242,18 @@ __global__ void __launch_bounds__(NT) norm_bwd_kernel(const NormBwdArgs p) {
       if (e < p.d) p.partial[(int64_t)blockIdx.x * p.d + e] = s;
     }
   } else {
+    float* partial = p.partial + (int64_t)blockIdx.x * p.d;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
+    for (int i = 0; i < VPT; ++i) {
+      const int e = Piece::index(first(i), 0);
+      if constexpr (VEC) {
+        store8(partial + e, p.d - e, (p.d & 3) == 0, dw[i]);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int e = Piece::index(first(i), j);
-        if (e < p.d) p.partial[(int64_t)blockIdx.x * p.d + e] = dw[i][j];
+        for (int j = 0; j < 8; ++j)
+          if (Piece::index(first(i), j) < p.d) partial[Piece::index(first(i), j)] = dw[i][j];
       }
+    }
   }
 }
 
@@ -398,7 +403,6 @@ int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
     else if (chunks <= 128) norm_bwd_kernel<T, 128, 128, 1, VEC><<<g, 128, 0, st>>>(a);
     else if (chunks <= 256) norm_bwd_kernel<T, 128, 128, 2, VEC><<<g, 128, 0, st>>>(a);
     else if (chunks <= 512) norm_bwd_kernel<T, 256, 256, 2, VEC><<<g, 256, 0, st>>>(a);
-    else if (chunks <= 768) norm_bwd_kernel<T, 384, 384, 2, VEC><<<g, 384, 0, st>>>(a);
     else if (chunks <= 1024) norm_bwd_kernel<T, 512, 512, 2, VEC><<<g, 512, 0, st>>>(a);
     else if (chunks <= kBwdLongest) norm_bwd_kernel<T, 512, 512, 4, VEC><<<g, 512, 0, st>>>(a);
     else {
