@@ -213,17 +213,26 @@ __device__ __forceinline__ void f8_add_shares(const F8Out& p, void* tile, int sh
   }
 }
 
+// The barriers around it, and all that the warps without work do.  Where registers have been moved between warpgroups each group calls its
+// part from its own branch: code they share is compiled for the smallest share.
+__device__ __forceinline__ void f8_join_begin() {
+  __syncwarp();
+  cluster_sync_all();
+}
+__device__ __forceinline__ void f8_join_end() {
+  __syncwarp();
+  // no CTA leaves while another one reads its share; what was read has arrived, so there is nothing to release
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
 template <typename TC, bool COLS_CONTIG, int TBN, int EW, bool PERMUTE>
 __device__ __forceinline__ void f8_split_join(const F8Out& p, void* tile, int splits, int share, int worker, int64_t row0, int64_t col0) {
-  cluster_sync_all();
+  f8_join_begin();
   if (worker >= 0) {
     if (splits == 2) f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 2>(p, tile, share, worker, row0, col0);
     else if (splits == 4) f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 4>(p, tile, share, worker, row0, col0);
     else f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 8>(p, tile, share, worker, row0, col0);
   }
-  __syncwarp();
-  // no CTA leaves while another one reads its share; what was read has arrived, so there is nothing to release
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+  f8_join_end();
 }
 
 // C := beta * C, and copies of operands into 16-byte aligned columns (ldd a multiple of 16 bytes); defined in f8_gemm.cu.

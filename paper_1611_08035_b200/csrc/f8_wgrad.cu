@@ -245,6 +245,10 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
         (void)mbar_wait_warp(drained, 0, kDrainLimitNs);
       }
     }
+    if (CTAS == 1 && p.splits > 1) {
+      f8_join_begin();
+      f8_join_end();
+    }
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     // The two warpgroups convert every other stage each, a warp 16 tokens of it: what a stage costs besides the conversion (the
@@ -310,6 +314,10 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
       }
     }
     if (!ok && lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+    if (CTAS == 1 && p.splits > 1) {
+      f8_join_begin();
+      f8_join_end();
+    }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
     const int quad = warp & 3, half = (warp - 12) >> 2;
@@ -348,16 +356,15 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
         if constexpr (CTAS == 1) f8_put_share<false, TBN, COLS>(ring, quad * 32 + lane, half * COLS, acc);
       }
     }
-  }
-  __syncwarp();
-  if constexpr (CTAS == 1) {
-    if (p.splits > 1) {
-      int tr, tc;
-      tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
-      f8_split_join<TC, false, TBN, EW, true>(p.out, ring, p.splits, share, warp >= 12 && ok ? tid - 384 : -1, (int64_t)tr * kRows,
-                                              (int64_t)tc * TBN);
+    if constexpr (CTAS == 1) {
+      if (p.splits > 1) {
+        int tr, tc;
+        tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
+        f8_split_join<TC, false, TBN, EW, true>(p.out, ring, p.splits, share, ok ? tid - 384 : -1, (int64_t)tr * kRows, (int64_t)tc * TBN);
+      }
     }
   }
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (CTAS == 2) cluster_sync_all();  // the pair's instructions read both CTAs' memory: neither leaves first

@@ -1,0 +1,144 @@
+"""A transformer block's norm and linear layer in 8 bits, from the library's operators:
+
+    h = x + residual,   y = rmsnorm(h) W^T
+
+The norm writes its result as e4m3 numbers with a scale for each 128 features (b2_rmsnorm_f8).  The product reads them as they
+are (b2_gemm_f8, against weights in 128 x 128 blocks), and so does the backward pass: the same 8-bit activation, kept
+instead of a 16-bit one, gives the weight gradient (b2_wgrad_f8), the same 8-bit weight read along its other index the
+gradient of the norm's result, and b2_rmsnorm_backward the gradients of x, the residual and the norm's weight.
+
+Activations are bfloat16 tensors [tokens, features]; sizes are free.  ``python -m paper_1611_08035_b200.layer8`` trains a small
+layer towards a target and times one step of a large one.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as b2
+
+F8, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def _blocks(n: int) -> int:
+    return (n + 127) // 128
+
+
+def _scratch(nbytes: int, device) -> torch.Tensor | None:
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def quantise(x: torch.Tensor, block: int = 1):
+    """x [rows, features] (bfloat16 or float32, contiguous) as e4m3 numbers and the e8m0 scales of its block x 128 tiles."""
+    t, d = x.shape
+    q = torch.empty(t, d, dtype=F8, device=x.device)
+    s = torch.empty((t + block - 1) // block, _blocks(d), dtype=E8, device=x.device)
+    b2.b2_quant_f8(d, t, block, x, d, q, d, s, s.shape[1])
+    return q, s
+
+
+def product(a, sa, block_a, ta, b, sb, block_b, m, n, k, out_dtype=torch.bfloat16):
+    """[n, m] = B A^T of block-scaled operands: b [n, k]; a [m, k] (ta 'T') or [k, m] (ta 'N')."""
+    c = torch.empty(n, m, dtype=out_dtype, device=a.device)
+    ws = _scratch(b2.b2_gemm_f8_workspace_bytes(ta, "N", m, n, k, a, a.shape[1], b, k), a.device)
+    b2.b2_gemm_f8(ta, "N", m, n, k, 1.0, a, a.shape[1], sa, sa.shape[1], block_a, b, k, sb, sb.shape[1], block_b, 0.0, c, m, ws)
+    return c
+
+
+class _NormLinear8(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, norm_weight, weight, w8, sw, eps):
+        ctx.set_materialize_grads(False)  # no gradient for h: nothing to add
+        t, d = x.shape
+        n = weight.shape[0]
+        h = torch.empty_like(x) if residual is not None else x
+        q, s = torch.empty(t, d, dtype=F8, device=x.device), torch.empty(t, _blocks(d), dtype=E8, device=x.device)
+        rstd = torch.empty(t, dtype=torch.float32, device=x.device)
+        b2.b2_rmsnorm_f8(d, t, x, d, residual, d, norm_weight, eps, h if residual is not None else None, d, q, d, s, s.shape[1], rstd)
+        y = product(w8, sw, 128, "T", q, s, 1, n, t, d)
+        ctx.save_for_backward(h, norm_weight, q, s, rstd, w8, sw)
+        ctx.has_residual = residual is not None
+        return y, h
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        h, norm_weight, q, s, rstd, w8, sw = ctx.saved_tensors
+        (t, d), n = h.shape, w8.shape[0]
+        dy = torch.zeros(t, n, dtype=h.dtype, device=h.device) if dy is None else dy.contiguous()
+        dq, ds = quantise(dy)
+        dnorm = product(w8, sw, 128, "N", dq, ds, 1, d, t, n)
+        dweight = torch.empty(n, d, dtype=torch.float32, device=h.device)
+        ws = _scratch(b2.b2_wgrad_f8_workspace_bytes(d, n, t, q, d, dy, n), h.device)
+        b2.b2_wgrad_f8(d, n, t, 1.0, q, d, s, s.shape[1], dy, n, 0.0, dweight, d, ws)
+        dx, dnw = torch.empty_like(h), torch.empty(d, dtype=torch.float32, device=h.device)
+        ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), h.device)
+        b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, None if dh is None else dh.contiguous(), d, dx, d, dnw, ws)
+        return dx, dx if ctx.has_residual else None, dnw.to(norm_weight.dtype), dweight, None, None, None
+
+
+class NormLinear8(torch.nn.Module):
+    """y, h = layer(x, residual): h = x + residual (x without one), y = rmsnorm(h) W^T.  W is kept in float32 for the optimiser
+    and in e4m3 for the products; call ``requantise()`` after every change of it."""
+
+    def __init__(self, features: int, outputs: int, eps: float = 1e-5, device="cuda"):
+        super().__init__()
+        self.eps = eps
+        self.norm_weight = torch.nn.Parameter(torch.ones(features, dtype=torch.bfloat16, device=device))
+        self.weight = torch.nn.Parameter(torch.randn(outputs, features, device=device) * features**-0.5)
+        self.requantise()
+
+    @torch.no_grad()
+    def requantise(self) -> None:
+        self.w8, self.sw = quantise(self.weight, 128)
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), self.norm_weight, self.weight, self.w8, self.sw, self.eps)
+
+
+def train(features: int = 512, outputs: int = 384, tokens: int = 1024, steps: int = 40, lr: float = 0.5, seed: int = 0):
+    """Losses of a layer that learns another one's results by gradient descent."""
+    torch.manual_seed(seed)
+    layer = NormLinear8(features, outputs)
+    target = torch.randn(outputs, features, device="cuda") * features**-0.5
+    losses = []
+    for _ in range(steps):
+        x, r = (torch.randn(tokens, features, device="cuda").bfloat16() for _ in range(2))
+        h = (x + r).float()
+        want = (h * torch.rsqrt(h.square().mean(1, keepdim=True) + layer.eps)) @ target.t()
+        y, _ = layer(x, r)
+        loss = (y.float() - want).square().mean()
+        loss.backward()
+        with torch.no_grad():
+            layer.weight -= lr * outputs * layer.weight.grad
+            layer.weight.grad = layer.norm_weight.grad = None
+        layer.requantise()
+        losses.append(loss.detach())
+    return [float(v) for v in losses]
+
+
+def main() -> None:
+    losses = train()
+    print(f"loss of a 512 -> 384 layer over {len(losses)} steps: {losses[0]:.3f} -> {losses[-1]:.4f}")
+    t, d = 8192, 8192
+    layer = NormLinear8(d, d)
+    x, r, dy = (torch.randn(t, d, device="cuda").bfloat16() for _ in range(3))
+    x.requires_grad_()
+
+    def step():
+        y, _ = layer(x, r)
+        y.backward(dy)
+        x.grad = layer.weight.grad = layer.norm_weight.grad = None
+
+    for _ in range(3):
+        step()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    for _ in range(10):
+        step()
+    end.record()
+    end.synchronize()
+    ms = begin.elapsed_time(end) / 10
+    print(f"forward and backward, {t} tokens, {d} -> {d}: {ms:.2f} ms, {6 * t * d * d / ms / 1e9:.0f} TFLOP/s")
+
+
+if __name__ == "__main__":
+    main()
