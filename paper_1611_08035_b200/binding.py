@@ -114,7 +114,21 @@ def lib() -> ctypes.CDLL:
             fn.restype = res
             fn.argtypes = args
         _lib = handle
+        _connect_calls(handle)
     return _lib
+
+
+def _connect_calls(handle) -> None:
+    """The 8-bit operators' functions below give way to those of ``_b2calls``, which read the same arguments without ctypes and fall
+    back on these for keywords and for whatever they do not take.  Without that module these do all of it."""
+    try:
+        from . import _b2calls
+    except ImportError:
+        return
+    names = ("b2_rmsnorm_f8", "b2_rmsnorm_backward", "b2_quant_f8", "b2_gemm_f8", "b2_wgrad_f8")
+    table = {n: (ctypes.cast(getattr(handle, n), c_void_p).value, globals()[n]) for n in names}
+    _b2calls.connect(B2Error, table)
+    globals().update({n: getattr(_b2calls, n) for n in names})
 
 
 def strerror(status: int) -> str:
@@ -456,8 +470,8 @@ def b2_gemm_strided_batched(transa, transb, m, n, k, alpha, A, lda, stride_a, B,
 
 
 # ---- linear layers in 8 bits --------------------------------------------------------------------------------
-# A decoding step makes these calls on a few tokens, where the GPU needs two or three microseconds: the checks are written
-# out, without loops or helper calls, because they cost as much.
+# A decoding step makes these calls on a few tokens, where the GPU needs two or three microseconds: once the library is loaded
+# the functions of csrc/calls.cpp take their place (norm of 8 tokens: 8.3 us a call here, of which ctypes takes 1.5, 5 there).
 _TYPES = {torch.float32: 1, torch.bfloat16: 2}  # B2_TYPE_*
 _SCALES = {torch.float8_e8m0fnu: 0, torch.float32: 1}  # B2_SCALE_*
 _E4M3, _E8M0, _F32, _BF16 = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float32, torch.bfloat16

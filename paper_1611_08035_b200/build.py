@@ -2,7 +2,8 @@
 
 Every ``csrc/*.cu`` is compiled to an object file under ``_build/`` and linked into
 ``libb2gemm.so`` beside this file.  Objects are rebuilt when their source, any header or the
-flags change.  ``python -m paper_1611_08035_b200.build`` runs it from a shell.
+flags change.  ``csrc/calls.cpp``, the quick way from Python into some of its entry points,
+becomes ``_b2calls.so`` beside it.  ``python -m paper_1611_08035_b200.build`` runs it from a shell.
 """
 from __future__ import annotations
 
@@ -19,6 +20,7 @@ CSRC = PKG_DIR / "csrc"
 INCLUDE = PKG_DIR.parent / "include"
 BUILD_DIR = PKG_DIR / "_build"
 LIB_PATH = PKG_DIR / "libb2gemm.so"
+CALLS_PATH = PKG_DIR / "_b2calls.so"
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -63,6 +65,30 @@ def _compile(src: Path, verbose: bool) -> Path:
     return obj
 
 
+def _build_calls(verbose: bool) -> None:
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    src = CSRC / "calls.cpp"
+    flags = ["-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    paths = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], str(Path(_nvcc()).resolve().parent.parent / "include")]
+    cmd = ["g++", *flags, *(f for p in paths for f in ("-isystem", p)), "-I", str(INCLUDE), str(src), "-o", str(CALLS_PATH),
+           *(f"-L{p}" for p in cpp_extension.library_paths()), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    h = hashlib.sha256(" ".join([torch.__version__, *cmd]).encode())
+    for f in (src, *sorted(INCLUDE.glob("*.h"))):
+        h.update(f.read_bytes())
+    stamp_file = BUILD_DIR / "calls.stamp"
+    if CALLS_PATH.exists() and stamp_file.exists() and stamp_file.read_text() == h.hexdigest():
+        return
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"g++ failed for {src.name}:\n{res.stderr[-8000:]}")
+    if verbose:
+        sys.stderr.write(f"[b2gemm build] compiled {src.name}\n")
+    stamp_file.write_text(h.hexdigest())
+
+
 def build(verbose: bool = False, force: bool = False) -> Path:
     """Compile and link ``libb2gemm.so``; returns its path."""
     BUILD_DIR.mkdir(exist_ok=True)
@@ -73,7 +99,7 @@ def build(verbose: bool = False, force: bool = False) -> Path:
     if not sources:
         raise RuntimeError("no CUDA sources found")
     # objects, stamps and logs of sources that no longer exist would be linked / reported: drop them
-    stems = {src.stem for src in sources}
+    stems = {src.stem for src in sources} | {"calls"}
     stale = False
     for f in list(BUILD_DIR.iterdir()):
         stem = f.name.split(".")[0]
@@ -91,6 +117,7 @@ def build(verbose: bool = False, force: bool = False) -> Path:
             raise RuntimeError(f"link failed:\n{res.stderr[-4000:]}")
         if verbose:
             sys.stderr.write(f"[b2gemm build] linked {LIB_PATH.name}\n")
+    _build_calls(verbose)
     return LIB_PATH
 
 

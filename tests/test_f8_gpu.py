@@ -425,3 +425,29 @@ def test_other_stream_and_long_columns(b2):
     stream.synchronize()
     assert torch.equal(x.view(t, ld)[:, :d], small.view(torch.uint8)) and torch.equal(s.view(torch.uint8), s2.view(torch.uint8))
     assert torch.equal(C1, C2) and b2.b2_device_status() == 0
+
+
+def test_call_forms(b2):
+    """Positional, keyword and unchecked calls, refused types and refused arguments, whichever way the binding takes."""
+    x = torch.randn(4, 128, device="cuda")
+    q, s = torch.empty(4, 128, dtype=F8, device="cuda"), torch.empty(4, 1, dtype=E8, device="cuda")
+    assert b2.b2_quant_f8(128, 4, 1, x, 128, q, 128, s, 1) == 0
+    first = q.clone()
+    assert b2.b2_quant_f8(128, 4, 1, x, 128, q, 128, s=s, lds=1) == 0 and torch.equal(q.view(torch.uint8), first.view(torch.uint8))
+    for call in (lambda **kw: b2.b2_quant_f8(128, 4, 3, x, 128, q, 128, s, 1, **kw), lambda **kw: b2.b2_quant_f8(d=128, t=4, block=3, x=x, ldx=128, q=q, ldq=128, s=s, lds=1, **kw)):
+        with pytest.raises(b2.B2Error) as e:
+            call()
+        assert e.value.status == -3
+        assert call(check=False) == -3
+    with pytest.raises(TypeError):
+        b2.b2_quant_f8(128, 4, 1, x.half(), 128, q, 128, s, 1)
+    with pytest.raises(TypeError):
+        b2.b2_quant_f8(128, 4, 1, x.cpu(), 128, q, 128, s, 1)
+    with pytest.raises(TypeError):
+        b2.b2_quant_f8(128, 4, 1)
+    C = torch.empty(4, 4, device="cuda")
+    with pytest.raises(b2.B2Error) as e:  # an operand that needs a workspace, without one
+        b2.b2_gemm_f8("T", "N", 4, 4, 100, 1.0, q, 100, s, 1, 1, q, 128, s, 1, 1, 0.0, C, 4)
+    assert e.value.status == 1003
+    with pytest.raises(TypeError):
+        b2.b2_wgrad_f8(128, 4, 4, 1.0, q, 128, s, 1, x, 128, 0.0, C, 128)
