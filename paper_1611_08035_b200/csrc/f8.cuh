@@ -5,7 +5,32 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "b2gemm.h"
+
 namespace b2 {
+
+// ---- launches that overlap the end of the kernel before ---------------------------------------------
+// Every kernel of the 8-bit operators lets its successor in the stream be launched as soon as all of its own CTAs run
+// (grid_started) and touches global memory only after its predecessor has completed and its writes are visible (grid_ready),
+// so that setting up overlaps with finishing.  Kernels launched without the attribute are not affected.
+__device__ __forceinline__ void grid_started() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void grid_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename... Params, typename... Args>
+inline int launch_overlapped_as(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, dim3 cluster, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid, cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = smem, cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim = {cluster.x, cluster.y, cluster.z};
+  cfg.attrs = at, cfg.numAttrs = cluster.x * cluster.y * cluster.z > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, Params(args)...) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+}
+template <typename... Params, typename... Args>
+inline int launch_overlapped(void (*kernel)(Params...), dim3 grid, unsigned threads, cudaStream_t st, const Args&... args) {
+  return launch_overlapped_as(kernel, grid, threads, 0, dim3(1), st, args...);
+}
 
 constexpr int kF8Block = 128;  // elements along the quantised (later summed) index that share a scale
 

@@ -79,6 +79,7 @@ template <typename TC>
 __global__ void __launch_bounds__(kThreads, 1)
     f8_fs_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char fs_smem_raw[];
+  grid_started();
   const uint32_t raw = smem_u32(fs_smem_raw);
   unsigned char* ring = fs_smem_raw + (((raw + 1023u) & ~1023u) - raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + kRing);
@@ -117,6 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync_all();  // the other CTA's barriers exist before anything arrives on them
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  grid_ready();
   const int tiles = p.tiles_r * p.tiles_c, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   bool ok = true;
 

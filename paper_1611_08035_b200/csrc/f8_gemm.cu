@@ -65,6 +65,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
   using Cfg = F8Cfg<TBN, MX>;
   constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES;
   extern __shared__ unsigned char f8_smem_raw[];
+  grid_started();
   const uint32_t raw = smem_u32(f8_smem_raw);
   unsigned char* ring = f8_smem_raw + (((raw + 1023u) & ~1023u) - raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + Cfg::RING);
@@ -101,6 +102,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  grid_ready();
 
   // split: the cluster's CTAs (blockIdx.y) share one tile; otherwise the grid walks over the tiles
   const int tiles = p.tiles_r * p.tiles_c, share = blockIdx.y;
@@ -322,6 +324,8 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
 
 // ---- operands whose columns are not 16-byte aligned are copied into columns that are --------------------
 __global__ void __launch_bounds__(256) f8_repitch_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, uint8_t* dst, int64_t ldd) {
+  grid_started();
+  grid_ready();
   const int64_t per = ldd / 16;
   for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < per * cols; i += (int64_t)gridDim.x * 256) {
     const int64_t c = i / per, r = (i - c * per) * 16;
@@ -335,6 +339,8 @@ __global__ void __launch_bounds__(256) f8_repitch_kernel(const uint8_t* src, int
 
 template <typename TC>
 __global__ void __launch_bounds__(256) f8_scale_c_kernel(int64_t m, int64_t n, float beta, TC* C, int64_t ldc) {
+  grid_started();
+  grid_ready();
   for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < m * n; i += (int64_t)gridDim.x * 256) {
     TC* c = C + i % m + i / m * ldc;
     f8_store1(c, beta == 0.0f ? 0.0f : beta * f8_load1(c));
@@ -367,16 +373,8 @@ int f8_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, int s
   a.tiles_r = (int)tr, a.tiles_c = (int)tc, a.splits = splits;
   a.group = 8;
   const int tiles = a.tiles_r * a.tiles_c, sms = sm_count_cached();
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = splits > 1 ? dim3((unsigned)tiles, (unsigned)splits) : dim3((unsigned)(tiles < sms ? tiles : sms));
-  cfg.blockDim = dim3(Cfg::NT);
-  cfg.dynamicSmemBytes = Cfg::SMEM;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {1, (unsigned)splits, 1};
-  cfg.attrs = at, cfg.numAttrs = splits > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kfn, a, mr, mc) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  return launch_overlapped_as(kfn, splits > 1 ? dim3((unsigned)tiles, (unsigned)splits) : dim3((unsigned)(tiles < sms ? tiles : sms)), Cfg::NT, Cfg::SMEM,
+                           dim3(1, (unsigned)splits), st, a, mr, mc);
 }
 
 // CTAs that share a tile's k range, and what the product then takes, in clocks: turns of CTAs over the SMs, a turn being its
@@ -439,14 +437,12 @@ F8Pack f8_pack_plan(bool an, bool bn, int64_t m, int64_t n, int64_t k, const voi
 }  // namespace
 
 int f8_repitch(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd, cudaStream_t st) {
-  f8_repitch_kernel<<<grid_for(ldd / 16 * cols), 256, 0, st>>>(static_cast<const uint8_t*>(src), ld, rows, cols, static_cast<uint8_t*>(dst), ldd);
-  return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  return launch_overlapped(f8_repitch_kernel, grid_for(ldd / 16 * cols), 256, st, static_cast<const uint8_t*>(src), ld, rows, cols, static_cast<uint8_t*>(dst), ldd);
 }
 int f8_scale_c(int64_t m, int64_t n, float beta, void* C, int64_t ldc, int type_c, cudaStream_t st) {
   if (beta == 1.0f) return B2_OK;
-  if (type_c == B2_TYPE_BF16) f8_scale_c_kernel<<<grid_for(m * n), 256, 0, st>>>(m, n, beta, static_cast<__nv_bfloat16*>(C), ldc);
-  else f8_scale_c_kernel<<<grid_for(m * n), 256, 0, st>>>(m, n, beta, static_cast<float*>(C), ldc);
-  return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  if (type_c == B2_TYPE_BF16) return launch_overlapped(f8_scale_c_kernel<__nv_bfloat16>, grid_for(m * n), 256, st, m, n, beta, static_cast<__nv_bfloat16*>(C), ldc);
+  return launch_overlapped(f8_scale_c_kernel<float>, grid_for(m * n), 256, st, m, n, beta, static_cast<float*>(C), ldc);
 }
 
 }  // namespace b2

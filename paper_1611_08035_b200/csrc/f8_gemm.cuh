@@ -97,16 +97,7 @@ int f8_pair_launch(Kernel kfn, std::atomic<bool>* configured, int threads, size_
   a.out.rows = r.n, a.out.cols = c.n, a.r_mn = r.mn, a.c_mn = c.mn, a.sr = r.s, a.sc = c.s;
   a.tiles_r = (int)tr, a.tiles_c = (int)tc, a.splits = 1, a.group = 8;
   const int tiles = a.tiles_r * a.tiles_c, pairs = sm_count_cached() / 2;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs));
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {2, 1, 1};
-  cfg.attrs = at, cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kfn, a, mr, mc) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  return launch_overlapped_as(kfn, dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs)), (unsigned)threads, smem, dim3(2), st, a, mr, mc);
 }
 
 // f8_mx.cu: products whose scales are both e8m0, 256 x 256 tiles; TC = float or __nv_bfloat16

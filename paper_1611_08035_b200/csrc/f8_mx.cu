@@ -45,6 +45,7 @@ template <typename TC, int CHUNK>
 __global__ void __launch_bounds__(kThreads, 1)
     f8_mx_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char mx_smem_raw[];
+  grid_started();
   const uint32_t raw = smem_u32(mx_smem_raw);
   unsigned char* ring = mx_smem_raw + (((raw + 1023u) & ~1023u) - raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + kRing);
@@ -81,6 +82,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync_all();  // the other CTA's barriers exist before anything arrives on them
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  grid_ready();
   const int tiles = p.tiles_r * p.tiles_c, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   bool ok = true;
 

@@ -41,6 +41,8 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
 // TPR threads to a token, each VPT groups of eight features (Warp256: which eight).
 template <typename T, int TPR, int VPT, bool VEC>
 __global__ void __launch_bounds__(TPR > 128 ? TPR : 128, TPR == 512 && VPT == 4 && sizeof(T) == 2 ? 2 : 1) norm_kernel(const NormArgs p) {
+  grid_started();
+  grid_ready();
   using Piece = Warp256<T, VEC>;
   constexpr int NT = TPR > 128 ? TPR : 128, RPC = NT / TPR;
   static_assert(RPC == 1 || TPR == 32, "rows that share a CTA meet at no barrier");
@@ -90,6 +92,8 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128, TPR == 512 && VPT == 4 
 // the second pass only, because H may be X or R.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs p) {
+  grid_started();
+  grid_ready();
   using Piece = Warp256<T, VEC>;
   __shared__ float part[32];
   const int64_t row = blockIdx.x;
@@ -135,22 +139,23 @@ int norm_launch(const NormArgs& a, cudaStream_t st) {
   const int64_t chunks = blocks_of(a.d, 8);
   if (a.t > 0x7fffffffLL) return B2_ERR_VARIANT;
   const unsigned t = (unsigned)a.t, t4 = (unsigned)blocks_of(a.t, 4);
+  int rc;
   if (a.t <= 2 * sm_count_cached() && chunks > 32 && chunks <= 1024) {
     // few tokens: one group of eight per thread, the shortest chain from the load to the store
-    if (chunks <= 128) norm_kernel<T, 128, 1, VEC><<<t, 128, 0, st>>>(a);
-    else if (chunks <= 256) norm_kernel<T, 256, 1, VEC><<<t, 256, 0, st>>>(a);
-    else if (chunks <= 512) norm_kernel<T, 512, 1, VEC><<<t, 512, 0, st>>>(a);
-    else norm_kernel<T, 1024, 1, VEC><<<t, 1024, 0, st>>>(a);
-  } else if (chunks <= 32) norm_kernel<T, 32, 1, VEC><<<t4, 128, 0, st>>>(a);
-  else if (chunks <= 64) norm_kernel<T, 32, 2, VEC><<<t4, 128, 0, st>>>(a);
-  else if (chunks <= 128) norm_kernel<T, 32, 4, VEC><<<t4, 128, 0, st>>>(a);
-  else if (chunks <= 256) norm_kernel<T, 128, 2, VEC><<<t, 128, 0, st>>>(a);
-  else if (chunks <= 512) norm_kernel<T, 128, 4, VEC><<<t, 128, 0, st>>>(a);
-  else if (chunks <= 768) norm_kernel<T, 192, 4, VEC><<<t, 192, 0, st>>>(a);
-  else if (chunks <= 1024) norm_kernel<T, 256, 4, VEC><<<t, 256, 0, st>>>(a);
-  else if (chunks <= 2048) norm_kernel<T, 512, 4, VEC><<<t, 512, 0, st>>>(a);
-  else norm_long_kernel<T, VEC><<<t, 1024, 0, st>>>(a);
-  return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+    if (chunks <= 128) rc = launch_overlapped(norm_kernel<T, 128, 1, VEC>, t, 128, st, a);
+    else if (chunks <= 256) rc = launch_overlapped(norm_kernel<T, 256, 1, VEC>, t, 256, st, a);
+    else if (chunks <= 512) rc = launch_overlapped(norm_kernel<T, 512, 1, VEC>, t, 512, st, a);
+    else rc = launch_overlapped(norm_kernel<T, 1024, 1, VEC>, t, 1024, st, a);
+  } else if (chunks <= 32) rc = launch_overlapped(norm_kernel<T, 32, 1, VEC>, t4, 128, st, a);
+  else if (chunks <= 64) rc = launch_overlapped(norm_kernel<T, 32, 2, VEC>, t4, 128, st, a);
+  else if (chunks <= 128) rc = launch_overlapped(norm_kernel<T, 32, 4, VEC>, t4, 128, st, a);
+  else if (chunks <= 256) rc = launch_overlapped(norm_kernel<T, 128, 2, VEC>, t, 128, st, a);
+  else if (chunks <= 512) rc = launch_overlapped(norm_kernel<T, 128, 4, VEC>, t, 128, st, a);
+  else if (chunks <= 768) rc = launch_overlapped(norm_kernel<T, 192, 4, VEC>, t, 192, st, a);
+  else if (chunks <= 1024) rc = launch_overlapped(norm_kernel<T, 256, 4, VEC>, t, 256, st, a);
+  else if (chunks <= 2048) rc = launch_overlapped(norm_kernel<T, 512, 4, VEC>, t, 512, st, a);
+  else rc = launch_overlapped(norm_long_kernel<T, VEC>, t, 1024, st, a);
+  return rc;
 }
 
 // ---- backward -------------------------------------------------------------------------------------------
@@ -168,6 +173,8 @@ struct NormBwdArgs {
 // end and leaves as one row of partial sums.  TPR threads to a token, NT / TPR tokens at a time (one, or one to a warp).
 template <typename T, int TPR, int NT, int VPT, bool VEC>
 __global__ void __launch_bounds__(NT) norm_bwd_kernel(const NormBwdArgs p) {
+  grid_started();
+  grid_ready();
   using Piece = Warp256<T, VEC>;
   constexpr int RPC = NT / TPR;
   static_assert(RPC == 1 || TPR == 32, "tokens that share a CTA meet at no barrier");
@@ -296,6 +303,8 @@ __device__ __forceinline__ void norm_bwd_token(const NormBwdArgs& p, int64_t row
 // and a second launch has to follow (norm_bwd_token_kernel, the same arithmetic).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) norm_bwd_few_kernel(const NormBwdArgs p, float* dw, int tokens) {
+  grid_started();
+  grid_ready();
   __shared__ float sums[32][65];
   if ((int)blockIdx.x < tokens) {
     norm_bwd_token<T, VEC>(p, blockIdx.x, &sums[0][0]);
@@ -337,12 +346,16 @@ __global__ void __launch_bounds__(256) norm_bwd_few_kernel(const NormBwdArgs p, 
 // Tokens too long for registers: dx from two readings of a token ...
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) norm_bwd_token_kernel(const NormBwdArgs p) {
+  grid_started();
+  grid_ready();
   __shared__ float part[8];
   norm_bwd_token<T, VEC>(p, blockIdx.x, part);
 }
 // ... and dw, before dx may overwrite dy or h, with a thread for every feature.
 template <typename T>
 __global__ void __launch_bounds__(256) norm_bwd_long_dw_kernel(const NormBwdArgs p) {
+  grid_started();
+  grid_ready();
   const int e = (int)(blockIdx.x * 256 + threadIdx.x);
   if (e >= p.d) return;
   float s = 0.0f;
@@ -353,6 +366,8 @@ __global__ void __launch_bounds__(256) norm_bwd_long_dw_kernel(const NormBwdArgs
 
 // dw[e] = sum over the rows of partial sums, always in the same order.
 __global__ void __launch_bounds__(512) norm_bwd_sum_kernel(const float* partial, int64_t rows, int64_t d, float* dw) {
+  grid_started();
+  grid_ready();
   __shared__ float part[16][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int64_t e = (int64_t)blockIdx.x * 32 + x;
@@ -389,29 +404,29 @@ template <typename T, bool VEC>
 int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
   const int64_t chunks = blocks_of(a.d, 8), rows = bwd_rows(a.d, a.t);
   if (a.t > 0x7fffffffLL) return B2_ERR_VARIANT;
+  int rc = B2_OK;
   if (a.t > 0 && bwd_few(a.d, a.t)) {
     const bool over = a.DX == a.DY || a.DX == a.H;
     const int tokens = over ? 0 : (int)a.t;
-    norm_bwd_few_kernel<T, VEC><<<(unsigned)(tokens + blocks_of(a.d, 64)), 256, 0, st>>>(a, dw, tokens);
-    if (over) norm_bwd_token_kernel<T, VEC><<<(unsigned)a.t, 256, 0, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+    rc = launch_overlapped(norm_bwd_few_kernel<T, VEC>, (unsigned)(tokens + blocks_of(a.d, 64)), 256, st, a, dw, tokens);
+    if (over && !rc) rc = launch_overlapped(norm_bwd_token_kernel<T, VEC>, (unsigned)a.t, 256, st, a);
+    return rc;
   }
   const unsigned g = (unsigned)rows;
   if (rows > 0) {
-    if (chunks <= 32) norm_bwd_kernel<T, 32, 256, 1, VEC><<<g, 256, 0, st>>>(a);
-    else if (chunks <= 64) norm_bwd_kernel<T, 32, 256, 2, VEC><<<g, 256, 0, st>>>(a);
-    else if (chunks <= 128) norm_bwd_kernel<T, 128, 128, 1, VEC><<<g, 128, 0, st>>>(a);
-    else if (chunks <= 256) norm_bwd_kernel<T, 128, 128, 2, VEC><<<g, 128, 0, st>>>(a);
-    else if (chunks <= 512) norm_bwd_kernel<T, 256, 256, 2, VEC><<<g, 256, 0, st>>>(a);
-    else if (chunks <= 1024) norm_bwd_kernel<T, 512, 512, 2, VEC><<<g, 512, 0, st>>>(a);
-    else if (chunks <= kBwdLongest) norm_bwd_kernel<T, 512, 512, 4, VEC><<<g, 512, 0, st>>>(a);
+    if (chunks <= 32) rc = launch_overlapped(norm_bwd_kernel<T, 32, 256, 1, VEC>, g, 256, st, a);
+    else if (chunks <= 64) rc = launch_overlapped(norm_bwd_kernel<T, 32, 256, 2, VEC>, g, 256, st, a);
+    else if (chunks <= 128) rc = launch_overlapped(norm_bwd_kernel<T, 128, 128, 1, VEC>, g, 128, st, a);
+    else if (chunks <= 256) rc = launch_overlapped(norm_bwd_kernel<T, 128, 128, 2, VEC>, g, 128, st, a);
+    else if (chunks <= 512) rc = launch_overlapped(norm_bwd_kernel<T, 256, 256, 2, VEC>, g, 256, st, a);
+    else if (chunks <= 1024) rc = launch_overlapped(norm_bwd_kernel<T, 512, 512, 2, VEC>, g, 512, st, a);
+    else if (chunks <= kBwdLongest) rc = launch_overlapped(norm_bwd_kernel<T, 512, 512, 4, VEC>, g, 512, st, a);
     else {
-      norm_bwd_long_dw_kernel<T><<<dim3((unsigned)blocks_of(a.d, 256), g), 256, 0, st>>>(a);
-      norm_bwd_token_kernel<T, VEC><<<(unsigned)a.t, 256, 0, st>>>(a);
+      rc = launch_overlapped(norm_bwd_long_dw_kernel<T>, dim3((unsigned)blocks_of(a.d, 256), g), 256, st, a);
+      if (!rc) rc = launch_overlapped(norm_bwd_token_kernel<T, VEC>, (unsigned)a.t, 256, st, a);
     }
   }
-  norm_bwd_sum_kernel<<<(unsigned)blocks_of(a.d, 32), 512, 0, st>>>(a.partial, rows, a.d, dw);
-  return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  return rc ? rc : launch_overlapped(norm_bwd_sum_kernel, (unsigned)blocks_of(a.d, 32), 512, st, a.partial, rows, (int64_t)a.d, dw);
 }
 
 bool type_ok(int type) { return type == B2_TYPE_F32 || type == B2_TYPE_BF16; }

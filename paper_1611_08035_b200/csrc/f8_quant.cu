@@ -37,6 +37,8 @@ __device__ __forceinline__ uint32_t max_bits(uint32_t m) { return sizeof(T) == 2
 // Q16: columns of Q on 16-byte boundaries, else on 8-byte ones.
 template <typename T, int U, bool Q16>
 __global__ void __launch_bounds__(256) quant_rows_kernel(const QuantArgs p, const FastDiv per_token, uint32_t total) {
+  grid_started();
+  grid_ready();
   const int l = threadIdx.x & 7;
   const uint32_t first = blockIdx.x * (32 * U) + (threadIdx.x >> 3);
   Raw8<T> raw[U][2];
@@ -76,6 +78,8 @@ __global__ void __launch_bounds__(256) quant_rows_kernel(const QuantArgs p, cons
 // Columns that start anywhere: two blocks of a token per warp.
 template <typename T, int U>
 __global__ void __launch_bounds__(256) quant_rows_anywhere_kernel(const QuantArgs p, const FastDiv per_token, uint32_t total) {
+  grid_started();
+  grid_ready();
   using Piece = Warp256<T, false>;
   const uint32_t first = blockIdx.x * (8 * U) + (threadIdx.x >> 5);
   Raw8<T> raw[U];
@@ -100,6 +104,8 @@ __global__ void __launch_bounds__(256) quant_rows_anywhere_kernel(const QuantArg
 // time, two rows (VEC) or one row twice as deep.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) quant_tiles_kernel(const QuantArgs p, int64_t blocks_d) {
+  grid_started();
+  grid_ready();
   __shared__ uint32_t part[8];
   const int64_t bt = blockIdx.x / blocks_d, bd = blockIdx.x - bt * blocks_d;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -161,16 +167,14 @@ int quant_launch(const QuantArgs& a, int block, bool vec, bool q16, cudaStream_t
     const int64_t per = vec ? nb : blocks_of(a.d, 256), total = per * a.t;
     if (a.t > 0x7fffffffLL || per > 0x7fffffffLL || total > 0x7fffffffLL - 32 * U) return B2_ERR_VARIANT;  // 2^38 numbers
     const FastDiv div = fast_div((uint32_t)per);
-    if (vec && q16) quant_rows_kernel<T, U, true><<<(unsigned)blocks_of(total, 32 * U), 256, 0, st>>>(a, div, (uint32_t)total);
-    else if (vec) quant_rows_kernel<T, U, false><<<(unsigned)blocks_of(total, 32 * U), 256, 0, st>>>(a, div, (uint32_t)total);
-    else quant_rows_anywhere_kernel<T, U><<<(unsigned)blocks_of(total, 8 * U), 256, 0, st>>>(a, div, (uint32_t)total);
-  } else {
-    const int64_t ctas = nb * blocks_of(a.t, kF8Block);
-    if (ctas > 0x7fffffffLL) return B2_ERR_VARIANT;
-    if (vec) quant_tiles_kernel<T, true><<<(unsigned)ctas, 256, 0, st>>>(a, nb);
-    else quant_tiles_kernel<T, false><<<(unsigned)ctas, 256, 0, st>>>(a, nb);
+    if (vec && q16) return launch_overlapped(quant_rows_kernel<T, U, true>, (unsigned)blocks_of(total, 32 * U), 256, st, a, div, (uint32_t)total);
+    if (vec) return launch_overlapped(quant_rows_kernel<T, U, false>, (unsigned)blocks_of(total, 32 * U), 256, st, a, div, (uint32_t)total);
+    return launch_overlapped(quant_rows_anywhere_kernel<T, U>, (unsigned)blocks_of(total, 8 * U), 256, st, a, div, (uint32_t)total);
   }
-  return cudaGetLastError() == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  const int64_t ctas = nb * blocks_of(a.t, kF8Block);
+  if (ctas > 0x7fffffffLL) return B2_ERR_VARIANT;
+  if (vec) return launch_overlapped(quant_tiles_kernel<T, true>, (unsigned)ctas, 256, st, a, nb);
+  return launch_overlapped(quant_tiles_kernel<T, false>, (unsigned)ctas, 256, st, a, nb);
 }
 
 }  // namespace

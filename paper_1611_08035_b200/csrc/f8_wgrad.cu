@@ -125,6 +125,7 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
   using Cfg = WgCfg<CTAS>;
   constexpr int EW = Cfg::EW, CW = Cfg::CW, COLS = Cfg::COLS, STAGES = Cfg::STAGES, TBN = Cfg::TBN;
   extern __shared__ unsigned char wg_smem_raw[];
+  grid_started();
   const uint32_t raw = smem_u32(wg_smem_raw);
   unsigned char* ring = wg_smem_raw + (((raw + 1023u) & ~1023u) - raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + Cfg::RING);
@@ -161,6 +162,7 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
   if (CTAS == 2) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  grid_ready();
 
   const int tiles = p.tiles_r * p.tiles_c, share = CTAS == 2 ? 0 : blockIdx.y;
   const int first = blockIdx.x / CTAS, stride = gridDim.x / CTAS;
@@ -406,16 +408,8 @@ int wg_launch(WgArgs a, int64_t m, int64_t n, int64_t k, const void* Q, int64_t 
   if (tr * tc > 0x3fffffffLL) return B2_ERR_VARIANT;
   a.tiles_r = (int)tr, a.tiles_c = (int)tc, a.splits = splits, a.group = 8;
   const int tiles = a.tiles_r * a.tiles_c, resident = sm_count_cached() / CTAS;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = splits > 1 ? dim3((unsigned)tiles, (unsigned)splits) : dim3((unsigned)((tiles < resident ? tiles : resident) * CTAS));
-  cfg.blockDim = dim3(Cfg::NT);
-  cfg.dynamicSmemBytes = Cfg::SMEM;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {(unsigned)CTAS, (unsigned)splits, 1};
-  cfg.attrs = at, cfg.numAttrs = CTAS * splits > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kfn, a, mq, my) == cudaSuccess ? B2_OK : B2_ERR_LAUNCH;
+  return launch_overlapped_as(kfn, splits > 1 ? dim3((unsigned)tiles, (unsigned)splits) : dim3((unsigned)((tiles < resident ? tiles : resident) * CTAS)), Cfg::NT,
+                           Cfg::SMEM, dim3(CTAS, (unsigned)splits), st, a, mq, my);
 }
 
 template <typename TC>
