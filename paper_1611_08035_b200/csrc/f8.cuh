@@ -10,8 +10,8 @@
 namespace b2 {
 
 // ---- launches that overlap the end of the kernel before ---------------------------------------------
-// Every kernel of the 8-bit operators lets its successor in the stream be launched as soon as all of its own CTAs run
-// (grid_started) and touches global memory only after its predecessor has completed and its writes are visible (grid_ready),
+// Every kernel of the 8-bit operators lets its successor in the stream be launched early (grid_started: as soon as its own CTAs run, the
+// products' as they come to their results, because a successor's CTAs that take the free places sooner take them unevenly) and touches global memory only after its predecessor has completed and its writes are visible (grid_ready),
 // so that setting up overlaps with finishing.  Kernels launched without the attribute are not affected.
 __device__ __forceinline__ void grid_started() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

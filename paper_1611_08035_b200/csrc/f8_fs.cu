@@ -79,7 +79,6 @@ template <typename TC>
 __global__ void __launch_bounds__(kThreads, 1)
     f8_fs_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char fs_smem_raw[];
-  grid_started();
   const uint32_t raw = smem_u32(fs_smem_raw);
   unsigned char* ring = fs_smem_raw + (((raw + 1023u) & ~1023u) - raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + kRing);
@@ -313,6 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           slot.next();
         }
       }
+      if (tile + pairs >= tiles) grid_started();
       const int64_t row0 = (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, col0 = (int64_t)tc * kBN + half * kCols;
       float acc[kCols];
 #pragma unroll

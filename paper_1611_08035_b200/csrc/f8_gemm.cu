@@ -65,7 +65,6 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
   using Cfg = F8Cfg<TBN, MX>;
   constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES;
   extern __shared__ unsigned char f8_smem_raw[];
-  grid_started();
   const uint32_t raw = smem_u32(f8_smem_raw);
   unsigned char* ring = f8_smem_raw + (((raw + 1023u) & ~1023u) - raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + Cfg::RING);
@@ -297,6 +296,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
         }
         __syncwarp();
       }
+      if (tile + (int)gridDim.x >= tiles) grid_started();
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
       } else if (p.splits > 1) {

@@ -45,7 +45,6 @@ template <typename TC, int CHUNK>
 __global__ void __launch_bounds__(kThreads, 1)
     f8_mx_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char mx_smem_raw[];
-  grid_started();
   const uint32_t raw = smem_u32(mx_smem_raw);
   unsigned char* ring = mx_smem_raw + (((raw + 1023u) & ~1023u) - raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + kRing);
@@ -263,6 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(leader_tempty);
       }
+      if (tile + pairs >= tiles) grid_started();
       const int64_t row0 = (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, col0 = (int64_t)tc * kBN + half * kCols;
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);

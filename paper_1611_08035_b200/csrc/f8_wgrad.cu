@@ -125,7 +125,6 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
   using Cfg = WgCfg<CTAS>;
   constexpr int EW = Cfg::EW, CW = Cfg::CW, COLS = Cfg::COLS, STAGES = Cfg::STAGES, TBN = Cfg::TBN;
   extern __shared__ unsigned char wg_smem_raw[];
-  grid_started();
   const uint32_t raw = smem_u32(wg_smem_raw);
   unsigned char* ring = wg_smem_raw + (((raw + 1023u) & ~1023u) - raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + Cfg::RING);
@@ -350,6 +349,7 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
         __syncwarp();
         if (lane == 0) arrive_leader(leader(&tempty[b]));
       }
+      if (tile + stride >= tiles) grid_started();
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
       } else if (p.splits == 1) {
