@@ -214,7 +214,18 @@ PyObject* connect(PyObject*, PyObject* args) {
   Py_RETURN_NONE;
 }
 
-#define B2_CALL(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL | METH_KEYWORDS, "The function of the same name in binding.py, called without ctypes."}
+// No C++ exception leaves a function that Python calls (a tensor without storage throws when it is asked for its address).
+template <PyObject* (*FN)(PyObject*, PyObject* const*, Py_ssize_t, PyObject*)>
+PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n, PyObject* names) {
+  try {
+    return FN(self, a, n, names);
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+#define B2_CALL(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<fn>)), METH_FASTCALL | METH_KEYWORDS, "The function of the same name in binding.py, called without ctypes."}
 PyMethodDef g_methods[] = {B2_CALL("b2_rmsnorm_f8", norm),   B2_CALL("b2_rmsnorm_backward", norm_bwd), B2_CALL("b2_quant_f8", quant),
                            B2_CALL("b2_gemm_f8", gemm),      B2_CALL("b2_wgrad_f8", wgrad),            {"connect", connect, METH_VARARGS, nullptr},
                            {nullptr, nullptr, 0, nullptr}};

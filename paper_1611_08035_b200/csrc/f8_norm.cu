@@ -300,7 +300,8 @@ __device__ __forceinline__ void norm_bwd_token(const NormBwdArgs& p, int64_t row
 
 // Few tokens, in one launch: the first `tokens` CTAs write dx of a token each, the others dw of 64 features each, reading dy and h
 // once more (from L2) instead of meeting the first ones' partial sums.  tokens is t, or 0 where dx is written over dy or h
-// and a second launch has to follow (norm_bwd_token_kernel, the same arithmetic).
+// and a second launch has to follow (norm_bwd_token_kernel, the same arithmetic).  Tokens too long for registers go the same
+// way; if there are many, CTAs (., y) take every gridDim.y-th group of 32 and leave partial sums.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) norm_bwd_few_kernel(const NormBwdArgs p, float* dw, int tokens) {
   grid_started();
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(256) norm_bwd_few_kernel(const NormBwdArgs p, 
   float s[8] = {};
   auto at = [&](int j) { return e0 + (VEC ? x * 8 + j : j * 8 + x); };
 #pragma unroll 4
-  for (int64_t row = y; row < p.t; row += 32) {
+  for (int64_t row = blockIdx.y * 32 + y; row < p.t; row += 32 * gridDim.y) {
     const T* DY = static_cast<const T*>(p.DY) + row * p.lddy;
     const T* H = static_cast<const T*>(p.H) + row * p.ldh;
     const float rstd = p.rstd[row];
@@ -339,29 +340,16 @@ __global__ void __launch_bounds__(256) norm_bwd_few_kernel(const NormBwdArgs p, 
     float v = 0.0f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) v += sums[i][threadIdx.x];
-    dw[e0 + threadIdx.x] = v;
+    (gridDim.y > 1 ? p.partial + (int64_t)blockIdx.y * p.d : dw)[e0 + threadIdx.x] = v;
   }
 }
 
-// Tokens too long for registers: dx from two readings of a token ...
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) norm_bwd_token_kernel(const NormBwdArgs p) {
   grid_started();
   grid_ready();
   __shared__ float part[8];
   norm_bwd_token<T, VEC>(p, blockIdx.x, part);
-}
-// ... and dw, before dx may overwrite dy or h, with a thread for every feature.
-template <typename T>
-__global__ void __launch_bounds__(256) norm_bwd_long_dw_kernel(const NormBwdArgs p) {
-  grid_started();
-  grid_ready();
-  const int e = (int)(blockIdx.x * 256 + threadIdx.x);
-  if (e >= p.d) return;
-  float s = 0.0f;
-  for (int64_t row = blockIdx.y; row < p.t; row += gridDim.y)
-    s += (float)static_cast<const T*>(p.DY)[row * p.lddy + e] * ((float)static_cast<const T*>(p.H)[row * p.ldh + e] * p.rstd[row]);
-  p.partial[(int64_t)blockIdx.y * p.d + e] = s;
 }
 
 // dw[e] = sum over the rows of partial sums, always in the same order.
@@ -384,14 +372,16 @@ __global__ void __launch_bounds__(512) norm_bwd_sum_kernel(const float* partial,
   }
 }
 
-constexpr int64_t kBwdLongest = 2048;  // groups of eight of the longest token held in registers
+constexpr int64_t kBwdLongest = 1024;  // groups of eight of the longest token held in registers
 
 // rows of partial sums: CTAs of the backward kernel
 int64_t bwd_rows(int64_t d, int64_t t) {
   const int64_t chunks = blocks_of(d, 8), sms = sm_count_cached();
-  int64_t rows;
-  if (chunks > kBwdLongest) rows = 16;
-  else rows = sms * (chunks <= 128 && chunks > 64 ? 6 : chunks <= 256 ? 4 : chunks <= 1024 ? 2 : 1);
+  if (chunks > kBwdLongest) {
+    const int64_t splits = blocks_of(t, 256);
+    return splits < 16 ? splits : 16;
+  }
+  const int64_t rows = sms * (chunks <= 128 && chunks > 64 ? 6 : chunks <= 256 ? 4 : 2);
   const int64_t most = blocks_of(t, chunks <= 64 ? 32 : 4);
   return rows < most ? rows : most;
 }
@@ -405,11 +395,13 @@ int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
   const int64_t chunks = blocks_of(a.d, 8), rows = bwd_rows(a.d, a.t);
   if (a.t > 0x7fffffffLL) return B2_ERR_VARIANT;
   int rc = B2_OK;
-  if (a.t > 0 && bwd_few(a.d, a.t)) {
-    const bool over = a.DX == a.DY || a.DX == a.H;
-    const int tokens = over ? 0 : (int)a.t;
-    rc = launch_overlapped(norm_bwd_few_kernel<T, VEC>, (unsigned)(tokens + blocks_of(a.d, 64)), 256, st, a, dw, tokens);
-    if (over && !rc) rc = launch_overlapped(norm_bwd_token_kernel<T, VEC>, (unsigned)a.t, 256, st, a);
+  if (a.t > 0 && (bwd_few(a.d, a.t) || chunks > kBwdLongest)) {
+    const bool few = bwd_few(a.d, a.t), apart = !few || a.DX == a.DY || a.DX == a.H;
+    const int tokens = apart ? 0 : (int)a.t;
+    const unsigned splits = few ? 1 : (unsigned)rows;
+    rc = launch_overlapped(norm_bwd_few_kernel<T, VEC>, dim3((unsigned)(tokens + blocks_of(a.d, 64)), splits), 256, st, a, dw, tokens);
+    if (!rc && splits > 1) rc = launch_overlapped(norm_bwd_sum_kernel, (unsigned)blocks_of(a.d, 32), 512, st, a.partial, rows, (int64_t)a.d, dw);
+    if (!rc && apart) rc = launch_overlapped(norm_bwd_token_kernel<T, VEC>, (unsigned)a.t, 256, st, a);
     return rc;
   }
   const unsigned g = (unsigned)rows;
@@ -419,12 +411,7 @@ int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
     else if (chunks <= 128) rc = launch_overlapped(norm_bwd_kernel<T, 128, 128, 1, VEC>, g, 128, st, a);
     else if (chunks <= 256) rc = launch_overlapped(norm_bwd_kernel<T, 128, 128, 2, VEC>, g, 128, st, a);
     else if (chunks <= 512) rc = launch_overlapped(norm_bwd_kernel<T, 256, 256, 2, VEC>, g, 256, st, a);
-    else if (chunks <= 1024) rc = launch_overlapped(norm_bwd_kernel<T, 512, 512, 2, VEC>, g, 512, st, a);
-    else if (chunks <= kBwdLongest) rc = launch_overlapped(norm_bwd_kernel<T, 512, 512, 4, VEC>, g, 512, st, a);
-    else {
-      rc = launch_overlapped(norm_bwd_long_dw_kernel<T>, dim3((unsigned)blocks_of(a.d, 256), g), 256, st, a);
-      if (!rc) rc = launch_overlapped(norm_bwd_token_kernel<T, VEC>, (unsigned)a.t, 256, st, a);
-    }
+    else rc = launch_overlapped(norm_bwd_kernel<T, 512, 512, 2, VEC>, g, 512, st, a);
   }
   return rc ? rc : launch_overlapped(norm_bwd_sum_kernel, (unsigned)blocks_of(a.d, 32), 512, st, a.partial, rows, (int64_t)a.d, dw);
 }
