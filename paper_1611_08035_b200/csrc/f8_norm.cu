@@ -353,21 +353,23 @@ __global__ void __launch_bounds__(256) norm_bwd_token_kernel(const NormBwdArgs p
 }
 
 // dw[e] = sum over the rows of partial sums, always in the same order.
-__global__ void __launch_bounds__(512) norm_bwd_sum_kernel(const float* partial, int64_t rows, int64_t d, float* dw) {
+__global__ void __launch_bounds__(1024) norm_bwd_sum_kernel(const float* partial, int64_t rows, int64_t d, float* dw) {
   grid_started();
   grid_ready();
-  __shared__ float part[16][33];
+  __shared__ float part[32][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int64_t e = (int64_t)blockIdx.x * 32 + x;
   float s = 0.0f;
-  if (e < d)
-    for (int64_t r = y; r < rows; r += 16) s += partial[r * d + e];
+  if (e < d) {
+#pragma unroll 4
+    for (int64_t r = y; r < rows; r += 32) s += partial[r * d + e];
+  }
   part[y][x] = s;
   __syncthreads();
   if (y == 0 && e < d) {
     s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += part[i][x];
+    for (int i = 0; i < 32; ++i) s += part[i][x];
     dw[e] = s;
   }
 }
@@ -382,7 +384,7 @@ int64_t bwd_rows(int64_t d, int64_t t) {
     return splits < 16 ? splits : 16;
   }
   const int64_t rows = sms * (chunks <= 128 && chunks > 64 ? 6 : chunks <= 256 ? 4 : 2);
-  const int64_t most = blocks_of(t, chunks <= 64 ? 32 : 4);
+  const int64_t most = blocks_of(t, chunks <= 64 ? 32 : chunks <= 256 ? 2 : 4);  // a few tokens each, as many CTAs as fit at a time
   return rows < most ? rows : most;
 }
 
@@ -400,7 +402,7 @@ int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
     const int tokens = apart ? 0 : (int)a.t;
     const unsigned splits = few ? 1 : (unsigned)rows;
     rc = launch_overlapped(norm_bwd_few_kernel<T, VEC>, dim3((unsigned)(tokens + blocks_of(a.d, 64)), splits), 256, st, a, dw, tokens);
-    if (!rc && splits > 1) rc = launch_overlapped(norm_bwd_sum_kernel, (unsigned)blocks_of(a.d, 32), 512, st, a.partial, rows, (int64_t)a.d, dw);
+    if (!rc && splits > 1) rc = launch_overlapped(norm_bwd_sum_kernel, (unsigned)blocks_of(a.d, 32), 1024, st, a.partial, rows, (int64_t)a.d, dw);
     if (!rc && apart) rc = launch_overlapped(norm_bwd_token_kernel<T, VEC>, (unsigned)a.t, 256, st, a);
     return rc;
   }
@@ -413,7 +415,7 @@ int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
     else if (chunks <= 512) rc = launch_overlapped(norm_bwd_kernel<T, 256, 256, 2, VEC>, g, 256, st, a);
     else rc = launch_overlapped(norm_bwd_kernel<T, 512, 512, 2, VEC>, g, 512, st, a);
   }
-  return rc ? rc : launch_overlapped(norm_bwd_sum_kernel, (unsigned)blocks_of(a.d, 32), 512, st, a.partial, rows, (int64_t)a.d, dw);
+  return rc ? rc : launch_overlapped(norm_bwd_sum_kernel, (unsigned)blocks_of(a.d, 32), 1024, st, a.partial, rows, (int64_t)a.d, dw);
 }
 
 bool type_ok(int type) { return type == B2_TYPE_F32 || type == B2_TYPE_BF16; }
