@@ -10,9 +10,11 @@
 namespace b2 {
 
 // ---- launches that overlap the end of the kernel before ---------------------------------------------
-// Every kernel of the 8-bit operators lets its successor in the stream be launched early (grid_started: as soon as its own CTAs run, the
-// products' as they come to their results, because a successor's CTAs that take the free places sooner take them unevenly) and touches global memory only after its predecessor has completed and its writes are visible (grid_ready),
-// so that setting up overlaps with finishing.  Kernels launched without the attribute are not affected.
+// Every kernel of the 8-bit operators lets its successor in the stream be launched early (grid_started) and touches global memory
+// only after its predecessor has completed and its writes are visible (grid_ready), so that setting up overlaps with finishing: a norm of
+// eight tokens, called again and again, takes 3.4 us instead of 4.0.  Early is as soon as all CTAs run, or, in the products, as they come to their
+// results: a successor's CTAs that come sooner take the places they find two to an SM (1001 x 999 x 1003: 10.3 us instead of 8.0).
+// Kernels launched without the attribute are not affected.
 __device__ __forceinline__ void grid_started() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename... Params, typename... Args>
@@ -73,7 +75,7 @@ __device__ __forceinline__ float e8m0_value(uint32_t b) {
 // ---- eight consecutive elements ----------------------------------------------------------------
 // As they lie in memory.  Loading and unpacking are two steps so that several loads are on their way before the first is
 // waited for: with the unpacking inside the load's branch, every load waited for the one before it (b2_quant_f8 of 16384 x
-// 8192 bf16: 120 us instead of 68).
+// 8192 bf16, eight numbers a load: 120 us instead of 84).
 template <typename T>
 struct Raw8 {
   uint32_t u[2 * sizeof(T)];
@@ -153,8 +155,8 @@ __device__ __forceinline__ void store8_f8(uint8_t* p, int64_t nv, bool vec, uint
 
 // Eight numbers of a row for every lane of a warp that covers 256 consecutive ones starting at `first`.  VEC: every row
 // starts on a 16-byte boundary and lane l holds numbers 8 l .. 8 l + 7, in whole loads; otherwise rows start anywhere and
-// lane l holds l, l + 32, .., so that the lanes of every (narrow) load are neighbours: 16384 rows of 1003 bf16 numbers quantise in
-// 28 us with eight narrow loads a lane at a distance of 16 bytes.
+// lane l holds l, l + 32, .., so that the lanes of every (narrow) load are neighbours (norm of 16384 x 1003 bf16: 50 us, 76 with narrow loads 16
+// bytes apart).
 template <typename T, bool VEC>
 struct Warp256 {
   __device__ __forceinline__ static int index(int first, int j) {

@@ -6,6 +6,10 @@
 // half of the fp32 pipe, and the reason why the tile's row scale and, for 128 x 128 blocks, its column scale are made one
 // factor a thread.
 //
+// What bounds it: those eight warps.  A block takes about 1000 clocks, 415 of them reading tensor memory (shared with the next block's
+// accumulation), the others barriers, scales and multiply-adds one after the other: 4096^3 in 78-88 us (1.6-1.8 PFLOP/s), 8192^3 in 531 us.
+// Sixteen warps of 64 columns read no faster (103 us); reading the next block's scales early cost registers (104 us).
+//
 // Warps of a CTA: 0 streams the operands (TMA), 1 issues the multiply-adds (leader only), 4-7 bring the scales of four
 // blocks at a time to shared memory, 8-15 scale, add and write C.
 #include <cuda.h>

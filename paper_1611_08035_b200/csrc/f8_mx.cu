@@ -7,6 +7,12 @@
 // multiply-adds; the leader's tensor core instruction reads both halves.  The sums stay in tensor memory (256 columns) for the
 // whole tile; 48 more columns hold the scales of sixteen blocks.
 //
+// What bounds it: power.  8192^3 takes 383 us in a burst and 440 us on and on (2.5 PFLOP/s), a block 581 clocks where the tensor pipe
+// needs 512, at 1.3 GHz under the board's power limit; without the limit (4096^3, one turn of four not full) 55 us.  Steps on the
+// way, 8192^3: 599 us with every warp fetching all scales, 501 with each word fetched once, 434 with two blocks a stage and a
+// converged issuing warp (its own instructions, 795 clocks a block, were what the pipe waited for), 407 with results staged for whole
+// lines, 383 without cluster-scope release on arrivals.
+//
 // Warps of a CTA: 0 streams the operands (TMA), 1 issues the multiply-adds (leader only), 4-7 put the scales
 // into tensor memory, four blocks at a time (byte = block, lane and column = row), 8-15 write C.
 #include <cuda.h>

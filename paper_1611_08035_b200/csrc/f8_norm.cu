@@ -3,9 +3,11 @@
 //   h = x + r,  rstd = 1/sqrt(mean(h^2) + eps),  y = h * rstd * w,  (q, s) = y quantised in blocks of 128 features
 //   dx = rstd * (g - xh * mean(g xh)) + dh,  dw = sum_t dy xh,     g = dy w, xh = h rstd
 //
-// Both are bound by memory: a token is read once, kept in registers over the sum that its norm needs, and written
-// once.  A thread holds groups of eight consecutive features (16 bytes of bf16), so sixteen neighbouring lanes hold
-// exactly one block of 128 and its largest magnitude is four shuffles away.
+// Both are bound by memory: a token is read once, kept in registers over the sum that its norm needs, and written once.  A
+// warp holds 256 consecutive features, exactly two blocks of 128, so that their largest magnitudes never leave it.
+// Measured, bf16: norm of 16384 x 8192 153 us (6.1 TB/s, 94 % of the copy rate), gradient of 16384 x 8192 181 us (5.9 TB/s); fp32: 270 us
+// (6.5 TB/s) and 326 us (6.6 TB/s).  Tokens of 1000 to 1024 features reach 4.0 to 4.9 TB/s, tokens whose length no thread count
+// divides or that do not start on 16 bytes about half.
 #include "b2gemm.h"
 #include "entry.h"
 #include "f8.cuh"

@@ -14,8 +14,10 @@
 // the leader's), warps 4-11 turn the 8-bit tile into the bf16 tile the multiply reads (128-byte swizzle), warps 12-19 add
 // the sums of kChunk stages to fp32 accumulators in registers (two tensor-memory buffers in turn) and write C.
 //
-// What bounds it: shared memory.  A stage's 512 clocks of tensor pipe come with 24 KB written by TMA, 8 KB read and 16 KB
-// written by the conversion and 32 KB read by the multiply: 640 clocks at 128 bytes each.
+// What bounds it: the conversion's instructions.  A stage is 512 clocks of tensor pipe and takes 750, in which the SM issues 2300 of 3000
+// possible instructions, three quarters of them conversion (30 for eight numbers, 5 of which look for NaNs, 3 % of the time); shared
+// memory, at 128 bytes a clock, would need 640 (24 KB written by TMA, 8 read and 16 written by the conversion, 32 read by the multiply).
+// 4096 x 4096 x 8192 takes 230 us in a burst (1.19 PFLOP/s) and 275 on and on; its 256 tiles are 3.5 turns of 74 pairs.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
