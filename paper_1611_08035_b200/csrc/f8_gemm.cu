@@ -382,22 +382,37 @@ int f8_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, int s
                            dim3(1, (unsigned)splits), st, a, mr, mc);
 }
 
-// CTAs that share a tile's k range, and what the product then takes, in clocks: turns of CTAs over the SMs, a turn being its
-// share of the blocks at 50 bytes of operands a clock, the rate at which one SM's copies arrived when measured, and adding the
-// shares, about 30 clocks a column of the tile when measured.  Clusters of eight do not fill every group of SMs.
-struct F8Split {
-  int s;
-  double clocks;
-};
-F8Split f8_split_for(int64_t tiles, int kb, int tbn, int resident) {
-  const double stage = (kRowStage + tbn * kF8Block) / 50.0, join = 30.0 * tbn;
-  F8Split best{1, 0.0};
-  for (int s = 1, log = 0; s <= kMaxSplit && (s == 1 || kb / s >= 2); s *= 2, ++log) {
-    const int64_t slots = (int64_t)sm_count_cached() * resident * (s == 8 ? 3 : 4) / 4;
-    const double clocks = (double)blocks_of(tiles * s, slots) * resident * (double)blocks_of(kb, s) * stage + (s > 1 ? join * (0.7 + 0.3 * log) : 0.0);
-    if (s == 1 || clocks < best.clocks) best = {s, clocks};
+// SMs that clusters of 2^log CTAs, one to an SM, can hold at once: a cluster stays within one group of SMs, and the groups are no multiples
+// of eight, nor alike on every GPU.
+int f8_cluster_slots(int log) {
+  static std::atomic<int> known[64][4];
+  const int sms = sm_count_cached();
+  int dev = -1;
+  if (log == 0 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sms;
+  int slots = known[dev][log].load(std::memory_order_acquire);
+  if (slots) return slots;
+  auto kfn = f8_gemm_kernel<128, float, true, true>;
+  using Cfg = F8Cfg<128, true>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(1, 1u << log), cfg.blockDim = Cfg::NT, cfg.dynamicSmemBytes = Cfg::SMEM;
+  cudaLaunchAttribute at = {};
+  at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim = {1, 1u << log, 1};
+  cfg.attrs = &at, cfg.numAttrs = 1;
+  int clusters = 0;
+  if (cudaFuncSetAttribute(kfn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&clusters, kfn, &cfg) != cudaSuccess || clusters < 1) {
+    (void)cudaGetLastError();
+    return sms * 3 / 4;
   }
-  return best;
+  slots = clusters << log;
+  known[dev][log].store(slots, std::memory_order_release);
+  return slots;
+}
+
+// Clocks of a block of 128 and of a join: 50 bytes of operands a clock, the rate at which one SM's copies arrived when measured, and about 30
+// clocks a column of the tile.
+F8Split f8_product_split(int64_t tiles, int kb, int tbn, int resident) {
+  return f8_split_for(tiles, kb, (kRowStage + tbn * kF8Block) / 50.0, 30.0 * tbn, resident);
 }
 
 template <typename TC, bool MX>
@@ -406,15 +421,15 @@ int f8_choose(const F8Args& a, const F8Operand& A, const F8Operand& B, int64_t k
   if (B.n <= 64 && !B.mn) {  // decoding: A's rows, tiles as narrow as n, two CTAs an SM
     const int tbn = B.n <= 16 ? 16 : B.n <= 32 ? 32 : 64;
     const int64_t tiles = blocks_of(A.n, kRows);
-    const int s = f8_split_for(tiles, a.kb, tbn, tiles >= sms ? 2 : 1).s;
+    const int s = f8_product_split(tiles, a.kb, tbn, tiles >= sms ? 2 : 1).s;
     if (tbn == 16) return f8_launch<16, TC, false, MX>(a, A, B, k, s, st);
     if (tbn == 32) return f8_launch<32, TC, false, MX>(a, A, B, k, s, st);
     return f8_launch<64, TC, false, MX>(a, A, B, k, s, st);
   }
   // pairs of CTAs as soon as single ones, with tiles a quarter of the size, would take more than one turn
   if (blocks_of(B.n, 256) * blocks_of(A.n, 256) * 4 > sms) return MX ? f8_mx_launch<TC>(a, B, A, k, st) : f8_fs_launch<TC>(a, B, A, k, st);
-  const F8Split wide = f8_split_for(blocks_of(B.n, kRows) * blocks_of(A.n, 128), a.kb, 128, 1);
-  const F8Split narrow = f8_split_for(blocks_of(B.n, kRows) * blocks_of(A.n, 64), a.kb, 64, 1);
+  const F8Split wide = f8_product_split(blocks_of(B.n, kRows) * blocks_of(A.n, 128), a.kb, 128, 1);
+  const F8Split narrow = f8_product_split(blocks_of(B.n, kRows) * blocks_of(A.n, 64), a.kb, 64, 1);
   // half as many columns a tile fetch more than half as much, but spare the join when they fill the SMs without a split
   if (narrow.clocks < wide.clocks) return f8_launch<64, TC, true, MX>(a, B, A, k, narrow.s, st);
   return f8_launch<128, TC, true, MX>(a, B, A, k, wide.s, st);
@@ -440,6 +455,18 @@ F8Pack f8_pack_plan(bool an, bool bn, int64_t m, int64_t n, int64_t k, const voi
 }
 
 }  // namespace
+
+// What the product takes, in clocks: turns of CTAs over the SMs, and adding the shares, half as long again for every doubling.
+// Measured with clusters that do not fit at once: weight gradient of 512 x 512 over 4096 tokens 20.1 us with 16 clusters of eight, 13.8 with four.
+F8Split f8_split_for(int64_t tiles, int stages, double stage, double join, int resident) {
+  F8Split best{1, 0.0};
+  for (int s = 1, log = 0; s <= kMaxSplit && (s == 1 || stages / s >= 2); s *= 2, ++log) {
+    const int64_t slots = (int64_t)f8_cluster_slots(log) * resident;
+    const double clocks = (double)blocks_of(tiles * s, slots) * resident * (double)blocks_of(stages, s) * stage + (s > 1 ? join * (0.7 + 0.3 * log) : 0.0);
+    if (s == 1 || clocks < best.clocks) best = {s, clocks};
+  }
+  return best;
+}
 
 int f8_repitch(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd, cudaStream_t st) {
   return launch_overlapped(f8_repitch_kernel, grid_for(ldd / 16 * cols), 256, st, static_cast<const uint8_t*>(src), ld, rows, cols, static_cast<uint8_t*>(dst), ldd);

@@ -18,22 +18,47 @@ __device__ __forceinline__ float f8_load1(const float* p) { return *p; }
 __device__ __forceinline__ float f8_load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void f8_store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void f8_store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-template <typename TC>
-__device__ __forceinline__ void f8_put(const F8Out& p, TC* c, float v) {
-  v *= p.alpha;
-  if (p.beta != 0.0f) v += p.beta * f8_load1(c);
-  f8_store1(c, v);
+__device__ __forceinline__ void f8_load4(const float* p, float v[4]) {
+  const float4 q = *reinterpret_cast<const float4*>(p);
+  v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+}
+__device__ __forceinline__ void f8_load4(const __nv_bfloat16* p, float v[4]) {
+  const uint2 q = *reinterpret_cast<const uint2*>(p);
+  v[0] = __uint_as_float(q.x << 16), v[1] = __uint_as_float(q.x & 0xffff0000u);
+  v[2] = __uint_as_float(q.y << 16), v[3] = __uint_as_float(q.y & 0xffff0000u);
+}
+__device__ __forceinline__ void f8_store4(float* p, const float v[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void f8_store4(__nv_bfloat16* p, const float v[4]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
 }
 
 // N accumulators of one row of a tile whose rows are contiguous in C (C[col * ldc + row]): neighbouring lanes, neighbouring rows.
+// Straight code with one test of beta: with one at every column a tile's 64 columns a warp took 4 us (a gradient of 4096 x 4096 over
+// 64 tokens 36 us, now 21).
 template <typename TC, int N>
-__device__ __forceinline__ void f8_emit_rows(const F8Out& p, int64_t row, int64_t col, const float* acc) {
-  if (row >= p.rows) return;
-  TC* C = static_cast<TC*>(p.C) + row;
+__device__ __forceinline__ void f8_emit_rows(const F8Out& p, int64_t row, int64_t col, float* acc) {
+  float beta = p.beta;
+  int64_t ldc = p.ldc;
+  asm volatile("" : "+f"(beta), "+l"(ldc));  // what follows from these is not kept in registers over the loop that fills acc
+  const int nv = row < p.rows ? (int)min((int64_t)N, p.cols - col) : 0;
+  TC* C = static_cast<TC*>(p.C) + row + col * ldc;
+  if (beta != 0.0f) {
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (col + j < p.cols) f8_put(p, C + (col + j) * p.ldc, acc[j]);
+    for (int j0 = 0; j0 < N; j0 += 8) {
+      float old[8];
+      const TC* c = C + j0 * ldc;
+#pragma unroll
+      for (int j = 0; j < 8; ++j, c += ldc) old[j] = j0 + j < nv ? f8_load1(c) : 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j0 + j] = p.alpha * acc[j0 + j] + beta * old[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] *= p.alpha;
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j, C += ldc)
+    if (j < nv) f8_store1(C, acc[j]);
 }
 
 // N consecutive accumulators each of 32 consecutive rows (row0 + lane), columns contiguous in C.  64 bytes of every row pass through shared memory at a time and leave as whole 64-byte pieces
@@ -43,11 +68,14 @@ constexpr int kEmitPitch = 80;  // bytes between staged rows: 16-byte pieces of 
 constexpr int kEmitBytes = 32 * kEmitPitch;
 template <typename TC, int N>
 __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int64_t col0, const float* acc, unsigned char* stage) {
+  float beta = p.beta;
+  int64_t ldc = p.ldc;
+  asm volatile("" : "+f"(beta), "+l"(ldc));  // what follows from these is not kept in registers over the loop that fills acc
   const int lane = threadIdx.x & 31, piece = lane & 3;
   TC* C = static_cast<TC*>(p.C);
   unsigned char* own = stage + lane * kEmitPitch;
   const unsigned char* swap = stage + (lane >> 2) * kEmitPitch + piece * 16;
-  if (sizeof(TC) == 2 && p.beta == 0.0f && p.vec) {
+  if (sizeof(TC) == 2 && beta == 0.0f && p.vec) {
 #pragma unroll
     for (int j = 0; j < N; j += 32) {
       __syncwarp();
@@ -65,10 +93,10 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
         const uint4 q = *reinterpret_cast<const uint4*>(swap + 8 * i * kEmitPitch);
         if (row < p.rows) {
           if (nv >= 8) {
-            *reinterpret_cast<uint4*>(C + row * p.ldc + col) = q;
+            *reinterpret_cast<uint4*>(C + row * ldc + col) = q;
           } else {
             const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-            uint16_t* c = reinterpret_cast<uint16_t*>(C + row * p.ldc + col);
+            uint16_t* c = reinterpret_cast<uint16_t*>(C + row * ldc + col);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               if (e < nv) c[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
@@ -76,50 +104,67 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
         }
       }
     }
-  } else {
+    return;
+  }
+  auto put = [&](int j) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<float4*>(own + 16 * i) = make_float4(p.alpha * acc[j + 4 * i], p.alpha * acc[j + 4 * i + 1], p.alpha * acc[j + 4 * i + 2], p.alpha * acc[j + 4 * i + 3]);
+    __syncwarp();
+  };
+  if (!p.vec) {  // columns of C that start anywhere: element by element, sixteen lanes to a row
 #pragma unroll
     for (int j = 0; j < N; j += 16) {
-      __syncwarp();
+      put(j);
+      float v[16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(own + 16 * i) = make_float4(p.alpha * acc[j + 4 * i], p.alpha * acc[j + 4 * i + 1], p.alpha * acc[j + 4 * i + 2], p.alpha * acc[j + 4 * i + 3]);
-      __syncwarp();
-      if (!p.vec) {  // columns of C that start anywhere: element by element, sixteen lanes to a row
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const float*>(stage + (2 * i + (lane >> 4)) * kEmitPitch + (lane & 15) * 4);
-        const int64_t col = col0 + j + (lane & 15), row = row0 + (lane >> 4);
-        const int64_t rows = col < p.cols ? p.rows - row : 0;
-        TC* c = C + row * p.ldc + col;
-        if (p.beta != 0.0f) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (2 * i < rows) v[i] += p.beta * f8_load1(c + 2 * i * p.ldc);
-        }
+      for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const float*>(stage + (2 * i + (lane >> 4)) * kEmitPitch + (lane & 15) * 4);
+      const int64_t col = col0 + j + (lane & 15), row = row0 + (lane >> 4);
+      const int rows = col < p.cols ? (int)min((int64_t)32, p.rows - row) : 0;
+      TC* c = C + row * ldc + col;
+      if (beta != 0.0f) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (2 * i < rows) f8_store1(c + 2 * i * p.ldc, v[i]);
-        continue;
+          if (2 * i < rows) v[i] += beta * f8_load1(c + 2 * i * ldc);
       }
-      const int64_t col = col0 + j + piece * 4, nv = p.cols - col;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (2 * i < rows) f8_store1(c + 2 * i * ldc, v[i]);
+    }
+    return;
+  }
+  // four lanes to a row; the old values of a lane's four rows are on their way at once
+  const int rows = (int)min((int64_t)32, p.rows - row0 - (lane >> 2));
+#pragma unroll
+  for (int j = 0; j < N; j += 16) {
+    put(j);
+    const int64_t col = col0 + j + piece * 4, nv = p.cols - col;
+    TC* c = C + (row0 + (lane >> 2)) * ldc + col;
+    if (nv >= 4) {
+      float old[4][4] = {};
+      if (beta != 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (8 * i < rows) f8_load4(c + 8 * i * ldc, old[i]);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + 8 * i + (lane >> 2);
-        const float4 q = *reinterpret_cast<const float4*>(swap + 8 * i * kEmitPitch);
-        float v[4] = {q.x, q.y, q.z, q.w};
-        if (row < p.rows) {
-          TC* c = C + row * p.ldc + col;
-          if (p.beta != 0.0f) {
+        float v[4];
+        f8_load4(reinterpret_cast<const float*>(swap + 8 * i * kEmitPitch), v);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e < nv) v[e] += p.beta * f8_load1(c + e);
-          }
-          if (sizeof(TC) == 4 && nv >= 4) {
-            *reinterpret_cast<float4*>(c) = make_float4(v[0], v[1], v[2], v[3]);
-          } else {
+        for (int e = 0; e < 4; ++e) v[e] = beta != 0.0f ? v[e] + beta * old[i][e] : v[e];
+        if (8 * i < rows) f8_store4(c + 8 * i * ldc, v);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e < nv) f8_store1(c + e, v[e]);
+        for (int e = 0; e < 3; ++e) {
+          float v = *reinterpret_cast<const float*>(swap + 8 * i * kEmitPitch + 4 * e);
+          if (8 * i < rows && e < nv) {
+            if (beta != 0.0f) v += beta * f8_load1(c + 8 * i * ldc + e);
+            f8_store1(c + 8 * i * ldc + e, v);
           }
         }
       }
@@ -133,6 +178,12 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
 // (one after the other, their latency made up most of a 1024^3 product: 21 us, now 6.4).  All threads of all CTAs of the cluster call this; the
 // 32 EW threads with worker >= 0 (numbered) add and write.  PERMUTE: row r of the tile is row kept_row(r) of C.
 constexpr int kMaxSplit = 8;  // 2, 4 or 8 CTAs
+struct F8Split {
+  int s;          // CTAs to a tile
+  double clocks;  // estimate of the product's time
+};
+// tiles, stages of a tile's k range, clocks of a stage, clocks of a join of two, CTAs that an SM holds; defined in f8_gemm.cu
+F8Split f8_split_for(int64_t tiles, int stages, double stage, double join, int resident);
 __host__ __device__ constexpr int share_pitch(int inner) { return inner + 4; }  // 16-byte pieces of consecutive lines in different banks
 __host__ __device__ constexpr int share_bytes(int tbn) { return 4 * (tbn * share_pitch(128) > 128 * share_pitch(tbn) ? tbn * share_pitch(128) : 128 * share_pitch(tbn)); }
 __device__ __forceinline__ int kept_row(int i) { return (i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1); }
@@ -186,18 +237,19 @@ __device__ __forceinline__ void f8_add_shares(const F8Out& p, void* tile, int sh
     if (COLS_CONTIG ? row < p.rows : col < p.cols) {
       TC* c = static_cast<TC*>(p.C) + (COLS_CONTIG ? row * p.ldc + col : col * p.ldc + row);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] *= p.alpha;
-        if (p.beta != 0.0f && e < nv) v[e] += p.beta * f8_load1(c + e);
+      for (int e = 0; e < 4; ++e) v[e] *= p.alpha;
+      if (p.beta != 0.0f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < nv) v[e] += p.beta * f8_load1(c + e);
       }
       if (!p.vec) {
         *reinterpret_cast<float4*>(static_cast<float*>(tile) + o * share_pitch(INNER) + in) = make_float4(v[0], v[1], v[2], v[3]);
       } else if (nv >= 4) {
-        if constexpr (sizeof(TC) == 4) *reinterpret_cast<float4*>(c) = make_float4(v[0], v[1], v[2], v[3]);
-        else *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        f8_store4(c, v);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 3; ++e)
           if (e < nv) f8_store1(c + e, v[e]);
       }
     }

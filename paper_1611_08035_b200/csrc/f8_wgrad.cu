@@ -419,8 +419,7 @@ int wg_choose(const WgArgs& a, int64_t m, int64_t n, int64_t k, const void* Q, i
   const int sms = sm_count_cached();
   if (blocks_of(m, 256) * blocks_of(n, 256) * 4 > sms) return wg_launch<2, TC>(a, m, n, k, Q, ldq, Y, ldy, 1, st);
   const int64_t tiles = blocks_of(m, kRows) * blocks_of(n, 128);
-  int s = 1;
-  while (s < kMaxSplit && tiles * s * 2 <= sms && a.kb / (s * 2) >= 2) s *= 2;
+  const int s = f8_split_for(tiles, a.kb, 730.0, 30.0 * 128, 1).s;  // a stage takes 0.38 us of conversion
   return wg_launch<1, TC>(a, m, n, k, Q, ldq, Y, ldy, s, st);
 }
 
