@@ -6,8 +6,8 @@
 // Both are bound by memory: a token is read once, kept in registers over the sum that its norm needs, and written once.  A
 // warp holds 256 consecutive features, exactly two blocks of 128, so that their largest magnitudes never leave it.
 // Measured, bf16: norm of 16384 x 8192 153 us (6.1 TB/s, 94 % of the copy rate), gradient of 16384 x 8192 181 us (5.9 TB/s); fp32: 270 us
-// (6.5 TB/s) and 326 us (6.6 TB/s).  Tokens of 1000 to 1024 features reach 4.0 to 4.9 TB/s, tokens whose length no thread count
-// divides or that do not start on 16 bytes about half.
+// (6.5 TB/s) and 326 us (6.6 TB/s).  Other lengths: norm of 2560 features 5.8, of 3184 4.2, of 10240 5.5 TB/s; gradient of 2560 4.6, of
+// 5120 4.4, of 7168 5.5 TB/s.  bf16 tokens that do not start on 16 bytes are read two bytes at a time: 1.8 TB/s.
 #include "b2gemm.h"
 #include "entry.h"
 #include "f8.cuh"
@@ -25,37 +25,40 @@ struct NormArgs {
   float eps;
 };
 
-// Sum over the TPR threads of a row; the same value in each of them.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* part) {
+__device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if constexpr (TPR > 32) {
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.0f;
+  return v;
+}
+// Sum over a CTA of NT threads (FULL) or at most as many; the same value in each of them.
+template <int NT, bool FULL>
+__device__ __forceinline__ float cta_sum(float v, float* part) {
+  v = warp_sum(v);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  if (!FULL && threadIdx.x < NT / 32 && threadIdx.x >= blockDim.x / 32) part[threadIdx.x] = 0.0f;  // the first warp has a lane for each missing one
+  __syncthreads();
+  v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < TPR / 32; ++i) v += part[i];
-  }
+  for (int i = 0; i < NT / 32; ++i) v += part[i];
   return v;
 }
 
-// TPR threads to a token, each VPT groups of eight features (Warp256: which eight).
-template <typename T, int TPR, int VPT, bool VEC>
-__global__ void __launch_bounds__(TPR > 128 ? TPR : 128, TPR == 512 && VPT == 4 && sizeof(T) == 2 ? 2 : 1) norm_kernel(const NormArgs p) {
+// WARP: a warp to a token, four tokens a CTA; otherwise the CTA, whose size is the token's.  A thread holds VPT groups of eight features
+// (Warp256: which eight).  FULL: the CTA has NT threads, which saves 4 % where it does (8192 x 8192 bf16 80 us, 83 with a width read at
+// run time); otherwise as many warps as the token fills (2560 x 16384: 70 us with the next power of two, 51).
+template <typename T, int VPT, int NT, bool WARP, bool VEC, bool FULL = true>
+__global__ void __launch_bounds__(NT, NT == 512 && VPT == 4 && sizeof(T) == 2 ? 2 : 1) norm_kernel(const NormArgs p) {
   grid_started();
   grid_ready();
   using Piece = Warp256<T, VEC>;
-  constexpr int NT = TPR > 128 ? TPR : 128, RPC = NT / TPR;
-  static_assert(RPC == 1 || TPR == 32, "rows that share a CTA meet at no barrier");
-  __shared__ float part[TPR > 32 ? TPR / 32 : 1];
-  const int64_t row = (int64_t)blockIdx.x * RPC + (RPC > 1 ? threadIdx.x / TPR : 0);
-  const int l = RPC > 1 ? threadIdx.x % TPR : threadIdx.x;
-  if (RPC > 1 && row >= p.t) return;  // whole warps
+  __shared__ float part[NT / 32];
+  const int64_t row = WARP ? (int64_t)blockIdx.x * (NT / 32) + threadIdx.x / 32 : blockIdx.x;
+  const int l = WARP ? threadIdx.x % 32 : threadIdx.x, width = WARP ? 32 : FULL ? NT : (int)blockDim.x;
+  if (WARP && row >= p.t) return;  // whole warps
   const T* X = static_cast<const T*>(p.X) + row * p.ldx;
   const T* R = p.R ? static_cast<const T*>(p.R) + row * p.ldr : nullptr;
   T* H = p.H ? static_cast<T*>(p.H) + row * p.ldh : nullptr;
-  auto first = [&](int i) { return ((l & ~31) + i * TPR) * 8; };
+  auto first = [&](int i) { return ((l & ~31) + i * width) * 8; };
   Raw8<T> rx[VPT], rr[VPT], rw[VPT];  // all loads first
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
@@ -78,7 +81,7 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128, TPR == 512 && VPT == 4 
 #pragma unroll
     for (int j = 0; j < 8; ++j) ss += v[i][j] * v[i][j];
   }
-  const float rstd = 1.0f / sqrtf(row_sum<TPR>(ss, part) / (float)p.d + p.eps);
+  const float rstd = 1.0f / sqrtf((WARP ? warp_sum(ss) : cta_sum<NT, FULL>(ss, part)) / (float)p.d + p.eps);
   if (p.rstd && l == 0) p.rstd[row] = rstd;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
@@ -121,7 +124,7 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs p) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) ss += v[j] * v[j];
   }
-  const float rstd = 1.0f / sqrtf(row_sum<1024>(ss, part) / (float)p.d + p.eps);
+  const float rstd = 1.0f / sqrtf(cta_sum<1024, true>(ss, part) / (float)p.d + p.eps);
   if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
   for (int first = (int)(threadIdx.x & ~31u) * 8; first < p.d; first += 8192) {  // the same for the lanes of a warp
     float y[8], w[8];
@@ -144,19 +147,29 @@ int norm_launch(const NormArgs& a, cudaStream_t st) {
   int rc;
   if (a.t <= 2 * sm_count_cached() && chunks > 32 && chunks <= 1024) {
     // few tokens: one group of eight per thread, the shortest chain from the load to the store
-    if (chunks <= 128) rc = launch_overlapped(norm_kernel<T, 128, 1, VEC>, t, 128, st, a);
-    else if (chunks <= 256) rc = launch_overlapped(norm_kernel<T, 256, 1, VEC>, t, 256, st, a);
-    else if (chunks <= 512) rc = launch_overlapped(norm_kernel<T, 512, 1, VEC>, t, 512, st, a);
-    else rc = launch_overlapped(norm_kernel<T, 1024, 1, VEC>, t, 1024, st, a);
-  } else if (chunks <= 32) rc = launch_overlapped(norm_kernel<T, 32, 1, VEC>, t4, 128, st, a);
-  else if (chunks <= 64) rc = launch_overlapped(norm_kernel<T, 32, 2, VEC>, t4, 128, st, a);
-  else if (chunks <= 128) rc = launch_overlapped(norm_kernel<T, 32, 4, VEC>, t4, 128, st, a);
-  else if (chunks <= 256) rc = launch_overlapped(norm_kernel<T, 128, 2, VEC>, t, 128, st, a);
-  else if (chunks <= 512) rc = launch_overlapped(norm_kernel<T, 128, 4, VEC>, t, 128, st, a);
-  else if (chunks <= 768) rc = launch_overlapped(norm_kernel<T, 192, 4, VEC>, t, 192, st, a);
-  else if (chunks <= 1024) rc = launch_overlapped(norm_kernel<T, 256, 4, VEC>, t, 256, st, a);
-  else if (chunks <= 2048) rc = launch_overlapped(norm_kernel<T, 512, 4, VEC>, t, 512, st, a);
-  else rc = launch_overlapped(norm_long_kernel<T, VEC>, t, 1024, st, a);
+    if (chunks <= 128) rc = launch_overlapped(norm_kernel<T, 1, 128, false, VEC>, t, 128, st, a);
+    else if (chunks <= 256) rc = launch_overlapped(norm_kernel<T, 1, 256, false, VEC>, t, 256, st, a);
+    else if (chunks <= 512) rc = launch_overlapped(norm_kernel<T, 1, 512, false, VEC>, t, 512, st, a);
+    else rc = launch_overlapped(norm_kernel<T, 1, 1024, false, VEC>, t, 1024, st, a);
+  } else if (chunks <= 32) rc = launch_overlapped(norm_kernel<T, 1, 128, true, VEC>, t4, 128, st, a);
+  else if (chunks <= 64) rc = launch_overlapped(norm_kernel<T, 2, 128, true, VEC>, t4, 128, st, a);
+  else if (chunks <= 128) rc = launch_overlapped(norm_kernel<T, 4, 128, true, VEC>, t4, 128, st, a);
+  else if (chunks <= 2048) {
+    int vpt = chunks <= 256 ? 2 : 4;  // groups of a thread: as many as leave the fewest threads without one
+    auto threads = [&](int v) { return 32 * blocks_of(chunks, 32 * v); };
+    for (int v = 4; v >= 2; --v)
+      if (threads(v) <= 256 && threads(v) * v < threads(vpt) * vpt) vpt = v;
+    const unsigned n = (unsigned)threads(vpt);
+    if (vpt == 2 && n == 128) rc = launch_overlapped(norm_kernel<T, 2, 128, false, VEC>, t, n, st, a);
+    else if (vpt == 2) rc = launch_overlapped(norm_kernel<T, 2, 256, false, VEC, false>, t, n, st, a);
+    else if (vpt == 3) rc = launch_overlapped(norm_kernel<T, 3, 256, false, VEC, false>, t, n, st, a);
+    else if (n == 128) rc = launch_overlapped(norm_kernel<T, 4, 128, false, VEC>, t, n, st, a);
+    else if (n == 192) rc = launch_overlapped(norm_kernel<T, 4, 192, false, VEC>, t, n, st, a);
+    else if (n == 256) rc = launch_overlapped(norm_kernel<T, 4, 256, false, VEC>, t, n, st, a);
+    else if (n < 256) rc = launch_overlapped(norm_kernel<T, 4, 256, false, VEC, false>, t, n, st, a);
+    else if (n == 512) rc = launch_overlapped(norm_kernel<T, 4, 512, false, VEC>, t, n, st, a);
+    else rc = launch_overlapped(norm_kernel<T, 4, 512, false, VEC, false>, t, n, st, a);
+  } else rc = launch_overlapped(norm_long_kernel<T, VEC>, t, 1024, st, a);
   return rc;
 }
 
@@ -171,10 +184,15 @@ struct NormBwdArgs {
   float* partial;  // [gridDim.x][d]
 };
 
+// CTAs of a size that an SM holds: 128 registers a thread of bf16, 170 of fp32
+constexpr int bwd_resident(size_t elem, int threads) {
+  const int n = (elem == 2 ? 512 : 384) / threads;
+  return n > 1 ? n : 1;
+}
 // A CTA walks over the tokens; a thread owns the same features of each of them, so that its share of dw stays in registers until the
 // end and leaves as one row of partial sums.  TPR threads to a token, NT / TPR tokens at a time (one, or one to a warp).
 template <typename T, int TPR, int NT, int VPT, bool VEC>
-__global__ void __launch_bounds__(NT) norm_bwd_kernel(const NormBwdArgs p) {
+__global__ void __launch_bounds__(NT, bwd_resident(sizeof(T), NT)) norm_bwd_kernel(const NormBwdArgs p) {
   grid_started();
   grid_ready();
   using Piece = Warp256<T, VEC>;
@@ -221,7 +239,7 @@ __global__ void __launch_bounds__(NT) norm_bwd_kernel(const NormBwdArgs p) {
       }
     }
     fetch(row + step);  // on its way while this token's sum is taken
-    const float mean = row_sum<TPR>(dot, part[parity]) / (float)p.d;  // two arrays in turn: one barrier a token
+    const float mean = (RPC > 1 ? warp_sum(dot) : cta_sum<TPR, true>(dot, part[parity])) / (float)p.d;  // two arrays in turn: one barrier a token
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       float dx[8], dy[8], xh[8], w[8], dh[8];
@@ -283,7 +301,7 @@ __device__ __forceinline__ void norm_bwd_token(const NormBwdArgs& p, int64_t row
 #pragma unroll
     for (int j = 0; j < 8; ++j) dot += dy[j] * w[j] * (h[j] * rstd);
   }
-  const float mean = row_sum<256>(dot, part) / (float)p.d;
+  const float mean = cta_sum<256, true>(dot, part) / (float)p.d;
   for (int first = (int)(threadIdx.x & ~31u) * 8; first < p.d; first += 2048) {
     Raw8<T> a, b, c, g;
     Piece::load(DY, first, p.d, a), Piece::load(H, first, p.d, b), Piece::load(W, first, p.d, c);
@@ -378,14 +396,24 @@ __global__ void __launch_bounds__(1024) norm_bwd_sum_kernel(const float* partial
 
 constexpr int64_t kBwdLongest = 1024;  // groups of eight of the longest token held in registers
 
+// threads of a CTA that holds a token of more than 64 groups, two groups a thread.  An SM holds as many CTAs of 192 as of 256; three warps
+// are slower than four in bf16 (1536 x 16384: 47 us against 42), not in fp32 (1152 x 4096: 19 against 25).
+int bwd_threads(int64_t chunks, size_t elem) {
+  const int n = 32 * (int)blocks_of(chunks, 64);
+  return n == 96 && elem == 2 ? 128 : n <= 160 ? n : n <= 256 ? 256 : 512;
+}
+// A group a thread for up to 128 groups where there are too few tokens for an SM to hold all the CTAs it could (1003 x 1001 fp32: 8.3 us
+// against 9.7; 896 x 16384 bf16 would take 33 against 28).
+bool bwd_short(int64_t chunks, int64_t t) { return chunks > 64 && chunks <= 128 && t < 12 * (int64_t)sm_count_cached(); }
+
 // rows of partial sums: CTAs of the backward kernel
-int64_t bwd_rows(int64_t d, int64_t t) {
+int64_t bwd_rows(int64_t d, int64_t t, size_t elem) {
   const int64_t chunks = blocks_of(d, 8), sms = sm_count_cached();
   if (chunks > kBwdLongest) {
     const int64_t splits = blocks_of(t, 256);
     return splits < 16 ? splits : 16;
   }
-  const int64_t rows = sms * (chunks <= 128 && chunks > 64 ? 6 : chunks <= 256 ? 4 : 2);
+  const int64_t rows = sms * (bwd_short(chunks, t) ? 6 : bwd_resident(elem, chunks <= 64 ? 256 : bwd_threads(chunks, elem)));
   const int64_t most = blocks_of(t, chunks <= 64 ? 32 : chunks <= 256 ? 2 : 4);  // a few tokens each, as many CTAs as fit at a time
   return rows < most ? rows : most;
 }
@@ -396,7 +424,7 @@ bool bwd_few(int64_t d, int64_t t) { return t <= 384 && t * d <= (int64_t)3 << 1
 
 template <typename T, bool VEC>
 int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
-  const int64_t chunks = blocks_of(a.d, 8), rows = bwd_rows(a.d, a.t);
+  const int64_t chunks = blocks_of(a.d, 8), rows = bwd_rows(a.d, a.t, sizeof(T));
   if (a.t > 0x7fffffffLL) return B2_ERR_VARIANT;
   int rc = B2_OK;
   if (a.t > 0 && (bwd_few(a.d, a.t) || chunks > kBwdLongest)) {
@@ -412,10 +440,15 @@ int norm_bwd_launch(const NormBwdArgs& a, float* dw, cudaStream_t st) {
   if (rows > 0) {
     if (chunks <= 32) rc = launch_overlapped(norm_bwd_kernel<T, 32, 256, 1, VEC>, g, 256, st, a);
     else if (chunks <= 64) rc = launch_overlapped(norm_bwd_kernel<T, 32, 256, 2, VEC>, g, 256, st, a);
-    else if (chunks <= 128) rc = launch_overlapped(norm_bwd_kernel<T, 128, 128, 1, VEC>, g, 128, st, a);
-    else if (chunks <= 256) rc = launch_overlapped(norm_bwd_kernel<T, 128, 128, 2, VEC>, g, 128, st, a);
-    else if (chunks <= 512) rc = launch_overlapped(norm_bwd_kernel<T, 256, 256, 2, VEC>, g, 256, st, a);
-    else rc = launch_overlapped(norm_bwd_kernel<T, 512, 512, 2, VEC>, g, 512, st, a);
+    else if (bwd_short(chunks, a.t)) rc = launch_overlapped(norm_bwd_kernel<T, 128, 128, 1, VEC>, g, 128, st, a);
+    else switch (bwd_threads(chunks, sizeof(T))) {
+      case 64: rc = launch_overlapped(norm_bwd_kernel<T, 64, 64, 2, VEC>, g, 64, st, a); break;
+      case 96: rc = launch_overlapped(norm_bwd_kernel<T, 96, 96, 2, VEC>, g, 96, st, a); break;
+      case 128: rc = launch_overlapped(norm_bwd_kernel<T, 128, 128, 2, VEC>, g, 128, st, a); break;
+      case 160: rc = launch_overlapped(norm_bwd_kernel<T, 160, 160, 2, VEC>, g, 160, st, a); break;
+      case 256: rc = launch_overlapped(norm_bwd_kernel<T, 256, 256, 2, VEC>, g, 256, st, a); break;
+      default: rc = launch_overlapped(norm_bwd_kernel<T, 512, 512, 2, VEC>, g, 512, st, a);
+    }
   }
   return rc ? rc : launch_overlapped(norm_bwd_sum_kernel, (unsigned)blocks_of(a.d, 32), 1024, st, a.partial, rows, (int64_t)a.d, dw);
 }
@@ -457,7 +490,8 @@ extern "C" int b2_rmsnorm_f8(int64_t d, int64_t t, int type, const void* X, int6
 
 extern "C" size_t b2_rmsnorm_backward_workspace_bytes(int64_t d, int64_t t) {
   if (d <= 0 || t <= 0) return 0;
-  return b2::round_up((size_t)b2::bwd_rows(d, t) * (size_t)d * sizeof(float), 256);
+  const int64_t a = b2::bwd_rows(d, t, 2), b = b2::bwd_rows(d, t, 4);
+  return b2::round_up((size_t)(a > b ? a : b) * (size_t)d * sizeof(float), 256);
 }
 
 extern "C" int b2_rmsnorm_backward(int64_t d, int64_t t, int type, const void* DY, int64_t lddy, const void* H, int64_t ldh,
