@@ -206,10 +206,8 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
           constexpr int CW = TBN >= 32 ? TBN / 32 : 1;
           uint32_t next[4 + CW];
           auto fetch = [&](int kb) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) next[i] = scale_word(p.sr, r0 + 32 * i, p.out.rows, kb, p.kb);
-#pragma unroll
-            for (int i = 0; i < CW; ++i) next[4 + i] = scale_word(p.sc, c0 + 32 * i, p.out.cols, kb, p.kb);
+            scale_words<4>(p.sr, r0, p.out.rows, kb, p.kb, next);
+            scale_words<CW>(p.sc, c0, p.out.cols, kb, p.kb, next + 4);
           };
           fetch(kb0 & ~3);
           for (int kb = kb0 & ~3; kb < kb1; kb += 4, slot.next()) {
@@ -328,16 +326,31 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
 }
 
 // ---- operands whose columns are not 16-byte aligned are copied into columns that are --------------------
-__global__ void __launch_bounds__(256) f8_repitch_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, uint8_t* dst, int64_t ldd) {
+__global__ void __launch_bounds__(256) f8_repitch_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, uint8_t* dst, int64_t ldd, const FastDiv per) {
   grid_started();
   grid_ready();
-  const int64_t per = ldd / 16;
-  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < per * cols; i += (int64_t)gridDim.x * 256) {
-    const int64_t c = i / per, r = (i - c * per) * 16;
+  const int64_t total = (int64_t)per.d * cols;
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t c = total <= 0x7fffffffLL ? (int64_t)div_by((uint32_t)i, per) : i / per.d, r = (i - c * per.d) * 16, n = rows - r;
+    const uint8_t* s = src + c * ld + r;
     uint32_t w[4] = {0, 0, 0, 0};
+    if ((r > 0 || c > 0) && (n >= 20 || (c + 1 < cols && ld >= 32))) {  // up to 3 bytes before and 19 after lie within the matrix
+      const uint32_t* a = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(s) & ~(uintptr_t)3);
+      const int shift = (int)(reinterpret_cast<uintptr_t>(s) & 3) * 8;
+      uint32_t v[5];
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (r + j < rows) w[j >> 2] |= (uint32_t)src[c * ld + r + j] << (8 * (j & 3));
+      for (int j = 0; j < 5; ++j) v[j] = a[j];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[j] = __funnelshift_r(v[j], v[j + 1], shift);
+        const int64_t left = n - 4 * j;
+        if (left < 4) w[j] = left > 0 ? w[j] & (0xffffffffu >> (32 - 8 * (int)left)) : 0u;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (j < n) w[j >> 2] |= (uint32_t)s[j] << (8 * (j & 3));
+    }
     *reinterpret_cast<uint4*>(dst + c * ldd + r) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
@@ -456,20 +469,22 @@ F8Pack f8_pack_plan(bool an, bool bn, int64_t m, int64_t n, int64_t k, const voi
 
 }  // namespace
 
-// What the product takes, in clocks: turns of CTAs over the SMs, and adding the shares, half as long again for every doubling.
+// What the product takes, in clocks: turns of CTAs over the SMs, and adding the shares, half as long again for every doubling.  CTAs of a
+// cluster are not persistent: each further turn begins anew, 3000 clocks to its first product, and joins at its end.
 // Measured with clusters that do not fit at once: weight gradient of 512 x 512 over 4096 tokens 20.1 us with 16 clusters of eight, 13.8 with four.
 F8Split f8_split_for(int64_t tiles, int stages, double stage, double join, int resident) {
   F8Split best{1, 0.0};
   for (int s = 1, log = 0; s <= kMaxSplit && (s == 1 || stages / s >= 2); s *= 2, ++log) {
-    const int64_t slots = (int64_t)f8_cluster_slots(log) * resident;
-    const double clocks = (double)blocks_of(tiles * s, slots) * resident * (double)blocks_of(stages, s) * stage + (s > 1 ? join * (0.7 + 0.3 * log) : 0.0);
+    const double turns = (double)blocks_of(tiles * s, (int64_t)f8_cluster_slots(log) * resident), work = (double)resident * (double)blocks_of(stages, s) * stage;
+    const double clocks = s == 1 ? turns * work : turns * (work + join * (0.7 + 0.3 * log)) + (turns - 1.0) * 3000.0;
     if (s == 1 || clocks < best.clocks) best = {s, clocks};
   }
   return best;
 }
 
 int f8_repitch(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd, cudaStream_t st) {
-  return launch_overlapped(f8_repitch_kernel, grid_for(ldd / 16 * cols), 256, st, static_cast<const uint8_t*>(src), ld, rows, cols, static_cast<uint8_t*>(dst), ldd);
+  return launch_overlapped(f8_repitch_kernel, grid_for(ldd / 16 * cols), 256, st, static_cast<const uint8_t*>(src), ld, rows, cols, static_cast<uint8_t*>(dst), ldd,
+                           fast_div((uint32_t)(ldd / 16)));
 }
 int f8_scale_c(int64_t m, int64_t n, float beta, void* C, int64_t ldc, int type_c, cudaStream_t st) {
   if (beta == 1.0f) return B2_OK;
@@ -538,8 +553,12 @@ extern "C" int b2_gemm_f8(char transa, char transb, int64_t m, int64_t n, int64_
   a.out.vec = columns_aligned(C, ldc, type_c == B2_TYPE_BF16 ? 2 : 4, 16);
   a.status = status_pointer();
   if (!a.status) return B2_ERR_LAUNCH;
-  const F8Operand oa{A, m, lda, an, {SA, an ? 1 : ldsa, an ? ldsa : 1, block_a == 1 ? 0 : 7, scale_type_a == B2_SCALE_F32}};
-  const F8Operand ob{B, n, ldb, !bn, {SB, bn ? ldsb : 1, bn ? 1 : ldsb, block_b == 1 ? 0 : 7, scale_type_b == B2_SCALE_F32}};
+  auto scale = [](const void* s, bool blocks_contiguous, int64_t ld, int block, int type) {
+    return F8Scale{s, blocks_contiguous ? ld : 1, blocks_contiguous ? 1 : ld, block == 1 ? 0 : 7, type == B2_SCALE_F32,
+                   type == B2_SCALE_E8M0 && blocks_contiguous && columns_aligned(s, ld, 1, 4)};
+  };
+  const F8Operand oa{A, m, lda, an, scale(SA, !an, ldsa, block_a, scale_type_a)};
+  const F8Operand ob{B, n, ldb, !bn, scale(SB, bn, ldsb, block_b, scale_type_b)};
   const bool mx = scale_type_a == B2_SCALE_E8M0 && scale_type_b == B2_SCALE_E8M0;
   if (type_c == B2_TYPE_BF16) return mx ? f8_choose<__nv_bfloat16, true>(a, oa, ob, k, st) : f8_choose<__nv_bfloat16, false>(a, oa, ob, k, st);
   return mx ? f8_choose<float, true>(a, oa, ob, k, st) : f8_choose<float, false>(a, oa, ob, k, st);

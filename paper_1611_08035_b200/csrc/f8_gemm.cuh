@@ -19,6 +19,7 @@ struct F8Scale {  // value for index i and block b: p[(i >> shift) * si + b * sb
   const void* p;
   int64_t si, sb;
   int shift, f32;
+  int words;  // bytes, four consecutive blocks at a time in aligned words
 };
 struct F8Args {
   F8Out out;
@@ -67,16 +68,27 @@ __device__ __forceinline__ uint32_t umma_idesc_mx(int m, int n, int a_mn, int b_
          ((uint32_t)(m >> 7) << 27) | ((uint32_t)byte << 29);
 }
 
-// Scale bytes of index i (clamped to the last one) for blocks b .. b+3, the first in the lowest byte; blocks beyond the
-// last are never multiplied with.
-__device__ __forceinline__ uint32_t scale_word(const F8Scale& s, int64_t i, int64_t extent, int b, int kb) {
-  const uint8_t* p = static_cast<const uint8_t*>(s.p) + ((i < extent ? i : extent - 1) >> s.shift) * s.si + (int64_t)b * s.sb;
-  if (s.sb == 1 && b + 4 <= kb && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return *reinterpret_cast<const uint32_t*>(p);
-  uint32_t w = 0;
+// Scale bytes of the indices i, i + 32, .. (clamped to the last one) for blocks b .. b+3, b a multiple of four, the first in the lowest
+// byte; blocks beyond the last are never multiplied with.  All loads come before the first use: joined one word after the other, the bytes of
+// 38 blocks kept a 512 x 512 product 10.6 us where 32 blocks, read in words, took 7.8.
+template <int N>
+__device__ __forceinline__ void scale_words(const F8Scale& s, int64_t i, int64_t extent, int b, int kb, uint32_t* w) {
+  const uint8_t* p[N];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (b + j < kb) w |= (uint32_t)p[j * s.sb] << (8 * j);
-  return w;
+  for (int n = 0; n < N; ++n)
+    p[n] = static_cast<const uint8_t*>(s.p) + ((i + 32 * n < extent ? i + 32 * n : extent - 1) >> s.shift) * s.si + (int64_t)b * s.sb;
+  if (s.words && b + 4 <= kb) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) w[n] = *reinterpret_cast<const uint32_t*>(p[n]);
+  } else {
+    uint32_t v[N][4];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[n][j] = b + j < kb ? p[n][j * s.sb] : 0u;
+#pragma unroll
+    for (int n = 0; n < N; ++n) w[n] = v[n][0] | v[n][1] << 8 | v[n][2] << 16 | v[n][3] << 24;
+  }
 }
 
 // Launch of a persistent kernel on pairs of CTAs with 256 x 256 tiles.

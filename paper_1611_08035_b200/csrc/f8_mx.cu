@@ -194,9 +194,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       // these warps spend their time on (all of them fetching all: 8192^3 514 us).
       uint32_t next[3];
       auto fetch = [&](int kb) {
-        next[0] = scale_word(p.sr, r0 + 32 * quad, p.out.rows, kb, p.kb);
-        next[1] = scale_word(p.sc, c0 + 64 * quad, p.out.cols, kb, p.kb);
-        next[2] = scale_word(p.sc, c0 + 64 * quad + 32, p.out.cols, kb, p.kb);
+        scale_words<1>(p.sr, r0 + 32 * quad, p.out.rows, kb, p.kb, next);
+        scale_words<2>(p.sc, c0 + 64 * quad, p.out.cols, kb, p.kb, next + 1);
       };
       fetch(0);
       for (int kb = 0; kb < p.kb; kb += 4, ++grp) {
