@@ -451,3 +451,47 @@ def test_call_forms(b2):
     assert e.value.status == 1003
     with pytest.raises(TypeError):
         b2.b2_wgrad_f8(128, 4, 4, 1.0, q, 128, s, 1, x, 128, 0.0, C, 128)
+
+
+WIDTHS = [264, 520, 776, 1100, 1152, 1536, 2080, 2560, 2561, 3184, 5120, 6272, 7176, 9000, 10240]
+
+
+@pytest.mark.parametrize("dt,res", [(BF, True), (F32, False)])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_norm_of_every_width(b2, d, dt, res):
+    """More tokens than one for each CTA, by every number of warps that a token can take."""
+    test_norm(b2, d, 320, 0, dt, res)
+    test_norm_backward(b2, d, 2 * 1024 * 1024 // d + 400, 0, dt, res)
+
+
+@pytest.mark.parametrize("d,t", [(520, 1700), (896, 2300), (1001, 2300)])
+def test_norm_backward_of_many_short_tokens(b2, d, t):
+    test_norm_backward(b2, d, t, 0, BF, True)
+    test_norm_backward(b2, d, t, 0, F32, False)
+
+
+@pytest.mark.parametrize("scale", ["e8m0", "f32"])
+@pytest.mark.parametrize("out", [BF, F32])
+@pytest.mark.parametrize("m,pad", [(2304, 0), (2302, 2), (2301, 3), (2303, 0)])
+def test_gemm_adds_to_large_results(b2, m, pad, out, scale):
+    """Tiles on pairs of CTAs added to C in whole 16-byte pieces, in parts of one, and one by one."""
+    run_gemm(b2, "T", "N", m, 2176, 300, scale=(scale, scale), out=out, alpha=1.5, beta=-0.5, pad=(0, 0, pad), seed=4)
+
+
+@pytest.mark.parametrize("m,n", [(200, 300), (300, 20), (2304, 2176)])
+@pytest.mark.parametrize("k", [384, 500, 890, 1400])
+def test_gemm_scales_in_words_and_bytes(b2, m, n, k):
+    run_gemm(b2, "T", "N", m, n, k, seed=5)
+    run_gemm(b2, "T", "N", m, n, k, ba=1, seed=6)
+
+
+@pytest.mark.parametrize("k", [1, 2, 3, 15, 17, 19, 20, 31, 33, 47])
+def test_gemm_of_short_odd_columns(b2, k):
+    run_gemm(b2, "T", "N", 40, 70, k, pad=(0, 1, 0), offset=(3, 0), out=F32, integers=True, exponents=(-1, 2), exact=True)
+    run_gemm(b2, "N", "T", k, k + 1, 140, pad=(1, 0, 0), offset=(0, 7), out=F32, integers=True, exponents=(-1, 2), exact=True)
+
+
+@pytest.mark.parametrize("out,beta", [(BF, 2.0), (F32, 0.0), (F32, 1.0)])
+@pytest.mark.parametrize("m,n,k", [(2304, 1536, 200), (2301, 1533, 130), (384, 1536, 1344), (288, 648, 6512), (640, 640, 2048)])
+def test_wgrad_of_every_split(b2, m, n, k, out, beta):
+    test_wgrad(b2, m, n, k, out, 0.5, beta)
