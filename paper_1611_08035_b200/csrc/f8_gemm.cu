@@ -326,9 +326,15 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
 }
 
 // ---- operands whose columns are not 16-byte aligned are copied into columns that are --------------------
-__global__ void __launch_bounds__(256) f8_repitch_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, uint8_t* dst, int64_t ldd, const FastDiv per) {
+// Both operands' in one launch: CTAs (., y) copy operand y.
+__global__ void __launch_bounds__(256) f8_repitch_kernel(const F8Copy first, const F8Copy second, const FastDiv per_first, const FastDiv per_second) {
   grid_started();
   grid_ready();
+  const F8Copy& p = blockIdx.y ? second : first;
+  const FastDiv per = blockIdx.y ? per_second : per_first;
+  const uint8_t* src = static_cast<const uint8_t*>(p.src);
+  uint8_t* dst = static_cast<uint8_t*>(p.dst);
+  const int64_t ld = p.ld, rows = p.rows, cols = p.cols, ldd = p.ldd;
   const int64_t total = (int64_t)per.d * cols;
   for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t c = total <= 0x7fffffffLL ? (int64_t)div_by((uint32_t)i, per) : i / per.d, r = (i - c * per.d) * 16, n = rows - r;
@@ -482,9 +488,10 @@ F8Split f8_split_for(int64_t tiles, int stages, double stage, double join, int r
   return best;
 }
 
-int f8_repitch(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t ldd, cudaStream_t st) {
-  return launch_overlapped(f8_repitch_kernel, grid_for(ldd / 16 * cols), 256, st, static_cast<const uint8_t*>(src), ld, rows, cols, static_cast<uint8_t*>(dst), ldd,
-                           fast_div((uint32_t)(ldd / 16)));
+int f8_repitch(const F8Copy* copies, int count, cudaStream_t st) {
+  const F8Copy &a = copies[0], &b = copies[count - 1];
+  const int64_t most = a.ldd / 16 * a.cols > b.ldd / 16 * b.cols ? a.ldd / 16 * a.cols : b.ldd / 16 * b.cols;
+  return launch_overlapped(f8_repitch_kernel, dim3(grid_for(most), (unsigned)count), 256, st, a, b, fast_div((uint32_t)(a.ldd / 16)), fast_div((uint32_t)(b.ldd / 16)));
 }
 int f8_scale_c(int64_t m, int64_t n, float beta, void* C, int64_t ldc, int type_c, cudaStream_t st) {
   if (beta == 1.0f) return B2_OK;
@@ -536,16 +543,20 @@ extern "C" int b2_gemm_f8(char transa, char transb, int64_t m, int64_t n, int64_
   if (m > kMost || n > kMost || k > kMost) return B2_ERR_VARIANT;
   const F8Pack pk = f8_pack_plan(an, bn, m, n, k, A, lda, B, ldb);
   if (pk.total && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < pk.total)) return B2_ERR_WORKSPACE;
+  F8Copy copies[2];
+  int count = 0;
   if (pk.a) {
-    const int rc = f8_repitch(A, lda, an ? m : k, an ? k : m, workspace, pk.lda, st);
-    if (rc) return rc;
+    copies[count++] = {A, lda, an ? m : k, an ? k : m, workspace, pk.lda};
     A = workspace, lda = pk.lda;
   }
   if (pk.b) {
     void* to = static_cast<char*>(workspace) + pk.off_b;
-    const int rc = f8_repitch(B, ldb, bn ? k : n, bn ? n : k, to, pk.ldb, st);
-    if (rc) return rc;
+    copies[count++] = {B, ldb, bn ? k : n, bn ? n : k, to, pk.ldb};
     B = to, ldb = pk.ldb;
+  }
+  if (count) {
+    const int rc = f8_repitch(copies, count, st);
+    if (rc) return rc;
   }
   F8Args a = {};
   a.kb = (int)blocks_of(k, kF8Block);

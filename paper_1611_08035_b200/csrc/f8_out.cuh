@@ -287,8 +287,14 @@ __device__ __forceinline__ void f8_split_join(const F8Out& p, void* tile, int sp
   f8_join_end();
 }
 
-// C := beta * C, and copies of operands into 16-byte aligned columns (ldd a multiple of 16 bytes); defined in f8_gemm.cu.
+// C := beta * C, and copies of one or two operands into 16-byte aligned columns (ldd a multiple of 16 bytes); defined in f8_gemm.cu.
 int f8_scale_c(int64_t m, int64_t n, float beta, void* C, int64_t ldc, int type_c, cudaStream_t st);
-int f8_repitch(const void* src, int64_t ld_bytes, int64_t row_bytes, int64_t cols, void* dst, int64_t ldd_bytes, cudaStream_t st);
+struct F8Copy {
+  const void* src;
+  int64_t ld, rows, cols;  // bytes
+  void* dst;
+  int64_t ldd;
+};
+int f8_repitch(const F8Copy* copies, int count, cudaStream_t st);
 
 }  // namespace b2

@@ -470,16 +470,20 @@ extern "C" int b2_wgrad_f8(int64_t m, int64_t n, int64_t k, float alpha, const v
   if (m > kMost || n > kMost || k > kMost) return B2_ERR_VARIANT;
   const WgPack pk = wg_pack_plan(m, n, k, Q, ldq, Y, ldy);
   if (pk.total && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < pk.total)) return B2_ERR_WORKSPACE;
+  F8Copy copies[2];
+  int count = 0;
   if (pk.q) {
-    const int rc = f8_repitch(Q, ldq, m, k, workspace, pk.ldq, st);
-    if (rc) return rc;
+    copies[count++] = {Q, ldq, m, k, workspace, pk.ldq};
     Q = workspace, ldq = pk.ldq;
   }
   if (pk.y) {
     void* to = static_cast<char*>(workspace) + pk.off_y;
-    const int rc = f8_repitch(Y, ldy * 2, n * 2, k, to, pk.ldy * 2, st);
-    if (rc) return rc;
+    copies[count++] = {Y, ldy * 2, n * 2, k, to, pk.ldy * 2};
     Y = to, ldy = pk.ldy;
+  }
+  if (count) {
+    const int rc = f8_repitch(copies, count, st);
+    if (rc) return rc;
   }
   WgArgs a = {};
   a.out.rows = m, a.out.cols = n, a.out.alpha = alpha, a.out.beta = beta, a.out.C = C, a.out.ldc = ldc;
