@@ -261,6 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+      f8_prefetch<TC>(p.out, true, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, 32, (int64_t)tc * kBN + half * kCols, kCols);
 #pragma unroll
       for (int j = 0; j < kCols / 2; ++j) acc2[j] = 0;
       for (int kb = 0; kb < p.kb; ++kb, ++ch) {

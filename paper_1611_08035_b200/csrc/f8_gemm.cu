@@ -15,7 +15,7 @@
 // lines.  For few columns (decoding: n <= 64) A gives the 128 rows and the tile is as narrow as n.  The k range may be split
 // over a cluster, whose CTAs add their shares through distributed shared memory.
 //
-// What bounds it: latencies.  1024^3 takes 6.4 us, of which the first operands take 2 and the results 1; adding shares of 128 x 128
+// What bounds it: latencies.  1024^3 takes 5.9 us, of which the first operands take 2 and the results 1; adding shares of 128 x 128
 // tiles takes 2 us (distributed shared memory delivers 14 bytes a clock), which is why narrow tiles come before splits.  Decoding
 // (8192 x 8 x 8192) takes 15.2 us for 64 MB of weights, 4.4 TB/s; the weights alone would take 10.3.
 #include <cuda.h>

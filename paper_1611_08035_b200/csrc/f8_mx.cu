@@ -233,6 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+      if constexpr (CHUNK == 0) f8_prefetch<TC>(p.out, true, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, 32, (int64_t)tc * kBN + half * kCols, kCols);
       if constexpr (CHUNK > 0) {
 #pragma unroll
         for (int j = 0; j < kCols; ++j) acc[j] = 0.0f;

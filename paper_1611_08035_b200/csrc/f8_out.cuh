@@ -32,6 +32,21 @@ __device__ __forceinline__ void f8_store4(__nv_bfloat16* p, const float v[4]) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
 }
 
+// Old values of `lines` runs of C on their way to L2 while the tile is computed: run i starts at element (outer + i) of the index that is not
+// contiguous in C and `first` of the one that is, and has `count` elements.  A warp's lanes share the runs.
+// 8192 x 8192 with beta: product over 256, fp32 scales, bf16 121 -> 108 us, fp32 161 -> 123, e8m0 bf16 104 -> 94; weight gradient over 4096 tokens
+// bf16 606 -> 484.  Not used by the e8m0 product in fp32, whose registers it takes from results without beta (78 -> 80.5 us), nor by
+// the weight gradient in fp32 (210 -> 237 over 256 tokens: its old values are then asked for too early).
+template <typename TC>
+__device__ __forceinline__ void f8_prefetch(const F8Out& p, bool cols_contiguous, int64_t outer, int lines, int64_t first, int count) {
+  if (p.beta == 0.0f) return;
+  const int64_t outers = cols_contiguous ? p.rows : p.cols, inners = cols_contiguous ? p.cols : p.rows;
+  for (int i = threadIdx.x & 31; i < lines; i += 32)
+    for (int e = 0; e < count; e += 128 / (int)sizeof(TC))
+      if (outer + i < outers && first + e < inners)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const TC*>(p.C) + (outer + i) * p.ldc + first + e));
+}
+
 // N accumulators of one row of a tile whose rows are contiguous in C (C[col * ldc + row]): neighbouring lanes, neighbouring rows.
 // Straight code with one test of beta: with one at every column a tile's 64 columns a warp took 4 us (a gradient of 4096 x 4096 over
 // 64 tokens 36 us, now 21).
@@ -175,7 +190,7 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
 // Joining the shares of a k split: the CTAs of a cluster (rank = share) have each put their sums of the same 128 x TBN tile
 // into their shared memory (f8_put_share), the index that is contiguous in C contiguous there too; each CTA adds all shares, in the
 // order of their rank, for its part of the other index, four numbers at a time and all ranks' numbers on their way at once
-// (one after the other, their latency made up most of a 1024^3 product: 21 us, now 6.4).  All threads of all CTAs of the cluster call this; the
+// (one after the other, their latency made up most of a 1024^3 product: 21 us, now 5.9).  All threads of all CTAs of the cluster call this; the
 // 32 EW threads with worker >= 0 (numbered) add and write.  PERMUTE: row r of the tile is row kept_row(r) of C.
 constexpr int kMaxSplit = 8;  // 2, 4 or 8 CTAs
 struct F8Split {

@@ -189,6 +189,7 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
       for (int tile = first; tile < tiles && ok; tile += stride) {
         int tr, tc;
         tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
+        if (sizeof(TC) == 2 && warp == 3) f8_prefetch<TC>(p.out, false, (int64_t)tc * TBN, TBN, (int64_t)(tr * CTAS + (int)rank) * kRows, kRows);
         const int x = warp == 0 ? (tr * CTAS + (int)rank) * kRows : tc * TBN + (int)rank * 128 + (warp - 2) * 64;
         for (int kb = kb0; kb < kb1; ++kb, pos.next()) {
           const int s = pos.s;
