@@ -466,7 +466,8 @@ int b2_quant_f8(int64_t d, int64_t t, int block, int type, const void* X, int64_
  *     C := alpha * sum_p op(A)_ip sA(i/block_a, p/128) * op(B)_pj sB(j/block_b, p/128) + beta * C
  * op(A) is m x k, op(B) k x n; block_a, block_b in {1, 128}; C in bf16 or fp32.  The scales are stored the way their
  * operand is: for transa 'T' (A stored k x m) SA is ceil(k/128) x ceil(m/block_a), for 'N' ceil(m/block_a) x ceil(k/128);
- * for transb 'N' SB is ceil(k/128) x ceil(n/block_b), for 'T' ceil(n/block_b) x ceil(k/128).  Accumulation in fp32.
+ * for transb 'N' SB is ceil(k/128) x ceil(n/block_b), for 'T' ceil(n/block_b) x ceil(k/128).  Accumulation in fp32; the
+ * tensor core, whose additions truncate, sums over at most 2048 (C in fp32) or 65536 (bf16) of k, its sums are added rounding to nearest.
  * A linear layer y = W x with W stored row by row (k contiguous) is ('T','N'), its input gradient W^T dy is ('N','N') on
  * the same weight and the same scales.
  * An operand whose base is not 16-byte aligned or whose leading dimension is not a multiple of 16 is first copied to

@@ -9,7 +9,8 @@
 //
 // Roles of a CTA: warp 0 streams both operands with TMA (128-byte swizzle) into the ring, warp 1 issues tcgen05.mma, the other
 // warps bring the scales and read the sums.  With e8m0 scales the tensor core applies them and the sums stay in tensor memory for
-// the whole tile; otherwise every block's sums are read (two buffers in turn) and added, times the scales, to fp32 accumulators.
+// as many blocks as chunk_blocks allows; otherwise every block's sums are read (two buffers in turn) and added, times the scales, to fp32
+// accumulators.  A second buffer for the chunks' sums would spare the pause of 0.3 us at each (1408 x 1408 x 8192 fp32 27.0 us, 25.5 in one chunk).
 //
 // The matrix whose index is contiguous in C (A, index i) is the MMA's column operand (tiles 128 x 128 or 128 x 64): results leave in whole
 // lines.  For few columns (decoding: n <= 64) A gives the 128 rows and the tile is as narrow as n.  The k range may be split
@@ -28,7 +29,7 @@
 namespace b2 {
 namespace {
 
-// MX: both scales are e8m0 and the tensor core applies them (f8_mx.cu describes how): the sums of a tile stay in tensor
+// MX: both scales are e8m0 and the tensor core applies them (f8_mx.cu describes how): the sums of a chunk stay in tensor
 // memory, behind them the scales of sixteen blocks.  Otherwise every block's sums are scaled and added in registers.
 template <int TBN, bool MX>
 struct F8Cfg {
@@ -65,10 +66,10 @@ __device__ __forceinline__ void umma_mx1(uint32_t tmem_d, uint64_t desc_a, uint6
 }
 
 template <int TBN, typename TC, bool COLS_CONTIG, bool MX>
-__global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
+__global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, MX && TBN <= 64 ? 2 : 1)
     f8_gemm_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   using Cfg = F8Cfg<TBN, MX>;
-  constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES;
+  constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES, CHUNK = chunk_blocks<TC>();
   extern __shared__ unsigned char f8_smem_raw[];
   const uint32_t raw = smem_u32(f8_smem_raw);
   unsigned char* ring = f8_smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -152,7 +153,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
     for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
       for (int kb = kb0; kb < kb1; ++kb, pos.next()) {
         const int s = pos.s, b = MX ? 0 : ch & 1, byte = kb & 3;
-        const bool first = !MX || kb == kb0, end = !MX || kb == kb1 - 1;
+        const bool first = !MX || kb == kb0 || kb % CHUNK == 0, end = !MX || kb == kb1 - 1 || kb % CHUNK == CHUNK - 1;
         const uint32_t behind = MX ? 1 : 2, round = (uint32_t)(MX ? ch : ch >> 1);
         if ((first && ch >= (int)behind && !mbar_wait_warp(&tempty[b], (round - 1) & 1)) ||
             (MX && (byte == 0 || kb == kb0) && !mbar_wait_warp(&sf_full[slot.s], slot.phase)) ||
@@ -201,51 +202,72 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, 1)
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
       const int64_t row = (int64_t)tr * kRows + quad * 32 + lane, col0 = (int64_t)tc * TBN + half * COLS;
       if constexpr (MX) {
-        if (half == 0) {  // four warps, one for each quarter of the lanes, bring the scales
-          const int64_t r0 = (int64_t)tr * kRows + lane, c0 = (int64_t)tc * TBN + lane;
-          constexpr int CW = TBN >= 32 ? TBN / 32 : 1;
-          uint32_t next[4 + CW];
-          auto fetch = [&](int kb) {
-            scale_words<4>(p.sr, r0, p.out.rows, kb, p.kb, next);
-            scale_words<CW>(p.sc, c0, p.out.cols, kb, p.kb, next + 4);
-          };
-          fetch(kb0 & ~3);
-          for (int kb = kb0 & ~3; kb < kb1; kb += 4, slot.next()) {
-            uint32_t w[8] = {};
+        const int64_t r0 = (int64_t)tr * kRows + lane, c0 = (int64_t)tc * TBN + lane;
+        constexpr int CW = TBN >= 32 ? TBN / 32 : 1;
+        uint32_t next[4 + CW];
+        auto fetch = [&](int kb) {
+          scale_words<4>(p.sr, r0, p.out.rows, kb, p.kb, next);
+          scale_words<CW>(p.sc, c0, p.out.cols, kb, p.kb, next + 4);
+        };
+        auto bring = [&](int kb) {  // the scales of four blocks to tensor memory
+          uint32_t w[8] = {};
 #pragma unroll
-            for (int i = 0; i < 4 + CW; ++i) w[i] = next[i];
-            if (kb + 4 < kb1) fetch(kb + 4);
-            if (groups < Cfg::SLOTS) {
-              ++groups;
-            } else if (!mbar_wait_warp(&sf_empty[slot.s], slot.phase ^ 1u)) {
-              ok = false;
-              break;
-            }
-            tc_fence_after();
-            const uint32_t sf = tmem + ((uint32_t)(quad * 32) << 16) + TBN + slot.s * Cfg::SF_COLS;
-            tmem_st4(sf, w[0], w[1], w[2], w[3]);
-            tmem_st4(sf + 4, w[4], w[5], w[6], w[7]);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sf_full[slot.s]);
+          for (int i = 0; i < 4 + CW; ++i) w[i] = next[i];
+          if (kb + 4 < kb1) fetch(kb + 4);
+          if (groups < Cfg::SLOTS) {
+            ++groups;
+          } else if (!mbar_wait_warp(&sf_empty[slot.s], slot.phase ^ 1u)) {
+            return ok = false;
           }
-        }
-        if (ok && !mbar_wait_warp(&tfull[0], (uint32_t)(ch & 1), kWaitLimitNs + (uint64_t)p.kb * 8192ull)) ok = false;
-        ++ch;
-        tc_fence_after();
-        if (ok) {
+          tc_fence_after();
+          const uint32_t sf = tmem + ((uint32_t)(quad * 32) << 16) + TBN + slot.s * Cfg::SF_COLS;
+          tmem_st4(sf, w[0], w[1], w[2], w[3]);
+          tmem_st4(sf + 4, w[4], w[5], w[6], w[7]);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sf_full[slot.s]);
+          slot.next();
+          return true;
+        };
+        auto sums = [&](auto take) {  // of one chunk, once its last product is there
+          if (!mbar_wait_warp(&tfull[0], (uint32_t)(ch & 1), kWaitLimitNs + (uint64_t)p.kb * 8192ull)) return ok = false;
+          ++ch;
+          tc_fence_after();
 #pragma unroll
-          for (int c0 = 0; c0 < COLS; c0 += 16) {
+          for (int j0 = 0; j0 < COLS; j0 += 16) {
             uint32_t v[16];
-            tmem_ld16_issue(taddr + (uint32_t)c0, v);
+            tmem_ld16_issue(taddr + (uint32_t)j0, v);
             tmem_ld_wait16(v);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[c0 + j] = __uint_as_float(v[j]);
+            for (int j = 0; j < 16; ++j) take(acc[j0 + j], __uint_as_float(v[j]));
           }
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&tempty[0]);
+          return true;
+        };
+        // Four warps (half 0), one for each quarter of the lanes, bring the scales; all read the sums.
+        const bool brings = half == 0;
+        if (brings) fetch(kb0 & ~3);
+        if (kb0 / CHUNK == (kb1 - 1) / CHUNK) {
+          for (int kb = kb0 & ~3; brings && kb < kb1; kb += 4)
+            if (!bring(kb)) break;
+          if (ok) sums([](float& s, float v) { s = v; });
+        } else {
+#pragma unroll
+          for (int j = 0; j < COLS; ++j) acc[j] = 0.0f;
+          // The slot for the scales of block kb is the one of 4 SLOTS blocks ago.  If those began a chunk, their products wait for the sums
+          // of the chunk before to be read, by these warps among others: that comes first.
+          int left = (kb1 - 1) / CHUNK - kb0 / CHUNK + 1;
+          for (int kb = brings ? kb0 & ~3 : kb1; left > 0; kb += 4) {
+            const int behind = kb - 4 * Cfg::SLOTS;
+            if (kb >= kb1 || (behind > kb0 && behind % CHUNK == 0)) {
+              if (!sums([](float& s, float v) { s += v; })) break;
+              --left;
+            }
+            if (kb < kb1 && !bring(kb)) break;
+          }
         }
       } else {
         float* scw = reinterpret_cast<float*>(scratch + ew * Cfg::SCRATCH);

@@ -43,6 +43,13 @@ struct F8Operand {
   F8Scale s;
 };
 
+// Blocks whose products are summed in tensor memory before the sum moves to fp32 registers.  The tensor core's additions truncate, so
+// that a sum which grows for long comes out too small: fp32 results over k = 262144, eight shares of 32768, were 1.8e-5 off (all terms of one sign,
+// mean), 32000 x 8 over 65536 without a split 5.9e-5; moved every 2048 the mean is 1e-6 and does not grow.  bf16, whose rounding is 2e-3, sees
+// sums over 65536 (6e-5), and without a limit 1.4e-3 at k = 4194304.
+template <typename TC>
+__host__ __device__ constexpr int chunk_blocks() { return sizeof(TC) == 4 ? 16 : 512; }
+
 // Matrix of bytes, `inner` contiguous; boxes of box_inner (128 or 64) bytes by box_outer, swizzled over their width.
 inline bool f8_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int box_outer, int box_inner = 128) {
   EncodeFn enc = tensor_map_encode_fn();

@@ -4,8 +4,8 @@
 //
 // A pair owns a 256 x 256 tile of C: each CTA fetches its 128 rows of the row operand and its 128 columns of the
 // column operand, so that shared memory is written and read 32 KB per block and SM where a CTA alone would need 48 for the same
-// multiply-adds; the leader's tensor core instruction reads both halves.  The sums stay in tensor memory (256 columns) for the
-// whole tile; 48 more columns hold the scales of sixteen blocks.
+// multiply-adds; the leader's tensor core instruction reads both halves.  The sums of a chunk of blocks stay in tensor
+// memory (256 columns); 48 more columns hold the scales of sixteen blocks.
 //
 // What bounds it: power.  8192^3 takes 383 us in a burst and 440 us on and on (2.5 PFLOP/s), a block 581 clocks where the tensor pipe
 // needs 512, at 1.3 GHz under the board's power limit; without the limit (4096^3, one turn of four not full) 55 us.  Steps on the
@@ -45,8 +45,7 @@ __device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64
       ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
       : "memory");
 }
-// CHUNK: blocks whose products are summed in tensor memory, whose additions truncate, before they are added to fp32
-// registers; 0: all of them.  A bf16 result does not see the difference.
+// CHUNK: chunk_blocks, or 0 where all blocks fit one chunk: then the accumulators are read once and no register holds them before.
 template <typename TC, int CHUNK>
 __global__ void __launch_bounds__(kThreads, 1)
     f8_mx_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
@@ -289,7 +288,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <typename TC>
 int f8_mx_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
   static std::atomic<bool> configured[64];
-  return f8_pair_launch(f8_mx_kernel<TC, sizeof(TC) == 4 ? 16 : 0>, configured, kThreads, kSmem, a, r, c, k, st);
+  constexpr int CHUNK = chunk_blocks<TC>();
+  if constexpr (sizeof(TC) == 2) {
+    static std::atomic<bool> configured_whole[64];
+    if (a.kb <= CHUNK) return f8_pair_launch(f8_mx_kernel<TC, 0>, configured_whole, kThreads, kSmem, a, r, c, k, st);
+  }
+  return f8_pair_launch(f8_mx_kernel<TC, CHUNK>, configured, kThreads, kSmem, a, r, c, k, st);
 }
 template int f8_mx_launch<float>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
 template int f8_mx_launch<__nv_bfloat16>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
