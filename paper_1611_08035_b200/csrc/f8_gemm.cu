@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, MX && TBN <= 64 ? 2 : 1)
   if (p.splits > 1) {
     int tr, tc;
     tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
-    f8_split_join<TC, COLS_CONTIG, TBN, EW, false>(p.out, ring, p.splits, share, warp >= 2 && ok ? tid - 64 : -1, (int64_t)tr * kRows,
+    f8_split_join<TC, COLS_CONTIG, TBN, EW, false>(p.out, ring, p.splits, share, warp >= 2 ? tid - 64 : -1, ok, (int64_t)tr * kRows,
                                                    (int64_t)tc * TBN);
   }
   tc_fence_before();

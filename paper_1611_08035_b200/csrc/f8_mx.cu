@@ -184,7 +184,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int quad = warp & 3;
     const uint32_t sf = tmem + kBN + ((uint32_t)(quad * 32) << 16);
     int grp = 0;
-    for (int tile = pair; tile < tiles && ok; tile += pairs) {
+    bool go = true;  // what the four warps agree on; ok is this warp's own
+    for (int tile = pair; tile < tiles && go; tile += pairs) {
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
       const int64_t r0 = (int64_t)tr * 2 * kRows + rank * kRows + lane, c0 = (int64_t)tc * kBN + lane;
@@ -201,14 +202,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int slot = grp % kSlots, r = grp / kSlots;
         uint32_t* words = sf_words + (grp & 1) * kSfCols * 32 + lane;
         words[quad * 32] = next[0], words[(4 + 2 * quad) * 32] = next[1], words[(5 + 2 * quad) * 32] = next[2];
-        asm volatile("bar.sync 1, 128;" ::: "memory");  // also: everyone has read the buffer of two groups ago
+        go = named_barrier_all<1, 128>(ok);  // also: everyone has read the buffer of two groups ago
+        if (!go) break;
         if (kb + 4 < p.kb) fetch(kb + 4);
         uint32_t w[kSfCols];
 #pragma unroll
         for (int i = 0; i < (int)kSfCols; ++i) w[i] = words[i * 32];
         if (r > 0 && !mbar_wait_warp(&sf_empty[slot], (uint32_t)((r - 1) & 1))) {
           ok = false;
-          break;
+          continue;  // to the barrier where the others are told
         }
         tc_fence_after();
 #pragma unroll

@@ -3,6 +3,7 @@
 #pragma once
 #include "common.cuh"
 #include "f8.cuh"
+#include "tcgen05.cuh"
 
 namespace b2 {
 
@@ -191,7 +192,7 @@ __device__ __forceinline__ void f8_emit_staged(const F8Out& p, int64_t row0, int
 // into their shared memory (f8_put_share), the index that is contiguous in C contiguous there too; each CTA adds all shares, in the
 // order of their rank, for its part of the other index, four numbers at a time and all ranks' numbers on their way at once
 // (one after the other, their latency made up most of a 1024^3 product: 21 us, now 5.9).  All threads of all CTAs of the cluster call this; the
-// 32 EW threads with worker >= 0 (numbered) add and write.  PERMUTE: row r of the tile is row kept_row(r) of C.
+// 32 EW threads with worker >= 0 (numbered) add and write, unless their waits have run out (ok, the same in a warp).  PERMUTE: row r of the tile is row kept_row(r) of C.
 constexpr int kMaxSplit = 8;  // 2, 4 or 8 CTAs
 struct F8Split {
   int s;          // CTAs to a tile
@@ -270,7 +271,7 @@ __device__ __forceinline__ void f8_add_shares(const F8Out& p, void* tile, int sh
     }
   }
   if (!p.vec) {  // columns of C that start anywhere: from this CTA's own part of its own share, which no other CTA reads, lane by lane
-    asm volatile("bar.sync 2, %0;" ::"n"(WORKERS) : "memory");
+    if (!named_barrier_all<2, WORKERS>(true)) return;
     for (int i = worker; i < PER * INNER; i += WORKERS) {
       const int o = share * PER + i / INNER, in = i % INNER;
       const int64_t row = row0 + (COLS_CONTIG ? o : in), col = col0 + (COLS_CONTIG ? in : o);
@@ -292,9 +293,11 @@ __device__ __forceinline__ void f8_join_end() {
   asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 template <typename TC, bool COLS_CONTIG, int TBN, int EW, bool PERMUTE>
-__device__ __forceinline__ void f8_split_join(const F8Out& p, void* tile, int splits, int share, int worker, int64_t row0, int64_t col0) {
+__device__ __forceinline__ void f8_split_join(const F8Out& p, void* tile, int splits, int share, int worker, bool ok, int64_t row0, int64_t col0) {
   f8_join_begin();
-  if (worker >= 0) {
+  if (worker >= 0 && !ok) {
+    if (!p.vec) (void)named_barrier_all<2, 32 * EW>(false);  // where the other workers wait for this warp
+  } else if (worker >= 0) {
     if (splits == 2) f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 2>(p, tile, share, worker, row0, col0);
     else if (splits == 4) f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 4>(p, tile, share, worker, row0, col0);
     else f8_add_shares<TC, COLS_CONTIG, TBN, EW, PERMUTE, 8>(p, tile, share, worker, row0, col0);

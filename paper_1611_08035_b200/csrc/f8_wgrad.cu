@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(WgCfg<CTAS>::NT, 1)
       if (p.splits > 1) {
         int tr, tc;
         tile_coords(blockIdx.x, p.tiles_r, p.tiles_c, p.group, tr, tc);
-        f8_split_join<TC, false, TBN, EW, true>(p.out, ring, p.splits, share, ok ? tid - 384 : -1, (int64_t)tr * kRows, (int64_t)tc * TBN);
+        f8_split_join<TC, false, TBN, EW, true>(p.out, ring, p.splits, share, tid - 384, ok, (int64_t)tr * kRows, (int64_t)tc * TBN);
       }
     }
   }

@@ -171,6 +171,23 @@ __device__ __forceinline__ bool mbar_test_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, mbar_test_wait(bar, parity) ? 1 : 0) != 0;
 }
 
+// Barrier ID of THREADS threads of a CTA, where every warp says whether its waits have come true so far; the same answer, whether all
+// have, for each of them.  A wait has its own limit in every warp, so that one may give up where its neighbour just sees the
+// completion: warps that meet at a barrier again decide there, together, whether they go on, and none leaves before.
+template <int ID, int THREADS>
+__device__ __forceinline__ bool named_barrier_all(bool ok) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.and.pred q, %2, %3, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"((uint32_t)ok), "n"(ID), "n"(THREADS)
+      : "memory");
+  return all != 0;
+}
+
 // Position in a ring of N stages and the parity of its current round.
 template <int N>
 struct RingPos {
