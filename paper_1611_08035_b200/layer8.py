@@ -13,6 +13,7 @@ layer towards a target and times one step of a large one.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as b2
 
@@ -60,6 +61,7 @@ class _NormLinear8(torch.autograd.Function):
         return y, h
 
     @staticmethod
+    @once_differentiable  # made of operators without a gradient: a loss that holds one of these gradients is refused
     def backward(ctx, dy, dh):
         h, norm_weight, q, s, rstd, w8, sw = ctx.saved_tensors
         (t, d), n = h.shape, w8.shape[0]

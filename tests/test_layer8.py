@@ -1,0 +1,122 @@
+"""The 8-bit layer's own work, without a GPU: a stand-in for the binding does the operators by their definitions (oracle/f8.py), reading the
+memory that the calls name and nothing else."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import f8
+from paper_1611_08035_b200 import layer8
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def columns(x, t, d, ld):
+    """t columns of d elements, ld apart, from where x begins; raises where they leave x's memory."""
+    return torch.as_strided(x.view(torch.uint8) if x.element_size() == 1 else x, (t, d), (ld, 1))
+
+
+def np64(x):
+    return x.detach().to(torch.float64).numpy()
+
+
+class StandIn:
+    def __init__(self):
+        self.calls, self.devices = [], []
+
+    def called(self, name):
+        self.calls.append(name)
+        self.devices.append(layer8_device[-1] if layer8_device else None)
+
+    def b2_quant_f8(self, d, t, block, x, ldx, q, ldq, s, lds):
+        self.called("quant")
+        qv, sv = f8.quantise(np64(columns(x, t, d, ldx)), block)
+        columns(q, t, d, ldq).copy_(torch.from_numpy(qv))
+        columns(s, *sv.shape, lds).copy_(torch.from_numpy(sv))
+
+    def b2_rmsnorm_f8(self, d, t, x, ldx, r, ldr, w, eps, h, ldh, q, ldq, s, lds, rstd):
+        self.called("norm")
+        hv, rv, yv = f8.rmsnorm(np64(columns(x, t, d, ldx)), None if r is None else np64(columns(r, t, d, ldr)), np64(columns(w, 1, d, d)[0]), eps)
+        if h is not None:
+            columns(h, t, d, ldh).copy_(torch.from_numpy(hv))
+        qv, sv = f8.quantise(yv)
+        columns(q, t, d, ldq).copy_(torch.from_numpy(qv))
+        columns(s, *sv.shape, lds).copy_(torch.from_numpy(sv))
+        rstd.copy_(torch.from_numpy(rv))
+
+    def b2_rmsnorm_backward_workspace_bytes(self, d, t):
+        return 0
+
+    def b2_gemm_f8_workspace_bytes(self, *a):
+        return 0
+
+    def b2_wgrad_f8_workspace_bytes(self, *a):
+        return 0
+
+    def b2_rmsnorm_backward(self, d, t, dy, lddy, h, ldh, rstd, w, dh, lddh, dx, lddx, dw, ws):
+        self.called("norm_backward")
+        a, b = f8.rmsnorm_backward(np64(columns(dy, t, d, lddy)), np64(columns(h, t, d, ldh)), np64(rstd), np64(columns(w, 1, d, d)[0]),
+                                   None if dh is None else np64(columns(dh, t, d, lddh)))
+        columns(dx, t, d, lddx).copy_(torch.from_numpy(a))
+        dw.copy_(torch.from_numpy(b))
+
+    def b2_gemm_f8(self, ta, tb, m, n, k, alpha, A, lda, SA, ldsa, ba, B, ldb, SB, ldsb, bb, beta, C, ldc, ws):
+        self.called("gemm" + ta)
+        assert tb == "N" and alpha == 1.0 and beta == 0.0
+        rows, cols = (m, k) if ta == "T" else (k, m)
+        qa, sa = f8.E4M3[columns(A, rows, cols, lda).numpy()], f8.e8m0(columns(SA, -(-rows // ba) if ta == "T" else -(-rows // 128), -(-cols // 128), ldsa).numpy())
+        if ta == "N":
+            qa, sa = qa.T, sa.T
+        qb, sb = f8.E4M3[columns(B, n, k, ldb).numpy()], f8.e8m0(columns(SB, -(-n // bb), -(-k // 128), ldsb).numpy())
+        columns(C, n, m, ldc).copy_(torch.from_numpy(f8.gemm(qa, sa, ba, qb, sb, bb)[0]))
+
+    def b2_wgrad_f8(self, m, n, k, alpha, Q, ldq, S, lds, Y, ldy, beta, C, ldc, ws):
+        self.called("wgrad")
+        q, s = f8.E4M3[columns(Q, k, m, ldq).numpy()], f8.e8m0(columns(S, k, -(-m // 128), lds).numpy())
+        columns(C, n, m, ldc).copy_(torch.from_numpy(f8.wgrad(q, s, np64(columns(Y, k, n, ldy)))[0]))
+
+
+layer8_device = []
+
+
+@pytest.fixture
+def ops(monkeypatch):
+    s = StandIn()
+    monkeypatch.setattr(layer8, "b2", s)
+    layer8_device.clear()
+    return s
+
+
+def make(d=256, n=128, t=5, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    torch.manual_seed(seed)
+    layer = layer8.NormLinear8(d, n, device="cpu")
+    x, r = (torch.randn(t, d, generator=g).to(BF).requires_grad_() for _ in range(2))
+    return layer, x, r
+
+
+def reference(layer, x, r):
+    h = x.float() + (0 if r is None else r.float())
+    return h * torch.rsqrt(h.square().mean(1, keepdim=True) + layer.eps) * layer.norm_weight.float() @ layer.weight.float().t()
+
+
+def off(a, b):
+    return float((a.detach().float() - b.detach().float()).norm() / b.detach().float().norm())
+
+
+def test_stand_in_gives_the_layer(ops):
+    layer, x, r = make()
+    y, h = layer(x, r)
+    y.float().square().sum().backward()
+    xf, rf = x.detach().float().requires_grad_(), r.detach().float().requires_grad_()
+    want = reference(layer, xf, rf)
+    want.square().sum().backward()
+    assert off(y, want) < 2 * 0.037 and off(x.grad, xf.grad) < 0.1 and torch.equal(x.grad, r.grad)
+
+
+def test_second_order_gradients_are_refused(ops):
+    """The backward pass is made of operators without a gradient: a loss with a gradient in it must not quietly lose that part."""
+    layer, x, r = make()
+    y, _ = layer(x, r)
+    (g,) = torch.autograd.grad(y.float().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (y.float().sum() + g.float().square().sum()).backward()
