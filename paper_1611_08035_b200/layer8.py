@@ -13,7 +13,6 @@ layer towards a target and times one step of a large one.
 from __future__ import annotations
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import binding as b2
 
@@ -45,6 +44,18 @@ def product(a, sa, block_a, ta, b, sb, block_b, m, n, k, out_dtype=torch.bfloat1
     return c
 
 
+class _Once(torch.autograd.Function):
+    """Gradients as they are, which cannot be differentiated again."""
+
+    @staticmethod
+    def forward(ctx, *grads):
+        return tuple(g.view_as(g) for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the 8-bit layer's gradients have no gradient of their own: it can be differentiated once")
+
+
 class _NormLinear8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, norm_weight, weight, w8, sw, eps):
@@ -61,8 +72,16 @@ class _NormLinear8(torch.autograd.Function):
         return y, h
 
     @staticmethod
-    @once_differentiable  # made of operators without a gradient: a loss that holds one of these gradients is refused
     def backward(ctx, dy, dh):
+        with torch.no_grad():
+            grads = _NormLinear8.gradients(ctx, dy, dh)
+        if torch.is_grad_enabled():  # someone wants to differentiate them: they depend on x and the weights, whatever dy does
+            once = iter(_Once.apply(*(g.detach().requires_grad_() for g in grads if g is not None)))
+            grads = tuple(None if g is None else next(once) for g in grads)
+        return grads
+
+    @staticmethod
+    def gradients(ctx, dy, dh):
         h, norm_weight, q, s, rstd, w8, sw = ctx.saved_tensors
         (t, d), n = h.shape, w8.shape[0]
         dy = torch.zeros(t, n, dtype=h.dtype, device=h.device) if dy is None else dy.contiguous()
