@@ -98,20 +98,35 @@ class _NormLinear8(torch.autograd.Function):
 
 class NormLinear8(torch.nn.Module):
     """y, h = layer(x, residual): h = x + residual (x without one), y = rmsnorm(h) W^T.  W is kept in float32 for the optimiser
-    and in e4m3 for the products; call ``requantise()`` after every change of it."""
+    and in e4m3 for the products.  The 8-bit one is made anew by the next call after the weight was changed in place, replaced, loaded or
+    moved; what changes it unseen by autograd (through ``weight.data``, or in a replayed CUDA graph) has to call ``requantise()``."""
 
     def __init__(self, features: int, outputs: int, eps: float = 1e-5, device="cuda"):
         super().__init__()
         self.eps = eps
         self.norm_weight = torch.nn.Parameter(torch.ones(features, dtype=torch.bfloat16, device=device))
         self.weight = torch.nn.Parameter(torch.randn(outputs, features, device=device) * features**-0.5)
-        self.requantise()
+        self._quantised = None
+        if self.weight.is_cuda:
+            self.requantise()
+
+    def _weight_state(self):
+        """The parameter and the number of changes that it has seen (a tuple: as an attribute of its own it would count as a second parameter)."""
+        return self.weight, None if self.weight.is_inference() else self.weight._version
 
     @torch.no_grad()
     def requantise(self) -> None:
         self.w8, self.sw = quantise(self.weight, 128)
+        self._quantised = self._weight_state()
+
+    def _apply(self, fn, recurse=True):
+        self._quantised = None  # parameters get new storage without a new version
+        return super()._apply(fn, recurse)
 
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        weight, version = self._weight_state()
+        if self._quantised is None or self._quantised[0] is not weight or self._quantised[1] != version:
+            self.requantise()
         return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), self.norm_weight, self.weight, self.w8, self.sw, self.eps)
 
 

@@ -1,5 +1,7 @@
 """The 8-bit layer's own work, without a GPU: a stand-in for the binding does the operators by their definitions (oracle/f8.py), reading the
 memory that the calls name and nothing else."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -120,3 +122,53 @@ def test_second_order_gradients_are_refused(ops):
     (g,) = torch.autograd.grad(y.float().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         (y.float().sum() + g.float().square().sum()).backward()
+
+
+def change_in_place(layer):
+    with torch.no_grad():
+        layer.weight.mul_(-2.0)
+    return layer
+
+
+def change_by_loading(layer):
+    layer.load_state_dict({"norm_weight": layer.norm_weight.detach().clone(), "weight": layer.weight.detach() * -2.0})
+    return layer
+
+
+def change_by_another_parameter(layer):
+    layer.weight = torch.nn.Parameter(layer.weight.detach() * -2.0)
+    return layer
+
+
+def change_of_a_copy(layer):
+    return change_in_place(copy.deepcopy(layer))
+
+
+def change_by_conversion(layer):  # what .to(), .cuda() and their kind do, here with a function that also changes the numbers
+    return layer._apply(lambda p: p * -2.0 if p.dim() == 2 else p)
+
+
+@pytest.mark.parametrize("change", [change_in_place, change_by_loading, change_by_another_parameter, change_of_a_copy, change_by_conversion])
+def test_weight_in_8_bits_follows_the_weight(ops, change):
+    """Whatever changes the weight without a word to the layer: the products read the new one."""
+    layer, x, r = make()
+    layer(x, r)
+    layer = change(layer)
+    y, _ = layer(x, r)
+    assert off(y, reference(layer, x, r)) < 2 * 0.037
+
+
+def test_weight_in_8_bits_is_made_once(ops):
+    layer, x, r = make()
+    before = layer.weight.detach().clone()
+    for _ in range(3):
+        y, _ = layer(x, r)
+        y.float().sum().backward()
+    assert ops.calls.count("norm") == 3 and ops.calls.count("quant") == 1 + 3  # the weight's, and each step's gradient
+    layer.requantise()
+    assert ops.calls.count("quant") == 5 and torch.equal(layer.weight, before)
+
+
+def test_state_is_the_weights_alone(ops):
+    layer, x, r = make()
+    assert set(layer.state_dict()) == {"norm_weight", "weight"} and len(list(layer.parameters())) == 2
