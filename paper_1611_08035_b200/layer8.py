@@ -28,7 +28,8 @@ def _scratch(nbytes: int, device) -> torch.Tensor | None:
 
 
 def quantise(x: torch.Tensor, block: int = 1):
-    """x [rows, features] (bfloat16 or float32, contiguous) as e4m3 numbers and the e8m0 scales of its block x 128 tiles."""
+    """x [rows, features] (bfloat16 or float32) as e4m3 numbers and the e8m0 scales of its block x 128 tiles."""
+    x = x.contiguous()
     t, d = x.shape
     q = torch.empty(t, d, dtype=F8, device=x.device)
     s = torch.empty((t + block - 1) // block, _blocks(d), dtype=E8, device=x.device)
@@ -123,11 +124,25 @@ class NormLinear8(torch.nn.Module):
         self._quantised = None  # parameters get new storage without a new version
         return super()._apply(fn, recurse)
 
+    def _check(self, x, residual):
+        """The operators take the extents of x and of the weight for everyone's: what has others would be read beyond its end."""
+        d = self.weight.shape[1]
+        if x.dim() != 2 or x.shape[1] != d:
+            raise ValueError(f"x is {tuple(x.shape)}; the layer takes [tokens, {d}]")
+        if residual is not None and residual.shape != x.shape:
+            raise ValueError(f"residual is {tuple(residual.shape)}, x {tuple(x.shape)}: both have one shape")
+        if self.norm_weight.shape != (d,):
+            raise ValueError(f"norm_weight is {tuple(self.norm_weight.shape)}; the weight has {d} features")
+        for name, v in (("residual", residual), ("norm_weight", self.norm_weight), ("weight", self.weight)):
+            if v is not None and v.device != x.device:
+                raise ValueError(f"{name} is on {v.device}, x on {x.device}")
+
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        self._check(x, residual)
         weight, version = self._weight_state()
         if self._quantised is None or self._quantised[0] is not weight or self._quantised[1] != version:
             self.requantise()
-        return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), self.norm_weight, self.weight, self.w8, self.sw, self.eps)
+        return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), self.norm_weight.contiguous(), self.weight, self.w8, self.sw, self.eps)
 
 
 def train(features: int = 512, outputs: int = 384, tokens: int = 1024, steps: int = 40, lr: float = 0.5, seed: int = 0):

@@ -172,3 +172,43 @@ def test_weight_in_8_bits_is_made_once(ops):
 def test_state_is_the_weights_alone(ops):
     layer, x, r = make()
     assert set(layer.state_dict()) == {"norm_weight", "weight"} and len(list(layer.parameters())) == 2
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_quantise_reads_any_layout(ops, transposed):
+    """What the operator is given are columns one after the other, whatever the tensor's strides: nothing beyond its memory, the same numbers."""
+    x = torch.randn(130, 200, generator=torch.Generator().manual_seed(1))
+    view = x.t().contiguous().t() if transposed else x[:1].expand(130, 200)
+    q, s = layer8.quantise(view, 128)
+    want_q, want_s = f8.quantise(np64(view), 128)
+    assert np.array_equal(q.view(torch.uint8).numpy(), want_q) and np.array_equal(s.view(torch.uint8).numpy(), want_s)
+
+
+def test_shapes_that_do_not_fit_are_refused(ops):
+    """Every operand's extent comes from x and the weight: another tensor's would be read beyond its end."""
+    layer, x, r = make(256, 128, 5)
+    for bad_x, bad_r in [(x, r[:1]), (x, r[:, :128]), (x, r[:4]), (x[:, :255], None), (torch.zeros(5, 257, dtype=BF), None), (x[0], None), (x[None], None),
+                         (x, r[None]), (x.detach().to("meta"), None)]:
+        with pytest.raises(ValueError):
+            layer(bad_x, bad_r)
+    layer.norm_weight = torch.nn.Parameter(torch.ones(1, dtype=BF))
+    with pytest.raises(ValueError):
+        layer(x, r)
+    assert "norm" not in ops.calls
+
+
+def test_strided_norm_weight(ops):
+    layer, x, r = make(256, 128, 5)
+    wide = torch.randn(512, generator=torch.Generator().manual_seed(2)).to(BF)
+    layer.norm_weight = torch.nn.Parameter(wide[::2])
+    y, _ = layer(x, r)
+    y.float().sum().backward()
+    assert off(y, reference(layer, x, r)) < 2 * 0.037 and layer.norm_weight.grad.shape == (256,)
+
+
+def test_no_tokens(ops):
+    layer, x, r = make(256, 128, 0)
+    y, h = layer(x, r)
+    assert y.shape == (0, 128) and h.shape == (0, 256)
+    (y.float().sum() + h.float().sum()).backward()
+    assert x.grad.shape == (0, 256) and bool((layer.weight.grad == 0).all()) and bool((layer.norm_weight.grad == 0).all())
