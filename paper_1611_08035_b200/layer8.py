@@ -33,7 +33,8 @@ def quantise(x: torch.Tensor, block: int = 1):
     t, d = x.shape
     q = torch.empty(t, d, dtype=F8, device=x.device)
     s = torch.empty((t + block - 1) // block, _blocks(d), dtype=E8, device=x.device)
-    b2.b2_quant_f8(d, t, block, x, d, q, d, s, s.shape[1])
+    with torch.cuda.device_of(x):  # calls go to a stream of the current device
+        b2.b2_quant_f8(d, t, block, x, d, q, d, s, s.shape[1])
     return q, s
 
 
@@ -41,7 +42,8 @@ def product(a, sa, block_a, ta, b, sb, block_b, m, n, k, out_dtype=torch.bfloat1
     """[n, m] = B A^T of block-scaled operands: b [n, k]; a [m, k] (ta 'T') or [k, m] (ta 'N')."""
     c = torch.empty(n, m, dtype=out_dtype, device=a.device)
     ws = _scratch(b2.b2_gemm_f8_workspace_bytes(ta, "N", m, n, k, a, a.shape[1], b, k), a.device)
-    b2.b2_gemm_f8(ta, "N", m, n, k, 1.0, a, a.shape[1], sa, sa.shape[1], block_a, b, k, sb, sb.shape[1], block_b, 0.0, c, m, ws)
+    with torch.cuda.device_of(a):
+        b2.b2_gemm_f8(ta, "N", m, n, k, 1.0, a, a.shape[1], sa, sa.shape[1], block_a, b, k, sb, sb.shape[1], block_b, 0.0, c, m, ws)
     return c
 
 
@@ -66,7 +68,8 @@ class _NormLinear8(torch.autograd.Function):
         h = torch.empty_like(x) if residual is not None else x
         q, s = torch.empty(t, d, dtype=F8, device=x.device), torch.empty(t, _blocks(d), dtype=E8, device=x.device)
         rstd = torch.empty(t, dtype=torch.float32, device=x.device)
-        b2.b2_rmsnorm_f8(d, t, x, d, residual, d, norm_weight, eps, h if residual is not None else None, d, q, d, s, s.shape[1], rstd)
+        with torch.cuda.device_of(x):
+            b2.b2_rmsnorm_f8(d, t, x, d, residual, d, norm_weight, eps, h if residual is not None else None, d, q, d, s, s.shape[1], rstd)
         y = product(w8, sw, 128, "T", q, s, 1, n, t, d)
         ctx.save_for_backward(h, norm_weight, q, s, rstd, w8, sw)
         ctx.has_residual = residual is not None
@@ -89,11 +92,12 @@ class _NormLinear8(torch.autograd.Function):
         dq, ds = quantise(dy)
         dnorm = product(w8, sw, 128, "N", dq, ds, 1, d, t, n)
         dweight = torch.empty(n, d, dtype=torch.float32, device=h.device)
-        ws = _scratch(b2.b2_wgrad_f8_workspace_bytes(d, n, t, q, d, dy, n), h.device)
-        b2.b2_wgrad_f8(d, n, t, 1.0, q, d, s, s.shape[1], dy, n, 0.0, dweight, d, ws)
         dx, dnw = torch.empty_like(h), torch.empty(d, dtype=torch.float32, device=h.device)
-        ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), h.device)
-        b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, None if dh is None else dh.contiguous(), d, dx, d, dnw, ws)
+        with torch.cuda.device_of(h):
+            ws = _scratch(b2.b2_wgrad_f8_workspace_bytes(d, n, t, q, d, dy, n), h.device)
+            b2.b2_wgrad_f8(d, n, t, 1.0, q, d, s, s.shape[1], dy, n, 0.0, dweight, d, ws)
+            ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), h.device)
+            b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, None if dh is None else dh.contiguous(), d, dx, d, dnw, ws)
         return dx, dx if ctx.has_residual else None, dnw.to(norm_weight.dtype), dweight, None, None, None
 
 

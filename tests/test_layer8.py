@@ -212,3 +212,24 @@ def test_no_tokens(ops):
     assert y.shape == (0, 128) and h.shape == (0, 256)
     (y.float().sum() + h.float().sum()).backward()
     assert x.grad.shape == (0, 256) and bool((layer.weight.grad == 0).all()) and bool((layer.norm_weight.grad == 0).all())
+
+
+class Guard:
+    """Stands for torch.cuda.device_of: notes for which tensor the current device is switched."""
+
+    def __init__(self, tensor):
+        self.tensor = tensor
+
+    def __enter__(self):
+        layer8_device.append(self.tensor.device)
+
+    def __exit__(self, *_):
+        layer8_device.pop()
+
+
+def test_launches_go_to_the_operands_device(ops, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "device_of", Guard)
+    layer, x, r = make()
+    y, h = layer(x, r)
+    (y.float().sum() + h.float().sum()).backward()
+    assert len(ops.devices) == 7 and all(d == x.device for d in ops.devices), list(zip(ops.calls, ops.devices))
