@@ -88,17 +88,29 @@ class _NormLinear8(torch.autograd.Function):
     def gradients(ctx, dy, dh):
         h, norm_weight, q, s, rstd, w8, sw = ctx.saved_tensors
         (t, d), n = h.shape, w8.shape[0]
-        dy = torch.zeros(t, n, dtype=h.dtype, device=h.device) if dy is None else dy.contiguous()
-        dq, ds = quantise(dy)
-        dnorm = product(w8, sw, 128, "N", dq, ds, 1, d, t, n)
-        dweight = torch.empty(n, d, dtype=torch.float32, device=h.device)
-        dx, dnw = torch.empty_like(h), torch.empty(d, dtype=torch.float32, device=h.device)
-        with torch.cuda.device_of(h):
-            ws = _scratch(b2.b2_wgrad_f8_workspace_bytes(d, n, t, q, d, dy, n), h.device)
-            b2.b2_wgrad_f8(d, n, t, 1.0, q, d, s, s.shape[1], dy, n, 0.0, dweight, d, ws)
-            ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), h.device)
-            b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, None if dh is None else dh.contiguous(), d, dx, d, dnw, ws)
-        return dx, dx if ctx.has_residual else None, dnw.to(norm_weight.dtype), dweight, None, None, None
+        wants_x, wants_norm, wants_weight = any(ctx.needs_input_grad[:2]), ctx.needs_input_grad[2], ctx.needs_input_grad[3]
+        fresh = torch.empty if dy is not None else torch.zeros
+        dx = dnw = dweight = None
+        if wants_norm:
+            dnw = fresh(d, dtype=torch.float32, device=h.device)
+        if wants_weight:
+            dweight = fresh(n, d, dtype=torch.float32, device=h.device)
+        if dy is None:  # a loss on h alone, which the norm and the product do not touch
+            dx = dh if wants_x else None
+        else:
+            dy = dy.contiguous()
+            with torch.cuda.device_of(h):
+                if wants_weight:
+                    ws = _scratch(b2.b2_wgrad_f8_workspace_bytes(d, n, t, q, d, dy, n), h.device)
+                    b2.b2_wgrad_f8(d, n, t, 1.0, q, d, s, s.shape[1], dy, n, 0.0, dweight, d, ws)
+                if wants_x or wants_norm:
+                    dq, ds = quantise(dy)
+                    dnorm = product(w8, sw, 128, "N", dq, ds, 1, d, t, n)
+                    dx = torch.empty_like(h)
+                    sums = torch.empty(d, dtype=torch.float32, device=h.device) if dnw is None else dnw
+                    ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), h.device)
+                    b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, None if dh is None else dh.contiguous(), d, dx, d, sums, ws)
+        return dx, dx if ctx.has_residual else None, None if dnw is None else dnw.to(norm_weight.dtype), dweight, None, None, None
 
 
 class NormLinear8(torch.nn.Module):

@@ -233,3 +233,28 @@ def test_launches_go_to_the_operands_device(ops, monkeypatch):
     y, h = layer(x, r)
     (y.float().sum() + h.float().sum()).backward()
     assert len(ops.devices) == 7 and all(d == x.device for d in ops.devices), list(zip(ops.calls, ops.devices))
+
+
+def test_only_wanted_gradients_are_computed(ops):
+    layer, x, r = make()
+    full = {"quant", "norm", "gemmT", "gemmN", "wgrad", "norm_backward"}
+
+    def backward(frozen, loss):
+        for name in ("x", "r", "norm_weight", "weight"):
+            v = {"x": x, "r": r}.get(name, getattr(layer, name, None))
+            v.grad = None
+            v.requires_grad_(name not in frozen)
+        y, h = layer(x, r)
+        ops.calls.clear()
+        loss(y.float(), h.float()).backward()
+        for name in frozen:
+            assert {"x": x, "r": r}.get(name, getattr(layer, name, None)).grad is None
+        return set(ops.calls)
+
+    y_loss, h_loss = (lambda y, h: (y * y).sum()), (lambda y, h: (h * h).sum())
+    assert backward((), y_loss) == full - {"norm", "gemmT"}
+    assert backward(("weight",), y_loss) == {"quant", "gemmN", "norm_backward"}
+    assert backward(("x", "r", "norm_weight"), y_loss) == {"wgrad"}
+    assert backward((), h_loss) == set()
+    h = x.detach() + r.detach()
+    assert torch.equal(x.grad, 2 * h) and torch.equal(r.grad, 2 * h) and bool((layer.weight.grad == 0).all()) and bool((layer.norm_weight.grad == 0).all())
