@@ -21,6 +21,7 @@ INCLUDE = PKG_DIR.parent / "include"
 BUILD_DIR = PKG_DIR / "_build"
 LIB_PATH = PKG_DIR / "libb2gemm.so"
 CALLS_PATH = PKG_DIR / "_b2calls.so"
+CALLS_STAMP = BUILD_DIR / "calls.stamp"
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -66,27 +67,41 @@ def _compile(src: Path, verbose: bool) -> Path:
 
 
 def _build_calls(verbose: bool) -> None:
+    """``_b2calls.so``.  The library does without it (binding.py then makes the calls through ctypes), so that a machine which cannot compile
+    it is told so and gets everything else."""
+    try:
+        _compile_calls(verbose)
+    except (ImportError, OSError, RuntimeError) as e:
+        for f in (CALLS_PATH, CALLS_STAMP):
+            f.unlink(missing_ok=True)
+        sys.stderr.write(f"[b2gemm build] without the quick calls from Python: {e}\n")
+
+
+def _compile_calls(verbose: bool) -> None:
     import sysconfig
 
     import torch
     from torch.utils import cpp_extension
-    src = CSRC / "calls.cpp"
+    src, fresh = CSRC / "calls.cpp", CALLS_PATH.with_suffix(f".{os.getpid()}.tmp")
     flags = ["-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
     paths = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], str(Path(_nvcc()).resolve().parent.parent / "include")]
-    cmd = ["g++", *flags, *(f for p in paths for f in ("-isystem", p)), "-I", str(INCLUDE), str(src), "-o", str(CALLS_PATH),
+    cmd = ["g++", *flags, *(f for p in paths for f in ("-isystem", p)), "-I", str(INCLUDE), str(src),
            *(f"-L{p}" for p in cpp_extension.library_paths()), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
     h = hashlib.sha256(" ".join([torch.__version__, *cmd]).encode())
     for f in (src, *sorted(INCLUDE.glob("*.h"))):
         h.update(f.read_bytes())
-    stamp_file = BUILD_DIR / "calls.stamp"
-    if CALLS_PATH.exists() and stamp_file.exists() and stamp_file.read_text() == h.hexdigest():
+    if CALLS_PATH.exists() and CALLS_STAMP.exists() and CALLS_STAMP.read_text() == h.hexdigest():
         return
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError(f"g++ failed for {src.name}:\n{res.stderr[-8000:]}")
+    try:
+        res = subprocess.run([*cmd, "-o", str(fresh)], capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError(f"g++ failed for {src.name}:\n{res.stderr[-8000:]}")
+        os.replace(fresh, CALLS_PATH)  # never half a file for another process to load
+    finally:
+        fresh.unlink(missing_ok=True)
     if verbose:
         sys.stderr.write(f"[b2gemm build] compiled {src.name}\n")
-    stamp_file.write_text(h.hexdigest())
+    CALLS_STAMP.write_text(h.hexdigest())
 
 
 def build(verbose: bool = False, force: bool = False) -> Path:
