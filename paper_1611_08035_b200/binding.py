@@ -118,6 +118,9 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_connected: dict = {}  # name -> (address in the library, the function below) of what _b2calls was connected to
+
+
 def _connect_calls(handle) -> None:
     """The 8-bit operators' functions below give way to those of ``_b2calls``, which read the same arguments without ctypes and fall
     back on these for keywords and for whatever they do not take.  Without that module these do all of it."""
@@ -128,6 +131,7 @@ def _connect_calls(handle) -> None:
     names = ("b2_rmsnorm_f8", "b2_rmsnorm_backward", "b2_quant_f8", "b2_gemm_f8", "b2_wgrad_f8")
     table = {n: (ctypes.cast(getattr(handle, n), c_void_p).value, globals()[n]) for n in names}
     _b2calls.connect(B2Error, table)
+    _connected.update(table)
     globals().update({n: getattr(_b2calls, n) for n in names})
 
 

@@ -73,7 +73,14 @@ void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
 PyObject* hand_over(const Entry& e, PyObject* const* a, Py_ssize_t n, PyObject* names) { return PyObject_Vectorcall(e.full, a, (size_t)n, names); }
 
-PyObject* result(const char* name, int rc) {
+// Calls the library and turns its answer into Python's.  Other threads run meanwhile: a launch waits when the stream is full, and what would
+// make room may be one of theirs (a callback on the host).
+template <typename Call>
+PyObject* result(const char* name, const Call& call) {
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call();
+  Py_END_ALLOW_THREADS
   if (rc == 0) return PyLong_FromLong(0);
   PyObject* err = PyObject_CallFunction(g_error, "si", name, rc);
   if (err) {
@@ -102,8 +109,9 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
   const int64_t lds = p.integer();
   void* rstd = p.typed(at::kFloat, true);
   if (names || !code || !p.all_read()) return hand_over(g_norm, a, n, names);
-  return result("b2_rmsnorm_f8", reinterpret_cast<decltype(&b2_rmsnorm_f8)>(g_norm.fn)(d, t, code, x->data_ptr(), ldx, r, ldr, w, (float)eps, h, ldh, q, ldq, s,
-                                                                                         lds, static_cast<float*>(rstd), stream()));
+  const auto fn = reinterpret_cast<decltype(&b2_rmsnorm_f8)>(g_norm.fn);
+  void *X = x->data_ptr(), *st = stream();
+  return result("b2_rmsnorm_f8", [&] { return fn(d, t, code, X, ldx, r, ldr, w, (float)eps, h, ldh, q, ldq, s, lds, static_cast<float*>(rstd), st); });
 }
 
 PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
@@ -124,10 +132,12 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names)
   void* dw = p.typed(at::kFloat);
   const at::Tensor* ws = p.tensor(true);
   if (names || !code || !p.all_read()) return hand_over(g_norm_bwd, a, n, names);
-  return result("b2_rmsnorm_backward",
-                reinterpret_cast<decltype(&b2_rmsnorm_backward)>(g_norm_bwd.fn)(d, t, code, dy->data_ptr(), lddy, h, ldh, static_cast<float*>(rstd), w, dh, lddh, dx,
-                                                                                 lddx, static_cast<float*>(dw), ws ? ws->data_ptr() : nullptr, ws ? ws->nbytes() : 0,
-                                                                                 stream()));
+  const auto fn = reinterpret_cast<decltype(&b2_rmsnorm_backward)>(g_norm_bwd.fn);
+  void *DY = dy->data_ptr(), *W = ws ? ws->data_ptr() : nullptr, *st = stream();
+  const size_t bytes = ws ? ws->nbytes() : 0;
+  return result("b2_rmsnorm_backward", [&] {
+    return fn(d, t, code, DY, lddy, h, ldh, static_cast<float*>(rstd), w, dh, lddh, dx, lddx, static_cast<float*>(dw), W, bytes, st);
+  });
 }
 
 PyObject* quant(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
@@ -141,7 +151,9 @@ PyObject* quant(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
   void* s = p.typed(at::kFloat8_e8m0fnu);
   const int64_t lds = p.integer();
   if (names || !code || block != (int)block || !p.all_read()) return hand_over(g_quant, a, n, names);
-  return result("b2_quant_f8", reinterpret_cast<decltype(&b2_quant_f8)>(g_quant.fn)(d, t, (int)block, code, x->data_ptr(), ldx, q, ldq, s, lds, stream()));
+  const auto fn = reinterpret_cast<decltype(&b2_quant_f8)>(g_quant.fn);
+  void *X = x->data_ptr(), *st = stream();
+  return result("b2_quant_f8", [&] { return fn(d, t, (int)block, code, X, ldx, q, ldq, s, lds, st); });
 }
 
 PyObject* gemm(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
@@ -163,9 +175,12 @@ PyObject* gemm(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
   const at::Tensor* ws = p.i < p.n ? p.tensor(true) : nullptr;
   const int code = type_code(C), ca = scale_code(SA), cb = scale_code(SB);
   if (names || !code || ca < 0 || cb < 0 || block_a != (int)block_a || block_b != (int)block_b || !p.all_read()) return hand_over(g_gemm, a, n, names);
-  return result("b2_gemm_f8", reinterpret_cast<decltype(&b2_gemm_f8)>(g_gemm.fn)(ta, tb, m, nn, k, (float)alpha, A, lda, SA->data_ptr(), ldsa, (int)block_a, ca, B, ldb,
-                                                                                   SB->data_ptr(), ldsb, (int)block_b, cb, (float)beta, C->data_ptr(), ldc, code,
-                                                                                   ws ? ws->data_ptr() : nullptr, ws ? ws->nbytes() : 0, stream()));
+  const auto fn = reinterpret_cast<decltype(&b2_gemm_f8)>(g_gemm.fn);
+  void *sa = SA->data_ptr(), *sb = SB->data_ptr(), *c = C->data_ptr(), *W = ws ? ws->data_ptr() : nullptr, *st = stream();
+  const size_t bytes = ws ? ws->nbytes() : 0;
+  return result("b2_gemm_f8", [&] {
+    return fn(ta, tb, m, nn, k, (float)alpha, A, lda, sa, ldsa, (int)block_a, ca, B, ldb, sb, ldsb, (int)block_b, cb, (float)beta, c, ldc, code, W, bytes, st);
+  });
 }
 
 PyObject* wgrad(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
@@ -184,8 +199,10 @@ PyObject* wgrad(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
   const at::Tensor* ws = p.i < p.n ? p.tensor(true) : nullptr;
   const int code = type_code(C);
   if (names || !code || !p.all_read()) return hand_over(g_wgrad, a, n, names);
-  return result("b2_wgrad_f8", reinterpret_cast<decltype(&b2_wgrad_f8)>(g_wgrad.fn)(m, nn, k, (float)alpha, Q, ldq, S, lds, Y, ldy, (float)beta, C->data_ptr(), ldc, code,
-                                                                                      ws ? ws->data_ptr() : nullptr, ws ? ws->nbytes() : 0, stream()));
+  const auto fn = reinterpret_cast<decltype(&b2_wgrad_f8)>(g_wgrad.fn);
+  void *c = C->data_ptr(), *W = ws ? ws->data_ptr() : nullptr, *st = stream();
+  const size_t bytes = ws ? ws->nbytes() : 0;
+  return result("b2_wgrad_f8", [&] { return fn(m, nn, k, (float)alpha, Q, ldq, S, lds, Y, ldy, (float)beta, c, ldc, code, W, bytes, st); });
 }
 
 // connect(error class, {name: (address in the library, function in binding.py)})
