@@ -37,7 +37,10 @@ struct F8Cfg {
   static constexpr int COLS = TBN / (EW / 4);               // accumulators of a thread
   static constexpr int NT = 64 + 32 * EW;
   static constexpr uint32_t STAGE = kRowStage + TBN * kF8Block;
-  static constexpr int STAGES = TBN == 128 ? 6 : TBN == 64 ? 4 : 5;  // of the narrow tiles, two CTAs share an SM
+  static constexpr int STAGES = TBN == 128 ? 6 : TBN == 64 ? 4 : 5;
+  // CTAs that an SM holds.  The one with 64 columns and scales in registers takes 175 of them a thread; kept to the 168 that two would leave it is
+  // slower where one is enough (8192 x 64 x 8192 20.6 us, 19.8).  That the split's rule counted two all the same cost 50304 x 64 over 4096 71.7 us, now 49.3.
+  static constexpr int RESIDENT = TBN < 64 || (TBN == 64 && MX) ? 2 : 1;
   static constexpr uint32_t RING = STAGE * STAGES;
   static constexpr int SLOTS = 4, SF_COLS = 8;              // scale ring in tensor memory: 4 columns for 128 rows, 4 for 128 columns
   static constexpr uint32_t TMEM = MX ? (TBN <= 32 ? 64 : TBN == 64 ? 128 : 256) : (TBN == 16 ? 32 : 2 * TBN);
@@ -45,6 +48,7 @@ struct F8Cfg {
   static constexpr int SCRATCH = kEmitBytes > COLS * 4 ? kEmitBytes : COLS * 4;  // of a warp: staged rows of C, or a block's column scales
   static constexpr size_t SMEM = 1024 + RING + 512 + EW * SCRATCH;
   static_assert(share_bytes(TBN) <= RING, "the split's shares pass through the ring");
+  static_assert(RESIDENT * (SMEM + 1024) <= 228 * 1024 && RESIDENT * TMEM <= 512, "shared and tensor memory of an SM");
 };
 
 __device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
@@ -66,7 +70,7 @@ __device__ __forceinline__ void umma_mx1(uint32_t tmem_d, uint64_t desc_a, uint6
 }
 
 template <int TBN, typename TC, bool COLS_CONTIG, bool MX>
-__global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, MX && TBN <= 64 ? 2 : 1)
+__global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, F8Cfg<TBN, MX>::RESIDENT)
     f8_gemm_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   using Cfg = F8Cfg<TBN, MX>;
   constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES, CHUNK = chunk_blocks<TC>();
@@ -459,10 +463,11 @@ F8Split f8_product_split(int64_t tiles, int kb, int tbn, int resident) {
 template <typename TC, bool MX>
 int f8_choose(const F8Args& a, const F8Operand& A, const F8Operand& B, int64_t k, cudaStream_t st) {
   const int sms = sm_count_cached();
-  if (B.n <= 64 && !B.mn) {  // decoding: A's rows, tiles as narrow as n, two CTAs an SM
+  if (B.n <= 64 && !B.mn) {  // decoding: A's rows, tiles as narrow as n
     const int tbn = B.n <= 16 ? 16 : B.n <= 32 ? 32 : 64;
     const int64_t tiles = blocks_of(A.n, kRows);
-    const int s = f8_product_split(tiles, a.kb, tbn, tiles >= sms ? 2 : 1).s;
+    const int resident = tbn == 16 ? F8Cfg<16, MX>::RESIDENT : tbn == 32 ? F8Cfg<32, MX>::RESIDENT : F8Cfg<64, MX>::RESIDENT;
+    const int s = f8_product_split(tiles, a.kb, tbn, tiles >= sms ? resident : 1).s;
     if (tbn == 16) return f8_launch<16, TC, false, MX>(a, A, B, k, s, st);
     if (tbn == 32) return f8_launch<32, TC, false, MX>(a, A, B, k, s, st);
     return f8_launch<64, TC, false, MX>(a, A, B, k, s, st);
@@ -497,13 +502,15 @@ F8Pack f8_pack_plan(bool an, bool bn, int64_t m, int64_t n, int64_t k, const voi
 
 }  // namespace
 
-// What the product takes, in clocks: turns of CTAs over the SMs, and adding the shares, half as long again for every doubling.  CTAs of a
-// cluster are not persistent: each further turn begins anew, 3000 clocks to its first product, and joins at its end.
+// What the product takes, in clocks: turns of CTAs over the SMs, and adding the shares, half as long again for every doubling.  Without a
+// split there is one CTA to an SM, which walks over its tiles (counted as if `resident` of them shared it, 50304 x 64 over 4096 with e8m0 scales was
+// split: 45.6 us, 42.6 without).  CTAs of a cluster are not persistent: each further turn begins anew, 3000 clocks to its first product, and joins at its end.
 // Measured with clusters that do not fit at once: weight gradient of 512 x 512 over 4096 tokens 20.1 us with 16 clusters of eight, 13.8 with four.
 F8Split f8_split_for(int64_t tiles, int stages, double stage, double join, int resident) {
   F8Split best{1, 0.0};
   for (int s = 1, log = 0; s <= kMaxSplit && (s == 1 || stages / s >= 2); s *= 2, ++log) {
-    const double turns = (double)blocks_of(tiles * s, (int64_t)f8_cluster_slots(log) * resident), work = (double)resident * (double)blocks_of(stages, s) * stage;
+    const int r = s == 1 ? 1 : resident;
+    const double turns = (double)blocks_of(tiles * s, (int64_t)f8_cluster_slots(log) * r), work = (double)r * (double)blocks_of(stages, s) * stage;
     const double clocks = s == 1 ? turns * work : turns * (work + join * (0.7 + 0.3 * log)) + (turns - 1.0) * 3000.0;
     if (s == 1 || clocks < best.clocks) best = {s, clocks};
   }
