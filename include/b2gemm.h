@@ -419,7 +419,8 @@ int b2_model_enumerate(int dtype, int top, char* json_out, size_t cap);
  *     s = the smallest power of two with a/s <= 448   (1 when a == 0, at least 2^-127),   q = v/s rounded to nearest even e4m3.
  * Fewer than 2^31 - 8192 features and 2^31 tokens, else B2_ERR_VARIANT.
  * Nothing saturates.  A block that holds a NaN or an infinity is stored as NaN throughout (scale byte 255, every q 0x7f).
- * Division by a power of two is exact, so q*s differs from v by the one rounding to e4m3; q*s is representable in bf16.
+ * Division by a power of two is exact, so q*s differs from v by the one rounding to e4m3; q*s is representable in bf16, except that a |v|
+ * of 1.9375 * 2^127 or more rounds to 2^128, which neither bf16 nor fp32 holds.
  */
 #define B2_TYPE_F32 1
 #define B2_TYPE_BF16 2
@@ -488,7 +489,7 @@ int b2_gemm_f8(char transa, char transb, int64_t m, int64_t n, int64_t k, float 
  * wrote them, m x k: k tokens of m features) and the gradient Y of the layer's result (bf16, n x k):
  *     C(i,j) := alpha * sum_p Q(i,p) * S(i/128, p) * Y(j,p) + beta * C(i,j)          (C m x n, bf16 or fp32)
  * Q*S enters the product as bf16 numbers, which hold it exactly (scales below 2^-124 excepted, whose smallest
- * numbers are subnormal in bf16), with fp32 accumulation.
+ * numbers are subnormal in bf16; 2^128 and more become infinite), with fp32 accumulation in pieces of at most 1024 tokens as in b2_gemm_f8.
  * An operand that is not 16-byte aligned (base and column) is first copied to the workspace, as in b2_gemm_f8.
  * Arguments: m 1, n 2, k 3, alpha 4, Q 5, ldq 6, S 7, lds 8, Y 9, ldy 10, beta 11, C 12, ldc 13, type_c 14.
  */
