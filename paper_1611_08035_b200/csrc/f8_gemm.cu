@@ -18,7 +18,7 @@
 //
 // What bounds it: latencies.  1024^3 takes 5.9 us, of which the first operands take 2 and the results 1; adding shares of 128 x 128
 // tiles takes 2 us (distributed shared memory delivers 14 bytes a clock), which is why narrow tiles come before splits.  Decoding
-// (8192 x 8 x 8192) takes 15.2 us for 64 MB of weights, 4.4 TB/s; the weights alone would take 10.3.
+// (8192 x 8 x 8192) takes 14.5 us (calls from Python 15.0) for 64 MB of weights, 4.6 TB/s; the weights alone would take 10.3.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -38,7 +38,7 @@ struct F8Cfg {
   static constexpr int NT = 64 + 32 * EW;
   static constexpr uint32_t STAGE = kRowStage + TBN * kF8Block;
   static constexpr int STAGES = TBN == 128 ? 6 : TBN == 64 ? 4 : 5;
-  // CTAs that an SM holds.  The one with 64 columns and scales in registers takes 175 of them a thread; kept to the 168 that two would leave it is
+  // CTAs that an SM holds.  The one with 64 columns and scales in registers takes 177 of them a thread; kept to the 168 that two would leave it is
   // slower where one is enough (8192 x 64 x 8192 20.6 us, 19.8).  That the split's rule counted two all the same cost 50304 x 64 over 4096 71.7 us, now 49.3.
   static constexpr int RESIDENT = TBN < 64 || (TBN == 64 && MX) ? 2 : 1;
   static constexpr uint32_t RING = STAGE * STAGES;

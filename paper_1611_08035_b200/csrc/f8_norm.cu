@@ -3,7 +3,7 @@
 //   h = x + r,  rstd = 1/sqrt(mean(h^2) + eps),  y = h * rstd * w,  (q, s) = y quantised in blocks of 128 features
 //   dx = rstd * (g - xh * mean(g xh)) + dh,  dw = sum_t dy xh,     g = dy w, xh = h rstd
 //
-// Both are bound by memory: a token is read once, kept in registers over the sum that its norm needs, and written once.  A
+// Sizes here are tokens x features.  Both are bound by memory: a token is read once, kept in registers over the sum that its norm needs, and written once.  A
 // warp holds 256 consecutive features, exactly two blocks of 128, so that their largest magnitudes never leave it.
 // Measured, bf16: norm of 16384 x 8192 153 us (6.1 TB/s, 94 % of the copy rate), gradient of 16384 x 8192 181 us (5.9 TB/s); fp32: 270 us
 // (6.5 TB/s) and 326 us (6.6 TB/s).  Other lengths: norm of 2560 features 5.8, of 3184 4.2, of 10240 5.5 TB/s; gradient of 2560 4.6, of
@@ -45,7 +45,7 @@ __device__ __forceinline__ float cta_sum(float v, float* part) {
 
 // WARP: a warp to a token, four tokens a CTA; otherwise the CTA, whose size is the token's.  A thread holds VPT groups of eight features
 // (Warp256: which eight).  FULL: the CTA has NT threads, which saves 4 % where it does (8192 x 8192 bf16 80 us, 83 with a width read at
-// run time); otherwise as many warps as the token fills (2560 x 16384: 70 us with the next power of two, 51).
+// run time); otherwise as many warps as the token fills (16384 x 2560: 70 us with the next power of two, 51).
 template <typename T, int VPT, int NT, bool WARP, bool VEC, bool FULL = true>
 __global__ void __launch_bounds__(NT, NT == 512 && VPT == 4 && sizeof(T) == 2 ? 2 : 1) norm_kernel(const NormArgs p) {
   grid_started();
@@ -397,13 +397,13 @@ __global__ void __launch_bounds__(1024) norm_bwd_sum_kernel(const float* partial
 constexpr int64_t kBwdLongest = 1024;  // groups of eight of the longest token held in registers
 
 // threads of a CTA that holds a token of more than 64 groups, two groups a thread.  An SM holds as many CTAs of 192 as of 256; three warps
-// are slower than four in bf16 (1536 x 16384: 47 us against 42), not in fp32 (1152 x 4096: 19 against 25).
+// are slower than four in bf16 (16384 x 1536: 47 us against 42), not in fp32 (4096 x 1152: 19 against 25).
 int bwd_threads(int64_t chunks, size_t elem) {
   const int n = 32 * (int)blocks_of(chunks, 64);
   return n == 96 && elem == 2 ? 128 : n <= 160 ? n : n <= 256 ? 256 : 512;
 }
-// A group a thread for up to 128 groups where there are too few tokens for an SM to hold all the CTAs it could (1003 x 1001 fp32: 8.3 us
-// against 9.7; 896 x 16384 bf16 would take 33 against 28).
+// A group a thread for up to 128 groups where there are too few tokens for an SM to hold all the CTAs it could (1001 x 1003 fp32: 8.3 us
+// against 9.7; 16384 x 896 bf16 would take 33 against 28).
 bool bwd_short(int64_t chunks, int64_t t) { return chunks > 64 && chunks <= 128 && t < 12 * (int64_t)sm_count_cached(); }
 
 // rows of partial sums: CTAs of the backward kernel
@@ -418,8 +418,8 @@ int64_t bwd_rows(int64_t d, int64_t t, size_t elem) {
   return rows < most ? rows : most;
 }
 
-// One launch where launches are what takes the time (bf16: 4096 x 8 3.0 us, 7.6 with two; 4096 x 300 6.1 and 8.7), two where the walk over
-// the tokens does (4096 x 1024: 21 us, 14 with two; fp32 1003 x 1001: 23 us and 11).
+// One launch where launches are what takes the time (bf16: 8 x 4096 3.0 us, 7.6 with two; 300 x 4096 6.1 and 8.7), two where the walk over
+// the tokens does (1024 x 4096: 21 us, 14 with two; fp32 1001 x 1003: 23 us and 11).
 bool bwd_few(int64_t d, int64_t t) { return t <= 384 && t * d <= (int64_t)3 << 19; }
 
 template <typename T, bool VEC>

@@ -191,7 +191,7 @@ int quant_launch(const QuantArgs& a, int block, bool vec, bool q16, cudaStream_t
   const int64_t ctas = nb * blocks_of(a.t, kF8Block);
   if (ctas > 0x7fffffffLL) return B2_ERR_VARIANT;
   if (vec) return launch_overlapped(quant_tiles_kernel<T, true, 1>, (unsigned)ctas, 256, st, a, nb);
-  // Few tiles of narrow accesses: four CTAs to each, so that all SMs have a share (1003 x 999 bf16 9.4 -> 5.5 us, fp32 5.8 -> 4.9).  With wide
+  // Few tiles of narrow accesses: four CTAs to each, so that all SMs have a share (999 x 1003 bf16 9.4 -> 5.5 us, fp32 5.8 -> 4.9).  With wide
   // accesses meeting costs more than sharing saves (1024 x 1024 bf16 2.7 us, 3.3 in clusters).
   if (ctas <= sm_count_cached()) return launch_overlapped_as(quant_tiles_kernel<T, false, 4>, dim3(4 * (unsigned)ctas), 256, 0, dim3(4), st, a, nb);
   return launch_overlapped(quant_tiles_kernel<T, false, 1>, (unsigned)ctas, 256, st, a, nb);
