@@ -12,6 +12,8 @@ layer towards a target and times one step of a large one.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import binding as b2
@@ -27,13 +29,21 @@ def _scratch(nbytes: int, device) -> torch.Tensor | None:
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _device_of(x):
+    """Makes x's device the current one, to a stream of which the calls go; costs nothing where it is (switching there and back takes 1.5 us)."""
+    return _HERE if x.is_cuda and x.get_device() == torch._C._cuda_getDevice() else torch.cuda.device_of(x)
+
+
 def quantise(x: torch.Tensor, block: int = 1):
     """x [rows, features] (bfloat16 or float32) as e4m3 numbers and the e8m0 scales of its block x 128 tiles."""
     x = x.contiguous()
     t, d = x.shape
     q = torch.empty(t, d, dtype=F8, device=x.device)
     s = torch.empty((t + block - 1) // block, _blocks(d), dtype=E8, device=x.device)
-    with torch.cuda.device_of(x):  # calls go to a stream of the current device
+    with _device_of(x):
         b2.b2_quant_f8(d, t, block, x, d, q, d, s, s.shape[1])
     return q, s
 
@@ -42,7 +52,7 @@ def product(a, sa, block_a, ta, b, sb, block_b, m, n, k, out_dtype=torch.bfloat1
     """[n, m] = B A^T of block-scaled operands: b [n, k]; a [m, k] (ta 'T') or [k, m] (ta 'N')."""
     c = torch.empty(n, m, dtype=out_dtype, device=a.device)
     ws = _scratch(b2.b2_gemm_f8_workspace_bytes(ta, "N", m, n, k, a, a.shape[1], b, k), a.device)
-    with torch.cuda.device_of(a):
+    with _device_of(a):
         b2.b2_gemm_f8(ta, "N", m, n, k, 1.0, a, a.shape[1], sa, sa.shape[1], block_a, b, k, sb, sb.shape[1], block_b, 0.0, c, m, ws)
     return c
 
@@ -68,7 +78,7 @@ class _NormLinear8(torch.autograd.Function):
         h = torch.empty_like(x) if residual is not None else x
         q, s = torch.empty(t, d, dtype=F8, device=x.device), torch.empty(t, _blocks(d), dtype=E8, device=x.device)
         rstd = torch.empty(t, dtype=torch.float32, device=x.device)
-        with torch.cuda.device_of(x):
+        with _device_of(x):
             b2.b2_rmsnorm_f8(d, t, x, d, residual, d, norm_weight, eps, h if residual is not None else None, d, q, d, s, s.shape[1], rstd)
         y = product(w8, sw, 128, "T", q, s, 1, n, t, d)
         ctx.save_for_backward(h, norm_weight, q, s, rstd, w8, sw)
@@ -77,40 +87,40 @@ class _NormLinear8(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy, dh):
-        with torch.no_grad():
+        if not torch.is_grad_enabled():
+            return _NormLinear8.gradients(ctx, dy, dh)
+        with torch.no_grad():  # someone wants to differentiate the gradients: they depend on x and the weights, whatever dy does
             grads = _NormLinear8.gradients(ctx, dy, dh)
-        if torch.is_grad_enabled():  # someone wants to differentiate them: they depend on x and the weights, whatever dy does
-            once = iter(_Once.apply(*(g.detach().requires_grad_() for g in grads if g is not None)))
-            grads = tuple(None if g is None else next(once) for g in grads)
-        return grads
+        once = iter(_Once.apply(*(g.detach().requires_grad_() for g in grads if g is not None)))
+        return tuple(None if g is None else next(once) for g in grads)
 
     @staticmethod
     def gradients(ctx, dy, dh):
         h, norm_weight, q, s, rstd, w8, sw = ctx.saved_tensors
-        (t, d), n = h.shape, w8.shape[0]
-        wants_x, wants_norm, wants_weight = any(ctx.needs_input_grad[:2]), ctx.needs_input_grad[2], ctx.needs_input_grad[3]
-        fresh = torch.empty if dy is not None else torch.zeros
+        wants_x, wants_residual, wants_norm, wants_weight = ctx.needs_input_grad[:4]
+        (t, d), n, device = h.shape, w8.shape[0], h.device
         dx = dnw = dweight = None
-        if wants_norm:
-            dnw = fresh(d, dtype=torch.float32, device=h.device)
-        if wants_weight:
-            dweight = fresh(n, d, dtype=torch.float32, device=h.device)
         if dy is None:  # a loss on h alone, which the norm and the product do not touch
-            dx = dh if wants_x else None
-        else:
-            dy = dy.contiguous()
-            with torch.cuda.device_of(h):
-                if wants_weight:
-                    ws = _scratch(b2.b2_wgrad_f8_workspace_bytes(d, n, t, q, d, dy, n), h.device)
-                    b2.b2_wgrad_f8(d, n, t, 1.0, q, d, s, s.shape[1], dy, n, 0.0, dweight, d, ws)
-                if wants_x or wants_norm:
-                    dq, ds = quantise(dy)
-                    dnorm = product(w8, sw, 128, "N", dq, ds, 1, d, t, n)
-                    dx = torch.empty_like(h)
-                    sums = torch.empty(d, dtype=torch.float32, device=h.device) if dnw is None else dnw
-                    ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), h.device)
-                    b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, None if dh is None else dh.contiguous(), d, dx, d, sums, ws)
-        return dx, dx if ctx.has_residual else None, None if dnw is None else dnw.to(norm_weight.dtype), dweight, None, None, None
+            if wants_norm:
+                dnw = torch.zeros_like(norm_weight)
+            if wants_weight:
+                dweight = torch.zeros(n, d, dtype=torch.float32, device=device)
+            return dh, dh if ctx.has_residual else None, dnw, dweight, None, None, None
+        dy = dy.contiguous()
+        with _device_of(h):
+            if wants_x or wants_residual or wants_norm:
+                dq, ds = quantise(dy)
+                dnorm = product(w8, sw, 128, "N", dq, ds, 1, d, t, n)
+            if wants_weight:
+                dweight = torch.empty(n, d, dtype=torch.float32, device=device)
+                ws = _scratch(b2.b2_wgrad_f8_workspace_bytes(d, n, t, q, d, dy, n), device)
+                b2.b2_wgrad_f8(d, n, t, 1.0, q, d, s, s.shape[1], dy, n, 0.0, dweight, d, ws)
+            if wants_x or wants_residual or wants_norm:
+                dx, dnw = torch.empty_like(h), torch.empty(d, dtype=torch.float32, device=device)
+                ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), device)
+                b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, None if dh is None else dh.contiguous(), d, dx, d, dnw, ws)
+                dnw = dnw.to(norm_weight.dtype) if wants_norm else None
+        return dx, dx if ctx.has_residual else None, dnw, dweight, None, None, None
 
 
 class NormLinear8(torch.nn.Module):
@@ -127,38 +137,36 @@ class NormLinear8(torch.nn.Module):
         if self.weight.is_cuda:
             self.requantise()
 
-    def _weight_state(self):
+    @staticmethod
+    def _state(weight):
         """The parameter and the number of changes that it has seen (a tuple: as an attribute of its own it would count as a second parameter)."""
-        return self.weight, None if self.weight.is_inference() else self.weight._version
+        return weight, None if weight.is_inference() else weight._version
 
     @torch.no_grad()
     def requantise(self) -> None:
         self.w8, self.sw = quantise(self.weight, 128)
-        self._quantised = self._weight_state()
+        self._quantised = self._state(self.weight)
 
     def _apply(self, fn, recurse=True):
         self._quantised = None  # parameters get new storage without a new version
         return super()._apply(fn, recurse)
 
-    def _check(self, x, residual):
-        """The operators take the extents of x and of the weight for everyone's: what has others would be read beyond its end."""
-        d = self.weight.shape[1]
-        if x.dim() != 2 or x.shape[1] != d:
-            raise ValueError(f"x is {tuple(x.shape)}; the layer takes [tokens, {d}]")
-        if residual is not None and residual.shape != x.shape:
-            raise ValueError(f"residual is {tuple(residual.shape)}, x {tuple(x.shape)}: both have one shape")
-        if self.norm_weight.shape != (d,):
-            raise ValueError(f"norm_weight is {tuple(self.norm_weight.shape)}; the weight has {d} features")
-        for name, v in (("residual", residual), ("norm_weight", self.norm_weight), ("weight", self.weight)):
-            if v is not None and v.device != x.device:
-                raise ValueError(f"{name} is on {v.device}, x on {x.device}")
-
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
-        self._check(x, residual)
-        weight, version = self._weight_state()
-        if self._quantised is None or self._quantised[0] is not weight or self._quantised[1] != version:
+        weight, norm_weight = self.weight, self.norm_weight
+        # The operators take the extents of x and of the weight for everyone's: what has others would be read beyond its end.
+        shape, d, device = x.shape, weight.shape[1], x.device
+        if len(shape) != 2 or shape[1] != d:
+            raise ValueError(f"x is {tuple(shape)}; the layer takes [tokens, {d}]")
+        if residual is not None and residual.shape != shape:
+            raise ValueError(f"residual is {tuple(residual.shape)}, x {tuple(shape)}: both have one shape")
+        if norm_weight.shape != (d,):
+            raise ValueError(f"norm_weight is {tuple(norm_weight.shape)}; the weight has {d} features")
+        if weight.device != device or norm_weight.device != device or (residual is not None and residual.device != device):
+            raise ValueError(f"x is on {device}, the weight on {weight.device}, the norm's on {norm_weight.device}, the residual on {None if residual is None else residual.device}")
+        of = self._quantised
+        if of is None or of[0] is not weight or of[1] != self._state(weight)[1]:
             self.requantise()
-        return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), self.norm_weight.contiguous(), self.weight, self.w8, self.sw, self.eps)
+        return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), norm_weight.contiguous(), weight, self.w8, self.sw, self.eps)
 
 
 def train(features: int = 512, outputs: int = 384, tokens: int = 1024, steps: int = 40, lr: float = 0.5, seed: int = 0):
