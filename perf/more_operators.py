@@ -7,7 +7,7 @@ gemm   z = op(A) op(B) + bias, c = act(z) + r, both operands e4m3 numbers with a
        gradient form c = op(A) op(B) act'(z), z given
 act    the activation's backward pass, dz = dy act'(z), with the bias's gradient (dz summed over the tokens) and dz in 8 bits
 adamw  one AdamW step over all tensors of some layers, its two moments in fp32 or in 8 bits (m and sqrt(v) as e4m3 numbers with
-       one power-of-two scale for 128 consecutive elements, rounded at random by a hash of the element's number)
+       one power-of-two scale for 128 consecutive elements, rounded at random by a hash of the elements' numbers)
 
 Storage is the library's: column-major with leading dimensions, so a torch tensor of shape [cols, ld].  A token is one
 column.  8-bit numbers and their scales are returned in their own floating types, i.e. as the values they stand for.
@@ -384,11 +384,20 @@ def _key(seed, step):
     return _mix(_mix(_mix(seed & LOW) ^ (seed >> 32 & LOW)) ^ (step & LOW))
 
 
+STEP = 0x9E3779B9
+
+
+def _random(e, key):
+    """Two lists of 20 random bits for the elements with the numbers e: a hash for every eight of them, and for each of the eight a step further."""
+    h = _mix(((e >> 3 & LOW) + _mix((e >> 35) + key & LOW)) & LOW)
+    return [((x + (e & 7) * STEP) & LOW) >> 12 for x in (h, _mix(h + STEP & LOW))]
+
+
 def _at_random(x, u):
-    """|x| <= 448 to a neighbouring e4m3 number: the mantissa is cut after a number below its last place was added, u in [0, 2^16) of 2^16."""
+    """|x| <= 448 to a neighbouring e4m3 number: the mantissa is cut after u, in [0, 2^20) of 2^20 of its last place, was added."""
     small = x < 2.0**-6  # numbers of one step, as in the binade above
     t = torch.where(small, x + 2.0**-6, x)
-    t = ((t.view(torch.int32) + (u * 16 + 8).to(torch.int32)) & -(1 << 20)).view(torch.float32)
+    t = ((t.view(torch.int32) + u.to(torch.int32)) & -(1 << 20)).view(torch.float32)
     return torch.where(small, t - 2.0**-6, t)
 
 
@@ -409,9 +418,7 @@ def _plain_adamw(st):
     size, root = a["lr"] / (1 - a["beta1"] ** a["step"]), (1 - a["beta2"] ** a["step"]) ** -0.5
     p = view("p").float() * (1 - a["lr"] * a["wd"]) - size * m / (r * root + a["eps"])
     if c["bits"] == 8:
-        e = torch.arange(nb * 128, device="cuda")
-        h = _mix(((e & LOW) + _mix((e >> 32) + _key(st["seed"], a["step"]) & LOW)) & LOW).view(nb, 128)
-        for name, x, u in (("m", m, h & 0xFFFF), ("v", r, h >> 16)):
+        for name, x, u in zip("mv", (m, r), _random(torch.arange(nb * 128, device="cuda").view(nb, 128), _key(st["seed"], a["step"]))):
             s = _scale_e8m0(x.abs().amax(1))
             y = x.abs() / s.float()[:, None]
             q = _at_random(y, u)
@@ -549,13 +556,12 @@ def _exact_adamw(c, st):
         if c["bits"] == 32:
             parts["m"].append(m), parts["v"].append(v)
             continue
-        e = torch.arange(128 * k.start, 128 * k.stop, device="cuda")
-        h = _mix((e + _mix(_key(st["seed"], a["step"]))) & LOW).view(-1, 128)  # fewer than 2^32 elements
-        for x, y, u in (("m", m, h & 0xFFFF), ("v", v**0.5, h >> 16)):
+        e = torch.arange(128 * k.start, 128 * k.stop, device="cuda").view(-1, 128)
+        for x, y, u in zip("mv", (m, v**0.5), _random(e, _key(st["seed"], a["step"]))):
             s = _power_of_two(y.abs().amax(1))
             w = y.abs() / s[:, None]
             step = _spacing(w)
-            q = torch.floor(w / step + (u.double() + 0.5) / 65536) * step
+            q = torch.floor(w / step + u.double() / 2**20) * step
             if x == "v":
                 q = torch.where(w > 0, q.clamp(min=2.0**-9), q)
             parts[x].append(torch.sign(y) * q), parts["s" + x].append(s)
