@@ -498,6 +498,96 @@ int b2_wgrad_f8(int64_t m, int64_t n, int64_t k, float alpha, const void* Q, int
                 const void* Y, int64_t ldy, float beta, void* C, int64_t ldc, int type_c, void* workspace,
                 size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * Activation functions of the calls below, in fp32: relu max(z, 0); gelu z Phi(z) with the normal distribution's Phi; gelu_tanh
+ * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; silu z / (1 + exp(-z)).  The derivative of relu at 0 is 0.  An infinite z gives the limits, NaN gives
+ * NaN.  Values are within 2^-20 of themselves or of 1, derivatives within 2^-18.
+ */
+#define B2_ACT_NONE 0
+#define B2_ACT_RELU 1
+#define B2_ACT_GELU 2
+#define B2_ACT_GELU_TANH 3
+#define B2_ACT_SILU 4
+#define B2_ACT_GRADIENT 16 /* b2_gemm_f8_act: or-ed to one of these */
+
+/*
+ * The product of b2_gemm_f8 with a layer's bias, activation and residual in the same pass:
+ *     z = alpha * sum_p op(A)_ip sA * op(B)_pj sB + bias_i,     c = act(z) + r
+ * or, with act | B2_ACT_GRADIENT, multiplied by the activation's derivative at a z that is given (the backward pass of such a layer, whose product
+ * is the gradient that reaches the activation; bias must then be NULL):
+ *     c = (alpha * sum_p op(A)_ip sA * op(B)_pj sB) * act'(z) + r
+ *   bias     m floats, or NULL.
+ *   Z        m x n: where z is stored, or NULL.  Gradient form: the z that is read (with B2_ACT_NONE not looked at).
+ *   R        m x n, or NULL.  R may be C.  In the gradient form Z may be C, too.
+ *   C        m x n: where c is stored, or NULL where Q is given.
+ *   type     of Z, R and C (B2_TYPE_*; it does not matter where there are none).
+ *   Q, S     c as e4m3 numbers m x n with a scale byte for each 128 features of a column (ceil(m/128) x n), by the quantisation rule above: what
+ *            b2_gemm_f8 takes as an operand with block 1 and b2_wgrad_f8 as its activation.  Or NULL.
+ * Everything is computed in fp32 from the unrounded sum; z and c are rounded once each, when they are stored, and Q is the rounding of the unrounded c.
+ * The first eighteen arguments, their numbers, the workspace (b2_gemm_f8_workspace_bytes), limits, and how the sums are accumulated are b2_gemm_f8's.
+ * alpha == 0 or k == 0 makes the sum 0 and reads neither A nor B.
+ * Arguments: .. 18 as b2_gemm_f8, act 19, bias 20, Z 21, ldz 22, R 23, ldr 24, C 25, ldc 26, type 27, Q 28, ldq 29, S 30, lds 31.  A leading dimension whose
+ * matrix is NULL is not looked at.
+ */
+int b2_gemm_f8_act(char transa, char transb, int64_t m, int64_t n, int64_t k, float alpha, const void* A, int64_t lda,
+                   const void* SA, int64_t ldsa, int block_a, int scale_type_a, const void* B, int64_t ldb, const void* SB,
+                   int64_t ldsb, int block_b, int scale_type_b, int act, const float* bias, void* Z, int64_t ldz,
+                   const void* R, int64_t ldr, void* C, int64_t ldc, int type, void* Q, int64_t ldq, void* S, int64_t lds,
+                   void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The backward pass of an activation and a bias: for every token (column) of DY, d x t,
+ *     dz = dy * act'(z)   (dz = dy with B2_ACT_NONE, where Z is not looked at),      db_i = sum over tokens of dz_i
+ * each where it is wanted: DZ (d x t), (Q, S) = dz quantised as b2_quant_f8 with block 1 does it, db (d floats).  db and Q come from the
+ * unrounded dz.  DZ may be DY or Z.  db is summed in an order that depends on d, t and the device only: the same bits on every call.  The
+ * workspace (device, 256-byte aligned) holds partial sums of db; without db it may be NULL.
+ * Arguments: d 1, t 2, type 3 (of DY, Z, DZ), act 4, DY 5, lddy 6, Z 7, ldz 8, DZ 9, lddz 10, Q 11, ldq 12, S 13, lds 14, db 15.
+ * Without tokens db is 0.
+ */
+size_t b2_act_backward_workspace_bytes(int64_t d, int64_t t);
+int b2_act_backward(int64_t d, int64_t t, int type, int act, const void* DY, int64_t lddy, const void* Z, int64_t ldz, void* DZ,
+                    int64_t lddz, void* Q, int64_t ldq, void* S, int64_t lds, float* db, void* workspace, size_t workspace_bytes,
+                    void* cuda_stream);
+
+/*
+ * One AdamW step over all tensors of a list at once.  With g' = g, or g * *grad_scale where that is given, for every element
+ *     m := beta1 m + (1 - beta1) g',     v := beta2 v + (1 - beta2) g'^2,
+ *     p := p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32 (the corrections and 1 - lr weight_decay in fp64, rounded once), p rounded once when it is stored; m and v enter p before they are rounded.
+ * A tensor's states are
+ *   state_bits 32: m and v, n floats each;
+ *   state_bits 8:  m and the square root of v as n e4m3 numbers each, with one scale byte (e8m0) for 128 consecutive elements in sm and sv
+ *     (ceil(n/128) bytes), scales by the quantisation rule above.  The rounding to e4m3 is random, to one of the two neighbours with
+ *     probabilities that keep the expectation (a step of beta2 = 0.999 changes the root of v by 5e-4 of itself; rounded to nearest, by steps of
+ *     6e-2 at least, it would never change).  A root that is not 0 is held as 2^-9 of its scale or more, so that no number is divided by eps alone for its
+ *     block's sake.
+ * The random numbers are a hash of seed, step and the element's number e (counted through the list; every tensor starts at the next multiple of 128), the same
+ * whatever the GPU.  With fmix = the 32-bit finaliser of MurmurHash3, lo and hi the halves of 64 bits, all sums modulo 2^32 and G = 0x9E3779B9,
+ *     key = fmix(fmix(fmix(lo(seed)) ^ hi(seed)) ^ lo(step)),     h = fmix(lo(e / 8) + fmix(hi(e / 8) + key)),     h' = fmix(h + G),
+ * the twenty random bits u are the high ones of h + (e mod 8) G for m and of h' + (e mod 8) G for the root of v: the magnitude divided by the scale, plus u / 2^20
+ * of the distance of e4m3 numbers there, is cut to an e4m3 number.
+ * Types of p and g: B2_TYPE_F32 or B2_TYPE_BF16, for each tensor.  Pointers are aligned to their type; those aligned to 16 bytes (states in 8 bits: to 4)
+ * are the fast ones.  No two tensors of a list may overlap, nor may a tensor occur twice.
+ * `tensors` is a HOST array, read before the call returns; a tensor with n = 0 is left out.  step counts from 1.  step_device and lr_device
+ * (DEVICE, or NULL), where given, are read when the call runs on the GPU, in the place of step and lr: a captured graph of the call follows them.
+ * grad_scale: DEVICE, one float, or NULL.
+ * Arguments: tensors 1, count 2, lr 3, beta1 4, beta2 5 (both in [0, 1)), eps 6 (>= 0), weight_decay 7, step 8.  lr and weight_decay are finite.
+ * A tensor that is not as it should be gives -1.
+ */
+typedef struct {
+  void* param;
+  const void* grad;
+  void *m, *v;
+  void *sm, *sv;        /* state_bits 8 */
+  int64_t n;            /* elements */
+  int32_t type_param, type_grad;
+  int32_t state_bits;   /* 8 or 32 */
+  int32_t reserved;     /* 0 */
+} b2_adamw_tensor;
+int b2_adamw(const b2_adamw_tensor* tensors, int count, double lr, double beta1, double beta2, double eps, double weight_decay,
+             int64_t step, uint64_t seed, const float* grad_scale, const float* lr_device, const int64_t* step_device,
+             void* cuda_stream);
+
 /* Static, NUL-terminated text for a return value of any call above. */
 const char* b2_strerror(int status);
 /* Static, NUL-terminated library version. */

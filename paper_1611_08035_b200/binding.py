@@ -93,6 +93,12 @@ _SIGNATURES = {
     "b2_model_register_updates": (c_int, [c_int, c_int, c_int, c_int, c_int, c_int, ctypes.POINTER(c_int)]),
     "b2_model_predict_variant": (c_int, [c_int, c_int, ctypes.POINTER(c_double), c_char_p, c_size_t]),
     "b2_model_enumerate": (c_int, [c_int, c_int, c_char_p, c_size_t]),
+    "b2_gemm_f8_act": (c_int, [c_char, c_char, c_int64, c_int64, c_int64, c_float] + 2 * [c_void_p, c_int64, c_void_p, c_int64, c_int, c_int]
+                       + [c_int, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_void_p, c_int64,
+                          c_void_p, c_size_t, c_void_p]),
+    "b2_act_backward_workspace_bytes": (c_size_t, [c_int64, c_int64]),
+    "b2_act_backward": (c_int, [c_int64, c_int64, c_int, c_int] + 5 * [c_void_p, c_int64] + [c_void_p, c_void_p, c_size_t, c_void_p]),
+    "b2_adamw": (c_int, [c_void_p, c_int] + 5 * [c_double] + [c_int64, ctypes.c_uint64, c_void_p, c_void_p, c_void_p, c_void_p]),
     "b2_strerror": (c_char_p, [c_int]),
     "b2_version": (c_char_p, []),
 }
@@ -128,7 +134,7 @@ def _connect_calls(handle) -> None:
         from . import _b2calls
     except ImportError:
         return
-    names = ("b2_rmsnorm_f8", "b2_rmsnorm_backward", "b2_quant_f8", "b2_gemm_f8", "b2_wgrad_f8")
+    names = ("b2_rmsnorm_f8", "b2_rmsnorm_backward", "b2_quant_f8", "b2_gemm_f8", "b2_wgrad_f8", "b2_gemm_f8_act", "b2_act_backward", "b2_adamw")
     table = {n: (ctypes.cast(getattr(handle, n), c_void_p).value, globals()[n]) for n in names}
     _b2calls.connect(B2Error, table)
     _connected.update(table)
@@ -576,4 +582,89 @@ def b2_wgrad_f8(m, n, k, alpha, Q, ldq, S, lds, Y, ldy, beta, C, ldc, workspace=
                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
     if rc and check:
         raise B2Error("b2_wgrad_f8", rc)
+    return rc
+
+
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU, ACT_GRADIENT = 0, 1, 2, 3, 4, 16  # B2_ACT_*
+
+
+def b2_gemm_f8_act(transa, transb, m, n, k, alpha, A, lda, SA, ldsa, block_a, B, ldb, SB, ldsb, block_b, act, bias, z, ldz, residual, ldr, c, ldc,
+                   q, ldq, s, lds, workspace=None, check=True) -> int:
+    """z = alpha*op(A)*op(B) + bias, c = act(z) + residual of block-scaled e4m3 matrices; or, with act | ACT_GRADIENT, c = alpha*op(A)*op(B) * act'(z) +
+    residual with z given.  z, residual, c: bfloat16 or float32 alike; q, s: c as e4m3 numbers with e8m0 scales; bias: float32.  bias, z, residual,
+    c or q (with s) may be None.  The workspace is b2_gemm_f8_workspace_bytes'."""
+    dt = next((t.dtype for t in (c, z, residual) if t is not None), _F32)
+    code, ca, cb = _TYPES.get(dt), _SCALES.get(SA.dtype), _SCALES.get(SB.dtype)
+    if not (code and ca is not None and cb is not None and A.dtype is _E4M3 and B.dtype is _E4M3 and A.is_cuda and B.is_cuda and SA.is_cuda and SB.is_cuda
+            and all(t is None or (t.dtype is dt and t.is_cuda) for t in (z, residual, c)) and (bias is None or (bias.dtype is _F32 and bias.is_cuda))
+            and (q is None or (q.dtype is _E4M3 and q.is_cuda)) and (s is None or (s.dtype is _E8M0 and s.is_cuda)) and (workspace is None or workspace.is_cuda)):
+        _refuse("b2_gemm_f8_act", ("A", A, (_E4M3,)), ("SA", SA, tuple(_SCALES)), ("B", B, (_E4M3,)), ("SB", SB, tuple(_SCALES)), ("bias", bias, (_F32,)),
+                ("c", c, tuple(_TYPES)), ("z", z, (dt,) if code else tuple(_TYPES)), ("residual", residual, (dt,) if code else tuple(_TYPES)), ("q", q, (_E4M3,)),
+                ("s", s, (_E8M0,)), ("workspace", workspace, (torch.uint8,)))
+    rc = (_lib or lib()).b2_gemm_f8_act(_tr(transa), _tr(transb), m, n, k, alpha, A.data_ptr(), lda, SA.data_ptr(), ldsa, block_a, ca, B.data_ptr(), ldb,
+                                        SB.data_ptr(), ldsb, block_b, cb, act, _ptr(bias) or None, _ptr(z) or None, ldz, _ptr(residual) or None, ldr,
+                                        _ptr(c) or None, ldc, code, _ptr(q) or None, ldq, _ptr(s) or None, lds, _ptr(workspace) or None,
+                                        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    if rc and check:
+        raise B2Error("b2_gemm_f8_act", rc)
+    return rc
+
+
+def b2_act_backward_workspace_bytes(d: int, t: int) -> int:
+    return lib().b2_act_backward_workspace_bytes(d, t)
+
+
+def b2_act_backward(d, t, act, dy, lddy, z, ldz, dz, lddz, q, ldq, s, lds, db, workspace=None, check=True) -> int:
+    """dz = dy * act'(z) and db = its sum over the tokens, dz also as e4m3 numbers q with e8m0 scales s.  dy, z, dz: bfloat16 or float32 alike; db: float32.
+    z may be None with ACT_NONE; dz, q (with s) and db where they are not wanted."""
+    dt = dy.dtype
+    if not (dt in _TYPES and dy.is_cuda and all(x is None or (x.dtype is dt and x.is_cuda) for x in (z, dz)) and (q is None or (q.dtype is _E4M3 and q.is_cuda))
+            and (s is None or (s.dtype is _E8M0 and s.is_cuda)) and (db is None or (db.dtype is _F32 and db.is_cuda)) and (workspace is None or workspace.is_cuda)):
+        _refuse("b2_act_backward", ("dy", dy, tuple(_TYPES)), ("z", z, (dt,)), ("dz", dz, (dt,)), ("q", q, (_E4M3,)), ("s", s, (_E8M0,)), ("db", db, (_F32,)),
+                ("workspace", workspace, (torch.uint8,)))
+    rc = (_lib or lib()).b2_act_backward(d, t, _TYPES[dt], act, dy.data_ptr(), lddy, _ptr(z) or None, ldz, _ptr(dz) or None, lddz, _ptr(q) or None, ldq,
+                                         _ptr(s) or None, lds, _ptr(db) or None, _ptr(workspace) or None,
+                                         0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    if rc and check:
+        raise B2Error("b2_act_backward", rc)
+    return rc
+
+
+class _AdamwTensor(ctypes.Structure):  # b2_adamw_tensor
+    _fields_ = [(f, c_void_p) for f in ("param", "grad", "m", "v", "sm", "sv")] + [("n", c_int64), ("type_param", ctypes.c_int32), ("type_grad", ctypes.c_int32),
+                                                                                 ("state_bits", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+def b2_adamw(params, grads, m, v, sm, sv, lr, beta1, beta2, eps, weight_decay, step, seed=0, grad_scale=None, check=True) -> int:
+    """One AdamW step, in place, over lists of contiguous tensors.  params, grads: bfloat16 or float32; m, v: float32, or float8_e4m3fn (v then holds the root of the
+    second moment) with float8_e8m0fnu scales sm, sv for 128 elements each.  sm and sv may be None, as may their entries for float32 states.  lr and
+    step are numbers, or CUDA tensors of one float32 and one int64 that are read when the call runs; grad_scale: a CUDA tensor of one float32, or None."""
+    count = len(params)
+    if any(len(x) != count for x in (grads, m, v)) or any(x is not None and len(x) != count for x in (sm, sv)):
+        raise ValueError("b2_adamw: the lists have different lengths")
+    table = (_AdamwTensor * max(count, 1))()
+    for i in range(count):
+        t = (params[i], grads[i], m[i], v[i], None if sm is None else sm[i], None if sv is None else sv[i])
+        n, bits = t[0].numel(), 8 if t[2].dtype is _E4M3 else 32
+        state = (_E4M3,) if bits == 8 else (_F32,)
+        kinds = (tuple(_TYPES), tuple(_TYPES), state, state)
+        if not all(x.is_cuda and x.dtype in k for x, k in zip(t, kinds)):
+            _refuse(f"b2_adamw: tensor {i}", *zip(("param", "grad", "m", "v"), t, kinds))
+        if not all(x.is_contiguous() and x.numel() == n for x in t[:4]):
+            raise ValueError(f"b2_adamw: tensor {i}: param, grad, m and v are contiguous and of one size; they have {[tuple(x.shape) for x in t[:4]]}")
+        if bits == 8:
+            for x in t[4:]:
+                if x is None or not x.is_cuda or x.dtype is not _E8M0 or not x.is_contiguous() or x.numel() != (n + 127) // 128:
+                    raise ValueError(f"b2_adamw: tensor {i}: states in 8 bits have contiguous float8_e8m0fnu scales, {(n + 127) // 128} of them")
+        table[i] = _AdamwTensor(*[_ptr(x) or None for x in t[:4]], *([_ptr(x) or None for x in t[4:]] if bits == 8 else (None, None)), n, _TYPES[t[0].dtype],
+                                _TYPES[t[1].dtype], bits, 0)
+    on_device = []
+    for name, x, dt in (("lr", lr, _F32), ("step", step, torch.int64), ("grad_scale", grad_scale, _F32)):
+        if isinstance(x, torch.Tensor) and (not x.is_cuda or x.dtype is not dt or x.numel() != 1):
+            raise TypeError(f"b2_adamw: {name} is {x.dtype} {tuple(x.shape)} on {x.device}; as a tensor it is one {dt} on a CUDA device")
+        on_device.append(x.data_ptr() if isinstance(x, torch.Tensor) else None)
+    rc = (_lib or lib()).b2_adamw(table, count, 0.0 if on_device[0] else lr, beta1, beta2, eps, weight_decay, 1 if on_device[1] else step, seed & 0xFFFFFFFFFFFFFFFF,
+                                  on_device[2], on_device[0], on_device[1], _stream())
+    if rc and check:
+        raise B2Error("b2_adamw", rc)
     return rc

@@ -1,0 +1,370 @@
+// One AdamW step over all tensors of a list, moments in fp32 or in 8 bits.
+//
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v / (1 - b2^t)) + eps)
+//
+// Bound by memory: 14 bytes an element with fp32 parameters, bf16 gradients and states in 8 bits, 28 with everything in fp32.  The list travels as a kernel
+// argument; a CTA finds its tensor by bisection among the tensors' first CTAs.  A warp holds 256 consecutive elements, two blocks of 128 of an 8-bit state, whose
+// largest magnitudes never leave it.
+//
+// States in 8 bits: m and r = sqrt(v) (half the exponent range of v, which e4m3's seventeen binades are then enough for) are rounded at random, so that the mean over
+// steps is right although a step moves r by less than half the distance of two e4m3 numbers.  The twenty random bits come from the element's number, a hash for
+// eight elements and an addition for each.  m and v are computed by single roundings in a fixed order (no fused multiply-adds), and so is r: then everyone who
+// computes them in fp32 comes to the same bits, and to the same side of a random rounding.
+#include <algorithm>
+#include <memory>
+#include <new>
+
+#include "b2gemm.h"
+#include "common.cuh"
+#include "entry.h"
+#include "f8.cuh"
+
+namespace b2 {
+namespace {
+
+struct AdamTensor {
+  void* p;
+  const void* g;
+  void *m, *v;
+  uint8_t *sm, *sv;
+  int64_t n;
+  uint64_t first;  // number of the first element, through the list
+  int vec;         // all pointers are aligned for whole loads
+};
+template <int MOST>
+struct AdamList {
+  int count;
+  uint32_t cta[MOST];  // first CTA of each tensor
+  AdamTensor t[MOST];
+};
+struct AdamStep {
+  float b1, a1, b2, a2, eps;   // a = 1 - b
+  float decay, size, root;     // 1 - lr wd, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
+  uint32_t key;
+  uint64_t seed;
+  const float *scale, *lr_device;
+  const int64_t* step_device;
+  double lr, wd, log_b1, log_b2;
+  int64_t step;
+};
+constexpr int kPieces = 2;                    // of 256 elements, a warp's
+constexpr int kUnit = 8 * 256 * kPieces;      // elements of a CTA
+
+// The finaliser of MurmurHash3 (Austin Appleby, public domain).
+__host__ __device__ __forceinline__ uint32_t fmix(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x85EBCA6Bu;
+  x = (x ^ (x >> 13)) * 0xC2B2AE35u;
+  return x ^ (x >> 16);
+}
+constexpr uint32_t kGolden = 0x9E3779B9u;
+__host__ __device__ __forceinline__ uint32_t adam_key(uint64_t seed, int64_t step) {
+  return fmix(fmix(fmix((uint32_t)seed) ^ (uint32_t)(seed >> 32)) ^ (uint32_t)step);
+}
+// What depends on the step's number and the learning rate.
+__host__ __device__ __forceinline__ void adam_factors(AdamStep& s, double lr, int64_t step) {
+  s.decay = (float)(1.0 - lr * s.wd);
+  s.size = (float)(lr / -expm1((double)step * s.log_b1));
+  s.root = (float)(1.0 / sqrt(-expm1((double)step * s.log_b2)));
+  s.key = adam_key(s.seed, step);
+}
+
+// Four e4m3 numbers of a word.
+__device__ __forceinline__ void f8_unpack4(uint32_t w, float* v) {
+  uint32_t lo, hi;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((uint16_t)w));
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((uint16_t)(w >> 16)));
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(v[0]), "=f"(v[1]) : "r"(lo));
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(v[2]), "=f"(v[3]) : "r"(hi));
+}
+// y, |y| <= 448, to a neighbouring e4m3 number: with 20 random bits added below the third place of the mantissa, the rest is cut.  Numbers below 2^-6 have
+// one distance, 2^-9, as those of the binade from 2^-6 on have, where they are taken for it.
+__device__ __forceinline__ float f8_at_random(float y, uint32_t bits20) {
+  const bool small = fabsf(y) < 0.015625f;
+  const float c = __uint_as_float((__float_as_uint(y) & 0x80000000u) | 0x3c800000u);  // 2^-6 with y's sign
+  float t = small ? __fadd_rn(y, c) : y;
+  t = __uint_as_float((__float_as_uint(t) + bits20) & 0xfff00000u);
+  return small ? __fadd_rn(t, -c) : t;
+}
+
+// m, v and p of one element, in place; r = sqrt(v).
+template <bool ROOT_GIVEN>
+__device__ __forceinline__ void adam_element(const AdamStep& s, float g, float& p, float& m, float& v, float& r) {
+  if (ROOT_GIVEN) v = __fmul_rn(r, r);
+  m = __fadd_rn(__fmul_rn(m, s.b1), __fmul_rn(g, s.a1));
+  v = __fadd_rn(__fmul_rn(v, s.b2), __fmul_rn(__fmul_rn(g, g), s.a2));
+  r = __fsqrt_rn(v);
+  p = __fadd_rn(__fmul_rn(p, s.decay), -__fdividef(s.size * m, fmaf(r, s.root, s.eps)));
+}
+
+template <typename TP, typename TG, int BITS, bool VEC>
+__device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep& s, float scale, int64_t at0) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t at = at0 + warp * 256 * kPieces;
+  if (at >= t.n) return;
+  const int n = (int)min((int64_t)(256 * kPieces), t.n - at);  // elements of this warp
+  TP* P = static_cast<TP*>(t.p) + at;
+  const TG* G = static_cast<const TG*>(t.g) + at;
+  using AtP = Warp256<TP, VEC>;
+  using AtG = Warp256<TG, VEC>;
+  using At4 = Warp256<float, VEC>;
+  Raw8<TP> p8[kPieces];
+  Raw8<TG> g8[kPieces];
+#pragma unroll
+  for (int u = 0; u < kPieces; ++u) {
+    AtP::load(P, 256 * u, n, p8[u]);
+    AtG::load(G, 256 * u, n, g8[u]);
+  }
+  if constexpr (BITS == 32) {
+    float *M = static_cast<float*>(t.m) + at, *V = static_cast<float*>(t.v) + at;
+    Raw8<float> m8[kPieces], v8[kPieces];
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) {
+      At4::load(M, 256 * u, n, m8[u]);
+      At4::load(V, 256 * u, n, v8[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) {
+      float p[8], g[8], m[8], v[8], r;
+      unpack8(p8[u], p), unpack8(g8[u], g), unpack8(m8[u], m), unpack8(v8[u], v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) adam_element<false>(s, __fmul_rn(g[j], scale), p[j], m[j], v[j], r);
+      AtP::store(P, 256 * u, n, p);
+      At4::store(M, 256 * u, n, m);
+      At4::store(V, 256 * u, n, v);
+    }
+  } else {
+    uint8_t *M = static_cast<uint8_t*>(t.m) + at, *R = static_cast<uint8_t*>(t.v) + at;
+    uint8_t *SM = t.sm + at / kF8Block, *SR = t.sv + at / kF8Block;
+    uint32_t m8[kPieces][2], r8[kPieces][2], sm[kPieces][2], sr[kPieces][2];
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        m8[u][h] = r8[u][h] = 0;
+        if constexpr (VEC) {
+          const int e = 256 * u + 8 * lane + 4 * h;
+          if (e + 4 <= n) {
+            m8[u][h] = *reinterpret_cast<const uint32_t*>(M + e), r8[u][h] = *reinterpret_cast<const uint32_t*>(R + e);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+              if (e + j < n) m8[u][h] |= (uint32_t)M[e + j] << (8 * j), r8[u][h] |= (uint32_t)R[e + j] << (8 * j);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int e = 256 * u + 128 * h + 32 * j + lane;
+            if (e < n) m8[u][h] |= (uint32_t)M[e] << (8 * j), r8[u][h] |= (uint32_t)R[e] << (8 * j);
+          }
+        }
+      }
+      // VEC: both halves of a lane's eight lie in block lane / 16; else half h is of block h
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int b = 2 * u + (VEC ? lane >> 4 : h);
+        sm[u][h] = b * kF8Block < n ? SM[b] : 127u, sr[u][h] = b * kF8Block < n ? SR[b] : 127u;
+      }
+    }
+    const uint64_t e0 = t.first + (uint64_t)at;
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) {
+      float p[8], g[8], m[8], r[8];
+      unpack8(p8[u], p), unpack8(g8[u], g);
+      f8_unpack4(m8[u][0], m), f8_unpack4(m8[u][1], m + 4), f8_unpack4(r8[u][0], r), f8_unpack4(r8[u][1], r + 4);
+      uint32_t most_m[2] = {0, 0}, most_r[2] = {0, 0};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float v;
+        m[j] = __fmul_rn(m[j], e8m0_value(sm[u][j >> 2])), r[j] = __fmul_rn(r[j], e8m0_value(sr[u][j >> 2]));
+        adam_element<true>(s, __fmul_rn(g[j], scale), p[j], m[j], v, r[j]);
+        most_m[j >> 2] = max(most_m[j >> 2], mag_bits(m[j])), most_r[j >> 2] = max(most_r[j >> 2], mag_bits(r[j]));
+      }
+      AtP::store(P, 256 * u, n, p);
+      if constexpr (VEC) {
+        uint32_t a = max(most_m[0], most_m[1]), b = max(most_r[0], most_r[1]);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o)), b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
+        most_m[0] = most_m[1] = a, most_r[0] = most_r[1] = b;
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) most_m[h] = __reduce_max_sync(0xffffffffu, most_m[h]), most_r[h] = __reduce_max_sync(0xffffffffu, most_r[h]);
+      }
+      uint32_t hm = 0, hr = 0;
+      auto hash = [&](uint64_t e) {
+        const uint64_t e8 = e >> 3;
+        hm = fmix((uint32_t)e8 + fmix((uint32_t)(e8 >> 32) + s.key)), hr = fmix(hm + kGolden);
+      };
+      if constexpr (VEC) hash(e0 + 256 * u + 8 * lane);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t byte_m = f8_scale_byte(most_m[h]), byte_r = f8_scale_byte(most_r[h]);
+        const float inv_m = byte_m == kScaleNan ? 0.0f : f8_inv_scale(byte_m), inv_r = byte_r == kScaleNan ? 0.0f : f8_inv_scale(byte_r);
+        float a[4], b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t i = 4 * h + j;
+          if constexpr (!VEC) {
+            const uint64_t e = e0 + 256 * u + 128 * h + 32 * j + lane;
+            hash(e), i = (uint32_t)e & 7u;
+          }
+          a[j] = f8_at_random(__fmul_rn(m[4 * h + j], inv_m), (hm + i * kGolden) >> 12);
+          const float y = __fmul_rn(r[4 * h + j], inv_r);
+          b[j] = f8_at_random(y, (hr + i * kGolden) >> 12);
+          b[j] = y > 0.0f ? fmaxf(b[j], 0.001953125f) : b[j];  // 2^-9
+        }
+        const uint32_t qm = byte_m == kScaleNan ? 0x7f7f7f7fu : f8_pack4(a[0], a[1], a[2], a[3]);
+        const uint32_t qr = byte_r == kScaleNan ? 0x7f7f7f7fu : f8_pack4(b[0], b[1], b[2], b[3]);
+        if constexpr (VEC) {
+          const int e = 256 * u + 8 * lane + 4 * h;
+          if (e + 4 <= n) {
+            *reinterpret_cast<uint32_t*>(M + e) = qm, *reinterpret_cast<uint32_t*>(R + e) = qr;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+              if (e + j < n) M[e + j] = (uint8_t)(qm >> (8 * j)), R[e + j] = (uint8_t)(qr >> (8 * j));
+          }
+          if (h == 0 && (lane & 15) == 0 && e < n) SM[2 * u + (lane >> 4)] = (uint8_t)byte_m, SR[2 * u + (lane >> 4)] = (uint8_t)byte_r;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int e = 256 * u + 128 * h + 32 * j + lane;
+            if (e < n) M[e] = (uint8_t)(qm >> (8 * j)), R[e] = (uint8_t)(qr >> (8 * j));
+          }
+          if (lane == 0 && 256 * u + 128 * h < n) SM[2 * u + h] = (uint8_t)byte_m, SR[2 * u + h] = (uint8_t)byte_r;
+        }
+      }
+    }
+  }
+}
+
+template <typename TP, typename TG, int BITS, int MOST>
+__global__ void __launch_bounds__(256) adamw_kernel(const __grid_constant__ AdamList<MOST> list, AdamStep s) {
+  grid_started();
+  int lo = 0, hi = list.count;  // the last tensor whose first CTA is not after this one
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (list.cta[mid] <= blockIdx.x) lo = mid;
+    else hi = mid;
+  }
+  const AdamTensor& t = list.t[lo];
+  grid_ready();
+  if (s.step_device || s.lr_device) adam_factors(s, s.lr_device ? (double)*s.lr_device : s.lr, s.step_device ? *s.step_device : s.step);
+  const float scale = s.scale ? *s.scale : 1.0f;
+  const int64_t at = (int64_t)(blockIdx.x - list.cta[lo]) * kUnit;
+  if (t.vec) adam_pieces<TP, TG, BITS, true>(t, s, scale, at);
+  else adam_pieces<TP, TG, BITS, false>(t, s, scale, at);
+}
+
+template <typename TP, typename TG, int BITS, int MOST>
+int adam_launch(const AdamList<MOST>& list, unsigned ctas, const AdamStep& s, cudaStream_t st) {
+  return launch_overlapped(adamw_kernel<TP, TG, BITS, MOST>, ctas, 256, st, list, s);
+}
+template <int MOST>
+int adam_launch_kind(int kind, const AdamList<MOST>& list, unsigned ctas, const AdamStep& s, cudaStream_t st) {
+  using F = float;
+  using B = __nv_bfloat16;
+  switch (kind) {
+    case 0: return adam_launch<F, F, 32>(list, ctas, s, st);
+    case 1: return adam_launch<F, B, 32>(list, ctas, s, st);
+    case 2: return adam_launch<B, F, 32>(list, ctas, s, st);
+    case 3: return adam_launch<B, B, 32>(list, ctas, s, st);
+    case 4: return adam_launch<F, F, 8>(list, ctas, s, st);
+    case 5: return adam_launch<F, B, 8>(list, ctas, s, st);
+    case 6: return adam_launch<B, F, 8>(list, ctas, s, st);
+    default: return adam_launch<B, B, 8>(list, ctas, s, st);
+  }
+}
+
+bool aligned(const void* p, int to) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)to == 0; }
+bool adam_valid(const b2_adamw_tensor& t) {
+  if (t.n < 0 || t.reserved != 0 || (t.state_bits != 8 && t.state_bits != 32)) return false;
+  if ((t.type_param != B2_TYPE_F32 && t.type_param != B2_TYPE_BF16) || (t.type_grad != B2_TYPE_F32 && t.type_grad != B2_TYPE_BF16)) return false;
+  if (t.n == 0) return true;
+  if (!t.param || !t.grad || !t.m || !t.v || (t.state_bits == 8 && (!t.sm || !t.sv))) return false;
+  const int states = t.state_bits == 8 ? 1 : 4;
+  return aligned(t.param, t.type_param == B2_TYPE_BF16 ? 2 : 4) && aligned(t.grad, t.type_grad == B2_TYPE_BF16 ? 2 : 4) && aligned(t.m, states) && aligned(t.v, states);
+}
+// Whether no parameter shares memory with another: a tensor that occurs twice would be updated by two CTAs at once.
+struct AdamRange {
+  uintptr_t begin, end;
+};
+bool adam_apart(const b2_adamw_tensor* tensors, int count, AdamRange* r) {
+  int n = 0;
+  for (int i = 0; i < count; ++i) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(tensors[i].param);
+    if (tensors[i].n > 0) r[n++] = {at, at + (uintptr_t)tensors[i].n * (tensors[i].type_param == B2_TYPE_BF16 ? 2 : 4)};
+  }
+  std::sort(r, r + n, [](const AdamRange& a, const AdamRange& b) { return a.begin < b.begin; });
+  for (int i = 1; i < n; ++i)
+    if (r[i].begin < r[i - 1].end) return false;
+  return true;
+}
+int adam_kind(const b2_adamw_tensor& t) { return (t.state_bits == 8 ? 4 : 0) + (t.type_param == B2_TYPE_BF16 ? 2 : 0) + (t.type_grad == B2_TYPE_BF16 ? 1 : 0); }
+
+// The tensors of one kind, MOST at a time.
+template <int MOST>
+int adam_run(const b2_adamw_tensor* tensors, int count, int kind, const AdamStep& s, cudaStream_t st) {
+  AdamList<MOST> list;
+  list.count = 0;
+  int64_t ctas = 0;
+  uint64_t first = 0;
+  auto flush = [&]() {
+    const int rc = list.count ? adam_launch_kind(kind, list, (unsigned)ctas, s, st) : B2_OK;
+    list.count = 0, ctas = 0;
+    return rc;
+  };
+  for (int i = 0; i < count; ++i) {
+    const b2_adamw_tensor& t = tensors[i];
+    if (t.n > 0 && adam_kind(t) == kind) {
+      const int64_t more = blocks_of(t.n, kUnit);
+      if (list.count == MOST || ctas + more > 0x7fffffffLL) {
+        const int rc = flush();
+        if (rc) return rc;
+      }
+      const int states = t.state_bits == 8 ? 4 : 16;
+      const bool vec = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.m, states) && aligned(t.v, states);
+      list.cta[list.count] = (uint32_t)ctas;
+      list.t[list.count++] = {t.param, t.grad, t.m, t.v, static_cast<uint8_t*>(t.sm), static_cast<uint8_t*>(t.sv), t.n, first, vec};
+      ctas += more;
+    }
+    first += (uint64_t)blocks_of(t.n, kF8Block) * kF8Block;
+  }
+  return flush();
+}
+
+}  // namespace
+}  // namespace b2
+
+extern "C" int b2_adamw(const b2_adamw_tensor* tensors, int count, double lr, double beta1, double beta2, double eps, double weight_decay,
+                        int64_t step, uint64_t seed, const float* grad_scale, const float* lr_device, const int64_t* step_device,
+                        void* cuda_stream) {
+  using namespace b2;
+  if (count > 0 && !tensors) return -1;
+  if (count < 0) return -2;
+  if (!lr_device && !(lr - lr == 0.0)) return -3;  // infinite or NaN
+  if (!(beta1 >= 0.0 && beta1 < 1.0)) return -4;
+  if (!(beta2 >= 0.0 && beta2 < 1.0)) return -5;
+  if (!(eps >= 0.0)) return -6;
+  if (!(weight_decay - weight_decay == 0.0)) return -7;
+  if (!step_device && step < 1) return -8;
+  int of_kind[8] = {};
+  for (int i = 0; i < count; ++i) {
+    if (!adam_valid(tensors[i]) || blocks_of(tensors[i].n, kUnit) > 0x7fffffffLL) return -1;
+    if (tensors[i].n > 0) ++of_kind[adam_kind(tensors[i])];
+  }
+  AdamRange few[32];
+  std::unique_ptr<AdamRange[]> many(count > 32 ? new (std::nothrow) AdamRange[count] : nullptr);
+  if (count > 32 && !many) return B2_ERR_LAUNCH;
+  if (!adam_apart(tensors, count, many ? many.get() : few)) return -1;
+  AdamStep s = {};
+  s.b1 = (float)beta1, s.a1 = (float)(1.0 - beta1), s.b2 = (float)beta2, s.a2 = (float)(1.0 - beta2), s.eps = (float)eps;
+  s.seed = seed, s.scale = grad_scale, s.lr_device = lr_device, s.step_device = step_device;
+  s.lr = lr, s.wd = weight_decay, s.log_b1 = log(beta1), s.log_b2 = log(beta2), s.step = step;
+  if (!lr_device && !step_device) adam_factors(s, lr, step);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  for (int kind = 0; kind < 8; ++kind) {
+    const int rc = of_kind[kind] == 0 ? B2_OK : of_kind[kind] <= 12 ? adam_run<12>(tensors, count, kind, s, st) : adam_run<240>(tensors, count, kind, s, st);
+    if (rc) return rc;
+  }
+  return B2_OK;
+}

@@ -79,9 +79,9 @@ __device__ __forceinline__ void scales_of(const F8Scale& s, int64_t i, int b, in
   for (int g = 0; g < kGroup; ++g) v[g] = f8_scale_at(s, i, min(b + g, kb - 1));
 }
 
-template <typename TC>
+template <typename TC, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1)
-    f8_fs_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
+    f8_fs_kernel(const F8ArgsOf<OUT> p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char fs_smem_raw[];
   const uint32_t raw = smem_u32(fs_smem_raw);
   unsigned char* ring = fs_smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -342,12 +342,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 }  // namespace
 
-template <typename TC>
-int f8_fs_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
+template <typename TC, typename OUT>
+int f8_fs_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
   static std::atomic<bool> configured[64];
-  return f8_pair_launch(f8_fs_kernel<TC>, configured, kThreads, kSmem, a, r, c, k, st);
+  return f8_pair_launch(f8_fs_kernel<TC, OUT>, configured, kThreads, kSmem, a, r, c, k, st);
 }
-template int f8_fs_launch<float>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
-template int f8_fs_launch<__nv_bfloat16>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_fs_launch<float>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_fs_launch<__nv_bfloat16>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_fs_launch<float>(F8ArgsOf<F8ActOut>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_fs_launch<__nv_bfloat16>(F8ArgsOf<F8ActOut>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
 
 }  // namespace b2

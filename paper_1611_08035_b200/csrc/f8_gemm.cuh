@@ -7,6 +7,7 @@
 #include "b2gemm.h"
 #include "entry.h"
 #include "f8.cuh"
+#include "f8_act.cuh"
 #include "f8_out.cuh"
 #include "tcgen05.cuh"
 
@@ -21,8 +22,10 @@ struct F8Scale {  // value for index i and block b: p[(i >> shift) * si + b * sb
   int shift, f32;
   int words;  // bytes, four consecutive blocks at a time in aligned words
 };
-struct F8Args {
-  F8Out out;
+// OUT: what becomes of the sums, F8Out or F8ActOut
+template <typename OUT>
+struct F8ArgsOf {
+  OUT out;
   int kb;              // blocks of 128 along the summed index
   int splits;          // CTAs of a cluster that share a tile's blocks
   int r_mn, c_mn;      // the operand's own index is contiguous (else the summed one)
@@ -99,8 +102,8 @@ __device__ __forceinline__ void scale_words(const F8Scale& s, int64_t i, int64_t
 }
 
 // Launch of a persistent kernel on pairs of CTAs with 256 x 256 tiles.
-template <typename Kernel>
-int f8_pair_launch(Kernel kfn, std::atomic<bool>* configured, int threads, size_t smem, F8Args a, const F8Operand& r, const F8Operand& c,
+template <typename Kernel, typename OUT>
+int f8_pair_launch(Kernel kfn, std::atomic<bool>* configured, int threads, size_t smem, F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c,
                    int64_t k, cudaStream_t st) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return B2_ERR_LAUNCH;
@@ -119,11 +122,11 @@ int f8_pair_launch(Kernel kfn, std::atomic<bool>* configured, int threads, size_
   return launch_overlapped_as(kfn, dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs)), (unsigned)threads, smem, dim3(2), st, a, mr, mc);
 }
 
-// f8_mx.cu: products whose scales are both e8m0, 256 x 256 tiles; TC = float or __nv_bfloat16
-template <typename TC>
-int f8_mx_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st);
+// f8_mx.cu: products whose scales are both e8m0, 256 x 256 tiles; TC = float or __nv_bfloat16, OUT = F8Out or F8ActOut
+template <typename TC, typename OUT>
+int f8_mx_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st);
 // f8_fs.cu: the same with scales of either type
-template <typename TC>
-int f8_fs_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st);
+template <typename TC, typename OUT>
+int f8_fs_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st);
 
 }  // namespace b2

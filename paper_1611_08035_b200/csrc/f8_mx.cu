@@ -46,9 +46,9 @@ __device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64
       : "memory");
 }
 // CHUNK: chunk_blocks, or 0 where all blocks fit one chunk: then the accumulators are read once and no register holds them before.
-template <typename TC, int CHUNK>
+template <typename TC, int CHUNK, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1)
-    f8_mx_kernel(const F8Args p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
+    f8_mx_kernel(const F8ArgsOf<OUT> p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char mx_smem_raw[];
   const uint32_t raw = smem_u32(mx_smem_raw);
   unsigned char* ring = mx_smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -287,17 +287,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 }  // namespace
 
-template <typename TC>
-int f8_mx_launch(F8Args a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
+template <typename TC, typename OUT>
+int f8_mx_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
   static std::atomic<bool> configured[64];
   constexpr int CHUNK = chunk_blocks<TC>();
   if constexpr (sizeof(TC) == 2) {
     static std::atomic<bool> configured_whole[64];
-    if (a.kb <= CHUNK) return f8_pair_launch(f8_mx_kernel<TC, 0>, configured_whole, kThreads, kSmem, a, r, c, k, st);
+    if (a.kb <= CHUNK) return f8_pair_launch(f8_mx_kernel<TC, 0, OUT>, configured_whole, kThreads, kSmem, a, r, c, k, st);
   }
-  return f8_pair_launch(f8_mx_kernel<TC, CHUNK>, configured, kThreads, kSmem, a, r, c, k, st);
+  return f8_pair_launch(f8_mx_kernel<TC, CHUNK, OUT>, configured, kThreads, kSmem, a, r, c, k, st);
 }
-template int f8_mx_launch<float>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
-template int f8_mx_launch<__nv_bfloat16>(F8Args, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_mx_launch<float>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_mx_launch<__nv_bfloat16>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_mx_launch<float>(F8ArgsOf<F8ActOut>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
+template int f8_mx_launch<__nv_bfloat16>(F8ArgsOf<F8ActOut>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
 
 }  // namespace b2
