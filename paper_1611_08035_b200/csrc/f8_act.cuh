@@ -9,6 +9,8 @@
 // consecutive features of a token, so that the largest magnitude of a block of 128 is at most one exchange away, and matrices pass through a warp's
 // staging rows in both directions: the thread that owns a token's row computes, the lanes together read and write whole pieces of rows.
 #pragma once
+#include <cuda.h>
+
 #include "act.cuh"
 #include "f8_out.cuh"
 
@@ -243,7 +245,7 @@ __device__ __forceinline__ void act_quantise_rows(const F8ActOut& p, int64_t row
     act_rows_out<uint8_t>(p.Q, p.ldq, p.vq, p.rows, p.cols, row0, col0 + j, stage);
   }
 }
-// A thread with whole blocks (the kernels on pairs of CTAs).
+// A thread with whole blocks: the kernels on pairs of CTAs, where a matrix's columns start anywhere.
 template <typename TC, int N>
 __device__ __forceinline__ void f8_emit_staged(const F8ActOut& p, int64_t row0, int64_t col0, float* acc, unsigned char* stage) {
   static_assert(N == kF8Block, "a thread holds one block of a token");
@@ -265,6 +267,203 @@ __device__ __forceinline__ bool act_emit_halves(const F8ActOut& p, int64_t row0,
   if (!named_barrier_all<3, 256>(true)) return false;
   m = max(m, swap[(ew ^ 4) * 32 + lane]);
   act_quantise_rows<N>(p, row0, col0, acc, m, ew < 4, stage);
+  return true;
+}
+
+// ---- tiles of pairs of CTAs --------------------------------------------------------------------------------------------------
+// A thread has a whole block, 128 consecutive features of one token.  Two warps a scheduler have little to hide latencies behind, so that what they do is kept short and
+// nothing in it waits for memory: matrices come and go by TMA through pieces of shared memory, 32 bytes of 32 rows each, swizzled so that the rows' owners read and write
+// them without conflicts (edges are the tensor maps'), what is read one or two pieces ahead; and the bias lies in shared memory.
+// Staged as act_emit_rows does it, 8192 x 4096 x 256 with bias, gelu, Z and Q took 107 us, now 69; with R read by its rows' owners, 64 bytes a row, 78.
+constexpr int kActPiece = 32 * 32;
+constexpr int kActBias = kF8Block * 4;
+// PIECES of a warp; where something is read, all but one are for that.
+template <int PIECES>
+struct F8ActTiles : F8ActOut {
+  static constexpr int WARP_BYTES = PIECES * kActPiece + kActBias;
+  CUtensorMap mz, mc, mq;  // of Z, C and Q where they are written
+  CUtensorMap min;         // of what is read: Z in the gradient form, else R
+};
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* smem, int c_inner, int c_outer) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c_inner), "r"(c_outer),
+               "r"(smem_u32(smem))
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void bulk_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+// A warp's pieces: the last OUT of them for results (all of them, or one where something is read), the others for what is read.
+template <int PIECES>
+struct ActPieces {
+  unsigned char* at;  // the pieces, then the bias
+  uint64_t* bars;     // PIECES - 1, one arrival each
+  int in = 0, out = 0;
+  uint32_t phase = 0;  // of the pieces to read, a bit each
+  int coming = 0;      // loads that have not been waited for
+
+  __device__ __forceinline__ unsigned char* mine(unsigned char* piece, int half) const {
+    const int lane = threadIdx.x & 31;
+    return piece + lane * 32 + ((lane >> 2 & 1) ^ half) * 16;
+  }
+  // 32 bytes of each lane's row to (col, row0 ..) of a matrix
+  __device__ __forceinline__ void put(const CUtensorMap* map, bool reads, int col, int row0, uint4 a, uint4 b) {
+    const bool first = (threadIdx.x & 31) == 0;
+    unsigned char* s = at + (reads ? PIECES - 1 : out) * kActPiece;
+    if (first) {
+      if (reads) bulk_wait_read<0>();
+      else bulk_wait_read<PIECES - 1>();
+    }
+    __syncwarp();
+    *reinterpret_cast<uint4*>(mine(s, 0)) = a;
+    *reinterpret_cast<uint4*>(mine(s, 1)) = b;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (first) {
+      tma_store_2d(map, s, col, row0);
+      bulk_commit();
+    }
+    out = out + 1 == PIECES ? 0 : out + 1;
+  }
+  // the next free piece is filled from (col, row0 ..); results that lay there have left
+  __device__ __forceinline__ void ask(const CUtensorMap* map, int col, int row0) {
+    const int i = in + coming < PIECES - 1 ? in + coming : in + coming - (PIECES - 1);
+    if ((threadIdx.x & 31) == 0) {
+      mbar_arrive_expect_tx(&bars[i], kActPiece);
+      tma_load_2d(at + i * kActPiece, map, col, row0, &bars[i]);
+    }
+    ++coming;
+  }
+  __device__ __forceinline__ bool arrived(uint64_t limit) { return mbar_wait_warp(&bars[in], phase >> in & 1u, limit); }
+  // 32 bytes of each lane's row, once they have arrived; the piece is free for the next ask
+  __device__ __forceinline__ bool take(uint4& a, uint4& b) {
+    if (!arrived(kWaitLimitNs)) return false;
+    a = *reinterpret_cast<const uint4*>(mine(at + in * kActPiece, 0));
+    b = *reinterpret_cast<const uint4*>(mine(at + in * kActPiece, 1));
+    // The loads come before the copy that refills the piece: without a fence nothing orders them (they were moved below it, and found the next numbers).
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    phase ^= 1u << in;
+    in = in + 1 == PIECES - 1 ? 0 : in + 1;
+    --coming;
+    return true;
+  }
+  __device__ __forceinline__ float* bias() const { return reinterpret_cast<float*>(at + PIECES * kActPiece); }
+  // no CTA leaves before its results have, nor before what it asked for has come (where a wait has run out)
+  __device__ __forceinline__ void drain() {
+    for (; coming > 0; --coming) {
+      (void)arrived(kDrainLimitNs);
+      phase ^= 1u << in;
+      in = in + 1 == PIECES - 1 ? 0 : in + 1;
+    }
+    if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+};
+// Before the sums are waited for: the bias of the tile's features, 0 beyond the matrix and where there is none, and the first pieces of what is read.
+template <typename TC, int PIECES>
+__device__ __forceinline__ void act_begin_tile(const F8ActTiles<PIECES>& p, int64_t row0, int64_t col0, ActPieces<PIECES>& pieces) {
+  if (row0 >= p.rows || col0 >= p.cols) return;  // the warp's part of an edge tile lies outside
+  const int64_t col = col0 + 4 * (threadIdx.x & 31);
+  float4 b = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (p.bias) {
+    if (p.vb && col + 4 <= p.cols) {
+      b = *reinterpret_cast<const float4*>(p.bias + col);
+    } else {
+      if (col < p.cols) b.x = p.bias[col];
+      if (col + 1 < p.cols) b.y = p.bias[col + 1];
+      if (col + 2 < p.cols) b.z = p.bias[col + 2];
+      if (col + 3 < p.cols) b.w = p.bias[col + 3];
+    }
+  }
+  if (p.Zin || p.R) {
+#pragma unroll
+    for (int i = 0; i < PIECES - 1; ++i)
+      if (col0 + i * (32 / (int)sizeof(TC)) < p.cols) pieces.ask(&p.min, (int)col0 + i * (32 / (int)sizeof(TC)), (int)row0);
+  }
+  __syncwarp();
+  reinterpret_cast<float4*>(pieces.bias())[threadIdx.x & 31] = b;
+  __syncwarp();
+}
+// False where a wait has run out.
+template <typename TC, int PIECES>
+__device__ __forceinline__ bool act_emit_tile(const F8ActTiles<PIECES>& p, int64_t row0, int64_t col0, float* acc, ActPieces<PIECES>& pieces) {
+  constexpr int G = 32, N = kF8Block, PIECE = 16 / (int)sizeof(TC), W = 2 * PIECE;  // numbers of 16 bytes, of a row of a piece
+  if (row0 >= p.rows || col0 >= p.cols) return true;
+  const int64_t row = row0 + (threadIdx.x & 31);
+  const int end = (int)min((int64_t)N, p.cols - col0);
+  const bool reads = p.Zin || p.R;
+  auto put = [&](const CUtensorMap* map, int c, const float* v) {
+#pragma unroll
+    for (int j = 0; j < G; j += W)
+      if (c + j < end) pieces.put(map, reads, (int)col0 + c + j, (int)row0, act_pack16<TC>(v + j), act_pack16<TC>(v + j + PIECE));
+  };
+  // 32 columns a turn of a loop that is not unrolled, through which the accumulators move
+#pragma unroll 1
+  for (int c = 0; c < N; c += G) {
+    float v[G];
+    const float4* b = reinterpret_cast<const float4*>(pieces.bias()) + c / 4;
+#pragma unroll
+    for (int j = 0; j < G; j += 4) {
+      const float4 f = b[j / 4];
+      const Two x = fma2({acc[j], acc[j + 1]}, both(p.alpha), {f.x, f.y}), y = fma2({acc[j + 2], acc[j + 3]}, both(p.alpha), {f.z, f.w});
+      v[j] = x.a, v[j + 1] = x.b, v[j + 2] = y.a, v[j + 3] = y.b;
+    }
+    if (c < end) {
+      if (p.Z) put(&p.mz, c, v);
+      if (reads) {
+#pragma unroll
+        for (int j = 0; j < G; j += W) {
+          if (c + j >= end) break;
+          uint4 x, y;
+          if (!pieces.take(x, y)) return false;
+          const int ahead = c + j + (PIECES - 1) * W;
+          if (ahead < end) pieces.ask(&p.min, (int)col0 + ahead, (int)row0);
+          float m[W];
+          act_unpack16<TC>(x, m);
+          act_unpack16<TC>(y, m + PIECE);
+          if (p.gradient) {
+            act_slopes<W>(p.act, v + j, m);
+            if (p.R) {  // read in the middle of the work
+              const TC* r = static_cast<const TC*>(p.R) + row * p.ldr + col0 + c + j;
+#pragma unroll
+              for (int e = 0; e < W; ++e) m[e] = row < p.rows && c + j + e < end ? f8_load1(r + e) : 0.0f;
+            }
+          } else {
+            act_values<W>(p.act, v + j);
+          }
+          if (p.R) {
+#pragma unroll
+            for (int e = 0; e < W; e += 2) {
+              const Two t = add2({v[j + e], v[j + e + 1]}, {m[e], m[e + 1]});
+              v[j + e] = t.a, v[j + e + 1] = t.b;
+            }
+          }
+        }
+      } else {
+        act_values<G>(p.act, v);
+      }
+      if (p.C) put(&p.mc, c, v);
+    }
+#pragma unroll
+    for (int j = 0; j < N - G; ++j) acc[j] = acc[j + G];
+#pragma unroll
+    for (int j = 0; j < G; ++j) acc[N - G + j] = v[j];
+  }
+  if (!p.Q) return true;
+  const uint32_t byte = f8_scale_byte(act_amax<N>(acc));
+  if (row < p.rows) p.S[row * p.lds + col0 / kF8Block] = (uint8_t)byte;
+  const float inv = byte == kScaleNan ? 0.0f : f8_inv_scale(byte);
+#pragma unroll
+  for (int j = 0; j < N; j += 32) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float* a = acc + j + 4 * i;
+      const Two x = mul2({a[0], a[1]}, both(inv)), y = mul2({a[2], a[3]}, both(inv));
+      w[i] = byte == kScaleNan ? 0x7f7f7f7fu : f8_pack4(x.a, x.b, y.a, y.b);
+    }
+    if (j < end) pieces.put(&p.mq, reads, (int)col0 + j, (int)row0, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+  }
   return true;
 }
 
@@ -477,5 +676,17 @@ __device__ __forceinline__ void f8_split_join(const F8ActOut& p, void* tile, int
   }
   f8_join_end();
 }
+
+// How the kernels on pairs of CTAs hand a tile over: shared memory of a warp, and whether it is by act_emit_tile.
+template <typename OUT>
+struct ActHandOver {
+  static constexpr int WARP_BYTES = kEmitBytes;
+  static constexpr bool TILES = false;
+};
+template <int PIECES>
+struct ActHandOver<F8ActTiles<PIECES>> {
+  static constexpr int WARP_BYTES = F8ActTiles<PIECES>::WARP_BYTES;
+  static constexpr bool TILES = true;
+};
 
 }  // namespace b2

@@ -16,6 +16,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "f8_gemm.cuh"
 
@@ -31,8 +32,9 @@ constexpr uint32_t kRing = kStageBytes * kStages;
 constexpr int kThreads = 512, kEW = 8, kCols = kBN / 2;
 constexpr int kSlots = 2, kGroup = 4;   // scale ring: slots of four blocks
 constexpr int kSlotFloats = kGroup * (kRows + kBN);  // [block][128 rows, 256 columns]
-constexpr size_t kSmem = 1024 + kRing + 512 + kSlots * kSlotFloats * 4 + kEW * kEmitBytes;
-static_assert(kSmem <= 232448, "a CTA's shared memory");
+template <typename OUT>
+constexpr size_t kSmem = 1024 + kRing + 512 + kSlots * kSlotFloats * 4 + kEW * ActHandOver<OUT>::WARP_BYTES;
+static_assert(kSmem<F8Out> <= 232448 && kSmem<F8ActTiles<2>> <= 232448, "a CTA's shared memory");
 
 __device__ __forceinline__ void umma_f8_pair(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -81,7 +83,7 @@ __device__ __forceinline__ void scales_of(const F8Scale& s, int64_t i, int b, in
 
 template <typename TC, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1)
-    f8_fs_kernel(const F8ArgsOf<OUT> p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
+    f8_fs_kernel(const __grid_constant__ F8ArgsOf<OUT> p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char fs_smem_raw[];
   const uint32_t raw = smem_u32(fs_smem_raw);
   unsigned char* ring = fs_smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -93,6 +95,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* tempty = tfull + 2;
   uint64_t* drained = tempty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+  [[maybe_unused]] uint64_t* act_bars = full + 32;  // 1 for each of the warps that write
   float* scales = reinterpret_cast<float*>(ring + kRing + 512);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -113,6 +116,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&tempty[b], 2 * kEW);
     }
     mbar_init(drained, 1);
+    if constexpr (ActHandOver<OUT>::TILES)
+      for (int i = 0; i < kEW * 1; ++i) mbar_init(&act_bars[i], 1);
     mbar_fence_init();
   }
   if (warp == 1) tmem_alloc_pair(tmem_slot, 2 * kBN);
@@ -253,7 +258,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int quad = warp & 3, half = (warp - 8) >> 2;
     const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
     const uint32_t leader_tempty = cluster_map_shared(smem_u32(tempty), 0);
-    unsigned char* stage = ring + kRing + 512 + kSlots * kSlotFloats * 4 + (warp - 8) * kEmitBytes;
+    unsigned char* stage = ring + kRing + 512 + kSlots * kSlotFloats * 4 + (warp - 8) * ActHandOver<OUT>::WARP_BYTES;
+    constexpr bool TILES = ActHandOver<OUT>::TILES;
+    [[maybe_unused]] ActPieces<2> pieces{stage, act_bars + (warp - 8) * 1};
     RingPos<kSlots> slot;
     uint64_t acc2[kCols / 2];
     const bool one_factor = p.sc.shift == 7;  // the columns of a half share a scale
@@ -262,6 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
       f8_prefetch<TC>(p.out, true, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, 32, (int64_t)tc * kBN + half * kCols, kCols);
+      if constexpr (TILES) act_begin_tile<TC>(p.out, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, (int64_t)tc * kBN + half * kCols, pieces);
 #pragma unroll
       for (int j = 0; j < kCols / 2; ++j) acc2[j] = 0;
       for (int kb = 0; kb < p.kb; ++kb, ++ch) {
@@ -328,10 +336,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+      } else if constexpr (TILES) {
+        if (!act_emit_tile<TC>(p.out, row0, col0, acc, pieces)) {
+          ok = false;
+          if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+        }
       } else {
         f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
       }
     }
+    if constexpr (TILES) pieces.drain();
   }
   __syncwarp();
   tc_fence_before();
@@ -344,8 +358,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 template <typename TC, typename OUT>
 int f8_fs_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
+  if constexpr (std::is_same<OUT, F8ActOut>::value) {
+    F8ActTiles<2> tiles;
+    if (f8_act_tiles<TC>(a.out, r.n, c.n, tiles)) return f8_fs_launch<TC>(f8_args_with(a, tiles), r, c, k, st);
+  }
   static std::atomic<bool> configured[64];
-  return f8_pair_launch(f8_fs_kernel<TC, OUT>, configured, kThreads, kSmem, a, r, c, k, st);
+  return f8_pair_launch(f8_fs_kernel<TC, OUT>, configured, kThreads, kSmem<OUT>, a, r, c, k, st);
 }
 template int f8_fs_launch<float>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
 template int f8_fs_launch<__nv_bfloat16>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);

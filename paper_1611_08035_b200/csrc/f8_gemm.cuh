@@ -101,6 +101,33 @@ __device__ __forceinline__ void scale_words(const F8Scale& s, int64_t i, int64_t
   }
 }
 
+// The epilogue's results as tensor maps, where all its matrices have 16-byte aligned columns.
+template <typename TC, int PIECES>
+bool f8_act_tiles(const F8ActOut& out, int64_t rows, int64_t cols, F8ActTiles<PIECES>& t) {
+  static_cast<F8ActOut&>(t) = out;
+  if ((out.Z || out.Zin) && !out.vz) return false;
+  if ((out.R && !out.vr) || (out.C && !out.vc) || (out.Q && !out.vq)) return false;
+  EncodeFn enc = tensor_map_encode_fn();
+  if (!enc) return false;
+  auto map = [&](CUtensorMap* to, const void* base, int64_t ld, int elem, CUtensorMapDataType type) {
+    if (!base) return true;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * (cuuint64_t)elem};
+    const cuuint32_t box[2] = {32u / (cuuint32_t)elem, 32u}, estr[2] = {1, 1};
+    return enc(to, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  const CUtensorMapDataType type = sizeof(TC) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  return map(&t.mz, out.Z, out.ldz, (int)sizeof(TC), type) && map(&t.mc, out.C, out.ldc, (int)sizeof(TC), type) && map(&t.mq, out.Q, out.ldq, 1, CU_TENSOR_MAP_DATA_TYPE_UINT8) &&
+         map(&t.min, out.Zin ? out.Zin : out.R, out.Zin ? out.ldz : out.ldr, (int)sizeof(TC), type);
+}
+template <typename OUT>
+F8ArgsOf<OUT> f8_args_with(const F8ArgsOf<F8ActOut>& a, const OUT& out) {
+  F8ArgsOf<OUT> b = {};
+  b.out = out, b.kb = a.kb, b.status = a.status;  // the launch sets the others
+  return b;
+}
+
 // Launch of a persistent kernel on pairs of CTAs with 256 x 256 tiles.
 template <typename Kernel, typename OUT>
 int f8_pair_launch(Kernel kfn, std::atomic<bool>* configured, int threads, size_t smem, F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c,

@@ -19,6 +19,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "f8_gemm.cuh"
 
@@ -34,7 +35,9 @@ constexpr uint32_t kRing = kStageBytes * kStages;
 constexpr int kThreads = 512, kEW = 8, kCols = kBN / 2;
 constexpr uint32_t kTmem = 512, kSfCols = 12;  // scales of four blocks: 128 rows in 4 columns, 256 columns in 8
 constexpr uint32_t kSfBytes = 2 * kSfCols * 32 * 4;
-constexpr size_t kSmem = 1024 + kRing + 512 + kSfBytes + kEW * kEmitBytes;
+template <typename OUT>
+constexpr size_t kSmem = 1024 + kRing + 512 + kSfBytes + kEW * ActHandOver<OUT>::WARP_BYTES;
+static_assert(kSmem<F8ActTiles<3>> <= 232448, "a CTA's shared memory");
 
 __device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                         uint32_t accumulate) {
@@ -48,7 +51,7 @@ __device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64
 // CHUNK: chunk_blocks, or 0 where all blocks fit one chunk: then the accumulators are read once and no register holds them before.
 template <typename TC, int CHUNK, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1)
-    f8_mx_kernel(const F8ArgsOf<OUT> p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
+    f8_mx_kernel(const __grid_constant__ F8ArgsOf<OUT> p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char mx_smem_raw[];
   const uint32_t raw = smem_u32(mx_smem_raw);
   unsigned char* ring = mx_smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -60,6 +63,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* tempty = tfull + 1;
   uint64_t* drained = tempty + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+  [[maybe_unused]] uint64_t* act_bars = full + 32;  // 2 for each of the warps that write
   uint32_t* sf_words = reinterpret_cast<uint32_t*>(ring + kRing + 512);  // [2][kSfCols][32]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -78,6 +82,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(tfull, 1);
     mbar_init(tempty, 2 * kEW);
     mbar_init(drained, 1);
+    if constexpr (ActHandOver<OUT>::TILES)
+      for (int i = 0; i < kEW * 2; ++i) mbar_init(&act_bars[i], 1);
     mbar_fence_init();
   }
   if (warp == 1) tmem_alloc_pair(tmem_slot, kTmem);
@@ -228,13 +234,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kCols);
     const uint32_t leader_tempty = cluster_map_shared(smem_u32(tempty), 0);
     const uint64_t limit = kWaitLimitNs + (uint64_t)p.kb * 8192ull;  // outlasts the k loop that it waits for
-    unsigned char* stage = ring + kRing + 512 + kSfBytes + (warp - 8) * kEmitBytes;
+    unsigned char* stage = ring + kRing + 512 + kSfBytes + (warp - 8) * ActHandOver<OUT>::WARP_BYTES;
+    constexpr bool TILES = ActHandOver<OUT>::TILES;
+    [[maybe_unused]] ActPieces<3> pieces{stage, act_bars + (warp - 8) * 2};
     float acc[kCols];
     int ch = 0;
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
-      if constexpr (CHUNK == 0) f8_prefetch<TC>(p.out, true, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, 32, (int64_t)tc * kBN + half * kCols, kCols);
+      if constexpr (CHUNK == 0 || TILES) f8_prefetch<TC>(p.out, true, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, 32, (int64_t)tc * kBN + half * kCols, kCols);
+      if constexpr (TILES) act_begin_tile<TC>(p.out, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, (int64_t)tc * kBN + half * kCols, pieces);
       if constexpr (CHUNK > 0) {
 #pragma unroll
         for (int j = 0; j < kCols; ++j) acc[j] = 0.0f;
@@ -273,10 +282,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int64_t row0 = (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, col0 = (int64_t)tc * kBN + half * kCols;
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+      } else if constexpr (TILES) {
+        if (!act_emit_tile<TC>(p.out, row0, col0, acc, pieces)) {
+          ok = false;
+          if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
+        }
       } else {
         f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
       }
     }
+    if constexpr (TILES) pieces.drain();
   }
   __syncwarp();
   tc_fence_before();
@@ -289,13 +304,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 template <typename TC, typename OUT>
 int f8_mx_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
+  if constexpr (std::is_same<OUT, F8ActOut>::value) {
+    F8ActTiles<3> tiles;
+    if (f8_act_tiles<TC>(a.out, r.n, c.n, tiles)) return f8_mx_launch<TC>(f8_args_with(a, tiles), r, c, k, st);
+  }
   static std::atomic<bool> configured[64];
   constexpr int CHUNK = chunk_blocks<TC>();
-  if constexpr (sizeof(TC) == 2) {
+  if constexpr (sizeof(TC) == 2 && !ActHandOver<OUT>::TILES) {
     static std::atomic<bool> configured_whole[64];
-    if (a.kb <= CHUNK) return f8_pair_launch(f8_mx_kernel<TC, 0, OUT>, configured_whole, kThreads, kSmem, a, r, c, k, st);
+    if (a.kb <= CHUNK) return f8_pair_launch(f8_mx_kernel<TC, 0, OUT>, configured_whole, kThreads, kSmem<OUT>, a, r, c, k, st);
   }
-  return f8_pair_launch(f8_mx_kernel<TC, CHUNK, OUT>, configured, kThreads, kSmem, a, r, c, k, st);
+  return f8_pair_launch(f8_mx_kernel<TC, CHUNK, OUT>, configured, kThreads, kSmem<OUT>, a, r, c, k, st);
 }
 template int f8_mx_launch<float>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
 template int f8_mx_launch<__nv_bfloat16>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
