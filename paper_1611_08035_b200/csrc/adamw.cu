@@ -14,6 +14,7 @@
 #include <memory>
 #include <new>
 
+#include "act.cuh"
 #include "b2gemm.h"
 #include "common.cuh"
 #include "entry.h"
@@ -47,7 +48,7 @@ struct AdamStep {
   double lr, wd, log_b1, log_b2;
   int64_t step;
 };
-constexpr int kPieces = 2;                    // of 256 elements, a warp's
+constexpr int kPieces = 2;                    // of 256 elements, a warp's: 512, four blocks of 8-bit states
 constexpr int kUnit = 8 * 256 * kPieces;      // elements of a CTA
 
 // The finaliser of MurmurHash3 (Austin Appleby, public domain).
@@ -133,38 +134,23 @@ __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep&
       At4::store(V, 256 * u, n, v);
     }
   } else {
+    static_assert(!VEC, "aligned elements are adam_512's");
     uint8_t *M = static_cast<uint8_t*>(t.m) + at, *R = static_cast<uint8_t*>(t.v) + at;
     uint8_t *SM = t.sm + at / kF8Block, *SR = t.sv + at / kF8Block;
-    uint32_t m8[kPieces][2], r8[kPieces][2], sm[kPieces][2], sr[kPieces][2];
+    uint32_t m8[kPieces][2], r8[kPieces][2], sm[kPieces][2], sr[kPieces][2];  // half h of a lane's numbers is of block h
 #pragma unroll
-    for (int u = 0; u < kPieces; ++u) {
+    for (int u = 0; u < kPieces; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         m8[u][h] = r8[u][h] = 0;
-        if constexpr (VEC) {
-          const int e = 256 * u + 8 * lane + 4 * h;
-          if (e + 4 <= n) {
-            m8[u][h] = *reinterpret_cast<const uint32_t*>(M + e), r8[u][h] = *reinterpret_cast<const uint32_t*>(R + e);
-          } else {
 #pragma unroll
-            for (int j = 0; j < 3; ++j)
-              if (e + j < n) m8[u][h] |= (uint32_t)M[e + j] << (8 * j), r8[u][h] |= (uint32_t)R[e + j] << (8 * j);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int e = 256 * u + 128 * h + 32 * j + lane;
-            if (e < n) m8[u][h] |= (uint32_t)M[e] << (8 * j), r8[u][h] |= (uint32_t)R[e] << (8 * j);
-          }
+        for (int j = 0; j < 4; ++j) {
+          const int e = 256 * u + 128 * h + 32 * j + lane;
+          if (e < n) m8[u][h] |= (uint32_t)M[e] << (8 * j), r8[u][h] |= (uint32_t)R[e] << (8 * j);
         }
-      }
-      // VEC: both halves of a lane's eight lie in block lane / 16; else half h is of block h
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int b = 2 * u + (VEC ? lane >> 4 : h);
+        const int b = 2 * u + h;
         sm[u][h] = b * kF8Block < n ? SM[b] : 127u, sr[u][h] = b * kF8Block < n ? SR[b] : 127u;
       }
-    }
     const uint64_t e0 = t.first + (uint64_t)at;
 #pragma unroll
     for (int u = 0; u < kPieces; ++u) {
@@ -180,65 +166,177 @@ __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep&
         most_m[j >> 2] = max(most_m[j >> 2], mag_bits(m[j])), most_r[j >> 2] = max(most_r[j >> 2], mag_bits(r[j]));
       }
       AtP::store(P, 256 * u, n, p);
-      if constexpr (VEC) {
-        uint32_t a = max(most_m[0], most_m[1]), b = max(most_r[0], most_r[1]);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o)), b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
-        most_m[0] = most_m[1] = a, most_r[0] = most_r[1] = b;
-      } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) most_m[h] = __reduce_max_sync(0xffffffffu, most_m[h]), most_r[h] = __reduce_max_sync(0xffffffffu, most_r[h]);
-      }
-      uint32_t hm = 0, hr = 0;
-      auto hash = [&](uint64_t e) {
-        const uint64_t e8 = e >> 3;
-        hm = fmix((uint32_t)e8 + fmix((uint32_t)(e8 >> 32) + s.key)), hr = fmix(hm + kGolden);
-      };
-      if constexpr (VEC) hash(e0 + 256 * u + 8 * lane);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t byte_m = f8_scale_byte(most_m[h]), byte_r = f8_scale_byte(most_r[h]);
+        const uint32_t byte_m = f8_scale_byte(__reduce_max_sync(0xffffffffu, most_m[h])), byte_r = f8_scale_byte(__reduce_max_sync(0xffffffffu, most_r[h]));
         const float inv_m = byte_m == kScaleNan ? 0.0f : f8_inv_scale(byte_m), inv_r = byte_r == kScaleNan ? 0.0f : f8_inv_scale(byte_r);
         float a[4], b[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          uint32_t i = 4 * h + j;
-          if constexpr (!VEC) {
-            const uint64_t e = e0 + 256 * u + 128 * h + 32 * j + lane;
-            hash(e), i = (uint32_t)e & 7u;
-          }
-          a[j] = f8_at_random(__fmul_rn(m[4 * h + j], inv_m), (hm + i * kGolden) >> 12);
+          const uint64_t e = e0 + 256 * u + 128 * h + 32 * j + lane, e8 = e >> 3;
+          const uint32_t hm = fmix((uint32_t)e8 + fmix((uint32_t)(e8 >> 32) + s.key)), hr = fmix(hm + kGolden), i = ((uint32_t)e & 7u) * kGolden;
+          a[j] = f8_at_random(__fmul_rn(m[4 * h + j], inv_m), (hm + i) >> 12);
           const float y = __fmul_rn(r[4 * h + j], inv_r);
-          b[j] = f8_at_random(y, (hr + i * kGolden) >> 12);
+          b[j] = f8_at_random(y, (hr + i) >> 12);
           b[j] = y > 0.0f ? fmaxf(b[j], 0.001953125f) : b[j];  // 2^-9
         }
         const uint32_t qm = byte_m == kScaleNan ? 0x7f7f7f7fu : f8_pack4(a[0], a[1], a[2], a[3]);
         const uint32_t qr = byte_r == kScaleNan ? 0x7f7f7f7fu : f8_pack4(b[0], b[1], b[2], b[3]);
-        if constexpr (VEC) {
-          const int e = 256 * u + 8 * lane + 4 * h;
-          if (e + 4 <= n) {
-            *reinterpret_cast<uint32_t*>(M + e) = qm, *reinterpret_cast<uint32_t*>(R + e) = qr;
-          } else {
 #pragma unroll
-            for (int j = 0; j < 3; ++j)
-              if (e + j < n) M[e + j] = (uint8_t)(qm >> (8 * j)), R[e + j] = (uint8_t)(qr >> (8 * j));
-          }
-          if (h == 0 && (lane & 15) == 0 && e < n) SM[2 * u + (lane >> 4)] = (uint8_t)byte_m, SR[2 * u + (lane >> 4)] = (uint8_t)byte_r;
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int e = 256 * u + 128 * h + 32 * j + lane;
-            if (e < n) M[e] = (uint8_t)(qm >> (8 * j)), R[e] = (uint8_t)(qr >> (8 * j));
-          }
-          if (lane == 0 && 256 * u + 128 * h < n) SM[2 * u + h] = (uint8_t)byte_m, SR[2 * u + h] = (uint8_t)byte_r;
+        for (int j = 0; j < 4; ++j) {
+          const int e = 256 * u + 128 * h + 32 * j + lane;
+          if (e < n) M[e] = (uint8_t)(qm >> (8 * j)), R[e] = (uint8_t)(qr >> (8 * j));
         }
+        if (lane == 0 && 256 * u + 128 * h < n) SM[2 * u + h] = (uint8_t)byte_m, SR[2 * u + h] = (uint8_t)byte_r;
       }
     }
   }
 }
 
+// ---- 512 aligned elements of a warp, states in 8 bits -------------------------------------------------------------------------
+// 14 bytes an element leave a GPU some eighty instructions for it, which one at a time they were not enough (109: 1000 us for 268 million elements, 574 by the bytes).  So this
+// path does as much as it can two numbers at a time and gives a lane sixteen consecutive elements (eight lanes to a block).  Numbers below 2^-6 of their scale, whose
+// distance is not the binade's, take a branch; a warp with a v for which the root below is not exact, or not finite, goes to adam_pieces before it has written anything.
+
+// Square roots, rounded to nearest: an approximation of the reciprocal root, and from it one Newton step on the root with the exact remainder (P. Markstein, IBM Journal of
+// Research and Development 34, 1990).  0, and 2^-100 to the largest finite number, give __fsqrt_rn's results: tried for every mantissa and both parities of the exponent.
+__device__ __forceinline__ float rsqrt_approx(float x) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ Two sqrt2_rn(Two v) {
+  const Two y = {rsqrt_approx(fmaxf(v.a, 0x1p-100f)), rsqrt_approx(fmaxf(v.b, 0x1p-100f))}, s = mul2(v, y), h = mul2(y, both(0.5f));
+  const Two e = fma2({-s.a, -s.b}, s, v);
+  return fma2(e, h, s);
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+// Sixteen magnitudes' largest, NaN where there is one, and smallest.
+struct Extent {
+  float most, least;
+};
+__device__ __forceinline__ Extent extent16(const float* x) {
+  Extent e{fabsf(x[0]), fabsf(x[0])};
+#pragma unroll
+  for (int j = 1; j < 16; ++j) e.most = max_nan(e.most, fabsf(x[j])), e.least = fminf(e.least, fabsf(x[j]));
+  return e;
+}
+// Sixteen numbers of a block as e4m3, with the random bits of two hashes.
+template <bool ROOT>
+__device__ __forceinline__ uint4 quantise16(const float* x, uint32_t byte, float least, uint32_t h0, uint32_t h1) {
+  if (byte == kScaleNan) return make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
+  const float inv = f8_inv_scale(byte);
+  const bool plain = least * inv >= 0.015625f;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float t[4];
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+      const Two y = mul2({x[4 * i + j], x[4 * i + j + 1]}, both(inv));
+      t[j] = y.a, t[j + 1] = y.b;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t bits = ((i < 2 ? h0 : h1) + (uint32_t)((4 * i + j) & 7) * kGolden) >> 12;
+      if (plain) {
+        t[j] = __uint_as_float((__float_as_uint(t[j]) + bits) & 0xfff00000u);
+      } else {
+        const float y = t[j];
+        t[j] = f8_at_random(y, bits);
+        if (ROOT) t[j] = y > 0.0f ? fmaxf(t[j], 0.001953125f) : t[j];
+      }
+    }
+    w[i] = f8_pack4(t[0], t[1], t[2], t[3]);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void load16(const float* p, uint4 (&q)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = reinterpret_cast<const uint4*>(p)[i];
+}
+__device__ __forceinline__ void load16(const __nv_bfloat16* p, uint4 (&q)[2]) { q[0] = reinterpret_cast<const uint4*>(p)[0], q[1] = reinterpret_cast<const uint4*>(p)[1]; }
+__device__ __forceinline__ Two pair16(const uint4 (&q)[4], int i) {
+  const uint4 w = q[i / 2];
+  return i & 1 ? Two{__uint_as_float(w.z), __uint_as_float(w.w)} : Two{__uint_as_float(w.x), __uint_as_float(w.y)};
+}
+__device__ __forceinline__ Two pair16(const uint4 (&q)[2], int i) {
+  const uint4 v = q[i / 4];
+  const uint32_t w = (i & 3) == 0 ? v.x : (i & 3) == 1 ? v.y : (i & 3) == 2 ? v.z : v.w;
+  return {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
+}
+__device__ __forceinline__ void store16(float* p, const float* v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const float* v) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    reinterpret_cast<uint4*>(p)[i] = make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]), pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
+}
+__device__ __forceinline__ void load8x16(const uint8_t* p, uint32_t (&w)[4]) {  // 8-byte aligned
+  const uint2 a = reinterpret_cast<const uint2*>(p)[0], b = reinterpret_cast<const uint2*>(p)[1];
+  w[0] = a.x, w[1] = a.y, w[2] = b.x, w[3] = b.y;
+}
+__device__ __forceinline__ void store8x16(uint8_t* p, uint4 w) {
+  reinterpret_cast<uint2*>(p)[0] = make_uint2(w.x, w.y), reinterpret_cast<uint2*>(p)[1] = make_uint2(w.z, w.w);
+}
+
+// False, with nothing written, where a root is not exact.
+template <typename TP, typename TG>
+__device__ __forceinline__ bool adam_512(const AdamTensor& t, const AdamStep& s, float scale, int64_t at) {
+  const int lane = threadIdx.x & 31, block = lane >> 3;
+  const int64_t e0 = at + 16 * lane;
+  TP* P = static_cast<TP*>(t.p) + e0;
+  uint8_t *M = static_cast<uint8_t*>(t.m) + e0, *R = static_cast<uint8_t*>(t.v) + e0, *SM = t.sm + at / kF8Block + block, *SR = t.sv + at / kF8Block + block;
+  uint4 pq[sizeof(TP)], gq[sizeof(TG)];
+  uint32_t mq[4], rq[4];
+  load16(P, pq);
+  load16(static_cast<const TG*>(t.g) + e0, gq);
+  load8x16(M, mq), load8x16(R, rq);
+  const float sm = e8m0_value(*SM), sr = e8m0_value(*SR);
+  float p[16], m[16], r[16];
+  uint32_t least_v = 0xffffffffu;  // of the bits of v, less one, so that 0 is the largest
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a[4], b[4];
+    f8_unpack4(mq[i], a), f8_unpack4(rq[i], b);
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+      const int k = 4 * i + j;
+      const Two g = mul2(pair16(gq, k / 2), both(scale));
+      const Two mo = mul2({a[j], a[j + 1]}, both(sm)), ro = mul2({b[j], b[j + 1]}, both(sr));
+      const Two mn = add2(mul2(mo, both(s.b1)), mul2(g, both(s.a1)));
+      const Two v = add2(mul2(mul2(ro, ro), both(s.b2)), mul2(mul2(g, g), both(s.a2)));
+      const Two rn = sqrt2_rn(v);
+      least_v = min(least_v, min(__float_as_uint(v.a) - 1u, __float_as_uint(v.b) - 1u));
+      const Two step = mul2(mul2(mn, both(s.size)), rcp_approx(fma2(rn, both(s.root), both(s.eps))));
+      const Two pn = add2(mul2(pair16(pq, k / 2), both(s.decay)), {-step.a, -step.b});
+      m[k] = mn.a, m[k + 1] = mn.b, r[k] = rn.a, r[k + 1] = rn.b, p[k] = pn.a, p[k + 1] = pn.b;
+    }
+  }
+  const Extent em = extent16(m), er = extent16(r);
+  if (__any_sync(0xffffffffu, least_v < 0x0d800000u - 1u || !(er.most <= 0x1p64f))) return false;  // 2^-100
+  store16(P, p);
+  float am = em.most, ar = er.most;
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) am = max_nan(am, __shfl_xor_sync(0xffffffffu, am, o)), ar = max_nan(ar, __shfl_xor_sync(0xffffffffu, ar, o));
+  const uint32_t bm = f8_scale_byte(__float_as_uint(am)), br = f8_scale_byte(__float_as_uint(ar));
+  const uint64_t e8 = (t.first + (uint64_t)e0) >> 3;  // even: both hashes have the same high half
+  const uint32_t high = fmix((uint32_t)(e8 >> 32) + s.key);
+  const uint32_t h0 = fmix((uint32_t)e8 + high), h1 = fmix((uint32_t)e8 + 1 + high);
+  store8x16(M, quantise16<false>(m, bm, em.least, h0, h1));
+  store8x16(R, quantise16<true>(r, br, er.least, fmix(h0 + kGolden), fmix(h1 + kGolden)));
+  if ((lane & 7) == 0) *SM = (uint8_t)bm, *SR = (uint8_t)br;
+  return true;
+}
+
 template <typename TP, typename TG, int BITS, int MOST>
-__global__ void __launch_bounds__(256) adamw_kernel(const __grid_constant__ AdamList<MOST> list, AdamStep s) {
+__global__ void __launch_bounds__(256, BITS == 8 ? 3 : 2) adamw_kernel(const __grid_constant__ AdamList<MOST> list, AdamStep s) {
   grid_started();
   int lo = 0, hi = list.count;  // the last tensor whose first CTA is not after this one
   while (hi - lo > 1) {
@@ -251,8 +349,14 @@ __global__ void __launch_bounds__(256) adamw_kernel(const __grid_constant__ Adam
   if (s.step_device || s.lr_device) adam_factors(s, s.lr_device ? (double)*s.lr_device : s.lr, s.step_device ? *s.step_device : s.step);
   const float scale = s.scale ? *s.scale : 1.0f;
   const int64_t at = (int64_t)(blockIdx.x - list.cta[lo]) * kUnit;
-  if (t.vec) adam_pieces<TP, TG, BITS, true>(t, s, scale, at);
-  else adam_pieces<TP, TG, BITS, false>(t, s, scale, at);
+  if constexpr (BITS == 8) {
+    const int64_t mine = at + (threadIdx.x >> 5) * (256 * kPieces);
+    if (t.vec && mine + 512 <= t.n && adam_512<TP, TG>(t, s, scale, mine)) return;
+    adam_pieces<TP, TG, 8, false>(t, s, scale, at);  // also what does not start on 16 bytes, and the ends
+  } else {
+    if (t.vec) adam_pieces<TP, TG, 32, true>(t, s, scale, at);
+    else adam_pieces<TP, TG, 32, false>(t, s, scale, at);
+  }
 }
 
 template <typename TP, typename TG, int BITS, int MOST>
@@ -321,7 +425,7 @@ int adam_run(const b2_adamw_tensor* tensors, int count, int kind, const AdamStep
         const int rc = flush();
         if (rc) return rc;
       }
-      const int states = t.state_bits == 8 ? 4 : 16;
+      const int states = t.state_bits == 8 ? 8 : 16;
       const bool vec = aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.m, states) && aligned(t.v, states);
       list.cta[list.count] = (uint32_t)ctas;
       list.t[list.count++] = {t.param, t.grad, t.m, t.v, static_cast<uint8_t*>(t.sm), static_cast<uint8_t*>(t.sv), t.n, first, vec};
