@@ -41,6 +41,8 @@ __device__ __forceinline__ float at_least(float x, float b) {
   return y;
 }
 
+__device__ __forceinline__ float larger_nan(float a, float b) { return at_least(a, b); }
+
 // Two numbers at a time: the packed fp32 instructions do both for one.
 struct Two {
   float a, b;

@@ -210,11 +210,6 @@ __device__ __forceinline__ Two sqrt2_rn(Two v) {
   const Two e = fma2({-s.a, -s.b}, s, v);
   return fma2(e, h, s);
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
 // Sixteen magnitudes' largest, NaN where there is one, and smallest.
 struct Extent {
   float most, least;
@@ -222,7 +217,7 @@ struct Extent {
 __device__ __forceinline__ Extent extent16(const float* x) {
   Extent e{fabsf(x[0]), fabsf(x[0])};
 #pragma unroll
-  for (int j = 1; j < 16; ++j) e.most = max_nan(e.most, fabsf(x[j])), e.least = fminf(e.least, fabsf(x[j]));
+  for (int j = 1; j < 16; ++j) e.most = larger_nan(e.most, fabsf(x[j])), e.least = fminf(e.least, fabsf(x[j]));
   return e;
 }
 // Sixteen numbers of a block as e4m3, with the random bits of two hashes.
@@ -324,7 +319,7 @@ __device__ __forceinline__ bool adam_512(const AdamTensor& t, const AdamStep& s,
   store16(P, p);
   float am = em.most, ar = er.most;
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) am = max_nan(am, __shfl_xor_sync(0xffffffffu, am, o)), ar = max_nan(ar, __shfl_xor_sync(0xffffffffu, ar, o));
+  for (int o = 4; o > 0; o >>= 1) am = larger_nan(am, __shfl_xor_sync(0xffffffffu, am, o)), ar = larger_nan(ar, __shfl_xor_sync(0xffffffffu, ar, o));
   const uint32_t bm = f8_scale_byte(__float_as_uint(am)), br = f8_scale_byte(__float_as_uint(ar));
   const uint64_t e8 = (t.first + (uint64_t)e0) >> 3;  // even: both hashes have the same high half
   const uint32_t high = fmix((uint32_t)(e8 >> 32) + s.key);

@@ -27,7 +27,7 @@ def test_gemm_act_refusals(b2):
 
 
 def test_act_backward_refusals(b2):
-    good = dict(d=200, t=300, type=1, act=4, DY=F, lddy=200, Z=F, ldz=200, DZ=F, lddz=200, Q=F, ldq=200, S=F, lds=2, db=F, ws=F, n=1 << 30)
+    good = dict(d=200, t=3000, type=1, act=4, DY=F, lddy=200, Z=F, ldz=200, DZ=F, lddz=200, Q=F, ldq=200, S=F, lds=2, db=F, ws=F, n=1 << 30)
 
     def call(**kw):
         return b2.lib().b2_act_backward(*{**good, **kw}.values(), None)
@@ -38,7 +38,7 @@ def test_act_backward_refusals(b2):
     assert call(ws=None) == 1003 and call(n=16) == 1003 and call(ws=ctypes.c_void_p(4100)) == 1003
     assert call(d=0, DY=None, Z=None) == 0 and call(DZ=None, Q=None, db=None) == 0
     assert b2.b2_act_backward_workspace_bytes(200, 0) == 0 and b2.b2_act_backward_workspace_bytes(200, 8) == 0
-    assert b2.b2_act_backward_workspace_bytes(200, 300) % 256 == 0
+    assert b2.b2_act_backward_workspace_bytes(200, 3000) % 256 == 0
 
 
 def test_adamw_refusals(b2):
