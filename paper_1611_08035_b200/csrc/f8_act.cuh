@@ -73,17 +73,21 @@ __device__ __forceinline__ void act_rows_out(T* M, int64_t ld, bool vec, int64_t
   if (vec) {
     const int64_t c = col + (lane & 3) * PIECE, nv = cols - c;
     const unsigned char* from = stage + (lane >> 2) * kEmitPitch + (lane & 3) * 16;
+    uint4 q[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t row = row0 + 8 * i + (lane >> 2);
-      if (row < rows) {
-        const uint4 q = *reinterpret_cast<const uint4*>(from + 8 * i * kEmitPitch);
-        if (nv >= PIECE) {
-          *reinterpret_cast<uint4*>(m + row * ld + c) = q;
-        } else {
-          const Bits* b = reinterpret_cast<const Bits*>(from + 8 * i * kEmitPitch);
-          for (int e = 0; e < nv; ++e) m[row * ld + c + e] = b[e];
-        }
+    for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const uint4*>(from + 8 * i * kEmitPitch);
+    Bits* to = m + (row0 + (lane >> 2)) * ld + c;
+    if (row0 + 32 <= rows && col + W <= cols) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i, to += 8 * ld) *reinterpret_cast<uint4*>(to) = q[i];
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i, to += 8 * ld) {
+        if (row0 + 8 * i + (lane >> 2) >= rows) break;
+        const Bits* b = reinterpret_cast<const Bits*>(from + 8 * i * kEmitPitch);
+        if (nv >= PIECE) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(b);
+        else
+          for (int e = 0; e < nv; ++e) to[e] = b[e];
       }
     }
   } else {  // columns that start anywhere: neighbouring lanes, neighbouring elements
@@ -116,19 +120,24 @@ __device__ __forceinline__ void act_get(const void* M, int64_t ld, bool vec, con
   if (vec) {
     const int64_t c = col + (lane & 3) * PIECE, nv = p.cols - c;
     unsigned char* to = stage + (lane >> 2) * kEmitPitch + (lane & 3) * 16;
+    const Bits* from = m + (row0 + (lane >> 2)) * ld + c;
     uint4 q[4];
+    if (row0 + 32 <= p.rows && col + W <= p.cols) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t row = row0 + 8 * i + (lane >> 2);
-      q[i] = make_uint4(0, 0, 0, 0);
-      if (row < p.rows && nv >= PIECE) q[i] = *reinterpret_cast<const uint4*>(m + row * ld + c);
-    }
+      for (int i = 0; i < 4; ++i, from += 8 * ld) q[i] = *reinterpret_cast<const uint4*>(from);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + 8 * i * kEmitPitch) = q[i];
-    if (nv > 0 && nv < PIECE) {
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + 8 * i * kEmitPitch) = q[i];
+    } else {
+#pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + 8 * i + (lane >> 2);
-        for (int e = 0; row < p.rows && e < nv; ++e) reinterpret_cast<Bits*>(to + 8 * i * kEmitPitch)[e] = m[row * ld + c + e];
+        q[i] = make_uint4(0, 0, 0, 0);
+        if (row0 + 8 * i + (lane >> 2) < p.rows && nv >= PIECE) q[i] = *reinterpret_cast<const uint4*>(from + 8 * i * ld);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + 8 * i * kEmitPitch) = q[i];
+      if (nv > 0 && nv < PIECE) {
+        for (int i = 0; i < 4 && row0 + 8 * i + (lane >> 2) < p.rows; ++i, from += 8 * ld)
+          for (int e = 0; e < nv; ++e) reinterpret_cast<Bits*>(to + 8 * i * kEmitPitch)[e] = from[e];
       }
     }
   } else {
@@ -155,6 +164,32 @@ __device__ __forceinline__ void f8_prefetch(const F8ActOut& p, bool, int64_t row
     for (int i = threadIdx.x & 31; i < lines; i += 32)
       for (int e = 0; e < count; e += 128 / (int)sizeof(TC))
         if (row0 + i < p.rows && first + e < p.cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(m + (row0 + i) * ld + first + e));
+  }
+}
+
+// The bias of `count` features from `first` on.
+__device__ __forceinline__ void act_prefetch_bias(const F8ActOut& p, int64_t first, int count, int64_t features) {
+  const int i = (threadIdx.x & 31) * 32;
+  if (p.bias && i < count && first + i < features) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.bias + first + i));
+}
+// What a warp of a small tile will read, on its way while the tile is computed: its rows (COLS_CONTIG) or columns, `count` numbers each; of a split's, the part that this CTA
+// will add up.
+template <typename TC, bool COLS_CONTIG, int TBN>
+__device__ __forceinline__ void act_prefetch_small(const F8ActOut& p, int64_t row0, int64_t col0, int ew, int workers, int splits, int share) {
+  constexpr int INNER = COLS_CONTIG ? TBN : 128, OUTER = COLS_CONTIG ? 128 : TBN;
+  const int64_t feature0 = COLS_CONTIG ? col0 : row0, token0 = COLS_CONTIG ? row0 : col0, features = COLS_CONTIG ? p.cols : p.rows, tokens = COLS_CONTIG ? p.rows : p.cols;
+  if (ew == 0) act_prefetch_bias(p, feature0, INNER, features);
+  const int per = OUTER / splits;
+  for (int o = ew * 32 + (threadIdx.x & 31); o < per; o += 32 * workers) {
+    const int64_t token = token0 + share * per + o;
+    if (token >= tokens) break;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const TC* m = static_cast<const TC*>(which ? p.R : p.Zin);
+      if (!m) continue;
+      m += token * (which ? p.ldr : p.ldz) + feature0;
+      for (int e = 0; e < INNER && feature0 + e < features; e += 128 / (int)sizeof(TC)) asm volatile("prefetch.global.L2 [%0];" ::"l"(m + e));
+    }
   }
 }
 
@@ -208,8 +243,10 @@ __device__ __forceinline__ void act_emit_rows(const F8ActOut& p, int64_t row0, i
         for (int h = 0; h < G; h += W) act_put<TC>(p.C, p.ldc, p.vc, p, row0, col + h, v + h, stage);
       }
     }
+    if (col + G > p.cols) {  // a block's largest magnitude is that of the matrix's own numbers
 #pragma unroll
-    for (int j = 0; j < G; ++j) v[j] = col + j < p.cols ? v[j] : 0.0f;  // a block's largest magnitude is that of the matrix's own numbers
+      for (int j = 0; j < G; ++j) v[j] = col + j < p.cols ? v[j] : 0.0f;
+    }
 #pragma unroll
     for (int j = 0; j < N - G; ++j) acc[j] = acc[j + G];
 #pragma unroll
@@ -468,67 +505,78 @@ __device__ __forceinline__ bool act_emit_tile(const F8ActTiles<PIECES>& p, int64
 }
 
 // ---- tiles whose rows are the features (decoding: few tokens) ---------------------------------------------------------
-// One feature of N tokens a lane, four warps to a block of 128 features; `swap`: 2 x 64 x 4 words.
+// One feature of N tokens a lane with its bias b, four warps to a block of 128 features; `swap`: 2 x 64 x 4 words.
 constexpr int kActColumnSwapBytes = 2 * 64 * 4 * 4;
+// A CTA comes here once, with nothing of this code in its instruction cache, and every line of it is waited for: hence few columns a turn.
 template <typename TC, int N>
-__device__ __forceinline__ bool act_emit_columns(const F8ActOut& p, int64_t row, int64_t col0, float* acc, uint32_t* swap, int quad, int round) {
-  constexpr int G = 16;
+__device__ __forceinline__ bool act_emit_columns(const F8ActOut& p, int64_t row, int64_t col0, float* acc, float b, uint32_t* swap, int quad, int round) {
+  constexpr int G = N <= 16 ? 4 : 8;
   const bool in = row < p.rows;
-  const float b = p.bias && in ? p.bias[row] : 0.0f;
+  const int cols = (int)min((int64_t)N, p.cols - col0), mine = in ? cols : 0;
+  swap += (round & 1) * 256;
 #pragma unroll 1
   for (int c = 0; c < N; c += G) {
-    const int64_t col = col0 + c;
-    const int nv = in ? (int)max((int64_t)0, min((int64_t)G, p.cols - col)) : 0;
-    float v[G], old[G];
+    float v[G];
 #pragma unroll
-    for (int j = 0; j < G; ++j) v[j] = p.alpha * acc[j] + b;
-    if (p.gradient) {
+    for (int j = 0; j < G; ++j) v[j] = acc[j];
+    if (c < cols) {
+      const int64_t col = col0 + c;
+      float old[G];
 #pragma unroll
-      for (int j = 0; j < G; ++j) old[j] = j < nv ? f8_load1(static_cast<const TC*>(p.Zin) + row + (col + j) * p.ldz) : 0.0f;
-      act_slopes<G>(p.act, v, old);
-    } else {
-      if (p.Z) {
+      for (int j = 0; j < G; ++j) v[j] = fmaf(p.alpha, v[j], b);
+      if (p.gradient) {
+#pragma unroll
+        for (int j = 0; j < G; ++j) old[j] = c + j < mine ? f8_load1(static_cast<const TC*>(p.Zin) + row + (col + j) * p.ldz) : 0.0f;
+        act_slopes<G>(p.act, v, old);
+      } else {
+        if (p.Z) {
+#pragma unroll
+          for (int j = 0; j < G; ++j)
+            if (c + j < mine) f8_store1(static_cast<TC*>(p.Z) + row + (col + j) * p.ldz, v[j]);
+        }
+        act_values<G>(p.act, v);
+      }
+      if (p.R) {
+#pragma unroll
+        for (int j = 0; j < G; ++j) old[j] = c + j < mine ? f8_load1(static_cast<const TC*>(p.R) + row + (col + j) * p.ldr) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < G; ++j) v[j] += old[j];
+      }
+      if (p.C) {
 #pragma unroll
         for (int j = 0; j < G; ++j)
-          if (j < nv) f8_store1(static_cast<TC*>(p.Z) + row + (col + j) * p.ldz, v[j]);
+          if (c + j < mine) f8_store1(static_cast<TC*>(p.C) + row + (col + j) * p.ldc, v[j]);
       }
-      act_values<G>(p.act, v);
-    }
-    if (p.R) {
+      if (p.Q) {
 #pragma unroll
-      for (int j = 0; j < G; ++j) old[j] = j < nv ? f8_load1(static_cast<const TC*>(p.R) + row + (col + j) * p.ldr) : 0.0f;
-#pragma unroll
-      for (int j = 0; j < G; ++j) v[j] += old[j];
-    }
-    if (p.C) {
-#pragma unroll
-      for (int j = 0; j < G; ++j)
-        if (j < nv) f8_store1(static_cast<TC*>(p.C) + row + (col + j) * p.ldc, v[j]);
+        for (int j = 0; j < G; ++j) {
+          v[j] = c + j < mine ? v[j] : 0.0f;
+          const uint32_t m = __reduce_max_sync(0xffffffffu, mag_bits(v[j]));
+          if ((threadIdx.x & 31) == 0) swap[4 * (c + j) + quad] = m;
+        }
+      }
     }
 #pragma unroll
     for (int j = 0; j < N - G; ++j) acc[j] = acc[j + G];
 #pragma unroll
-    for (int j = 0; j < G; ++j) acc[N - G + j] = j < nv ? v[j] : 0.0f;
+    for (int j = 0; j < G; ++j) acc[N - G + j] = v[j];
   }
   if (!p.Q) return true;
-  swap += (round & 1) * 256;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const uint32_t m = __reduce_max_sync(0xffffffffu, mag_bits(acc[j]));
-    if ((threadIdx.x & 31) == (j & 31)) swap[4 * j + quad] = m;
-  }
   if (!named_barrier_all<3, 128>(true)) return false;
-  const int nv = (int)min((int64_t)N, p.cols - col0);
   uint8_t* q = p.Q + row + col0 * p.ldq;
+  uint8_t* s = (row & (kF8Block - 1)) == 0 && in ? p.S + col0 * p.lds + row / kF8Block : nullptr;
+#pragma unroll 1
+  for (int c = 0; c < cols; c += G) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const uint4 w = *reinterpret_cast<const uint4*>(swap + 4 * j);
-    const uint32_t byte = f8_scale_byte(max(max(w.x, w.y), max(w.z, w.w)));
-    const uint32_t e = byte == kScaleNan ? 0x7fu : f8_pack4(acc[j] * f8_inv_scale(byte), 0.0f, 0.0f, 0.0f) & 255u;
-    if (in && j < nv) {
-      q[j * p.ldq] = (uint8_t)e;
-      if ((row & (kF8Block - 1)) == 0) p.S[(col0 + j) * p.lds + row / kF8Block] = (uint8_t)byte;
+    for (int j = 0; j < G; ++j) {
+      const uint4 w = *reinterpret_cast<const uint4*>(swap + 4 * (c + j));
+      const uint32_t byte = f8_scale_byte(max(max(w.x, w.y), max(w.z, w.w)));
+      const uint32_t e = byte == kScaleNan ? 0x7fu : f8_pack4(acc[j] * f8_inv_scale(byte), 0.0f, 0.0f, 0.0f) & 255u;
+      if (c + j < mine) q[(c + j) * p.ldq] = (uint8_t)e;
+      if (s && c + j < cols) s[(c + j) * p.lds] = (uint8_t)byte;
     }
+#pragma unroll
+    for (int j = 0; j < N - G; ++j) acc[j] = acc[j + G];
   }
   return true;
 }
@@ -635,6 +683,7 @@ __device__ __forceinline__ void act_add_shares(const F8ActOut& p, void* tile, in
   }
 #pragma unroll 1
   for (int i = worker; i < PIECES; i += WORKERS) {  // whole warps: PIECES is a multiple of 32.  The sums move through sum[0], as in act_emit_rows
+    if ((COLS_CONTIG ? row0 : col0) + share * PER + (i - lane) / (INNER / 4) >= tokens) break;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {

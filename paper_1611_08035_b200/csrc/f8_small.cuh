@@ -192,6 +192,11 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, F8Cfg<TBN, MX>::RESIDENT)
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
       const int64_t row = (int64_t)tr * kRows + quad * 32 + lane, col0 = (int64_t)tc * TBN + half * COLS;
+      [[maybe_unused]] float bias = 0.0f;  // of a row that is a feature
+      if constexpr (ACT) {
+        act_prefetch_small<TC, COLS_CONTIG, TBN>(p.out, (int64_t)tr * kRows, (int64_t)tc * TBN, ew, EW, p.splits, share);
+        if (!COLS_CONTIG && p.splits == 1 && p.out.bias && row < p.out.rows) bias = p.out.bias[row];
+      }
       if constexpr (MX) {
         const int64_t r0 = (int64_t)tr * kRows + lane, c0 = (int64_t)tc * TBN + lane;
         constexpr int CW = TBN >= 32 ? TBN / 32 : 1;
@@ -326,7 +331,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, F8Cfg<TBN, MX>::RESIDENT)
       } else if constexpr (ACT && COLS_CONTIG) {  // half a block: never with Q
         act_emit_rows<TC, COLS>(p.out, row - lane, col0, acc, scratch + ew * Cfg::SCRATCH);
       } else if constexpr (ACT) {
-        ok = act_emit_columns<TC, COLS>(p.out, row, col0, acc, reinterpret_cast<uint32_t*>(scratch + kActSwapAt), quad, round++);
+        ok = act_emit_columns<TC, COLS>(p.out, row, col0, acc, bias, reinterpret_cast<uint32_t*>(scratch + kActSwapAt), quad, round++);
       } else if constexpr (COLS_CONTIG) {
         f8_emit_staged<TC, COLS>(p.out, row - lane, col0, acc, scratch + ew * Cfg::SCRATCH);
       } else {
