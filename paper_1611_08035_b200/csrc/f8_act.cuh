@@ -309,91 +309,80 @@ __device__ __forceinline__ bool act_emit_halves(const F8ActOut& p, int64_t row0,
 
 // ---- tiles of pairs of CTAs --------------------------------------------------------------------------------------------------
 // A thread has a whole block, 128 consecutive features of one token.  Two warps a scheduler have little to hide latencies behind, so that what they do is kept short and
-// nothing in it waits for memory: matrices come and go by TMA through pieces of shared memory, 32 bytes of 32 rows each, swizzled so that the rows' owners read and write
-// them without conflicts (edges are the tensor maps'), what is read one or two pieces ahead; and the bias lies in shared memory.
-// Staged as act_emit_rows does it, 8192 x 4096 x 256 with bias, gelu, Z and Q took 107 us, now 69; with R read by its rows' owners, 64 bytes a row, 78.
+// nothing in it waits for memory: matrices pass through pieces of shared memory, 32 bytes of 32 rows each, swizzled so that the rows' owners read and write them
+// without conflicts.  Results leave by TMA (edges are the tensor maps'); what is read comes by cp.async, two pieces ahead; the bias lies in shared memory.
+// Clocks of a warp's part of a tile, bf16: sums, alpha and bias 2700, gelu 5500 (4100 of it the unit for exp and 1/x), a result 3000-3600, 8-bit result 2800.
+// What it was before, 8192 x 4096 x 256: staged both ways as act_emit_rows does it, with bias, gelu, Z and Q 107 us, now 65; R read by its rows' owners, 64 bytes a row, 78 (now 56); by
+// TMA, whose small loads wait behind the operands' large ones, the gradient of gelu with C and Q 96, 9400 clocks of a tile for Z alone (now 80).
 constexpr int kActPiece = 32 * 32;
 constexpr int kActBias = kF8Block * 4;
-// PIECES of a warp; where something is read, all but one are for that.
+// PIECES of a warp: one for results, the others on their way to be read
 template <int PIECES>
 struct F8ActTiles : F8ActOut {
   static constexpr int WARP_BYTES = PIECES * kActPiece + kActBias;
   CUtensorMap mz, mc, mq;  // of Z, C and Q where they are written
-  CUtensorMap min;         // of what is read: Z in the gradient form, else R
 };
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* smem, int c_inner, int c_outer) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c_inner), "r"(c_outer),
                "r"(smem_u32(smem))
                : "memory");
 }
-template <int N>
-__device__ __forceinline__ void bulk_wait_read() {
-  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
-}
-// A warp's pieces: the last OUT of them for results (all of them, or one where something is read), the others for what is read.
+// A warp's pieces: the last for results (where nothing is read, the last two), the others for what is read.
 template <int PIECES>
 struct ActPieces {
   unsigned char* at;  // the pieces, then the bias
-  uint64_t* bars;     // PIECES - 1, one arrival each
-  int in = 0, out = 0;
-  uint32_t phase = 0;  // of the pieces to read, a bit each
-  int coming = 0;      // loads that have not been waited for
 
-  __device__ __forceinline__ unsigned char* mine(unsigned char* piece, int half) const {
+  __device__ __forceinline__ static unsigned char* mine(unsigned char* piece, int row, int half) { return piece + row * 32 + ((row >> 2 & 1) ^ half) * 16; }
+  // COUNT times 32 bytes of each lane's row to (col, row0 ..), `step` columns apart, as far as they lie before `end`
+  template <int COUNT>
+  __device__ __forceinline__ void put(const CUtensorMap* map, int col, int step, int end, int row0, const uint4* w) {
     const int lane = threadIdx.x & 31;
-    return piece + lane * 32 + ((lane >> 2 & 1) ^ half) * 16;
-  }
-  // 32 bytes of each lane's row to (col, row0 ..) of a matrix
-  __device__ __forceinline__ void put(const CUtensorMap* map, bool reads, int col, int row0, uint4 a, uint4 b) {
-    const bool first = (threadIdx.x & 31) == 0;
-    unsigned char* s = at + (reads ? PIECES - 1 : out) * kActPiece;
-    if (first) {
-      if (reads) bulk_wait_read<0>();
-      else bulk_wait_read<PIECES - 1>();
-    }
+    unsigned char* s = at + (PIECES - COUNT) * kActPiece;
+    if (lane == 0) bulk_wait_read_all();
     __syncwarp();
-    *reinterpret_cast<uint4*>(mine(s, 0)) = a;
-    *reinterpret_cast<uint4*>(mine(s, 1)) = b;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      *reinterpret_cast<uint4*>(mine(s + i * kActPiece, lane, 0)) = w[2 * i];
+      *reinterpret_cast<uint4*>(mine(s + i * kActPiece, lane, 1)) = w[2 * i + 1];
+    }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
-    if (first) {
-      tma_store_2d(map, s, col, row0);
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i)
+        if (col + i * step < end) tma_store_2d(map, s + i * kActPiece, col + i * step, row0);
       bulk_commit();
     }
-    out = out + 1 == PIECES ? 0 : out + 1;
   }
-  // the next free piece is filled from (col, row0 ..); results that lay there have left
-  __device__ __forceinline__ void ask(const CUtensorMap* map, int col, int row0) {
-    const int i = in + coming < PIECES - 1 ? in + coming : in + coming - (PIECES - 1);
-    if ((threadIdx.x & 31) == 0) {
-      mbar_arrive_expect_tx(&bars[i], kActPiece);
-      tma_load_2d(at + i * kActPiece, map, col, row0, &bars[i]);
+  // piece `i` of those to read is filled from rows row0 .. of M, 32 bytes from column col on; 0 beyond the matrix
+  template <typename TC>
+  __device__ __forceinline__ void ask(int i, const void* M, int64_t ld, const F8ActOut& p, int64_t row0, int64_t col) {
+    constexpr int H = 16 / (int)sizeof(TC);
+    const int lane = threadIdx.x & 31, half = lane & 1;
+    const int64_t left = p.cols - col - half * H;
+    const int bytes = left >= H ? 16 : left > 0 ? (int)left * (int)sizeof(TC) : 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = u * 16 + (lane >> 1);
+      const bool in = row0 + r < p.rows && bytes > 0;
+      cp_async_zfill<16>(mine(at + i * kActPiece, r, half), static_cast<const TC*>(M) + (in ? (row0 + r) * ld + col + half * H : 0), in ? bytes : 0);
     }
-    ++coming;
   }
-  __device__ __forceinline__ bool arrived(uint64_t limit) { return mbar_wait_warp(&bars[in], phase >> in & 1u, limit); }
-  // 32 bytes of each lane's row, once they have arrived; the piece is free for the next ask
-  __device__ __forceinline__ bool take(uint4& a, uint4& b) {
-    if (!arrived(kWaitLimitNs)) return false;
-    a = *reinterpret_cast<const uint4*>(mine(at + in * kActPiece, 0));
-    b = *reinterpret_cast<const uint4*>(mine(at + in * kActPiece, 1));
-    // The loads come before the copy that refills the piece: without a fence nothing orders them (they were moved below it, and found the next numbers).
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  // 32 bytes of each lane's row, once they have arrived: all but the newest AHEAD - 1 pieces have
+  template <int AHEAD>
+  __device__ __forceinline__ void take(int i, uint4& a, uint4& b) const {
+    const int lane = threadIdx.x & 31;
+    cp_async_wait<AHEAD - 1>();
     __syncwarp();
-    phase ^= 1u << in;
-    in = in + 1 == PIECES - 1 ? 0 : in + 1;
-    --coming;
-    return true;
+    a = *reinterpret_cast<const uint4*>(mine(at + i * kActPiece, lane, 0));
+    b = *reinterpret_cast<const uint4*>(mine(at + i * kActPiece, lane, 1));
+    __syncwarp();
   }
   __device__ __forceinline__ float* bias() const { return reinterpret_cast<float*>(at + PIECES * kActPiece); }
-  // no CTA leaves before its results have, nor before what it asked for has come (where a wait has run out)
-  __device__ __forceinline__ void drain() {
-    for (; coming > 0; --coming) {
-      (void)arrived(kDrainLimitNs);
-      phase ^= 1u << in;
-      in = in + 1 == PIECES - 1 ? 0 : in + 1;
-    }
+  // no CTA leaves before its results have
+  __device__ __forceinline__ void drain() const {
     if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    cp_async_wait<0>();
   }
 };
 // Before the sums are waited for: the bias of the tile's features, 0 beyond the matrix and where there is none, and the first pieces of what is read.
@@ -413,27 +402,41 @@ __device__ __forceinline__ void act_begin_tile(const F8ActTiles<PIECES>& p, int6
     }
   }
   if (p.Zin || p.R) {
+    cp_async_wait<0>();  // an edge tile before this one leaves pieces that it did not take
 #pragma unroll
-    for (int i = 0; i < PIECES - 1; ++i)
-      if (col0 + i * (32 / (int)sizeof(TC)) < p.cols) pieces.ask(&p.min, (int)col0 + i * (32 / (int)sizeof(TC)), (int)row0);
+    for (int i = 0; i < PIECES - 1; ++i) {
+      pieces.template ask<TC>(i, p.Zin ? p.Zin : p.R, p.Zin ? p.ldz : p.ldr, p, row0, col0 + i * (32 / (int)sizeof(TC)));
+      cp_async_commit();
+    }
   }
   __syncwarp();
   reinterpret_cast<float4*>(pieces.bias())[threadIdx.x & 31] = b;
   __syncwarp();
 }
-// False where a wait has run out.
 template <typename TC, int PIECES>
-__device__ __forceinline__ bool act_emit_tile(const F8ActTiles<PIECES>& p, int64_t row0, int64_t col0, float* acc, ActPieces<PIECES>& pieces) {
-  constexpr int G = 32, N = kF8Block, PIECE = 16 / (int)sizeof(TC), W = 2 * PIECE;  // numbers of 16 bytes, of a row of a piece
-  if (row0 >= p.rows || col0 >= p.cols) return true;
+__device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64_t row0, int64_t col0, float* acc, ActPieces<PIECES>& pieces) {
+  constexpr int G = 32, N = kF8Block, H = 16 / (int)sizeof(TC), W = 2 * H, AHEAD = PIECES - 1;  // numbers of 16 bytes, of a row of a piece
+  if (row0 >= p.rows || col0 >= p.cols) return;
   const int64_t row = row0 + (threadIdx.x & 31);
   const int end = (int)min((int64_t)N, p.cols - col0);
-  const bool reads = p.Zin || p.R;
+  const void* M = p.Zin ? p.Zin : p.R;  // what is read
+  const int64_t ldm = p.Zin ? p.ldz : p.ldr;
   auto put = [&](const CUtensorMap* map, int c, const float* v) {
+    if (M || PIECES == 2) {
 #pragma unroll
-    for (int j = 0; j < G; j += W)
-      if (c + j < end) pieces.put(map, reads, (int)col0 + c + j, (int)row0, act_pack16<TC>(v + j), act_pack16<TC>(v + j + PIECE));
+      for (int j = 0; j < G; j += W) {
+        const uint4 w[2] = {act_pack16<TC>(v + j), act_pack16<TC>(v + j + H)};
+        if (c + j < end) pieces.template put<1>(map, (int)col0 + c + j, W, (int)col0 + end, (int)row0, w);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < G; j += 2 * W) {
+        const uint4 w[4] = {act_pack16<TC>(v + j), act_pack16<TC>(v + j + H), act_pack16<TC>(v + j + W), act_pack16<TC>(v + j + W + H)};
+        if (c + j < end) pieces.template put<2>(map, (int)col0 + c + j, W, (int)col0 + end, (int)row0, w);
+      }
+    }
   };
+  int in = 0;  // the piece that is taken next
   // 32 columns a turn of a loop that is not unrolled, through which the accumulators move
 #pragma unroll 1
   for (int c = 0; c < N; c += G) {
@@ -447,17 +450,18 @@ __device__ __forceinline__ bool act_emit_tile(const F8ActTiles<PIECES>& p, int64
     }
     if (c < end) {
       if (p.Z) put(&p.mz, c, v);
-      if (reads) {
+      if (M) {
 #pragma unroll
         for (int j = 0; j < G; j += W) {
-          if (c + j >= end) break;
           uint4 x, y;
-          if (!pieces.take(x, y)) return false;
-          const int ahead = c + j + (PIECES - 1) * W;
-          if (ahead < end) pieces.ask(&p.min, (int)col0 + ahead, (int)row0);
+          pieces.template take<AHEAD>(in, x, y);
+          const int ahead = c + j + AHEAD * W;
+          if (ahead < N) pieces.template ask<TC>(in, M, ldm, p, row0, col0 + ahead);
+          cp_async_commit();  // also where nothing was asked for: take counts
+          in = in + 1 == AHEAD ? 0 : in + 1;
           float m[W];
           act_unpack16<TC>(x, m);
-          act_unpack16<TC>(y, m + PIECE);
+          act_unpack16<TC>(y, m + H);
           if (p.gradient) {
             act_slopes<W>(p.act, v + j, m);
             if (p.R) {  // read in the middle of the work
@@ -486,8 +490,11 @@ __device__ __forceinline__ bool act_emit_tile(const F8ActTiles<PIECES>& p, int64
 #pragma unroll
     for (int j = 0; j < G; ++j) acc[N - G + j] = v[j];
   }
-  if (!p.Q) return true;
-  const uint32_t byte = f8_scale_byte(act_amax<N>(acc));
+  if (!p.Q) return;
+  float most[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < N; ++j) most[j & 3] = larger_nan(most[j & 3], fabsf(acc[j]));
+  const uint32_t byte = f8_scale_byte(__float_as_uint(larger_nan(larger_nan(most[0], most[1]), larger_nan(most[2], most[3]))));
   if (row < p.rows) p.S[row * p.lds + col0 / kF8Block] = (uint8_t)byte;
   const float inv = byte == kScaleNan ? 0.0f : f8_inv_scale(byte);
 #pragma unroll
@@ -499,9 +506,9 @@ __device__ __forceinline__ bool act_emit_tile(const F8ActTiles<PIECES>& p, int64
       const Two x = mul2({a[0], a[1]}, both(inv)), y = mul2({a[2], a[3]}, both(inv));
       w[i] = byte == kScaleNan ? 0x7f7f7f7fu : f8_pack4(x.a, x.b, y.a, y.b);
     }
-    if (j < end) pieces.put(&p.mq, reads, (int)col0 + j, (int)row0, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+    const uint4 q[2] = {make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7])};
+    if (j < end) pieces.template put<1>(&p.mq, (int)col0 + j, 32, (int)col0 + end, (int)row0, q);
   }
-  return true;
 }
 
 // ---- tiles whose rows are the features (decoding: few tokens) ---------------------------------------------------------

@@ -95,7 +95,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* tempty = tfull + 2;
   uint64_t* drained = tempty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
-  [[maybe_unused]] uint64_t* act_bars = full + 32;  // 1 for each of the warps that write
   float* scales = reinterpret_cast<float*>(ring + kRing + 512);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -116,8 +115,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&tempty[b], 2 * kEW);
     }
     mbar_init(drained, 1);
-    if constexpr (ActHandOver<OUT>::TILES)
-      for (int i = 0; i < kEW * 1; ++i) mbar_init(&act_bars[i], 1);
     mbar_fence_init();
   }
   if (warp == 1) tmem_alloc_pair(tmem_slot, 2 * kBN);
@@ -260,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t leader_tempty = cluster_map_shared(smem_u32(tempty), 0);
     unsigned char* stage = ring + kRing + 512 + kSlots * kSlotFloats * 4 + (warp - 8) * ActHandOver<OUT>::WARP_BYTES;
     constexpr bool TILES = ActHandOver<OUT>::TILES;
-    [[maybe_unused]] ActPieces<2> pieces{stage, act_bars + (warp - 8) * 1};
+    [[maybe_unused]] ActPieces<2> pieces{stage};
     RingPos<kSlots> slot;
     uint64_t acc2[kCols / 2];
     const bool one_factor = p.sc.shift == 7;  // the columns of a half share a scale
@@ -337,10 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
       } else if constexpr (TILES) {
-        if (!act_emit_tile<TC>(p.out, row0, col0, acc, pieces)) {
-          ok = false;
-          if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-        }
+        act_emit_tile<TC>(p.out, row0, col0, acc, pieces);
       } else {
         f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
       }

@@ -118,8 +118,7 @@ bool f8_act_tiles(const F8ActOut& out, int64_t rows, int64_t cols, F8ActTiles<PI
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
   const CUtensorMapDataType type = sizeof(TC) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
-  return map(&t.mz, out.Z, out.ldz, (int)sizeof(TC), type) && map(&t.mc, out.C, out.ldc, (int)sizeof(TC), type) && map(&t.mq, out.Q, out.ldq, 1, CU_TENSOR_MAP_DATA_TYPE_UINT8) &&
-         map(&t.min, out.Zin ? out.Zin : out.R, out.Zin ? out.ldz : out.ldr, (int)sizeof(TC), type);
+  return map(&t.mz, out.Z, out.ldz, (int)sizeof(TC), type) && map(&t.mc, out.C, out.ldc, (int)sizeof(TC), type) && map(&t.mq, out.Q, out.ldq, 1, CU_TENSOR_MAP_DATA_TYPE_UINT8);
 }
 template <typename OUT>
 F8ArgsOf<OUT> f8_args_with(const F8ArgsOf<F8ActOut>& a, const OUT& out) {

@@ -63,7 +63,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* tempty = tfull + 1;
   uint64_t* drained = tempty + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
-  [[maybe_unused]] uint64_t* act_bars = full + 32;  // 2 for each of the warps that write
   uint32_t* sf_words = reinterpret_cast<uint32_t*>(ring + kRing + 512);  // [2][kSfCols][32]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -82,8 +81,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(tfull, 1);
     mbar_init(tempty, 2 * kEW);
     mbar_init(drained, 1);
-    if constexpr (ActHandOver<OUT>::TILES)
-      for (int i = 0; i < kEW * 2; ++i) mbar_init(&act_bars[i], 1);
     mbar_fence_init();
   }
   if (warp == 1) tmem_alloc_pair(tmem_slot, kTmem);
@@ -236,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t limit = kWaitLimitNs + (uint64_t)p.kb * 8192ull;  // outlasts the k loop that it waits for
     unsigned char* stage = ring + kRing + 512 + kSfBytes + (warp - 8) * ActHandOver<OUT>::WARP_BYTES;
     constexpr bool TILES = ActHandOver<OUT>::TILES;
-    [[maybe_unused]] ActPieces<3> pieces{stage, act_bars + (warp - 8) * 2};
+    [[maybe_unused]] ActPieces<3> pieces{stage};
     float acc[kCols];
     int ch = 0;
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
@@ -283,10 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) {
         if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
       } else if constexpr (TILES) {
-        if (!act_emit_tile<TC>(p.out, row0, col0, acc, pieces)) {
-          ok = false;
-          if (lane == 0) atomicExch(p.status, (int)B2_ERR_TIMEOUT);
-        }
+        act_emit_tile<TC>(p.out, row0, col0, acc, pieces);
       } else {
         f8_emit_staged<TC, kCols>(p.out, row0, col0, acc, stage);
       }
