@@ -78,7 +78,7 @@ __device__ __forceinline__ Two rcp_approx(Two x) { return {rcp_approx(x.a), rcp_
 __device__ __forceinline__ Two at_most(Two x, float b) { return {at_most(x.a, b), at_most(x.b, b)}; }
 __device__ __forceinline__ Two at_least(Two x, float b) { return {at_least(x.a, b), at_least(x.b, b)}; }
 
-// -Phi(-x) for x >= 0, and exp(-x^2/2)
+// e = exp(-x^2/2), and h with Phi(-x) = -e h, for x >= 0
 __device__ __forceinline__ Two minus_tail(Two x, Two& e) {
   e = exp2_approx(mul2(mul2(x, x), both(-0.72134752f)));
   const Two t = rcp_approx(fma2(both(0.3f), x, both(1.0f)));
@@ -90,17 +90,19 @@ __device__ __forceinline__ Two minus_tail(Two x, Two& e) {
   p = fma2(p, t, both(-0.10017596185207367f));
   p = fma2(p, t, both(-0.12071213126182556f));
   p = fma2(p, t, both(-0.11963200569152832f));
-  return mul2(mul2(e, t), p);
+  return mul2(t, p);
 }
+__device__ __forceinline__ float with_sign(float x, float s) { return __uint_as_float((__float_as_uint(x) & 0x7fffffffu) | (__float_as_uint(s) & 0x80000000u)); }
 __device__ __forceinline__ Two gelu_value(Two z) {  // z > 0: z (1 - Phi(-z))
   Two e;
-  const Two x = at_most(Two{fabsf(z.a), fabsf(z.b)}, 64.0f);
-  return fma2(x, minus_tail(x, e), Two{fmaxf(z.a, 0.0f), fmaxf(z.b, 0.0f)});
+  const Two x = at_most(Two{fabsf(z.a), fabsf(z.b)}, 64.0f), h = minus_tail(x, e);
+  return fma2(mul2(x, e), h, Two{fmaxf(z.a, 0.0f), fmaxf(z.b, 0.0f)});
 }
-__device__ __forceinline__ Two gelu_slope(Two z) {
+__device__ __forceinline__ Two gelu_slope(Two z) {  // what it is above 1/2 changes its sign with z: 1/2 - Phi(-x) + x phi(x), not below 0
   Two e;
-  const Two x = at_most(at_least(z, -64.0f), 64.0f), h = minus_tail(Two{fabsf(x.a), fabsf(x.b)}, e);
-  return fma2(mul2(x, both(0.39894228f)), e, Two{x.a > 0.0f ? 1.0f + h.a : -h.a, x.b > 0.0f ? 1.0f + h.b : -h.b});
+  const Two x = at_most(Two{fabsf(z.a), fabsf(z.b)}, 64.0f), h = minus_tail(x, e);
+  const Two w = fma2(e, fma2(x, both(0.39894228f), h), both(0.5f));
+  return add2(both(0.5f), Two{with_sign(w.a, z.a), with_sign(w.b, z.b)});
 }
 // z s(w) with w = z (one + cubic z^2): silu has one = 1, cubic = 0; gelu_tanh 2 sqrt(2/pi) (1, 0.044715)
 struct Sigmoid {

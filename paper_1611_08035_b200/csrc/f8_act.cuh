@@ -354,19 +354,25 @@ struct ActPieces {
       bulk_commit();
     }
   }
-  // piece `i` of those to read is filled from rows row0 .. of M, 32 bytes from column col on; 0 beyond the matrix
+  // Where this lane's shares of what is read begin, two rows of 16 bytes a piece, at the tile's first column.
+  const unsigned char *base = nullptr, *from = nullptr, *from16 = nullptr;
+  int left = 0, left16 = 0;  // bytes of those rows
   template <typename TC>
-  __device__ __forceinline__ void ask(int i, const void* M, int64_t ld, const F8ActOut& p, int64_t row0, int64_t col) {
-    constexpr int H = 16 / (int)sizeof(TC);
-    const int lane = threadIdx.x & 31, half = lane & 1;
-    const int64_t left = p.cols - col - half * H;
-    const int bytes = left >= H ? 16 : left > 0 ? (int)left * (int)sizeof(TC) : 0;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = u * 16 + (lane >> 1);
-      const bool in = row0 + r < p.rows && bytes > 0;
-      cp_async_zfill<16>(mine(at + i * kActPiece, r, half), static_cast<const TC*>(M) + (in ? (row0 + r) * ld + col + half * H : 0), in ? bytes : 0);
-    }
+  __device__ __forceinline__ void read_from(const void* M, int64_t ld, const F8ActOut& p, int64_t row0, int64_t col0) {
+    const int lane = threadIdx.x & 31, r = lane >> 1;
+    base = static_cast<const unsigned char*>(M);
+    from = reinterpret_cast<const unsigned char*>(static_cast<const TC*>(M) + (row0 + r) * ld + col0) + (lane & 1) * 16;
+    from16 = from + 16 * ld * (int64_t)sizeof(TC);
+    const int bytes = (int)min((int64_t)kF8Block, p.cols - col0) * (int)sizeof(TC) - (lane & 1) * 16;
+    left = row0 + r < p.rows ? bytes : 0, left16 = row0 + r + 16 < p.rows ? bytes : 0;
+  }
+  // piece `i` of those to read is filled with 32 bytes of every row, `at_byte` of the tile; 0 beyond the matrix
+  __device__ __forceinline__ void ask(int i, int at_byte) {
+    const int lane = threadIdx.x & 31;
+    unsigned char* to = mine(at + i * kActPiece, lane >> 1, lane & 1);  // sixteen rows on the swizzle is the same
+    const int a = min(16, left - at_byte), b = min(16, left16 - at_byte);
+    cp_async_zfill<16>(to, a > 0 ? from + at_byte : base, max(a, 0));
+    cp_async_zfill<16>(to + 512, b > 0 ? from16 + at_byte : base, max(b, 0));
   }
   // 32 bytes of each lane's row, once they have arrived: all but the newest AHEAD - 1 pieces have
   template <int AHEAD>
@@ -403,9 +409,10 @@ __device__ __forceinline__ void act_begin_tile(const F8ActTiles<PIECES>& p, int6
   }
   if (p.Zin || p.R) {
     cp_async_wait<0>();  // an edge tile before this one leaves pieces that it did not take
+    pieces.template read_from<TC>(p.Zin ? p.Zin : p.R, p.Zin ? p.ldz : p.ldr, p, row0, col0);
 #pragma unroll
     for (int i = 0; i < PIECES - 1; ++i) {
-      pieces.template ask<TC>(i, p.Zin ? p.Zin : p.R, p.Zin ? p.ldz : p.ldr, p, row0, col0 + i * (32 / (int)sizeof(TC)));
+      pieces.ask(i, 32 * i);
       cp_async_commit();
     }
   }
@@ -419,10 +426,9 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
   if (row0 >= p.rows || col0 >= p.cols) return;
   const int64_t row = row0 + (threadIdx.x & 31);
   const int end = (int)min((int64_t)N, p.cols - col0);
-  const void* M = p.Zin ? p.Zin : p.R;  // what is read
-  const int64_t ldm = p.Zin ? p.ldz : p.ldr;
+  const bool reads = p.Zin || p.R;
   auto put = [&](const CUtensorMap* map, int c, const float* v) {
-    if (M || PIECES == 2) {
+    if (reads || PIECES == 2) {
 #pragma unroll
       for (int j = 0; j < G; j += W) {
         const uint4 w[2] = {act_pack16<TC>(v + j), act_pack16<TC>(v + j + H)};
@@ -437,7 +443,8 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
     }
   };
   int in = 0;  // the piece that is taken next
-  // 32 columns a turn of a loop that is not unrolled, through which the accumulators move
+  // 32 columns a turn of a loop that is not unrolled, through which the accumulators move: fetching instructions costs as much as they do (64 a turn: gradient of gelu with C and
+  // Q 102 us instead of 88)
 #pragma unroll 1
   for (int c = 0; c < N; c += G) {
     float v[G];
@@ -450,13 +457,13 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
     }
     if (c < end) {
       if (p.Z) put(&p.mz, c, v);
-      if (M) {
+      if (reads) {
 #pragma unroll
         for (int j = 0; j < G; j += W) {
           uint4 x, y;
           pieces.template take<AHEAD>(in, x, y);
           const int ahead = c + j + AHEAD * W;
-          if (ahead < N) pieces.template ask<TC>(in, M, ldm, p, row0, col0 + ahead);
+          if (ahead < N) pieces.ask(in, ahead * (int)sizeof(TC));
           cp_async_commit();  // also where nothing was asked for: take counts
           in = in + 1 == AHEAD ? 0 : in + 1;
           float m[W];
