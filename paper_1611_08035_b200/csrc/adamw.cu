@@ -198,6 +198,8 @@ __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep&
 // path does as much as it can two numbers at a time and gives a lane sixteen consecutive elements (eight lanes to a block).  Numbers below 2^-6 of their scale, whose
 // distance is not the binade's, take a branch; a warp with a v for which the root below is not exact, or not finite, goes to adam_pieces before it has written anything.
 
+// A sum of products that are rounded before: the packed addition is joined with them to a multiply-add (4 of 16 million first moments fell to the other side of their rounding).
+__device__ __forceinline__ Two sum_rn(Two x, Two y) { return {__fadd_rn(x.a, y.a), __fadd_rn(x.b, y.b)}; }
 // Square roots, rounded to nearest: an approximation of the reciprocal root, and from it one Newton step on the root with the exact remainder (P. Markstein, IBM Journal of
 // Research and Development 34, 1990).  0, and 2^-100 to the largest finite number, give __fsqrt_rn's results: tried for every mantissa and both parities of the exponent.
 __device__ __forceinline__ float rsqrt_approx(float x) {
@@ -305,8 +307,8 @@ __device__ __forceinline__ bool adam_512(const AdamTensor& t, const AdamStep& s,
       const int k = 4 * i + j;
       const Two g = mul2(pair16(gq, k / 2), both(scale));
       const Two mo = mul2({a[j], a[j + 1]}, both(sm)), ro = mul2({b[j], b[j + 1]}, both(sr));
-      const Two mn = add2(mul2(mo, both(s.b1)), mul2(g, both(s.a1)));
-      const Two v = add2(mul2(mul2(ro, ro), both(s.b2)), mul2(mul2(g, g), both(s.a2)));
+      const Two mn = sum_rn(mul2(mo, both(s.b1)), mul2(g, both(s.a1)));
+      const Two v = sum_rn(mul2(mul2(ro, ro), both(s.b2)), mul2(mul2(g, g), both(s.a2)));
       const Two rn = sqrt2_rn(v);
       least_v = min(least_v, min(__float_as_uint(v.a) - 1u, __float_as_uint(v.b) - 1u));
       const Two step = mul2(mul2(mn, both(s.size)), rcp_approx(fma2(rn, both(s.root), both(s.eps))));

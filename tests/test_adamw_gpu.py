@@ -258,3 +258,23 @@ def test_more_than_32_bits_of_elements(b2):
         assert np.array_equal(f8.e8m0(s[first // 128 :].view(torch.uint8).cpu().numpy()), want_s)
         assert int((np64(x[first:].float()) != q).sum()) <= 3
     assert bool((p[: n - tail] == 0).all()) and bool((p[n - tail :] != 0).any())
+
+
+def test_aligned_and_other_tensors_agree(b2):
+    """The fast way of aligned tensors and the other one hold the same bits: m and v are computed by the same single roundings."""
+    n = 1 << 24
+    g = torch.Generator(device="cuda").manual_seed(0)
+    gr = 1e-3 * torch.randn(n, device="cuda", generator=g)
+    qm, qr = (torch.randint(0, 256, (n,), device="cuda", generator=g).to(torch.uint8) for _ in range(2))
+    qm[(qm & 0x7F) == 0x7F] = 0
+    qr = qr.clamp(1, 0x7E)
+    results = []
+    for offset in (0, 1):
+        t = {k: torch.empty(n + offset, dtype=x.dtype, device="cuda") for k, x in (("p", gr), ("g", gr), ("m", qm), ("v", qr))}
+        for k, x in (("p", gr), ("g", gr), ("m", qm), ("v", qr)):
+            t[k][offset:] = x
+        t = {k: x[offset:] if k in "pg" else x[offset:].view(F8) for k, x in t.items()}
+        t |= {k: torch.full((n // 128,), b, dtype=torch.uint8, device="cuda").view(E8) for k, b in (("sm", 106), ("sv", 109))}
+        call(b2, [t])
+        results.append([t[k].view(torch.uint8).clone() for k in ("m", "v", "sm", "sv")])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
