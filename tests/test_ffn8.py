@@ -14,6 +14,10 @@ from test_layer8 import BF, StandIn, columns, np64, off
 class StandInFfn(StandIn):
     ACT_NONE, ACT_GRADIENT = binding.ACT_NONE, binding.ACT_GRADIENT
 
+    def b2_rmsnorm_f8(self, d, t, *args):
+        *args, rstd = args
+        super().b2_rmsnorm_f8(d, t, *args, torch.empty(t) if rstd is None else rstd)
+
     def b2_act_backward_workspace_bytes(self, d, t):
         return 0
 
