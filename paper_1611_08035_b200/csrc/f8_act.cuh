@@ -310,13 +310,12 @@ __device__ __forceinline__ bool act_emit_halves(const F8ActOut& p, int64_t row0,
 // ---- tiles of pairs of CTAs --------------------------------------------------------------------------------------------------
 // A thread has a whole block, 128 consecutive features of one token.  Two warps a scheduler have little to hide latencies behind, so that what they do is kept short and
 // nothing in it waits for memory: matrices pass through pieces of shared memory, 32 bytes of 32 rows each, swizzled so that the rows' owners read and write them
-// without conflicts.  Results leave by TMA (edges are the tensor maps'); what is read comes by cp.async, two pieces ahead; the bias lies in shared memory.
+// without conflicts.  Results leave by TMA (edges are the tensor maps'); what is read comes by cp.async, a piece ahead; the bias lies in shared memory.
 // Clocks of a warp's part of a tile, bf16: sums, alpha and bias 2700, gelu 5500 (4100 of it the unit for exp and 1/x), a result 3000-3600, 8-bit result 2800.
 // What it was before, 8192 x 4096 x 256: staged both ways as act_emit_rows does it, with bias, gelu, Z and Q 107 us, now 65; R read by its rows' owners, 64 bytes a row, 78 (now 56); by
 // TMA, whose small loads wait behind the operands' large ones, the gradient of gelu with C and Q 96, 9400 clocks of a tile for Z alone (now 80).
 constexpr int kActPiece = 32 * 32;
 constexpr int kActBias = kF8Block * 4;
-// PIECES of a warp: one for results, the others on their way to be read
 template <int PIECES>
 struct F8ActTiles : F8ActOut {
   static constexpr int WARP_BYTES = PIECES * kActPiece + kActBias;
@@ -327,7 +326,7 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void*
                "r"(smem_u32(smem))
                : "memory");
 }
-// A warp's pieces: the last for results (where nothing is read, the last two), the others for what is read.
+// A warp's pieces: the first for what is read, the others for results.
 template <int PIECES>
 struct ActPieces {
   unsigned char* at;  // the pieces, then the bias
@@ -366,22 +365,23 @@ struct ActPieces {
     const int bytes = (int)min((int64_t)kF8Block, p.cols - col0) * (int)sizeof(TC) - (lane & 1) * 16;
     left = row0 + r < p.rows ? bytes : 0, left16 = row0 + r + 16 < p.rows ? bytes : 0;
   }
-  // piece `i` of those to read is filled with 32 bytes of every row, `at_byte` of the tile; 0 beyond the matrix
-  __device__ __forceinline__ void ask(int i, int at_byte) {
+  // the piece to read is filled with 32 bytes of every row, `at_byte` of the tile; 0 beyond the matrix
+  __device__ __forceinline__ void ask(int at_byte) {
     const int lane = threadIdx.x & 31;
-    unsigned char* to = mine(at + i * kActPiece, lane >> 1, lane & 1);  // sixteen rows on the swizzle is the same
+    unsigned char* to = mine(at, lane >> 1, lane & 1);  // sixteen rows on the swizzle is the same
     const int a = min(16, left - at_byte), b = min(16, left16 - at_byte);
     cp_async_zfill<16>(to, a > 0 ? from + at_byte : base, max(a, 0));
     cp_async_zfill<16>(to + 512, b > 0 ? from16 + at_byte : base, max(b, 0));
+    cp_async_commit();
   }
-  // 32 bytes of each lane's row, once they have arrived: all but the newest AHEAD - 1 pieces have
-  template <int AHEAD>
-  __device__ __forceinline__ void take(int i, uint4& a, uint4& b) const {
+  // 32 bytes of each lane's row, once they have arrived
+  __device__ __forceinline__ void take(uint4& a, uint4& b) const {
     const int lane = threadIdx.x & 31;
-    cp_async_wait<AHEAD - 1>();
+    unsigned char* piece = at;
+    cp_async_wait<0>();
     __syncwarp();
-    a = *reinterpret_cast<const uint4*>(mine(at + i * kActPiece, lane, 0));
-    b = *reinterpret_cast<const uint4*>(mine(at + i * kActPiece, lane, 1));
+    a = *reinterpret_cast<const uint4*>(mine(piece, lane, 0));
+    b = *reinterpret_cast<const uint4*>(mine(piece, lane, 1));
     __syncwarp();
   }
   __device__ __forceinline__ float* bias() const { return reinterpret_cast<float*>(at + PIECES * kActPiece); }
@@ -408,13 +408,9 @@ __device__ __forceinline__ void act_begin_tile(const F8ActTiles<PIECES>& p, int6
     }
   }
   if (p.Zin || p.R) {
-    cp_async_wait<0>();  // an edge tile before this one leaves pieces that it did not take
+    cp_async_wait<0>();  // an edge tile before this one leaves a piece that it did not take
     pieces.template read_from<TC>(p.Zin ? p.Zin : p.R, p.Zin ? p.ldz : p.ldr, p, row0, col0);
-#pragma unroll
-    for (int i = 0; i < PIECES - 1; ++i) {
-      pieces.ask(i, 32 * i);
-      cp_async_commit();
-    }
+    pieces.ask(0);
   }
   __syncwarp();
   reinterpret_cast<float4*>(pieces.bias())[threadIdx.x & 31] = b;
@@ -422,13 +418,13 @@ __device__ __forceinline__ void act_begin_tile(const F8ActTiles<PIECES>& p, int6
 }
 template <typename TC, int PIECES>
 __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64_t row0, int64_t col0, float* acc, ActPieces<PIECES>& pieces) {
-  constexpr int G = 32, N = kF8Block, H = 16 / (int)sizeof(TC), W = 2 * H, AHEAD = PIECES - 1;  // numbers of 16 bytes, of a row of a piece
+  constexpr int G = 32, N = kF8Block, H = 16 / (int)sizeof(TC), W = 2 * H;  // numbers of 16 bytes, of a row of a piece
   if (row0 >= p.rows || col0 >= p.cols) return;
   const int64_t row = row0 + (threadIdx.x & 31);
   const int end = (int)min((int64_t)N, p.cols - col0);
   const bool reads = p.Zin || p.R;
   auto put = [&](const CUtensorMap* map, int c, const float* v) {
-    if (reads || PIECES == 2) {
+    if (PIECES == 2) {
 #pragma unroll
       for (int j = 0; j < G; j += W) {
         const uint4 w[2] = {act_pack16<TC>(v + j), act_pack16<TC>(v + j + H)};
@@ -442,18 +438,25 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
       }
     }
   };
-  int in = 0;  // the piece that is taken next
   // 32 columns a turn of a loop that is not unrolled, through which the accumulators move: fetching instructions costs as much as they do (64 a turn: gradient of gelu with C and
   // Q 102 us instead of 88)
 #pragma unroll 1
   for (int c = 0; c < N; c += G) {
     float v[G];
-    const float4* b = reinterpret_cast<const float4*>(pieces.bias()) + c / 4;
+    if (p.bias) {
+      const float4* b = reinterpret_cast<const float4*>(pieces.bias()) + c / 4;
 #pragma unroll
-    for (int j = 0; j < G; j += 4) {
-      const float4 f = b[j / 4];
-      const Two x = fma2({acc[j], acc[j + 1]}, both(p.alpha), {f.x, f.y}), y = fma2({acc[j + 2], acc[j + 3]}, both(p.alpha), {f.z, f.w});
-      v[j] = x.a, v[j + 1] = x.b, v[j + 2] = y.a, v[j + 3] = y.b;
+      for (int j = 0; j < G; j += 4) {
+        const float4 f = b[j / 4];
+        const Two x = fma2({acc[j], acc[j + 1]}, both(p.alpha), {f.x, f.y}), y = fma2({acc[j + 2], acc[j + 3]}, both(p.alpha), {f.z, f.w});
+        v[j] = x.a, v[j + 1] = x.b, v[j + 2] = y.a, v[j + 3] = y.b;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < G; j += 2) {
+        const Two x = mul2({acc[j], acc[j + 1]}, both(p.alpha));
+        v[j] = x.a, v[j + 1] = x.b;
+      }
     }
     if (c < end) {
       if (p.Z) put(&p.mz, c, v);
@@ -461,11 +464,8 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
 #pragma unroll
         for (int j = 0; j < G; j += W) {
           uint4 x, y;
-          pieces.template take<AHEAD>(in, x, y);
-          const int ahead = c + j + AHEAD * W;
-          if (ahead < N) pieces.ask(in, ahead * (int)sizeof(TC));
-          cp_async_commit();  // also where nothing was asked for: take counts
-          in = in + 1 == AHEAD ? 0 : in + 1;
+          pieces.take(x, y);
+          if (c + j + W < N) pieces.ask((c + j + W) * (int)sizeof(TC));
           float m[W];
           act_unpack16<TC>(x, m);
           act_unpack16<TC>(y, m + H);
@@ -504,17 +504,22 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
   const uint32_t byte = f8_scale_byte(__float_as_uint(larger_nan(larger_nan(most[0], most[1]), larger_nan(most[2], most[3]))));
   if (row < p.rows) p.S[row * p.lds + col0 / kF8Block] = (uint8_t)byte;
   const float inv = byte == kScaleNan ? 0.0f : f8_inv_scale(byte);
+  constexpr int Q = PIECES - 1 < 2 ? 1 : 2;  // pieces of 32 numbers at a time
 #pragma unroll
-  for (int j = 0; j < N; j += 32) {
-    uint32_t w[8];
+  for (int j = 0; j < N; j += 32 * Q) {
+    uint4 q[2 * Q];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float* a = acc + j + 4 * i;
-      const Two x = mul2({a[0], a[1]}, both(inv)), y = mul2({a[2], a[3]}, both(inv));
-      w[i] = byte == kScaleNan ? 0x7f7f7f7fu : f8_pack4(x.a, x.b, y.a, y.b);
+    for (int i = 0; i < 2 * Q; ++i) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float* a = acc + j + 16 * i + 4 * e;
+        const Two x = mul2({a[0], a[1]}, both(inv)), y = mul2({a[2], a[3]}, both(inv));
+        w[e] = byte == kScaleNan ? 0x7f7f7f7fu : f8_pack4(x.a, x.b, y.a, y.b);
+      }
+      q[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    const uint4 q[2] = {make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7])};
-    if (j < end) pieces.template put<1>(&p.mq, (int)col0 + j, 32, (int)col0 + end, (int)row0, q);
+    if (j < end) pieces.template put<Q>(&p.mq, (int)col0 + j, 32, (int)col0 + end, (int)row0, q);
   }
 }
 
