@@ -48,8 +48,9 @@ struct AdamStep {
   double lr, wd, log_b1, log_b2;
   int64_t step;
 };
-constexpr int kPieces = 2;                    // of 256 elements, a warp's: 512, four blocks of 8-bit states
-constexpr int kUnit = 8 * 256 * kPieces;      // elements of a CTA
+// A warp has PIECES times 256 elements: two, or one where the list is too short to give every SM several CTAs of that (ten tensors of 790 thousand elements 7.7 us on the GPU with two,
+// 4.7 with one).
+__host__ __device__ constexpr int unit(int pieces) { return 8 * 256 * pieces; }  // elements of a CTA
 
 // The finaliser of MurmurHash3 (Austin Appleby, public domain).
 __host__ __device__ __forceinline__ uint32_t fmix(uint32_t x) {
@@ -97,34 +98,34 @@ __device__ __forceinline__ void adam_element(const AdamStep& s, float g, float& 
   p = __fadd_rn(__fmul_rn(p, s.decay), -__fdividef(s.size * m, fmaf(r, s.root, s.eps)));
 }
 
-template <typename TP, typename TG, int BITS, bool VEC>
+template <typename TP, typename TG, int BITS, bool VEC, int PIECES>
 __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep& s, float scale, int64_t at0) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t at = at0 + warp * 256 * kPieces;
+  const int64_t at = at0 + warp * 256 * PIECES;
   if (at >= t.n) return;
-  const int n = (int)min((int64_t)(256 * kPieces), t.n - at);  // elements of this warp
+  const int n = (int)min((int64_t)(256 * PIECES), t.n - at);  // elements of this warp
   TP* P = static_cast<TP*>(t.p) + at;
   const TG* G = static_cast<const TG*>(t.g) + at;
   using AtP = Warp256<TP, VEC>;
   using AtG = Warp256<TG, VEC>;
   using At4 = Warp256<float, VEC>;
-  Raw8<TP> p8[kPieces];
-  Raw8<TG> g8[kPieces];
+  Raw8<TP> p8[PIECES];
+  Raw8<TG> g8[PIECES];
 #pragma unroll
-  for (int u = 0; u < kPieces; ++u) {
+  for (int u = 0; u < PIECES; ++u) {
     AtP::load(P, 256 * u, n, p8[u]);
     AtG::load(G, 256 * u, n, g8[u]);
   }
   if constexpr (BITS == 32) {
     float *M = static_cast<float*>(t.m) + at, *V = static_cast<float*>(t.v) + at;
-    Raw8<float> m8[kPieces], v8[kPieces];
+    Raw8<float> m8[PIECES], v8[PIECES];
 #pragma unroll
-    for (int u = 0; u < kPieces; ++u) {
+    for (int u = 0; u < PIECES; ++u) {
       At4::load(M, 256 * u, n, m8[u]);
       At4::load(V, 256 * u, n, v8[u]);
     }
 #pragma unroll
-    for (int u = 0; u < kPieces; ++u) {
+    for (int u = 0; u < PIECES; ++u) {
       float p[8], g[8], m[8], v[8], r;
       unpack8(p8[u], p), unpack8(g8[u], g), unpack8(m8[u], m), unpack8(v8[u], v);
 #pragma unroll
@@ -134,12 +135,12 @@ __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep&
       At4::store(V, 256 * u, n, v);
     }
   } else {
-    static_assert(!VEC, "aligned elements are adam_512's");
+    static_assert(!VEC, "aligned elements are adam_aligned's");
     uint8_t *M = static_cast<uint8_t*>(t.m) + at, *R = static_cast<uint8_t*>(t.v) + at;
     uint8_t *SM = t.sm + at / kF8Block, *SR = t.sv + at / kF8Block;
-    uint32_t m8[kPieces][2], r8[kPieces][2], sm[kPieces][2], sr[kPieces][2];  // half h of a lane's numbers is of block h
+    uint32_t m8[PIECES][2], r8[PIECES][2], sm[PIECES][2], sr[PIECES][2];  // half h of a lane's numbers is of block h
 #pragma unroll
-    for (int u = 0; u < kPieces; ++u)
+    for (int u = 0; u < PIECES; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         m8[u][h] = r8[u][h] = 0;
@@ -153,7 +154,7 @@ __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep&
       }
     const uint64_t e0 = t.first + (uint64_t)at;
 #pragma unroll
-    for (int u = 0; u < kPieces; ++u) {
+    for (int u = 0; u < PIECES; ++u) {
       float p[8], g[8], m[8], r[8];
       unpack8(p8[u], p), unpack8(g8[u], g);
       f8_unpack4(m8[u][0], m), f8_unpack4(m8[u][1], m + 4), f8_unpack4(r8[u][0], r), f8_unpack4(r8[u][1], r + 4);
@@ -193,9 +194,9 @@ __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep&
   }
 }
 
-// ---- 512 aligned elements of a warp, states in 8 bits -------------------------------------------------------------------------
+// ---- 512 or 256 aligned elements of a warp, states in 8 bits -----------------------------------------------------------------
 // 14 bytes an element leave a GPU some eighty instructions for it, which one at a time they were not enough (109: 1000 us for 268 million elements, 574 by the bytes).  So this
-// path does as much as it can two numbers at a time and gives a lane sixteen consecutive elements (eight lanes to a block).  Numbers below 2^-6 of their scale, whose
+// path does as much as it can two numbers at a time and gives a lane sixteen (or eight) consecutive elements, eight (or sixteen) lanes to a block.  Numbers below 2^-6 of their scale, whose
 // distance is not the binade's, take a branch; a warp with a v for which the root below is not exact, or not finite, goes to adam_pieces before it has written anything.
 
 // A sum of products that are rounded before: the packed addition is joined with them to a multiply-add (4 of 16 million first moments fell to the other side of their rounding).
@@ -212,25 +213,29 @@ __device__ __forceinline__ Two sqrt2_rn(Two v) {
   const Two e = fma2({-s.a, -s.b}, s, v);
   return fma2(e, h, s);
 }
-// Sixteen magnitudes' largest, NaN where there is one, and smallest.
+// E magnitudes' largest, NaN where there is one, and smallest.
 struct Extent {
   float most, least;
 };
-__device__ __forceinline__ Extent extent16(const float* x) {
+template <int E>
+__device__ __forceinline__ Extent extent_of(const float* x) {
   Extent e{fabsf(x[0]), fabsf(x[0])};
 #pragma unroll
-  for (int j = 1; j < 16; ++j) e.most = larger_nan(e.most, fabsf(x[j])), e.least = fminf(e.least, fabsf(x[j]));
+  for (int j = 1; j < E; ++j) e.most = larger_nan(e.most, fabsf(x[j])), e.least = fminf(e.least, fabsf(x[j]));
   return e;
 }
-// Sixteen numbers of a block as e4m3, with the random bits of two hashes.
-template <bool ROOT>
-__device__ __forceinline__ uint4 quantise16(const float* x, uint32_t byte, float least, uint32_t h0, uint32_t h1) {
-  if (byte == kScaleNan) return make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
+// E numbers of a block as e4m3, with the random bits of a hash for each eight of them.
+template <bool ROOT, int E>
+__device__ __forceinline__ void quantise_at_random(const float* x, uint32_t byte, float least, const uint32_t (&h)[2], uint32_t (&w)[E / 4]) {
+  if (byte == kScaleNan) {
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) w[i] = 0x7f7f7f7fu;
+    return;
+  }
   const float inv = f8_inv_scale(byte);
   const bool plain = least * inv >= 0.015625f;
-  uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < E / 4; ++i) {
     float t[4];
 #pragma unroll
     for (int j = 0; j < 4; j += 2) {
@@ -239,7 +244,7 @@ __device__ __forceinline__ uint4 quantise16(const float* x, uint32_t byte, float
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t bits = ((i < 2 ? h0 : h1) + (uint32_t)((4 * i + j) & 7) * kGolden) >> 12;
+      const uint32_t bits = (h[i / 2] + (uint32_t)((4 * i + j) & 7) * kGolden) >> 12;
       if (plain) {
         t[j] = __uint_as_float((__float_as_uint(t[j]) + bits) & 0xfff00000u);
       } else {
@@ -250,89 +255,100 @@ __device__ __forceinline__ uint4 quantise16(const float* x, uint32_t byte, float
     }
     w[i] = f8_pack4(t[0], t[1], t[2], t[3]);
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void load16(const float* p, uint4 (&q)[4]) {
+// 4 Q bytes of a lane as they lie in memory, aligned to 16
+template <int Q>
+__device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[Q]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) q[i] = reinterpret_cast<const uint4*>(p)[i];
+  for (int i = 0; i < Q / 4; ++i) {
+    const uint4 q = static_cast<const uint4*>(p)[i];
+    w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+  }
 }
-__device__ __forceinline__ void load16(const __nv_bfloat16* p, uint4 (&q)[2]) { q[0] = reinterpret_cast<const uint4*>(p)[0], q[1] = reinterpret_cast<const uint4*>(p)[1]; }
-__device__ __forceinline__ Two pair16(const uint4 (&q)[4], int i) {
-  const uint4 w = q[i / 2];
-  return i & 1 ? Two{__uint_as_float(w.z), __uint_as_float(w.w)} : Two{__uint_as_float(w.x), __uint_as_float(w.y)};
+template <typename T, int Q>
+__device__ __forceinline__ Two pair_at(const uint32_t (&w)[Q], int i) {
+  if constexpr (sizeof(T) == 2) return {__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)};
+  else return {__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])};
 }
-__device__ __forceinline__ Two pair16(const uint4 (&q)[2], int i) {
-  const uint4 v = q[i / 4];
-  const uint32_t w = (i & 3) == 0 ? v.x : (i & 3) == 1 ? v.y : (i & 3) == 2 ? v.z : v.w;
-  return {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
-}
-__device__ __forceinline__ void store16(float* p, const float* v) {
+template <typename T, int E>
+__device__ __forceinline__ void store_numbers(T* p, const float* v) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-}
-__device__ __forceinline__ void store16(__nv_bfloat16* p, const float* v) {
+  for (int i = 0; i < E; i += 8) {
+    float x[8];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    reinterpret_cast<uint4*>(p)[i] = make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]), pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
+    for (int j = 0; j < 8; ++j) x[j] = v[i + j];
+    store8(p + i, 8, true, x);
+  }
 }
-__device__ __forceinline__ void load8x16(const uint8_t* p, uint32_t (&w)[4]) {  // 8-byte aligned
-  const uint2 a = reinterpret_cast<const uint2*>(p)[0], b = reinterpret_cast<const uint2*>(p)[1];
-  w[0] = a.x, w[1] = a.y, w[2] = b.x, w[3] = b.y;
+// E bytes, aligned to 8
+template <int E>
+__device__ __forceinline__ void load_bytes(const uint8_t* p, uint32_t (&w)[E / 4]) {
+#pragma unroll
+  for (int i = 0; i < E / 8; ++i) {
+    const uint2 a = reinterpret_cast<const uint2*>(p)[i];
+    w[2 * i] = a.x, w[2 * i + 1] = a.y;
+  }
 }
-__device__ __forceinline__ void store8x16(uint8_t* p, uint4 w) {
-  reinterpret_cast<uint2*>(p)[0] = make_uint2(w.x, w.y), reinterpret_cast<uint2*>(p)[1] = make_uint2(w.z, w.w);
+template <int E>
+__device__ __forceinline__ void store_bytes(uint8_t* p, const uint32_t (&w)[E / 4]) {
+#pragma unroll
+  for (int i = 0; i < E / 8; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
 }
 
 // False, with nothing written, where a root is not exact.
-template <typename TP, typename TG>
-__device__ __forceinline__ bool adam_512(const AdamTensor& t, const AdamStep& s, float scale, int64_t at) {
-  const int lane = threadIdx.x & 31, block = lane >> 3;
-  const int64_t e0 = at + 16 * lane;
+template <typename TP, typename TG, int E>
+__device__ __forceinline__ bool adam_aligned(const AdamTensor& t, const AdamStep& s, float scale, int64_t at) {
+  constexpr int L = kF8Block / E;  // lanes of a block
+  const int lane = threadIdx.x & 31, block = lane / L;
+  const int64_t e0 = at + E * lane;
   TP* P = static_cast<TP*>(t.p) + e0;
   uint8_t *M = static_cast<uint8_t*>(t.m) + e0, *R = static_cast<uint8_t*>(t.v) + e0, *SM = t.sm + at / kF8Block + block, *SR = t.sv + at / kF8Block + block;
-  uint4 pq[sizeof(TP)], gq[sizeof(TG)];
-  uint32_t mq[4], rq[4];
-  load16(P, pq);
-  load16(static_cast<const TG*>(t.g) + e0, gq);
-  load8x16(M, mq), load8x16(R, rq);
+  uint32_t pq[E * sizeof(TP) / 4], gq[E * sizeof(TG) / 4], mq[E / 4], rq[E / 4];
+  load_words(P, pq);
+  load_words(static_cast<const TG*>(t.g) + e0, gq);
+  load_bytes<E>(M, mq), load_bytes<E>(R, rq);
   const float sm = e8m0_value(*SM), sr = e8m0_value(*SR);
-  float p[16], m[16], r[16];
+  float p[E], m[E], r[E];
   uint32_t least_v = 0xffffffffu;  // of the bits of v, less one, so that 0 is the largest
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < E / 4; ++i) {
     float a[4], b[4];
     f8_unpack4(mq[i], a), f8_unpack4(rq[i], b);
 #pragma unroll
     for (int j = 0; j < 4; j += 2) {
       const int k = 4 * i + j;
-      const Two g = mul2(pair16(gq, k / 2), both(scale));
+      const Two g = mul2(pair_at<TG>(gq, k / 2), both(scale));
       const Two mo = mul2({a[j], a[j + 1]}, both(sm)), ro = mul2({b[j], b[j + 1]}, both(sr));
       const Two mn = sum_rn(mul2(mo, both(s.b1)), mul2(g, both(s.a1)));
       const Two v = sum_rn(mul2(mul2(ro, ro), both(s.b2)), mul2(mul2(g, g), both(s.a2)));
       const Two rn = sqrt2_rn(v);
       least_v = min(least_v, min(__float_as_uint(v.a) - 1u, __float_as_uint(v.b) - 1u));
       const Two step = mul2(mul2(mn, both(s.size)), rcp_approx(fma2(rn, both(s.root), both(s.eps))));
-      const Two pn = add2(mul2(pair16(pq, k / 2), both(s.decay)), {-step.a, -step.b});
+      const Two pn = add2(mul2(pair_at<TP>(pq, k / 2), both(s.decay)), {-step.a, -step.b});
       m[k] = mn.a, m[k + 1] = mn.b, r[k] = rn.a, r[k + 1] = rn.b, p[k] = pn.a, p[k + 1] = pn.b;
     }
   }
-  const Extent em = extent16(m), er = extent16(r);
+  const Extent em = extent_of<E>(m), er = extent_of<E>(r);
   if (__any_sync(0xffffffffu, least_v < 0x0d800000u - 1u || !(er.most <= 0x1p64f))) return false;  // 2^-100
-  store16(P, p);
+  store_numbers<TP, E>(P, p);
   float am = em.most, ar = er.most;
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) am = larger_nan(am, __shfl_xor_sync(0xffffffffu, am, o)), ar = larger_nan(ar, __shfl_xor_sync(0xffffffffu, ar, o));
+  for (int o = L / 2; o > 0; o >>= 1) am = larger_nan(am, __shfl_xor_sync(0xffffffffu, am, o)), ar = larger_nan(ar, __shfl_xor_sync(0xffffffffu, ar, o));
   const uint32_t bm = f8_scale_byte(__float_as_uint(am)), br = f8_scale_byte(__float_as_uint(ar));
-  const uint64_t e8 = (t.first + (uint64_t)e0) >> 3;  // even: both hashes have the same high half
+  const uint64_t e8 = (t.first + (uint64_t)e0) >> 3;  // even where there are two hashes: both have the same high half
   const uint32_t high = fmix((uint32_t)(e8 >> 32) + s.key);
-  const uint32_t h0 = fmix((uint32_t)e8 + high), h1 = fmix((uint32_t)e8 + 1 + high);
-  store8x16(M, quantise16<false>(m, bm, em.least, h0, h1));
-  store8x16(R, quantise16<true>(r, br, er.least, fmix(h0 + kGolden), fmix(h1 + kGolden)));
-  if ((lane & 7) == 0) *SM = (uint8_t)bm, *SR = (uint8_t)br;
+  uint32_t h[2], g[2], w[E / 4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) h[i] = fmix((uint32_t)e8 + (uint32_t)i + high), g[i] = fmix(h[i] + kGolden);
+  quantise_at_random<false, E>(m, bm, em.least, h, w);
+  store_bytes<E>(M, w);
+  quantise_at_random<true, E>(r, br, er.least, g, w);
+  store_bytes<E>(R, w);
+  if (lane % L == 0) *SM = (uint8_t)bm, *SR = (uint8_t)br;
   return true;
 }
 
-template <typename TP, typename TG, int BITS, int MOST>
+template <typename TP, typename TG, int BITS, int MOST, int PIECES>
 __global__ void __launch_bounds__(256, BITS == 8 ? 3 : 2) adamw_kernel(const __grid_constant__ AdamList<MOST> list, AdamStep s) {
   grid_started();
   int lo = 0, hi = list.count;  // the last tensor whose first CTA is not after this one
@@ -345,34 +361,34 @@ __global__ void __launch_bounds__(256, BITS == 8 ? 3 : 2) adamw_kernel(const __g
   grid_ready();
   if (s.step_device || s.lr_device) adam_factors(s, s.lr_device ? (double)*s.lr_device : s.lr, s.step_device ? *s.step_device : s.step);
   const float scale = s.scale ? *s.scale : 1.0f;
-  const int64_t at = (int64_t)(blockIdx.x - list.cta[lo]) * kUnit;
+  const int64_t at = (int64_t)(blockIdx.x - list.cta[lo]) * unit(PIECES);
   if constexpr (BITS == 8) {
-    const int64_t mine = at + (threadIdx.x >> 5) * (256 * kPieces);
-    if (t.vec && mine + 512 <= t.n && adam_512<TP, TG>(t, s, scale, mine)) return;
-    adam_pieces<TP, TG, 8, false>(t, s, scale, at);  // also what does not start on 16 bytes, and the ends
+    const int64_t mine = at + (threadIdx.x >> 5) * (256 * PIECES);
+    if (t.vec && mine + 256 * PIECES <= t.n && adam_aligned<TP, TG, 8 * PIECES>(t, s, scale, mine)) return;
+    adam_pieces<TP, TG, 8, false, PIECES>(t, s, scale, at);  // also what does not start on 16 bytes, and the ends
   } else {
-    if (t.vec) adam_pieces<TP, TG, 32, true>(t, s, scale, at);
-    else adam_pieces<TP, TG, 32, false>(t, s, scale, at);
+    if (t.vec) adam_pieces<TP, TG, 32, true, PIECES>(t, s, scale, at);
+    else adam_pieces<TP, TG, 32, false, PIECES>(t, s, scale, at);
   }
 }
 
-template <typename TP, typename TG, int BITS, int MOST>
+template <typename TP, typename TG, int BITS, int PIECES, int MOST>
 int adam_launch(const AdamList<MOST>& list, unsigned ctas, const AdamStep& s, cudaStream_t st) {
-  return launch_overlapped(adamw_kernel<TP, TG, BITS, MOST>, ctas, 256, st, list, s);
+  return launch_overlapped(adamw_kernel<TP, TG, BITS, MOST, PIECES>, ctas, 256, st, list, s);
 }
-template <int MOST>
+template <int PIECES, int MOST>
 int adam_launch_kind(int kind, const AdamList<MOST>& list, unsigned ctas, const AdamStep& s, cudaStream_t st) {
   using F = float;
   using B = __nv_bfloat16;
   switch (kind) {
-    case 0: return adam_launch<F, F, 32>(list, ctas, s, st);
-    case 1: return adam_launch<F, B, 32>(list, ctas, s, st);
-    case 2: return adam_launch<B, F, 32>(list, ctas, s, st);
-    case 3: return adam_launch<B, B, 32>(list, ctas, s, st);
-    case 4: return adam_launch<F, F, 8>(list, ctas, s, st);
-    case 5: return adam_launch<F, B, 8>(list, ctas, s, st);
-    case 6: return adam_launch<B, F, 8>(list, ctas, s, st);
-    default: return adam_launch<B, B, 8>(list, ctas, s, st);
+    case 0: return adam_launch<F, F, 32, PIECES>(list, ctas, s, st);
+    case 1: return adam_launch<F, B, 32, PIECES>(list, ctas, s, st);
+    case 2: return adam_launch<B, F, 32, PIECES>(list, ctas, s, st);
+    case 3: return adam_launch<B, B, 32, PIECES>(list, ctas, s, st);
+    case 4: return adam_launch<F, F, 8, PIECES>(list, ctas, s, st);
+    case 5: return adam_launch<F, B, 8, PIECES>(list, ctas, s, st);
+    case 6: return adam_launch<B, F, 8, PIECES>(list, ctas, s, st);
+    default: return adam_launch<B, B, 8, PIECES>(list, ctas, s, st);
   }
 }
 
@@ -403,21 +419,21 @@ bool adam_apart(const b2_adamw_tensor* tensors, int count, AdamRange* r) {
 int adam_kind(const b2_adamw_tensor& t) { return (t.state_bits == 8 ? 4 : 0) + (t.type_param == B2_TYPE_BF16 ? 2 : 0) + (t.type_grad == B2_TYPE_BF16 ? 1 : 0); }
 
 // The tensors of one kind, MOST at a time.
-template <int MOST>
+template <int PIECES, int MOST>
 int adam_run(const b2_adamw_tensor* tensors, int count, int kind, const AdamStep& s, cudaStream_t st) {
   AdamList<MOST> list;
   list.count = 0;
   int64_t ctas = 0;
   uint64_t first = 0;
   auto flush = [&]() {
-    const int rc = list.count ? adam_launch_kind(kind, list, (unsigned)ctas, s, st) : B2_OK;
+    const int rc = list.count ? adam_launch_kind<PIECES>(kind, list, (unsigned)ctas, s, st) : B2_OK;
     list.count = 0, ctas = 0;
     return rc;
   };
   for (int i = 0; i < count; ++i) {
     const b2_adamw_tensor& t = tensors[i];
     if (t.n > 0 && adam_kind(t) == kind) {
-      const int64_t more = blocks_of(t.n, kUnit);
+      const int64_t more = blocks_of(t.n, unit(PIECES));
       if (list.count == MOST || ctas + more > 0x7fffffffLL) {
         const int rc = flush();
         if (rc) return rc;
@@ -449,9 +465,10 @@ extern "C" int b2_adamw(const b2_adamw_tensor* tensors, int count, double lr, do
   if (!(weight_decay - weight_decay == 0.0)) return -7;
   if (!step_device && step < 1) return -8;
   int of_kind[8] = {};
+  double elements[8] = {};
   for (int i = 0; i < count; ++i) {
-    if (!adam_valid(tensors[i]) || blocks_of(tensors[i].n, kUnit) > 0x7fffffffLL) return -1;
-    if (tensors[i].n > 0) ++of_kind[adam_kind(tensors[i])];
+    if (!adam_valid(tensors[i]) || blocks_of(tensors[i].n, unit(1)) > 0x7fffffffLL) return -1;
+    if (tensors[i].n > 0) ++of_kind[adam_kind(tensors[i])], elements[adam_kind(tensors[i])] += (double)tensors[i].n;
   }
   AdamRange few[32];
   std::unique_ptr<AdamRange[]> many(count > 32 ? new (std::nothrow) AdamRange[count] : nullptr);
@@ -464,7 +481,9 @@ extern "C" int b2_adamw(const b2_adamw_tensor* tensors, int count, double lr, do
   if (!lr_device && !step_device) adam_factors(s, lr, step);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   for (int kind = 0; kind < 8; ++kind) {
-    const int rc = of_kind[kind] == 0 ? B2_OK : of_kind[kind] <= 12 ? adam_run<12>(tensors, count, kind, s, st) : adam_run<240>(tensors, count, kind, s, st);
+    if (of_kind[kind] == 0) continue;
+    const bool few = of_kind[kind] <= 12, small = elements[kind] < (double)unit(2) * 3 * sm_count_cached();
+    const int rc = !few ? adam_run<2, 240>(tensors, count, kind, s, st) : small ? adam_run<1, 12>(tensors, count, kind, s, st) : adam_run<2, 12>(tensors, count, kind, s, st);
     if (rc) return rc;
   }
   return B2_OK;
