@@ -201,17 +201,28 @@ __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep&
 
 // A sum of products that are rounded before: the packed addition is joined with them to a multiply-add (4 of 16 million first moments fell to the other side of their rounding).
 __device__ __forceinline__ Two sum_rn(Two x, Two y) { return {__fadd_rn(x.a, y.a), __fadd_rn(x.b, y.b)}; }
-// Square roots, rounded to nearest: an approximation of the reciprocal root, and from it one Newton step on the root with the exact remainder (P. Markstein, IBM Journal of
-// Research and Development 34, 1990).  0, and 2^-100 to the largest finite number, give __fsqrt_rn's results: tried for every mantissa and both parities of the exponent.
+// Minus the square roots of -n, n <= 0, rounded to nearest: an approximation of the reciprocal root, and from it one Newton step on the root with the exact remainder (P.
+// Markstein, IBM Journal of Research and Development 34, 1990); all signs turned, so that none is in the way of the packed instructions.  0, and 2^-100 to the largest finite
+// number, give __fsqrt_rn's results: tried for every mantissa and both parities of the exponent.
 __device__ __forceinline__ float rsqrt_approx(float x) {
   float y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ Two sqrt2_rn(Two v) {
-  const Two y = {rsqrt_approx(fmaxf(v.a, 0x1p-100f)), rsqrt_approx(fmaxf(v.b, 0x1p-100f))}, s = mul2(v, y), h = mul2(y, both(0.5f));
-  const Two e = fma2({-s.a, -s.b}, s, v);
-  return fma2(e, h, s);
+__device__ __forceinline__ Two minus_sqrt2_rn(Two n) {
+  const Two y = {rsqrt_approx(fmaxf(-n.a, 0x1p-100f)), rsqrt_approx(fmaxf(-n.b, 0x1p-100f))}, s = mul2(n, y), h = mul2(y, both(0.5f));
+  return fma2(fma2(s, s, n), h, s);
+}
+// of three magnitudes
+__device__ __forceinline__ float largest_nan(float a, float b, float c) {
+  float y;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ float smallest(float a, float b, float c) {
+  float y;
+  asm("min.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
 }
 // E magnitudes' largest, NaN where there is one, and smallest.
 struct Extent {
@@ -221,10 +232,10 @@ template <int E>
 __device__ __forceinline__ Extent extent_of(const float* x) {
   Extent e{fabsf(x[0]), fabsf(x[0])};
 #pragma unroll
-  for (int j = 1; j < E; ++j) e.most = larger_nan(e.most, fabsf(x[j])), e.least = fminf(e.least, fabsf(x[j]));
-  return e;
+  for (int j = 1; j + 1 < E; j += 2) e.most = largest_nan(e.most, x[j], x[j + 1]), e.least = smallest(e.least, x[j], x[j + 1]);
+  return {largest_nan(e.most, x[E - 1], x[E - 1]), smallest(e.least, x[E - 1], x[E - 1])};
 }
-// E numbers of a block as e4m3, with the random bits of a hash for each eight of them.
+// E numbers of a block as e4m3, with the random bits of a hash for each eight of them.  ROOT: they are the roots' negatives.
 template <bool ROOT, int E>
 __device__ __forceinline__ void quantise_at_random(const float* x, uint32_t byte, float least, const uint32_t (&h)[2], uint32_t (&w)[E / 4]) {
   if (byte == kScaleNan) {
@@ -232,8 +243,8 @@ __device__ __forceinline__ void quantise_at_random(const float* x, uint32_t byte
     for (int i = 0; i < E / 4; ++i) w[i] = 0x7f7f7f7fu;
     return;
   }
-  const float inv = f8_inv_scale(byte);
-  const bool plain = least * inv >= 0.015625f;
+  const float inv = ROOT ? -f8_inv_scale(byte) : f8_inv_scale(byte);
+  const bool plain = least * fabsf(inv) >= 0.015625f;
 #pragma unroll
   for (int i = 0; i < E / 4; ++i) {
     float t[4];
@@ -308,8 +319,7 @@ __device__ __forceinline__ bool adam_aligned(const AdamTensor& t, const AdamStep
   load_words(static_cast<const TG*>(t.g) + e0, gq);
   load_bytes<E>(M, mq), load_bytes<E>(R, rq);
   const float sm = e8m0_value(*SM), sr = e8m0_value(*SR);
-  float p[E], m[E], r[E];
-  uint32_t least_v = 0xffffffffu;  // of the bits of v, less one, so that 0 is the largest
+  float p[E], m[E], r[E];  // r: minus the root
 #pragma unroll
   for (int i = 0; i < E / 4; ++i) {
     float a[4], b[4];
@@ -320,16 +330,20 @@ __device__ __forceinline__ bool adam_aligned(const AdamTensor& t, const AdamStep
       const Two g = mul2(pair_at<TG>(gq, k / 2), both(scale));
       const Two mo = mul2({a[j], a[j + 1]}, both(sm)), ro = mul2({b[j], b[j + 1]}, both(sr));
       const Two mn = sum_rn(mul2(mo, both(s.b1)), mul2(g, both(s.a1)));
-      const Two v = sum_rn(mul2(mul2(ro, ro), both(s.b2)), mul2(mul2(g, g), both(s.a2)));
-      const Two rn = sqrt2_rn(v);
-      least_v = min(least_v, min(__float_as_uint(v.a) - 1u, __float_as_uint(v.b) - 1u));
-      const Two step = mul2(mul2(mn, both(s.size)), rcp_approx(fma2(rn, both(s.root), both(s.eps))));
-      const Two pn = add2(mul2(pair_at<TP>(pq, k / 2), both(s.decay)), {-step.a, -step.b});
+      const Two minus_v = sum_rn(mul2(mul2(ro, ro), both(-s.b2)), mul2(mul2(g, g), both(-s.a2)));
+      const Two rn = minus_sqrt2_rn(minus_v);
+      const Two inv = rcp_approx(fma2(rn, both(-s.root), both(s.eps)));
+      const Two pn = fma2(mul2(mn, both(-s.size)), inv, mul2(pair_at<TP>(pq, k / 2), both(s.decay)));
       m[k] = mn.a, m[k + 1] = mn.b, r[k] = rn.a, r[k + 1] = rn.b, p[k] = pn.a, p[k + 1] = pn.b;
     }
   }
   const Extent em = extent_of<E>(m), er = extent_of<E>(r);
-  if (__any_sync(0xffffffffu, least_v < 0x0d800000u - 1u || !(er.most <= 0x1p64f))) return false;  // 2^-100
+  bool exact = er.most <= 0x1p64f;  // not NaN
+  if (er.least < 0x1p-50f) {
+#pragma unroll
+    for (int k = 0; k < E; ++k) exact = exact && (r[k] == 0.0f || r[k] <= -0x1p-50f);
+  }
+  if (!__all_sync(0xffffffffu, exact)) return false;
   store_numbers<TP, E>(P, p);
   float am = em.most, ar = er.most;
 #pragma unroll
