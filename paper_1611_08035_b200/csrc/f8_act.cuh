@@ -316,7 +316,8 @@ __device__ __forceinline__ bool act_emit_halves(const F8ActOut& p, int64_t row0,
 // TMA, whose small loads wait behind the operands' large ones, the gradient of gelu with C and Q 96, 9400 clocks of a tile for Z alone (now 80).
 constexpr int kActPiece = 32 * 32;
 constexpr int kActBias = kF8Block * 4;
-template <int PIECES>
+// GRADIENT: the form with a kernel of its own, so that either's instructions are few.
+template <int PIECES, bool GRADIENT>
 struct F8ActTiles : F8ActOut {
   static constexpr int WARP_BYTES = PIECES * kActPiece + kActBias;
   CUtensorMap mz, mc, mq;  // of Z, C and Q where they are written
@@ -392,12 +393,12 @@ struct ActPieces {
   }
 };
 // Before the sums are waited for: the bias of the tile's features, 0 beyond the matrix and where there is none, and the first pieces of what is read.
-template <typename TC, int PIECES>
-__device__ __forceinline__ void act_begin_tile(const F8ActTiles<PIECES>& p, int64_t row0, int64_t col0, ActPieces<PIECES>& pieces) {
+template <typename TC, int PIECES, bool GRADIENT>
+__device__ __forceinline__ void act_begin_tile(const F8ActTiles<PIECES, GRADIENT>& p, int64_t row0, int64_t col0, ActPieces<PIECES>& pieces) {
   if (row0 >= p.rows || col0 >= p.cols) return;  // the warp's part of an edge tile lies outside
   const int64_t col = col0 + 4 * (threadIdx.x & 31);
   float4 b = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  if (p.bias) {
+  if (!GRADIENT && p.bias) {
     if (p.vb && col + 4 <= p.cols) {
       b = *reinterpret_cast<const float4*>(p.bias + col);
     } else {
@@ -407,22 +408,24 @@ __device__ __forceinline__ void act_begin_tile(const F8ActTiles<PIECES>& p, int6
       if (col + 3 < p.cols) b.w = p.bias[col + 3];
     }
   }
-  if (p.Zin || p.R) {
+  if (GRADIENT || p.R) {
     cp_async_wait<0>();  // an edge tile before this one leaves a piece that it did not take
-    pieces.template read_from<TC>(p.Zin ? p.Zin : p.R, p.Zin ? p.ldz : p.ldr, p, row0, col0);
+    pieces.template read_from<TC>(GRADIENT ? p.Zin : p.R, GRADIENT ? p.ldz : p.ldr, p, row0, col0);
     pieces.ask(0);
   }
-  __syncwarp();
-  reinterpret_cast<float4*>(pieces.bias())[threadIdx.x & 31] = b;
-  __syncwarp();
+  if (!GRADIENT) {
+    __syncwarp();
+    reinterpret_cast<float4*>(pieces.bias())[threadIdx.x & 31] = b;
+    __syncwarp();
+  }
 }
-template <typename TC, int PIECES>
-__device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64_t row0, int64_t col0, float* acc, ActPieces<PIECES>& pieces) {
+template <typename TC, int PIECES, bool GRADIENT>
+__device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES, GRADIENT>& p, int64_t row0, int64_t col0, float* acc, ActPieces<PIECES>& pieces) {
   constexpr int G = 32, N = kF8Block, H = 16 / (int)sizeof(TC), W = 2 * H;  // numbers of 16 bytes, of a row of a piece
   if (row0 >= p.rows || col0 >= p.cols) return;
   const int64_t row = row0 + (threadIdx.x & 31);
   const int end = (int)min((int64_t)N, p.cols - col0);
-  const bool reads = p.Zin || p.R;
+  const bool reads = GRADIENT || p.R;
   auto put = [&](const CUtensorMap* map, int c, const float* v) {
     if (PIECES == 2) {
 #pragma unroll
@@ -443,7 +446,7 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
 #pragma unroll 1
   for (int c = 0; c < N; c += G) {
     float v[G];
-    if (p.bias) {
+    if (!GRADIENT && p.bias) {
       const float4* b = reinterpret_cast<const float4*>(pieces.bias()) + c / 4;
 #pragma unroll
       for (int j = 0; j < G; j += 4) {
@@ -459,7 +462,7 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
       }
     }
     if (c < end) {
-      if (p.Z) put(&p.mz, c, v);
+      if (!GRADIENT && p.Z) put(&p.mz, c, v);
       if (reads) {
 #pragma unroll
         for (int j = 0; j < G; j += W) {
@@ -469,7 +472,7 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
           float m[W];
           act_unpack16<TC>(x, m);
           act_unpack16<TC>(y, m + H);
-          if (p.gradient) {
+          if constexpr (GRADIENT) {
             act_slopes<W>(p.act, v + j, m);
             if (p.R) {  // read in the middle of the work
               const TC* r = static_cast<const TC*>(p.R) + row * p.ldr + col0 + c + j;
@@ -487,7 +490,7 @@ __device__ __forceinline__ void act_emit_tile(const F8ActTiles<PIECES>& p, int64
             }
           }
         }
-      } else {
+      } else if constexpr (!GRADIENT) {
         act_values<G>(p.act, v);
       }
       if (p.C) put(&p.mc, c, v);
@@ -751,9 +754,9 @@ struct ActHandOver {
   static constexpr int WARP_BYTES = kEmitBytes;
   static constexpr bool TILES = false;
 };
-template <int PIECES>
-struct ActHandOver<F8ActTiles<PIECES>> {
-  static constexpr int WARP_BYTES = F8ActTiles<PIECES>::WARP_BYTES;
+template <int PIECES, bool GRADIENT>
+struct ActHandOver<F8ActTiles<PIECES, GRADIENT>> {
+  static constexpr int WARP_BYTES = F8ActTiles<PIECES, GRADIENT>::WARP_BYTES;
   static constexpr bool TILES = true;
 };
 

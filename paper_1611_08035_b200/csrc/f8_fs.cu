@@ -34,7 +34,7 @@ constexpr int kSlots = 2, kGroup = 4;   // scale ring: slots of four blocks
 constexpr int kSlotFloats = kGroup * (kRows + kBN);  // [block][128 rows, 256 columns]
 template <typename OUT>
 constexpr size_t kSmem = 1024 + kRing + 512 + kSlots * kSlotFloats * 4 + kEW * ActHandOver<OUT>::WARP_BYTES;
-static_assert(kSmem<F8Out> <= 232448 && kSmem<F8ActTiles<2>> <= 232448, "a CTA's shared memory");
+static_assert(kSmem<F8Out> <= 232448 && kSmem<F8ActTiles<2, false>> <= 232448, "a CTA's shared memory");
 
 __device__ __forceinline__ void umma_f8_pair(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -353,8 +353,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <typename TC, typename OUT>
 int f8_fs_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
   if constexpr (std::is_same<OUT, F8ActOut>::value) {
-    F8ActTiles<2> tiles;
+    F8ActTiles<2, false> tiles;
+    F8ActTiles<2, true> gradient;
     if (f8_act_tiles<TC>(a.out, r.n, c.n, tiles)) return f8_fs_launch<TC>(f8_args_with(a, tiles), r, c, k, st);
+    if (f8_act_tiles<TC>(a.out, r.n, c.n, gradient)) return f8_fs_launch<TC>(f8_args_with(a, gradient), r, c, k, st);
   }
   static std::atomic<bool> configured[64];
   return f8_pair_launch(f8_fs_kernel<TC, OUT>, configured, kThreads, kSmem<OUT>, a, r, c, k, st);

@@ -102,8 +102,9 @@ __device__ __forceinline__ void scale_words(const F8Scale& s, int64_t i, int64_t
 }
 
 // The epilogue's results as tensor maps, where all its matrices have 16-byte aligned columns.
-template <typename TC, int PIECES>
-bool f8_act_tiles(const F8ActOut& out, int64_t rows, int64_t cols, F8ActTiles<PIECES>& t) {
+template <typename TC, int PIECES, bool GRADIENT>
+bool f8_act_tiles(const F8ActOut& out, int64_t rows, int64_t cols, F8ActTiles<PIECES, GRADIENT>& t) {
+  if ((out.gradient != 0) != GRADIENT) return false;
   static_cast<F8ActOut&>(t) = out;
   if ((out.Z || out.Zin) && !out.vz) return false;
   if ((out.R && !out.vr) || (out.C && !out.vc) || (out.Q && !out.vq)) return false;

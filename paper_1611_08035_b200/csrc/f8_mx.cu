@@ -37,7 +37,7 @@ constexpr uint32_t kTmem = 512, kSfCols = 12;  // scales of four blocks: 128 row
 constexpr uint32_t kSfBytes = 2 * kSfCols * 32 * 4;
 template <typename OUT>
 constexpr size_t kSmem = 1024 + kRing + 512 + kSfBytes + kEW * ActHandOver<OUT>::WARP_BYTES;
-static_assert(kSmem<F8ActTiles<3>> <= 232448, "a CTA's shared memory");
+static_assert(kSmem<F8ActTiles<3, false>> <= 232448, "a CTA's shared memory");
 
 __device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                         uint32_t accumulate) {
@@ -299,8 +299,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <typename TC, typename OUT>
 int f8_mx_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_t k, cudaStream_t st) {
   if constexpr (std::is_same<OUT, F8ActOut>::value) {
-    F8ActTiles<3> tiles;
+    F8ActTiles<3, false> tiles;
+    F8ActTiles<3, true> gradient;
     if (f8_act_tiles<TC>(a.out, r.n, c.n, tiles)) return f8_mx_launch<TC>(f8_args_with(a, tiles), r, c, k, st);
+    if (f8_act_tiles<TC>(a.out, r.n, c.n, gradient)) return f8_mx_launch<TC>(f8_args_with(a, gradient), r, c, k, st);
   }
   static std::atomic<bool> configured[64];
   constexpr int CHUNK = chunk_blocks<TC>();
