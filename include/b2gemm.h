@@ -520,6 +520,7 @@ int b2_wgrad_f8(int64_t m, int64_t n, int64_t k, float alpha, const void* Q, int
  *   Z        m x n: where z is stored, or NULL.  Gradient form: the z that is read (with B2_ACT_NONE not looked at).
  *   R        m x n, or NULL.  R may be C.  In the gradient form Z may be C, too.
  *   C        m x n: where c is stored, or NULL where Q is given.
+ *            No other two of Z, R, C, Q, S and the operands may overlap where one of them is written.
  *   type     of Z, R and C (B2_TYPE_*; it does not matter where there are none).
  *   Q, S     c as e4m3 numbers m x n with a scale byte for each 128 features of a column (ceil(m/128) x n), by the quantisation rule above: what
  *            b2_gemm_f8 takes as an operand with block 1 and b2_wgrad_f8 as its activation.  Or NULL.
@@ -539,7 +540,7 @@ int b2_gemm_f8_act(char transa, char transb, int64_t m, int64_t n, int64_t k, fl
  * The backward pass of an activation and a bias: for every token (column) of DY, d x t,
  *     dz = dy * act'(z)   (dz = dy with B2_ACT_NONE, where Z is not looked at),      db_i = sum over tokens of dz_i
  * each where it is wanted: DZ (d x t), (Q, S) = dz quantised as b2_quant_f8 with block 1 does it, db (d floats).  db and Q come from the
- * unrounded dz.  DZ may be DY or Z.  db is summed in an order that depends on d, t and the device only: the same bits on every call.  The
+ * unrounded dz.  DZ may be DY or Z; nothing else that is written may overlap another matrix.  db is summed in an order that depends on d, t and the device only: the same bits on every call.  The
  * workspace (device, 256-byte aligned) holds partial sums of db; without db it may be NULL.
  * Arguments: d 1, t 2, type 3 (of DY, Z, DZ), act 4, DY 5, lddy 6, Z 7, ldz 8, DZ 9, lddz 10, Q 11, ldq 12, S 13, lds 14, db 15.
  * Without tokens db is 0.
@@ -566,7 +567,7 @@ int b2_act_backward(int64_t d, int64_t t, int type, int act, const void* DY, int
  *     key = fmix(fmix(fmix(lo(seed)) ^ hi(seed)) ^ lo(step)),     h = fmix(lo(e / 8) + fmix(hi(e / 8) + key)),     h' = fmix(h + G),
  * the twenty random bits u are the high ones of h + (e mod 8) G for m and of h' + (e mod 8) G for the root of v: the magnitude divided by the scale, plus u / 2^20
  * of the distance of e4m3 numbers there, is cut to an e4m3 number.
- * Types of p and g: B2_TYPE_F32 or B2_TYPE_BF16, for each tensor.  Pointers are aligned to their type; those aligned to 16 bytes (states in 8 bits: to 4)
+ * Types of p and g: B2_TYPE_F32 or B2_TYPE_BF16, for each tensor.  Pointers are aligned to their type; those aligned to 16 bytes (states in 8 bits: to 8)
  * are the fast ones.  No two tensors of a list may overlap, nor may a tensor occur twice.
  * `tensors` is a HOST array, read before the call returns; a tensor with n = 0 is left out.  step counts from 1.  step_device and lr_device
  * (DEVICE, or NULL), where given, are read when the call runs on the GPU, in the place of step and lr: a captured graph of the call follows them.

@@ -5,7 +5,8 @@
 // The inner sums are exact products accumulated in fp32 in tensor memory; a stage of the shared-memory ring holds
 // exactly one block (128 bytes of e4m3), so that the factor of a stage is a number per row times a number per column.
 //
-// This file has the entry points and the kernel for small products, one CTA to a tile; large ones go to pairs of CTAs (f8_mx.cu, f8_fs.cu).
+// This file has the entry points, of products alone and of those with an epilogue (f8_act.cuh); f8_small.cuh has the kernel for small products, one CTA to a tile; large ones go to
+// pairs of CTAs (f8_mx.cu, f8_fs.cu).
 //
 // Roles of a CTA: warp 0 streams both operands with TMA (128-byte swizzle) into the ring, warp 1 issues tcgen05.mma, the other
 // warps bring the scales and read the sums.  With e8m0 scales the tensor core applies them and the sums stay in tensor memory for
