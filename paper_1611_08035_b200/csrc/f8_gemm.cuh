@@ -101,7 +101,8 @@ __device__ __forceinline__ void scale_words(const F8Scale& s, int64_t i, int64_t
   }
 }
 
-// The epilogue's results as tensor maps, where all its matrices have 16-byte aligned columns.
+// The epilogue's results as tensor maps, where all its matrices have 16-byte aligned columns.  A copy out of shared memory ends at whole 16 bytes, not at the matrix's last row: where
+// that is within 16 bytes, it would write what lies behind.
 template <typename TC, int PIECES, bool GRADIENT>
 bool f8_act_tiles(const F8ActOut& out, int64_t rows, int64_t cols, F8ActTiles<PIECES, GRADIENT>& t) {
   if ((out.gradient != 0) != GRADIENT) return false;
@@ -112,6 +113,7 @@ bool f8_act_tiles(const F8ActOut& out, int64_t rows, int64_t cols, F8ActTiles<PI
   if (!enc) return false;
   auto map = [&](CUtensorMap* to, const void* base, int64_t ld, int elem, CUtensorMapDataType type) {
     if (!base) return true;
+    if (cols * elem % 16 != 0) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)ld * (cuuint64_t)elem};
     const cuuint32_t box[2] = {32u / (cuuint32_t)elem, 32u}, estr[2] = {1, 1};

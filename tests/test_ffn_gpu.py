@@ -160,6 +160,14 @@ def test_strides(b2, m, n, k, pad, offset):
     run_product(b2, m, n, k, "silu", pad=pad, offset=offset, out=BF if pad != 5 else F32, seed=7)
 
 
+@pytest.mark.parametrize("scale,out", [("e8m0", BF), ("e8m0", F32), ("f32", BF)])
+@pytest.mark.parametrize("m", [1601, 1602, 1604, 1606, 1607, 1608, 1609, 1612, 1616])
+def test_padding_behind_odd_sizes(b2, m, scale, out):
+    """Aligned columns whose last number is within 16 bytes: what lies between there and the next column stays as it is, in every result."""
+    for parts in ({"q": True, "z": True}, {"q": False, "z": False}, {"q": False, "gradient": True, "ta": "N"}):
+        run_product(b2, m, 1500, 140, "silu", scale=scale, out=out, pad=(-m) % 16 + 16, seed=11, **parts)
+
+
 @pytest.mark.parametrize("ta,tb,ba,bb", [("T", "T", 1, 128), ("N", "T", 128, 1), ("N", "N", 1, 1), ("T", "N", 128, 128)])
 @pytest.mark.parametrize("m,n,k", [(260, 7, 200), (300, 200, 130), (1600, 1500, 140)])
 def test_layouts(b2, m, n, k, ta, tb, ba, bb):
