@@ -518,7 +518,7 @@ int b2_wgrad_f8(int64_t m, int64_t n, int64_t k, float alpha, const void* Q, int
  *     c = (alpha * sum_p op(A)_ip sA * op(B)_pj sB) * act'(z) + r
  *   bias     m floats, or NULL.
  *   Z        m x n: where z is stored, or NULL.  Gradient form: the z that is read (with B2_ACT_NONE not looked at).
- *   R        m x n, or NULL.  R may be C.  In the gradient form Z may be C, too.
+ *   R        m x n, or NULL.  R may be C (with its leading dimension).  In the gradient form Z may be C, too.
  *   C        m x n: where c is stored, or NULL where Q is given.
  *            No other two of Z, R, C, Q, S and the operands may overlap where one of them is written.
  *   type     of Z, R and C (B2_TYPE_*; it does not matter where there are none).
@@ -540,7 +540,7 @@ int b2_gemm_f8_act(char transa, char transb, int64_t m, int64_t n, int64_t k, fl
  * The backward pass of an activation and a bias: for every token (column) of DY, d x t,
  *     dz = dy * act'(z)   (dz = dy with B2_ACT_NONE, where Z is not looked at),      db_i = sum over tokens of dz_i
  * each where it is wanted: DZ (d x t), (Q, S) = dz quantised as b2_quant_f8 with block 1 does it, db (d floats).  db and Q come from the
- * unrounded dz.  DZ may be DY or Z; nothing else that is written may overlap another matrix.  db is summed in an order that depends on d, t and the device only: the same bits on every call.  The
+ * unrounded dz.  DZ may be DY or Z (with its leading dimension); nothing else that is written may overlap another matrix.  db is summed in an order that depends on d, t and the device only: the same bits on every call.  The
  * workspace (device, 256-byte aligned) holds partial sums of db; without db it may be NULL.
  * Arguments: d 1, t 2, type 3 (of DY, Z, DZ), act 4, DY 5, lddy 6, Z 7, ldz 8, DZ 9, lddz 10, Q 11, ldq 12, S 13, lds 14, db 15.
  * Without tokens db is 0.

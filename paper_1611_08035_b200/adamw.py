@@ -14,12 +14,17 @@ F8, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 STATES = ("m", "v", "sm", "sv")
 
 
+def capturing(x: torch.Tensor) -> bool:
+    """Whether what is done with x now goes into a CUDA graph."""
+    return x.is_cuda and torch.cuda.is_current_stream_capturing()
+
+
 class AdamW(torch.optim.Optimizer):
     """``torch.optim.AdamW``'s update for float32 and bfloat16 parameters on CUDA devices.
 
     state_bits  8 or 32; tensors of fewer than ``least_8bit`` elements keep 32.
     capturable  keeps the learning rate and the number of the step (a group's, not a parameter's) on the device, where a captured graph of ``step()`` follows them: change
-                ``group["lr"]`` by ``fill_``.  The first step is made before the capture.
+                ``group["lr"]`` by ``fill_``.  Every parameter's first step is made before the capture; one in it is refused, as is a captured step of a group that is not capturable.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=8, least_8bit=4096, capturable=False, seed=0):
@@ -70,6 +75,8 @@ class AdamW(torch.optim.Optimizer):
                 if p.grad.is_sparse:
                     raise RuntimeError("AdamW does not take sparse gradients")
                 st = self.state[p]
+                if (not st or not group["capturable"]) and capturing(p):
+                    raise RuntimeError("a captured step has capturable=True and was made once before, without the capture: its states' first values and its number would be a replay's")
                 if not st:
                     st.update(self._new_state(p, group))
                 st["step"] += 1
@@ -82,8 +89,8 @@ class AdamW(torch.optim.Optimizer):
                     lr, step = self._device_numbers(group, device)
                     step += 1
                 with _device_of(lists[0][0]):
-                    b2.b2_adamw(*lists, lr if isinstance(lr, torch.Tensor) and lr.is_cuda else float(lr), *group["betas"], group["eps"], group["weight_decay"], step,
-                                group["seed"] + (number << 32), grad_scale)
+                    b2.b2_adamw(*lists, lr.to(device) if isinstance(lr, torch.Tensor) and lr.is_cuda else float(lr), *group["betas"], group["eps"], group["weight_decay"], step,
+                                group["seed"] + (number << 32), None if grad_scale is None else grad_scale.to(device))
                 torch.autograd.graph.increment_version(lists[0])  # what is made of the parameters (8-bit copies) is made anew
         return loss
 

@@ -12,10 +12,12 @@ one step of a large one.
 """
 from __future__ import annotations
 
+import weakref
+
 import torch
 
 from . import binding as b2
-from .adamw import AdamW
+from .adamw import AdamW, capturing
 from .layer8 import E8, F8, _blocks, _device_of, _Once, _scratch, product, quantise
 
 ACTIVATIONS = {"none": b2.ACT_NONE, "relu": b2.ACT_RELU, "gelu": b2.ACT_GELU, "gelu_tanh": b2.ACT_GELU_TANH, "silu": b2.ACT_SILU}
@@ -113,7 +115,10 @@ class _FeedForward8(torch.autograd.Function):
 class FeedForward8(torch.nn.Module):
     """y = block(x, residual).  The weights are kept in float32 for the optimiser and in e4m3 for the products; the 8-bit ones are made anew by the next call after a
     weight was changed in place, replaced, loaded or moved; what changes it unseen by autograd (a replayed CUDA graph) has to call ``requantise()``, which a captured
-    training step does itself, first.  It can be differentiated once."""
+    training step does itself, first.  It can be differentiated once.
+
+    In a CUDA graph that is captured, an eager autograd graph of the same block must not be alive unless it was made on the capturing stream (its leaves would add up their gradients
+    on the stream that it was made on, outside the capture): such a call is refused."""
 
     def __init__(self, features: int, hidden: int, activation: str = "gelu", bias: bool = True, eps: float = 1e-5, device="cuda"):
         super().__init__()
@@ -124,6 +129,11 @@ class FeedForward8(torch.nn.Module):
         self.up_bias = torch.nn.Parameter(torch.zeros(hidden, device=device)) if bias else None
         self.down_bias = torch.nn.Parameter(torch.zeros(features, device=device)) if bias else None
         self._quantised: dict = {}
+        self._captured: list = []  # 8-bit weights that captured graphs read
+        self._graphs: list = []    # autograd graphs through the block that may be alive, each with its stream
+
+    def __getstate__(self):
+        return super().__getstate__() | {"_quantised": {}, "_captured": [], "_graphs": []}
 
     @staticmethod
     def _state(weight):
@@ -133,7 +143,7 @@ class FeedForward8(torch.nn.Module):
     def requantise(self) -> None:
         for name in ("up", "down"):  # new ones: a backward pass that is still to come reads the old
             weight = getattr(self, name)
-            self._quantised[name] = (quantise(weight, 128), self._state(weight))
+            self._quantised[name] = (quantise(weight, 128), self._state(weight), capturing(weight))
 
     def _apply(self, fn, recurse=True):
         self._quantised = {}  # parameters get new storage without a new version
@@ -154,15 +164,28 @@ class FeedForward8(torch.nn.Module):
         for name, p in (*others, ("residual", residual)):
             if p is not None and p.device != x.device:
                 raise ValueError(f"x is on {x.device}, {name} on {p.device}")
+        in_capture = capturing(x)
         for name in ("up", "down"):
             of = self._quantised.get(name)
             now = self._state(getattr(self, name))
-            if of is None or of[1][0] is not now[0] or of[1][1:] != now[1:]:  # a tuple's == would compare the parameters' numbers
+            # A tuple's == would compare the parameters' numbers.  What a capture made is there when its graph has run, not before.
+            if of is None or of[1][0] is not now[0] or of[1][1:] != now[1:] or (of[2] and not in_capture):
                 self.requantise()
                 break
         inputs = (x.contiguous(), None if residual is None else residual.contiguous(), self.norm_weight.contiguous(), self.up, self.up_bias, self.down, self.down_bias)
         keep = torch.is_grad_enabled() and any(p is not None and p.requires_grad for p in inputs)
-        return _FeedForward8.apply(*inputs, tuple(self._quantised[n][0] for n in ("up", "down")), self.act, self.eps, keep)
+        quantised = tuple(self._quantised[n][0] for n in ("up", "down"))
+        if in_capture:
+            self._captured.append(quantised)
+        if not keep:
+            return _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep)
+        stream = torch.cuda.current_stream(x.device).cuda_stream if x.is_cuda else 0
+        self._graphs = [g for g in self._graphs if g[0]() is not None]
+        if in_capture and any(s != stream for _, s in self._graphs):
+            raise RuntimeError("an autograd graph of this block from another stream is alive: delete its results, or make it on the stream that captures")
+        y = _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep)
+        self._graphs.append((weakref.ref(y.grad_fn), stream))
+        return y
 
 
 def train(features: int = 256, hidden: int = 512, tokens: int = 1024, steps: int = 60, lr: float = 3e-3, seed: int = 0, state_bits: int = 8):

@@ -1,6 +1,7 @@
 """The feed-forward block's and the optimiser's own work, without a GPU: a stand-in for the binding does the operators by their definitions (oracle/f8.py, oracle/ffn.py), reading
 the memory that the calls name and nothing else."""
 import copy
+import io
 
 import numpy as np
 import pytest
@@ -112,6 +113,35 @@ def test_second_order_gradients_are_refused(ops):
         g.float().square().sum().backward()
 
 
+def test_captures(ops, monkeypatch):
+    """What a capture made is no one else's, what it reads stays, and it is refused while an eager graph from another stream lives."""
+    block, x, r = make()
+    y = block(x, r)
+    now = [True]
+    monkeypatch.setattr(ffn8, "capturing", lambda x: now[0])
+    block._graphs[0] = (block._graphs[0][0], 7)  # as if from another stream
+    with pytest.raises(RuntimeError, match="alive"):
+        block(x, r)
+    with torch.no_grad():
+        block(x, r)  # no gradients, nothing to add up
+    del y
+    eager = ops.calls.count("quant")
+    old = block._quantised["up"][0]
+    block(x, r)
+    assert ops.calls.count("quant") == eager and any(q[0] is old for q in block._captured)
+    block.requantise()
+    assert any(q[0] is old for q in block._captured)
+    block(x, r)
+    assert ops.calls.count("quant") == eager + 2
+    now[0] = False
+    block(x, r)
+    assert ops.calls.count("quant") == eager + 4
+    y = block(x, r)
+    assert ops.calls.count("quant") == eager + 4
+    torch.save(block, io.BytesIO())
+    assert torch.equal(copy.deepcopy(block)(x, r), y)
+
+
 def test_refusals(ops):
     block, x, r = make()
     for bad in (x[:, :255], x.float(), x[0]):
@@ -150,6 +180,13 @@ def test_optimiser_hands_over_what_belongs_together(monkeypatch):
         opt.step()
     with pytest.raises(ValueError):
         adamw.AdamW([torch.nn.Parameter(torch.zeros(4, 6).t())])
+    done = len(calls)
+    monkeypatch.setattr(adamw, "capturing", lambda x: True)
+    for capturable in (False, True):  # its number would be the replay's, its first states too
+        opt = adamw.AdamW([c], capturable=capturable)
+        with pytest.raises(RuntimeError, match="capture"):
+            opt.step()
+    assert len(calls) == done
     with pytest.raises(ValueError):
         adamw.AdamW([a], betas=(0.9, 1.0))
     assert np.isfinite(float(a.detach().sum()))

@@ -256,6 +256,44 @@ def test_training_step_captured(b2):
     assert b2.b2_device_status() == 0
 
 
+def test_captures_and_eager_calls_side_by_side(b2):
+    """A captured call keeps the 8-bit weights that it reads, one that makes its own leaves eager calls theirs, and one beside a living eager graph is refused."""
+    torch.manual_seed(6)
+    block = ffn8.FeedForward8(256, 512)
+    x = torch.randn(40, 256, device="cuda").bfloat16()
+    with torch.no_grad():
+        want = block(x)
+        graph, own = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            y = block(x)
+        with torch.cuda.graph(own):
+            block.requantise()
+            z = block(x)
+        assert torch.equal(block(x), want)  # before either graph has run
+        block.up.mul_(2.0)
+        changed = block(x)
+        filler = [torch.full((512 * 256,), 255, dtype=torch.uint8, device="cuda") for _ in range(8)]  # where freed weights were
+        graph.replay(), own.replay()
+        assert torch.equal(y, want) and torch.equal(z, changed) and not torch.equal(want, changed)
+        del filler
+    alive = block(x)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="alive"):
+        with torch.cuda.graph(graph):
+            block(x)
+    alive.sum().backward()
+    optimiser = AdamW(block.parameters())
+    optimiser.step()
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="capturable"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            optimiser.step()
+    torch.cuda.synchronize()
+    assert b2.b2_device_status() == 0
+
+
 def test_training_runs(b2):
     for bits in (8, 32):
         losses = ffn8.train(steps=3, state_bits=bits)
