@@ -91,11 +91,21 @@ __device__ __forceinline__ void act_rows_out(T* M, int64_t ld, bool vec, int64_t
       }
     }
   } else {  // columns that start anywhere: neighbouring lanes, neighbouring elements
+    const int r0 = lane / L, e0 = lane % L;
+    Bits* to = m + (row0 + r0) * ld + col + e0;
+    const unsigned char* from = stage + r0 * kEmitPitch + e0 * (int)sizeof(T);
+    if (row0 + 32 <= rows && col + W <= cols) {
+#pragma unroll 16
+      for (int i = 0; i < W; ++i) {
+        to[i % D * 32] = *reinterpret_cast<const Bits*>(from + i / D * (32 / L) * kEmitPitch + i % D * 32 * (int)sizeof(T));
+        if (i % D == D - 1) to += 32 / L * ld;
+      }
+    } else {
 #pragma unroll 4
-    for (int i = 0; i < W; ++i) {
-      const int r = W < 32 ? 2 * i + lane / L : i / D, e = W < 32 ? lane % L : i % D * 32 + lane;
-      const int64_t row = row0 + r, c = col + e;
-      if (row < rows && c < cols) m[row * ld + c] = *reinterpret_cast<const Bits*>(stage + r * kEmitPitch + e * (int)sizeof(T));
+      for (int i = 0; i < W; ++i) {
+        const int64_t row = row0 + r0 + i / D * (32 / L), c = col + e0 + i % D * 32;
+        if (row < rows && c < cols) m[row * ld + c] = *reinterpret_cast<const Bits*>(from + i / D * (32 / L) * kEmitPitch + i % D * 32 * (int)sizeof(T));
+      }
     }
   }
 }
@@ -112,7 +122,7 @@ __device__ __forceinline__ void act_put(void* M, int64_t ld, bool vec, const F8A
 template <typename T>
 __device__ __forceinline__ void act_get(const void* M, int64_t ld, bool vec, const F8ActOut& p, int64_t row0, int64_t col, float* v, unsigned char* stage) {
   using Bits = typename ActBits<T>::type;
-  constexpr int W = act_width<T>(), PIECE = 16 / (int)sizeof(T), L = W < 32 ? W : 32, D = W < 32 ? 1 : W / 32;  // lanes to a row, turns to a row
+  constexpr int W = act_width<T>(), PIECE = 16 / (int)sizeof(T), L = W < 32 ? W : 32, RW = 32 / L;  // lanes to a row, rows of a turn
   const int lane = threadIdx.x & 31;
   const Bits* m = static_cast<const Bits*>(M);
   const unsigned char* own = stage + lane * kEmitPitch;
@@ -141,12 +151,13 @@ __device__ __forceinline__ void act_get(const void* M, int64_t ld, bool vec, con
       }
     }
   } else {
-#pragma unroll 8
-    for (int i = 0; i < W; ++i) {
-      const int r = W < 32 ? 2 * i + lane / L : i / D, e = W < 32 ? lane % L : i % D * 32 + lane;
-      const int64_t row = row0 + r, c = col + e;
-      *reinterpret_cast<Bits*>(stage + r * kEmitPitch + e * (int)sizeof(T)) = row < p.rows && c < p.cols ? m[row * ld + c] : (Bits)0;
-    }
+    const int r0 = lane / L;
+    const int64_t c = col + lane % L;
+    const Bits* from = m + (row0 + r0) * ld + c;
+    unsigned char* to = stage + r0 * kEmitPitch + lane % L * (int)sizeof(T);
+    const int here = c < p.cols ? (int)min((int64_t)32, p.rows - row0) : 0;  // rows
+#pragma unroll 16
+    for (int i = 0; i < W; ++i, from += RW * ld) *reinterpret_cast<Bits*>(to + i * RW * kEmitPitch) = r0 + i * RW < here ? *from : (Bits)0;
   }
   __syncwarp();
 #pragma unroll
