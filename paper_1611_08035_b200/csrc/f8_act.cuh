@@ -145,9 +145,17 @@ __device__ __forceinline__ void act_get(const void* M, int64_t ld, bool vec, con
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + 8 * i * kEmitPitch) = q[i];
-      if (nv > 0 && nv < PIECE) {
-        for (int i = 0; i < 4 && row0 + 8 * i + (lane >> 2) < p.rows; ++i, from += 8 * ld)
-          for (int e = 0; e < nv; ++e) reinterpret_cast<Bits*>(to + 8 * i * kEmitPitch)[e] = from[e];
+      if (nv > 0 && nv < PIECE) {  // all on their way together
+        const int here = (int)min((int64_t)32, p.rows - row0) - (lane >> 2);
+        Bits x[4][PIECE - 1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < PIECE - 1; ++e) x[i][e] = e < nv && 8 * i < here ? from[8 * i * ld + e] : (Bits)0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < PIECE - 1; ++e) reinterpret_cast<Bits*>(to + 8 * i * kEmitPitch)[e] = x[i][e];
       }
     }
   } else {
