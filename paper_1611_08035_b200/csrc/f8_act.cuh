@@ -3,7 +3,7 @@
 //   z = alpha * sum + bias,  c = act(z) + r        or, gradient form,        c = alpha * sum * act'(Z) + r
 //
 // with Z, C stored as they are and (Q, S) = c quantised, each where it is wanted.  All of it in fp32 from the unrounded sum; every result is rounded once, when
-// it is stored, so that Q does not depend on C's type.
+// it is stored: Q from the unrounded c, not from C.
 //
 // A feature is an index of C that is contiguous, a token the other one.  Where results leave in whole tiles a thread holds 64 or 128
 // consecutive features of a token, so that the largest magnitude of a block of 128 is at most one exchange away, and matrices pass through a warp's

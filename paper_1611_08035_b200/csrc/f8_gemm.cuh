@@ -3,6 +3,7 @@
 #include <cuda.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "b2gemm.h"
 #include "entry.h"
@@ -27,6 +28,7 @@ template <typename OUT>
 struct F8ArgsOf {
   OUT out;
   int kb;              // blocks of 128 along the summed index
+  int chunk;           // F8ActOut: blocks whose products are summed in tensor memory, a power of two
   int splits;          // CTAs of a cluster that share a tile's blocks
   int r_mn, c_mn;      // the operand's own index is contiguous (else the summed one)
   int tiles_r, tiles_c, group;
@@ -52,6 +54,15 @@ struct F8Operand {
 // sums over 65536 (6e-5), and without a limit 1.4e-3 at k = 4194304.
 template <typename TC>
 __host__ __device__ constexpr int chunk_blocks() { return sizeof(TC) == 4 ? 16 : 512; }
+// Results in 8 bits beside bf16 ones: a sum that is off by 6e-5 puts one number in a thousand on the other side of a border.  32 blocks (4096) keep it to some 4e-6 for every k; the 16 of
+// fp32 halve that, but a tile's second chunk then waits for the warps that are still busy with the tile before (up projection 16384 x 8192 x 4096 418 -> 482 us, gradient of gelu 490 -> 590), and
+// against 64 bits q is off by 4.7e-5 instead of 4.9e-5 there.
+constexpr int kChunkOfQ = 32;
+template <typename TC, typename OUT>
+__host__ __device__ int chunk_blocks_of(const F8ArgsOf<OUT>& a) {
+  if constexpr (std::is_same<OUT, F8Out>::value) return chunk_blocks<TC>();
+  else return a.chunk;
+}
 
 // Matrix of bytes, `inner` contiguous; boxes of box_inner (128 or 64) bytes by box_outer, swizzled over their width.
 inline bool f8_map(CUtensorMap* map, const void* base, int64_t inner, int64_t outer, int64_t ld, int box_outer, int box_inner = 128) {
@@ -126,7 +137,7 @@ bool f8_act_tiles(const F8ActOut& out, int64_t rows, int64_t cols, F8ActTiles<PI
 template <typename OUT>
 F8ArgsOf<OUT> f8_args_with(const F8ArgsOf<F8ActOut>& a, const OUT& out) {
   F8ArgsOf<OUT> b = {};
-  b.out = out, b.kb = a.kb, b.status = a.status;  // the launch sets the others
+  b.out = out, b.kb = a.kb, b.chunk = a.chunk, b.status = a.status;  // the launch sets the others
   return b;
 }
 

@@ -51,8 +51,8 @@ __device__ __forceinline__ void umma_mx(uint32_t tmem_d, uint64_t desc_a, uint64
       ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
       : "memory");
 }
-// CHUNK: chunk_blocks, or 0 where all blocks fit one chunk: then the accumulators are read once and no register holds them before.
-template <typename TC, int CHUNK, typename OUT>
+// CHUNKS: false where all blocks fit one chunk: then the accumulators are read once and no register holds them before.
+template <typename TC, bool CHUNKS, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1)
     f8_mx_kernel(const __grid_constant__ F8ArgsOf<OUT> p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   extern __shared__ unsigned char mx_smem_raw[];
@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tmem_slot;
   grid_ready();
   const int tiles = p.tiles_r * p.tiles_c, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int chunk = chunk_blocks_of<TC>(p);
   bool ok = true;
 
   if (warp < 4) {
@@ -151,7 +152,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           tc_fence_after();
-          const bool two = kb + 1 < p.kb, last = kb + 2 >= p.kb, end = last || (CHUNK && in + kPerStage == CHUNK);
+          const bool two = kb + 1 < p.kb, last = kb + 2 >= p.kb, end = last || (CHUNKS && in + kPerStage == chunk);
           const uint64_t da = umma_desc_advance(da0, (uint32_t)s * kStageBytes), db = umma_desc_advance(db0, (uint32_t)s * kStageBytes);
           const uint32_t sfa = tmem + kBN + slot.s * kSfCols, idesc = idesc0 | ((uint32_t)byte << 4) | ((uint32_t)byte << 29);
           if (elect_one()) {
@@ -242,19 +243,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int tile = pair; tile < tiles && ok; tile += pairs) {
       int tr, tc;
       tile_coords(tile, p.tiles_r, p.tiles_c, p.group, tr, tc);
-      if constexpr (CHUNK == 0 || TILES) f8_prefetch<TC>(p.out, true, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, 32, (int64_t)tc * kBN + half * kCols, kCols);
+      if constexpr (!CHUNKS || TILES) f8_prefetch<TC>(p.out, true, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, 32, (int64_t)tc * kBN + half * kCols, kCols);
       if constexpr (TILES) act_begin_tile<TC>(p.out, (int64_t)tr * 2 * kRows + rank * kRows + quad * 32, (int64_t)tc * kBN + half * kCols, pieces);
-      if constexpr (CHUNK > 0) {
+      if constexpr (CHUNKS) {
 #pragma unroll
         for (int j = 0; j < kCols; ++j) acc[j] = 0.0f;
       }
-      for (int kb = 0; kb < p.kb; kb += CHUNK ? CHUNK : p.kb, ++ch) {
+      for (int kb = 0; kb < p.kb; kb += CHUNKS ? chunk : p.kb, ++ch) {
         if (!mbar_wait_warp(tfull, (uint32_t)(ch & 1), limit)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        if constexpr (CHUNK == 0) {
+        if constexpr (!CHUNKS) {
           uint32_t v[kCols / 32][32];
 #pragma unroll
           for (int i = 0; i < kCols / 32; ++i) tmem_ld32_issue(taddr + 32 * i, v[i]);
@@ -308,12 +309,11 @@ int f8_mx_launch(F8ArgsOf<OUT> a, const F8Operand& r, const F8Operand& c, int64_
     if (f8_act_tiles<TC>(a.out, r.n, c.n, gradient)) return f8_mx_launch<TC>(f8_args_with(a, gradient), r, c, k, st);
   }
   static std::atomic<bool> configured[64];
-  constexpr int CHUNK = chunk_blocks<TC>();
   if constexpr (sizeof(TC) == 2 && !ActHandOver<OUT>::TILES) {
     static std::atomic<bool> configured_whole[64];
-    if (a.kb <= CHUNK) return f8_pair_launch(f8_mx_kernel<TC, 0, OUT>, configured_whole, kThreads, kSmem<OUT>, a, r, c, k, st);
+    if (a.kb <= chunk_blocks_of<TC>(a)) return f8_pair_launch(f8_mx_kernel<TC, false, OUT>, configured_whole, kThreads, kSmem<OUT>, a, r, c, k, st);
   }
-  return f8_pair_launch(f8_mx_kernel<TC, CHUNK, OUT>, configured, kThreads, kSmem<OUT>, a, r, c, k, st);
+  return f8_pair_launch(f8_mx_kernel<TC, true, OUT>, configured, kThreads, kSmem<OUT>, a, r, c, k, st);
 }
 template int f8_mx_launch<float>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);
 template int f8_mx_launch<__nv_bfloat16>(F8ArgsOf<F8Out>, const F8Operand&, const F8Operand&, int64_t, cudaStream_t);

@@ -59,7 +59,7 @@ template <int TBN, typename TC, bool COLS_CONTIG, bool MX, typename OUT>
 __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, F8Cfg<TBN, MX>::RESIDENT)
     f8_gemm_kernel(const F8ArgsOf<OUT> p, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c) {
   using Cfg = F8Cfg<TBN, MX>;
-  constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES, CHUNK = chunk_blocks<TC>();
+  constexpr int EW = Cfg::EW, COLS = Cfg::COLS, STAGES = Cfg::STAGES;
   constexpr bool ACT = std::is_same<OUT, F8ActOut>::value;
   extern __shared__ unsigned char f8_smem_raw[];
   const uint32_t raw = smem_u32(f8_smem_raw);
@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, F8Cfg<TBN, MX>::RESIDENT)
   // split: the cluster's CTAs (blockIdx.y) share one tile; otherwise the grid walks over the tiles
   const int tiles = p.tiles_r * p.tiles_c, share = blockIdx.y;
   const int kb0 = (int)((int64_t)p.kb * share / p.splits), kb1 = (int)((int64_t)p.kb * (share + 1) / p.splits);
+  const int chunk = chunk_blocks_of<TC>(p), chunk_log = 31 - __clz(chunk);
   bool ok = true;
   float acc[COLS];
 
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, F8Cfg<TBN, MX>::RESIDENT)
     for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
       for (int kb = kb0; kb < kb1; ++kb, pos.next()) {
         const int s = pos.s, b = MX ? 0 : ch & 1, byte = kb & 3;
-        const bool first = !MX || kb == kb0 || kb % CHUNK == 0, end = !MX || kb == kb1 - 1 || kb % CHUNK == CHUNK - 1;
+        const bool first = !MX || kb == kb0 || (kb & (chunk - 1)) == 0, end = !MX || kb == kb1 - 1 || (kb & (chunk - 1)) == chunk - 1;
         const uint32_t behind = MX ? 1 : 2, round = (uint32_t)(MX ? ch : ch >> 1);
         if ((first && ch >= (int)behind && !mbar_wait_warp(&tempty[b], (round - 1) & 1)) ||
             (MX && (byte == 0 || kb == kb0) && !mbar_wait_warp(&sf_full[slot.s], slot.phase)) ||
@@ -246,7 +247,8 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, F8Cfg<TBN, MX>::RESIDENT)
         // Four warps (half 0), one for each quarter of the lanes, bring the scales; all read the sums.
         const bool brings = half == 0;
         if (brings) fetch(kb0 & ~3);
-        if (kb0 / CHUNK == (kb1 - 1) / CHUNK) {
+        const int first_chunk = kb0 >> chunk_log, last_chunk = (kb1 - 1) >> chunk_log;
+        if (first_chunk == last_chunk) {
           for (int kb = kb0 & ~3; brings && kb < kb1; kb += 4)
             if (!bring(kb)) break;
           if (ok) sums([](float& s, float v) { s = v; });
@@ -255,10 +257,10 @@ __global__ void __launch_bounds__(F8Cfg<TBN, MX>::NT, F8Cfg<TBN, MX>::RESIDENT)
           for (int j = 0; j < COLS; ++j) acc[j] = 0.0f;
           // The slot for the scales of block kb is the one of 4 SLOTS blocks ago.  If those began a chunk, their products wait for the sums
           // of the chunk before to be read, by these warps among others: that comes first.
-          int left = (kb1 - 1) / CHUNK - kb0 / CHUNK + 1;
+          int left = last_chunk - first_chunk + 1;
           for (int kb = brings ? kb0 & ~3 : kb1; left > 0; kb += 4) {
             const int behind = kb - 4 * Cfg::SLOTS;
-            if (kb >= kb1 || (behind > kb0 && behind % CHUNK == 0)) {
+            if (kb >= kb1 || (behind > kb0 && (behind & (chunk - 1)) == 0)) {
               if (!sums([](float& s, float v) { s += v; })) break;
               --left;
             }
