@@ -590,6 +590,13 @@ int b2_adamw(const b2_adamw_tensor* tensors, int count, double lr, double beta1,
              int64_t step, uint64_t seed, const float* grad_scale, const float* lr_device, const int64_t* step_device,
              void* cuda_stream);
 
+/*
+ * For callers that keep data between calls (an operand in 8 bits that several products read).
+ * b2_graph_capture_id: *id is the number of the capture into a CUDA graph that the stream takes part in, another one for every capture of a process, and 0
+ * where it is in none: what a capture makes exists once its graph has run, so that only calls of the same capture may read it.  Returns 0, -2 or B2_ERR_LAUNCH.
+ */
+int b2_graph_capture_id(void* cuda_stream, uint64_t* id);
+
 /* Static, NUL-terminated text for a return value of any call above. */
 const char* b2_strerror(int status);
 /* Static, NUL-terminated library version. */

@@ -8,15 +8,11 @@ from __future__ import annotations
 import torch
 
 from . import binding as b2
+from .capture import capturing
 from .layer8 import _device_of
 
 F8, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 STATES = ("m", "v", "sm", "sv")
-
-
-def capturing(x: torch.Tensor) -> bool:
-    """Whether what is done with x now goes into a CUDA graph."""
-    return x.is_cuda and torch.cuda.is_current_stream_capturing()
 
 
 class AdamW(torch.optim.Optimizer):

@@ -99,6 +99,7 @@ _SIGNATURES = {
     "b2_act_backward_workspace_bytes": (c_size_t, [c_int64, c_int64]),
     "b2_act_backward": (c_int, [c_int64, c_int64, c_int, c_int] + 5 * [c_void_p, c_int64] + [c_void_p, c_void_p, c_size_t, c_void_p]),
     "b2_adamw": (c_int, [c_void_p, c_int] + 5 * [c_double] + [c_int64, ctypes.c_uint64, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "b2_graph_capture_id": (c_int, [c_void_p, ctypes.POINTER(ctypes.c_uint64)]),
     "b2_strerror": (c_char_p, [c_int]),
     "b2_version": (c_char_p, []),
 }
@@ -668,3 +669,12 @@ def b2_adamw(params, grads, m, v, sm, sv, lr, beta1, beta2, eps, weight_decay, s
     if rc and check:
         raise B2Error("b2_adamw", rc)
     return rc
+
+
+def b2_graph_capture_id(stream: int) -> int:
+    """The number of the capture that a stream (its handle) is in; 0 where it is in none."""
+    number = ctypes.c_uint64()
+    rc = lib().b2_graph_capture_id(stream, ctypes.byref(number))
+    if rc:
+        raise B2Error("b2_graph_capture_id", rc)
+    return number.value

@@ -17,7 +17,8 @@ import weakref
 import torch
 
 from . import binding as b2
-from .adamw import AdamW, capturing
+from .adamw import AdamW
+from .capture import capture_id, capturing
 from .layer8 import E8, F8, _blocks, _device_of, _Once, _scratch, product, quantise
 
 ACTIVATIONS = {"none": b2.ACT_NONE, "relu": b2.ACT_RELU, "gelu": b2.ACT_GELU, "gelu_tanh": b2.ACT_GELU_TANH, "silu": b2.ACT_SILU}
@@ -143,7 +144,7 @@ class FeedForward8(torch.nn.Module):
     def requantise(self) -> None:
         for name in ("up", "down"):  # new ones: a backward pass that is still to come reads the old
             weight = getattr(self, name)
-            self._quantised[name] = (quantise(weight, 128), self._state(weight), capturing(weight))
+            self._quantised[name] = (quantise(weight, 128), self._state(weight), capture_id(weight) if capturing(weight) else 0)
 
     def _apply(self, fn, recurse=True):
         self._quantised = {}  # parameters get new storage without a new version
@@ -164,27 +165,27 @@ class FeedForward8(torch.nn.Module):
         for name, p in (*others, ("residual", residual)):
             if p is not None and p.device != x.device:
                 raise ValueError(f"x is on {x.device}, {name} on {p.device}")
-        in_capture = capturing(x)
+        stream = torch.cuda.current_stream(x.device).cuda_stream if x.is_cuda else 0
+        in_capture = capture_id(x) if capturing(x) else 0
+        parameters = (self.norm_weight, self.up, self.up_bias, self.down, self.down_bias)
+        keep = torch.is_grad_enabled() and any(p is not None and p.requires_grad for p in (x, residual, *parameters))
+        if keep and in_capture and any(g() is not None and s != stream for g, s in self._graphs):
+            raise RuntimeError("an autograd graph of this block from another stream is alive: delete its results, or make it on the stream that captures")
         for name in ("up", "down"):
             of = self._quantised.get(name)
             now = self._state(getattr(self, name))
-            # A tuple's == would compare the parameters' numbers.  What a capture made is there when its graph has run, not before.
-            if of is None or of[1][0] is not now[0] or of[1][1:] != now[1:] or (of[2] and not in_capture):
+            # A tuple's == would compare the parameters' numbers.  What a capture made is there when its graph has run: it is for calls of the same capture.
+            if of is None or of[1][0] is not now[0] or of[1][1:] != now[1:] or of[2] not in (0, in_capture):
                 self.requantise()
                 break
         inputs = (x.contiguous(), None if residual is None else residual.contiguous(), self.norm_weight.contiguous(), self.up, self.up_bias, self.down, self.down_bias)
-        keep = torch.is_grad_enabled() and any(p is not None and p.requires_grad for p in inputs)
         quantised = tuple(self._quantised[n][0] for n in ("up", "down"))
         if in_capture:
             self._captured.append(quantised)
         if not keep:
             return _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep)
-        stream = torch.cuda.current_stream(x.device).cuda_stream if x.is_cuda else 0
-        self._graphs = [g for g in self._graphs if g[0]() is not None]
-        if in_capture and any(s != stream for _, s in self._graphs):
-            raise RuntimeError("an autograd graph of this block from another stream is alive: delete its results, or make it on the stream that captures")
         y = _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep)
-        self._graphs.append((weakref.ref(y.grad_fn), stream))
+        self._graphs = [g for g in self._graphs if g[0]() is not None] + [(weakref.ref(y.grad_fn), stream)]
         return y
 
 
