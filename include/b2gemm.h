@@ -103,7 +103,7 @@ int b2_sgemm_variant(int variant, char transa, char transb, int64_t m, int64_t n
  * stop computing and return, leaving C unspecified.  b2_device_status synchronises `cuda_stream`,
  * returns that word (B2_OK when nothing happened) and clears it; B2_ERR_LAUNCH when the
  * synchronisation or the copy fails.  It is the only call of this library that blocks besides
- * the host-buffer forms.
+ * the host-buffer forms and b2_event_finish.
  */
 int b2_device_status(void* cuda_stream);
 /*
@@ -594,8 +594,11 @@ int b2_adamw(const b2_adamw_tensor* tensors, int count, double lr, double beta1,
  * For callers that keep data between calls (an operand in 8 bits that several products read).
  * b2_graph_capture_id: *id is the number of the capture into a CUDA graph that the stream takes part in, another one for every capture of a process, and 0
  * where it is in none: what a capture makes exists once its graph has run, so that only calls of the same capture may read it.  Returns 0, -2 or B2_ERR_LAUNCH.
+ * b2_event_finish: waits on the host for an event (a cudaEvent_t cast to void*) that was recorded outside any capture, also where the thread captures: what was
+ * made before the event is there when the graph runs.  Returns 0, -1 or B2_ERR_LAUNCH.
  */
 int b2_graph_capture_id(void* cuda_stream, uint64_t* id);
+int b2_event_finish(void* cuda_event);
 
 /* Static, NUL-terminated text for a return value of any call above. */
 const char* b2_strerror(int status);

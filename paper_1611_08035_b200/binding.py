@@ -100,6 +100,7 @@ _SIGNATURES = {
     "b2_act_backward": (c_int, [c_int64, c_int64, c_int, c_int] + 5 * [c_void_p, c_int64] + [c_void_p, c_void_p, c_size_t, c_void_p]),
     "b2_adamw": (c_int, [c_void_p, c_int] + 5 * [c_double] + [c_int64, ctypes.c_uint64, c_void_p, c_void_p, c_void_p, c_void_p]),
     "b2_graph_capture_id": (c_int, [c_void_p, ctypes.POINTER(ctypes.c_uint64)]),
+    "b2_event_finish": (c_int, [c_void_p]),
     "b2_strerror": (c_char_p, [c_int]),
     "b2_version": (c_char_p, []),
 }
@@ -678,3 +679,10 @@ def b2_graph_capture_id(stream: int) -> int:
     if rc:
         raise B2Error("b2_graph_capture_id", rc)
     return number.value
+
+
+def b2_event_finish(event: int) -> None:
+    """Waits on the host for an event (its handle) of no capture, also in the middle of one."""
+    rc = lib().b2_event_finish(event)
+    if rc:
+        raise B2Error("b2_event_finish", rc)

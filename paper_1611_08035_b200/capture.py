@@ -14,3 +14,33 @@ def capturing(x: torch.Tensor) -> bool:
 def capture_id(x: torch.Tensor) -> int:
     """The number of the capture that what is done with x now goes into; every capture has another one.  (1 for what is not on a GPU.)"""
     return binding.b2_graph_capture_id(torch.cuda.current_stream(x.device).cuda_stream) if x.is_cuda else 1
+
+
+class Made:
+    """Tensors that one call leaves for later ones: who reads them on another stream waits for the work that makes them, and their memory is given away after him.
+
+    capture: the number of the capture that they are made in, or 0."""
+
+    __slots__ = ("tensors", "capture", "_event", "_streams")
+
+    def __init__(self, tensors, capture: int):
+        self.tensors, self.capture, self._event, self._streams = tensors, capture, None, set()
+        if tensors[0].is_cuda:
+            stream = torch.cuda.current_stream(tensors[0].device)
+            self._event = stream.record_event()
+            self._streams.add(stream.cuda_stream)
+
+    def use(self, capture: int) -> None:
+        """What is enqueued now on the current stream, in the capture of that number or in none, may read the tensors.  A graph that is captured has to keep them alive."""
+        if self._event is None:
+            return
+        if capture and not self.capture:  # its graph may run on any stream
+            binding.b2_event_finish(self._event.cuda_event)
+            return
+        device = self.tensors[0].device
+        if binding._raw_stream(device.index) not in self._streams:
+            stream = torch.cuda.current_stream(device)
+            stream.wait_event(self._event)
+            for t in self.tensors:
+                t.record_stream(stream)
+            self._streams.add(stream.cuda_stream)

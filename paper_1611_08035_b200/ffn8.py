@@ -18,7 +18,7 @@ import torch
 
 from . import binding as b2
 from .adamw import AdamW
-from .capture import capture_id, capturing
+from .capture import Made, capture_id, capturing
 from .layer8 import E8, F8, _blocks, _device_of, _Once, _scratch, product, quantise
 
 ACTIVATIONS = {"none": b2.ACT_NONE, "relu": b2.ACT_RELU, "gelu": b2.ACT_GELU, "gelu_tanh": b2.ACT_GELU_TANH, "silu": b2.ACT_SILU}
@@ -142,9 +142,10 @@ class FeedForward8(torch.nn.Module):
 
     @torch.no_grad()
     def requantise(self) -> None:
-        for name in ("up", "down"):  # new ones: a backward pass that is still to come reads the old
-            weight = getattr(self, name)
-            self._quantised[name] = (quantise(weight, 128), self._state(weight), capture_id(weight) if capturing(weight) else 0)
+        weights = {name: getattr(self, name) for name in ("up", "down")}
+        pairs = {name: quantise(weight, 128) for name, weight in weights.items()}  # new ones: a backward pass that is still to come reads the old
+        made = Made([t for pair in pairs.values() for t in pair], capture_id(self.up) if capturing(self.up) else 0)
+        self._quantised = {name: (pairs[name], self._state(weight), made) for name, weight in weights.items()}
 
     def _apply(self, fn, recurse=True):
         self._quantised = {}  # parameters get new storage without a new version
@@ -175,11 +176,13 @@ class FeedForward8(torch.nn.Module):
             of = self._quantised.get(name)
             now = self._state(getattr(self, name))
             # A tuple's == would compare the parameters' numbers.  What a capture made is there when its graph has run: it is for calls of the same capture.
-            if of is None or of[1][0] is not now[0] or of[1][1:] != now[1:] or of[2] not in (0, in_capture):
+            if of is None or of[1][0] is not now[0] or of[1][1:] != now[1:] or of[2].capture not in (0, in_capture):
                 self.requantise()
                 break
         inputs = (x.contiguous(), None if residual is None else residual.contiguous(), self.norm_weight.contiguous(), self.up, self.up_bias, self.down, self.down_bias)
-        quantised = tuple(self._quantised[n][0] for n in ("up", "down"))
+        (up, _, made), (down, _, _) = (self._quantised[n] for n in ("up", "down"))
+        made.use(in_capture)
+        quantised = (up, down)
         if in_capture:
             self._captured.append(quantised)
         if not keep:

@@ -52,3 +52,7 @@ def test_a_refused_capture_leaves_nothing_behind(ops, capture):  # noqa: F811
 def test_the_number_of_a_capture_has_to_have_a_place(b2):
     assert b2.lib().b2_graph_capture_id(None, None) == -2
     assert "b2_graph_capture_id" in binding.EXPORTED_SYMBOLS
+
+
+def test_no_event_is_refused(b2):
+    assert b2.lib().b2_event_finish(None) == -1
