@@ -18,7 +18,8 @@
  *     b2_zgemm4m_static (B2_ZGEMM4M_STATIC_BYTES of device memory on every GPU that loads the
  *     library), two device status words (b2_device_status), per-device caches of symbol
  *     addresses, shared-memory attributes and the SM count, per host thread the last sixteen
- *     kernel choices of the selector (a pure function of the problem's shape), and, for the
+ *     kernel choices of the selector (a pure function of the problem's shape), a table of
+ *     watched graphs (b2_graph_watch), and, for the
  *     host-buffer forms, two helper streams and a few events per device.  None of it carries
  *     results from one call to the next.
  *   - Threads: the per-device caches are filled on first use through atomic slots and one-time
@@ -599,6 +600,14 @@ int b2_adamw(const b2_adamw_tensor* tensors, int count, double lr, double beta1,
  */
 int b2_graph_capture_id(void* cuda_stream, uint64_t* id);
 int b2_event_finish(void* cuda_event);
+/*
+ * b2_graph_watch: watches the graph that the stream is captured into; *watch is what the other two take.  b2_graph_gone: 1 once that graph and every executable
+ * form of it have been destroyed and have run, so that what it reads may be freed; else 0.  b2_graph_unwatch ends the watch, before or after.  4096 watches at a time.
+ * b2_graph_watch returns 0, -1 where the stream is not captured, -2, B2_ERR_STATIC_LIMIT or B2_ERR_LAUNCH; b2_graph_unwatch 0, or -1 for what is no watch.
+ */
+int b2_graph_watch(void* cuda_stream, int* watch);
+int b2_graph_gone(int watch);
+int b2_graph_unwatch(int watch);
 
 /* Static, NUL-terminated text for a return value of any call above. */
 const char* b2_strerror(int status);

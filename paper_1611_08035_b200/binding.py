@@ -101,6 +101,9 @@ _SIGNATURES = {
     "b2_adamw": (c_int, [c_void_p, c_int] + 5 * [c_double] + [c_int64, ctypes.c_uint64, c_void_p, c_void_p, c_void_p, c_void_p]),
     "b2_graph_capture_id": (c_int, [c_void_p, ctypes.POINTER(ctypes.c_uint64)]),
     "b2_event_finish": (c_int, [c_void_p]),
+    "b2_graph_watch": (c_int, [c_void_p, ctypes.POINTER(c_int)]),
+    "b2_graph_gone": (c_int, [c_int]),
+    "b2_graph_unwatch": (c_int, [c_int]),
     "b2_strerror": (c_char_p, [c_int]),
     "b2_version": (c_char_p, []),
 }
@@ -149,6 +152,9 @@ def strerror(status: int) -> str:
 
 def version() -> str:
     return lib().b2_version().decode()
+
+
+STATIC_LIMIT = 1005  # B2_ERR_STATIC_LIMIT
 
 
 class B2Error(RuntimeError):
@@ -686,3 +692,22 @@ def b2_event_finish(event: int) -> None:
     rc = lib().b2_event_finish(event)
     if rc:
         raise B2Error("b2_event_finish", rc)
+
+
+def b2_graph_watch(stream: int) -> int:
+    """A watch of the graph that a stream (its handle) is captured into."""
+    watch = c_int()
+    rc = lib().b2_graph_watch(stream, ctypes.byref(watch))
+    if rc:
+        raise B2Error("b2_graph_watch", rc)
+    return watch.value
+
+
+def b2_graph_gone(watch: int) -> bool:
+    return bool(lib().b2_graph_gone(watch))
+
+
+def b2_graph_unwatch(watch: int) -> None:
+    rc = lib().b2_graph_unwatch(watch)
+    if rc:
+        raise B2Error("b2_graph_unwatch", rc)

@@ -1,6 +1,8 @@
 """What modules that keep data on the GPU between calls need to know of CUDA graphs and streams."""
 from __future__ import annotations
 
+import weakref
+
 import torch
 
 from . import binding
@@ -44,3 +46,21 @@ class Made:
             for t in self.tensors:
                 t.record_stream(stream)
             self._streams.add(stream.cuda_stream)
+
+
+class GraphWatch:
+    """Tells when the graph that is being captured on x's current stream is gone, and with it who may read what was kept for it."""
+
+    def __init__(self, x: torch.Tensor, capture: int):
+        self.capture, self._watch = capture, None
+        if x.is_cuda:
+            try:
+                self._watch = binding.b2_graph_watch(torch.cuda.current_stream(x.device).cuda_stream)
+            except binding.B2Error as e:  # too many: what was kept for this one stays
+                if e.status != binding.STATIC_LIMIT:
+                    raise
+                return
+            weakref.finalize(self, binding.b2_graph_unwatch, self._watch).atexit = False
+
+    def gone(self) -> bool:
+        return self._watch is not None and binding.b2_graph_gone(self._watch)

@@ -18,7 +18,7 @@ import torch
 
 from . import binding as b2
 from .adamw import AdamW
-from .capture import Made, capture_id, capturing
+from .capture import GraphWatch, Made, capture_id, capturing
 from .layer8 import E8, F8, _blocks, _device_of, _Once, _scratch, product, quantise
 
 ACTIVATIONS = {"none": b2.ACT_NONE, "relu": b2.ACT_RELU, "gelu": b2.ACT_GELU, "gelu_tanh": b2.ACT_GELU_TANH, "silu": b2.ACT_SILU}
@@ -130,7 +130,7 @@ class FeedForward8(torch.nn.Module):
         self.up_bias = torch.nn.Parameter(torch.zeros(hidden, device=device)) if bias else None
         self.down_bias = torch.nn.Parameter(torch.zeros(features, device=device)) if bias else None
         self._quantised: dict = {}
-        self._captured: list = []  # 8-bit weights that captured graphs read
+        self._captured: list = []  # 8-bit weights that captured graphs read, each with a watch of the graph
         self._graphs: list = []    # autograd graphs through the block that may be alive, each with its stream
 
     def __getstate__(self):
@@ -142,10 +142,15 @@ class FeedForward8(torch.nn.Module):
 
     @torch.no_grad()
     def requantise(self) -> None:
+        self._let_go()
         weights = {name: getattr(self, name) for name in ("up", "down")}
         pairs = {name: quantise(weight, 128) for name, weight in weights.items()}  # new ones: a backward pass that is still to come reads the old
         made = Made([t for pair in pairs.values() for t in pair], capture_id(self.up) if capturing(self.up) else 0)
         self._quantised = {name: (pairs[name], self._state(weight), made) for name, weight in weights.items()}
+
+    def _let_go(self) -> None:
+        """Of what was kept for graphs that are gone."""
+        self._captured = [c for c in self._captured if not c[2].gone()]
 
     def _apply(self, fn, recurse=True):
         self._quantised = {}  # parameters get new storage without a new version
@@ -183,8 +188,10 @@ class FeedForward8(torch.nn.Module):
         (up, _, made), (down, _, _) = (self._quantised[n] for n in ("up", "down"))
         made.use(in_capture)
         quantised = (up, down)
-        if in_capture:
-            self._captured.append(quantised)
+        if in_capture and not made.capture:
+            self._let_go()
+            if not any(c[0] is up and c[2].capture == in_capture for c in self._captured):
+                self._captured.append((up, down, GraphWatch(x, in_capture)))
         if not keep:
             return _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep)
         y = _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep)

@@ -56,3 +56,29 @@ def test_the_number_of_a_capture_has_to_have_a_place(b2):
 
 def test_no_event_is_refused(b2):
     assert b2.lib().b2_event_finish(None) == -1
+
+
+def test_kept_once_for_each_capture(ops, capture):  # noqa: F811
+    block, x, r = make()
+    with torch.no_grad():
+        block(x, r)
+        capture[0] = 1
+        for _ in range(3):
+            block(x, r)
+        assert len(block._captured) == 1
+        capture[0] = 2
+        block(x, r)
+        assert len(block._captured) == 2  # the other graph may go first
+        block.requantise()
+        block(x, r)  # made in the capture: its graph's own
+        assert len(block._captured) == 2
+        for kept in block._captured:
+            kept[2].gone = lambda: True
+        block.requantise()
+        assert not block._captured
+
+
+def test_what_is_no_watch_is_refused(b2):
+    for watch in (-1, 0, 4096):
+        assert b2.lib().b2_graph_gone(watch) == 0 and b2.lib().b2_graph_unwatch(watch) == -1
+    assert b2.lib().b2_graph_watch(None, None) == -2
