@@ -17,6 +17,7 @@ import contextlib
 import torch
 
 from . import binding as b2
+from .capture import Made
 
 F8, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
@@ -144,8 +145,11 @@ class NormLinear8(torch.nn.Module):
 
     @torch.no_grad()
     def requantise(self) -> None:
-        self.w8, self.sw = quantise(self.weight, 128)
-        self._quantised = self._state(self.weight)
+        self.w8, self.sw = pair = quantise(self.weight, 128)
+        self._quantised = (*self._state(self.weight), Made(pair, 0))
+
+    def __getstate__(self):
+        return super().__getstate__() | {"_quantised": None}
 
     def _apply(self, fn, recurse=True):
         self._quantised = None  # parameters get new storage without a new version
@@ -166,7 +170,9 @@ class NormLinear8(torch.nn.Module):
         of = self._quantised
         if of is None or of[0] is not weight or of[1] != self._state(weight)[1]:
             self.requantise()
-        return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), norm_weight.contiguous(), weight, self.w8, self.sw, self.eps)
+        made = self._quantised[2]
+        made.use(0)
+        return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), norm_weight.contiguous(), weight, *made.tensors, self.eps)
 
 
 def train(features: int = 512, outputs: int = 384, tokens: int = 1024, steps: int = 40, lr: float = 0.5, seed: int = 0):
