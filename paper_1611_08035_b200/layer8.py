@@ -17,7 +17,7 @@ import contextlib
 import torch
 
 from . import binding as b2
-from .capture import Made
+from .capture import GraphWatch, Made, capture_id, capturing
 
 F8, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
@@ -127,7 +127,8 @@ class _NormLinear8(torch.autograd.Function):
 class NormLinear8(torch.nn.Module):
     """y, h = layer(x, residual): h = x + residual (x without one), y = rmsnorm(h) W^T.  W is kept in float32 for the optimiser
     and in e4m3 for the products.  The 8-bit one is made anew by the next call after the weight was changed in place, replaced, loaded or
-    moved; what changes it unseen by autograd (through ``weight.data``, or in a replayed CUDA graph) has to call ``requantise()``."""
+    moved; what changes it unseen by autograd (through ``weight.data``, or in a replayed CUDA graph) has to call ``requantise()``.  What a captured graph reads of it is kept while the
+    graph lives, and what one makes of it is read by calls of the same capture alone."""
 
     def __init__(self, features: int, outputs: int, eps: float = 1e-5, device="cuda"):
         super().__init__()
@@ -135,6 +136,7 @@ class NormLinear8(torch.nn.Module):
         self.norm_weight = torch.nn.Parameter(torch.ones(features, dtype=torch.bfloat16, device=device))
         self.weight = torch.nn.Parameter(torch.randn(outputs, features, device=device) * features**-0.5)
         self._quantised = None
+        self._captured: list = []  # 8-bit weights that captured graphs read, each with a watch of the graph
         if self.weight.is_cuda:
             self.requantise()
 
@@ -145,11 +147,16 @@ class NormLinear8(torch.nn.Module):
 
     @torch.no_grad()
     def requantise(self) -> None:
+        self._let_go()
         self.w8, self.sw = pair = quantise(self.weight, 128)
-        self._quantised = (*self._state(self.weight), Made(pair, 0))
+        self._quantised = (*self._state(self.weight), Made(pair, capture_id(self.weight) if capturing(self.weight) else 0))
 
     def __getstate__(self):
-        return super().__getstate__() | {"_quantised": None}
+        return super().__getstate__() | {"_quantised": None, "_captured": []}
+
+    def _let_go(self) -> None:
+        """Of what was kept for graphs that are gone."""
+        self._captured = [c for c in self._captured if not c[1].gone()]
 
     def _apply(self, fn, recurse=True):
         self._quantised = None  # parameters get new storage without a new version
@@ -167,11 +174,16 @@ class NormLinear8(torch.nn.Module):
             raise ValueError(f"norm_weight is {tuple(norm_weight.shape)}; the weight has {d} features")
         if weight.device != device or norm_weight.device != device or (residual is not None and residual.device != device):
             raise ValueError(f"x is on {device}, the weight on {weight.device}, the norm's on {norm_weight.device}, the residual on {None if residual is None else residual.device}")
-        of = self._quantised
-        if of is None or of[0] is not weight or of[1] != self._state(weight)[1]:
+        of, in_capture = self._quantised, capture_id(x) if capturing(x) else 0
+        # What a capture made is there when its graph has run: it is for calls of the same capture.
+        if of is None or of[0] is not weight or of[1] != self._state(weight)[1] or of[2].capture not in (0, in_capture):
             self.requantise()
         made = self._quantised[2]
-        made.use(0)
+        made.use(in_capture)
+        if in_capture and not made.capture:
+            self._let_go()
+            if not any(c[0] is made.tensors and c[1].capture == in_capture for c in self._captured):
+                self._captured.append((made.tensors, GraphWatch(x, in_capture)))
         return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), norm_weight.contiguous(), weight, *made.tensors, self.eps)
 
 

@@ -1,0 +1,52 @@
+"""The 8-bit layer in several captures, without a GPU: captures are told apart by their numbers, the operators are test_layer8.py's stand-in."""
+import copy
+
+import pytest
+import torch
+
+from paper_1611_08035_b200 import layer8
+from test_layer8 import make, ops  # noqa: F401
+
+
+@pytest.fixture
+def capture(monkeypatch):
+    """The number of the capture that calls go into; 0: none."""
+    now = [0]
+    monkeypatch.setattr(layer8, "capturing", lambda x: now[0] != 0, raising=False)
+    monkeypatch.setattr(layer8, "capture_id", lambda x: now[0], raising=False)
+    return now
+
+
+def test_what_one_capture_made_is_not_another_ones(ops, capture):  # noqa: F811
+    layer, x, r = make()
+    made = lambda: ops.calls.count("quant")  # noqa: E731
+    with torch.no_grad():
+        capture[0] = 5
+        layer(x, r), layer(x, r)
+        assert made() == 1
+        capture[0] = 6  # whose graph may run before the other's
+        layer(x, r), layer(x, r)
+        assert made() == 2
+        capture[0] = 0  # before either has run
+        layer(x, r)
+        assert made() == 3
+        capture[0] = 7
+        layer(x, r)  # what eager calls made is everyone's
+        assert made() == 3
+
+
+def test_what_a_graph_reads_is_kept_for_it(ops, capture):  # noqa: F811
+    layer, x, r = make()
+    with torch.no_grad():
+        layer(x, r)
+        old = layer.w8
+        capture[0] = 1
+        layer(x, r), layer(x, r)
+        capture[0] = 0
+        layer.requantise()
+        assert [c[0][0] is old for c in layer._captured] == [True]
+        assert not copy.deepcopy(layer)._captured
+        for kept in layer._captured:
+            kept[1].gone = lambda: True
+        layer.requantise()
+        assert not layer._captured
