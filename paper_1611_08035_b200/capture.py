@@ -8,6 +8,13 @@ import torch
 from . import binding
 
 
+def stream_of(x: torch.Tensor) -> int:
+    """The handle of the current stream of x's device; 0 for what is not on a GPU."""
+    if not x.is_cuda:
+        return 0
+    return binding._raw_stream(x.device.index) if binding._raw_stream is not None else torch.cuda.current_stream(x.device).cuda_stream
+
+
 def capturing(x: torch.Tensor) -> bool:
     """Whether what is done with x now goes into a CUDA graph."""
     return x.is_cuda and torch.cuda.is_current_stream_capturing()
@@ -15,7 +22,7 @@ def capturing(x: torch.Tensor) -> bool:
 
 def capture_id(x: torch.Tensor) -> int:
     """The number of the capture that what is done with x now goes into; every capture has another one.  (1 for what is not on a GPU.)"""
-    return binding.b2_graph_capture_id(torch.cuda.current_stream(x.device).cuda_stream) if x.is_cuda else 1
+    return binding.b2_graph_capture_id(stream_of(x)) if x.is_cuda else 1
 
 
 class Made:
@@ -39,9 +46,8 @@ class Made:
         if capture and not self.capture:  # its graph may run on any stream
             binding.b2_event_finish(self._event.cuda_event)
             return
-        device = self.tensors[0].device
-        if binding._raw_stream(device.index) not in self._streams:
-            stream = torch.cuda.current_stream(device)
+        if stream_of(self.tensors[0]) not in self._streams:
+            stream = torch.cuda.current_stream(self.tensors[0].device)
             stream.wait_event(self._event)
             for t in self.tensors:
                 t.record_stream(stream)
@@ -55,7 +61,7 @@ class GraphWatch:
         self.capture, self._watch = capture, None
         if x.is_cuda:
             try:
-                self._watch = binding.b2_graph_watch(torch.cuda.current_stream(x.device).cuda_stream)
+                self._watch = binding.b2_graph_watch(stream_of(x))
             except binding.B2Error as e:  # too many: what was kept for this one stays
                 if e.status != binding.STATIC_LIMIT:
                     raise

@@ -18,7 +18,7 @@ import torch
 
 from . import binding as b2
 from .adamw import AdamW
-from .capture import GraphWatch, Made, capture_id, capturing
+from .capture import GraphWatch, Made, capture_id, capturing, stream_of
 from .layer8 import E8, F8, _blocks, _device_of, _Once, _scratch, product, quantise
 
 ACTIVATIONS = {"none": b2.ACT_NONE, "relu": b2.ACT_RELU, "gelu": b2.ACT_GELU, "gelu_tanh": b2.ACT_GELU_TANH, "silu": b2.ACT_SILU}
@@ -171,7 +171,7 @@ class FeedForward8(torch.nn.Module):
         for name, p in (*others, ("residual", residual)):
             if p is not None and p.device != x.device:
                 raise ValueError(f"x is on {x.device}, {name} on {p.device}")
-        stream = torch.cuda.current_stream(x.device).cuda_stream if x.is_cuda else 0
+        stream = stream_of(x)
         in_capture = capture_id(x) if capturing(x) else 0
         parameters = (self.norm_weight, self.up, self.up_bias, self.down, self.down_bias)
         keep = torch.is_grad_enabled() and any(p is not None and p.requires_grad for p in (x, residual, *parameters))

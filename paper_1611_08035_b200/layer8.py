@@ -13,11 +13,12 @@ layer towards a target and times one step of a large one.
 from __future__ import annotations
 
 import contextlib
+import weakref
 
 import torch
 
 from . import binding as b2
-from .capture import GraphWatch, Made, capture_id, capturing
+from .capture import GraphWatch, Made, capture_id, capturing, stream_of
 
 F8, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
@@ -128,7 +129,10 @@ class NormLinear8(torch.nn.Module):
     """y, h = layer(x, residual): h = x + residual (x without one), y = rmsnorm(h) W^T.  W is kept in float32 for the optimiser
     and in e4m3 for the products.  The 8-bit one is made anew by the next call after the weight was changed in place, replaced, loaded or
     moved; what changes it unseen by autograd (through ``weight.data``, or in a replayed CUDA graph) has to call ``requantise()``.  What a captured graph reads of it is kept while the
-    graph lives, and what one makes of it is read by calls of the same capture alone."""
+    graph lives, and what one makes of it is read by calls of the same capture alone.
+
+    In a CUDA graph that is captured, an eager autograd graph of the same layer must not be alive unless it was made on the capturing stream (its leaves would add up their gradients
+    on the stream that it was made on, outside the capture): such a call is refused."""
 
     def __init__(self, features: int, outputs: int, eps: float = 1e-5, device="cuda"):
         super().__init__()
@@ -137,6 +141,7 @@ class NormLinear8(torch.nn.Module):
         self.weight = torch.nn.Parameter(torch.randn(outputs, features, device=device) * features**-0.5)
         self._quantised = None
         self._captured: list = []  # 8-bit weights that captured graphs read, each with a watch of the graph
+        self._graphs: list = []  # autograd graphs through the layer that may be alive, each with its stream
         if self.weight.is_cuda:
             self.requantise()
 
@@ -152,7 +157,7 @@ class NormLinear8(torch.nn.Module):
         self._quantised = (*self._state(self.weight), Made(pair, capture_id(self.weight) if capturing(self.weight) else 0))
 
     def __getstate__(self):
-        return super().__getstate__() | {"_quantised": None, "_captured": []}
+        return super().__getstate__() | {"_quantised": None, "_captured": [], "_graphs": []}
 
     def _let_go(self) -> None:
         """Of what was kept for graphs that are gone."""
@@ -175,6 +180,10 @@ class NormLinear8(torch.nn.Module):
         if weight.device != device or norm_weight.device != device or (residual is not None and residual.device != device):
             raise ValueError(f"x is on {device}, the weight on {weight.device}, the norm's on {norm_weight.device}, the residual on {None if residual is None else residual.device}")
         of, in_capture = self._quantised, capture_id(x) if capturing(x) else 0
+        stream = stream_of(x)
+        keep = torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or norm_weight.requires_grad or (residual is not None and residual.requires_grad))
+        if keep and in_capture and any(g() is not None and s != stream for g, s in self._graphs):
+            raise RuntimeError("an autograd graph of this layer from another stream is alive: delete its results, or make it on the stream that captures")
         # What a capture made is there when its graph has run: it is for calls of the same capture.
         if of is None or of[0] is not weight or of[1] != self._state(weight)[1] or of[2].capture not in (0, in_capture):
             self.requantise()
@@ -184,7 +193,10 @@ class NormLinear8(torch.nn.Module):
             self._let_go()
             if not any(c[0] is made.tensors and c[1].capture == in_capture for c in self._captured):
                 self._captured.append((made.tensors, GraphWatch(x, in_capture)))
-        return _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), norm_weight.contiguous(), weight, *made.tensors, self.eps)
+        y, h = _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), norm_weight.contiguous(), weight, *made.tensors, self.eps)
+        if keep:
+            self._graphs = [g for g in self._graphs if g[0]() is not None] + [(weakref.ref(y.grad_fn), stream)]
+        return y, h
 
 
 def train(features: int = 512, outputs: int = 384, tokens: int = 1024, steps: int = 40, lr: float = 0.5, seed: int = 0):

@@ -50,3 +50,23 @@ def test_what_a_graph_reads_is_kept_for_it(ops, capture):  # noqa: F811
             kept[1].gone = lambda: True
         layer.requantise()
         assert not layer._captured
+
+
+def test_a_capture_beside_a_living_graph_is_refused(ops, capture):  # noqa: F811
+    """Its leaves would add up their gradients on the other graph's stream, outside the capture."""
+    layer, x, r = make()
+    y = layer(x, r)
+    layer._graphs[0] = (layer._graphs[0][0], 7)  # as if from another stream
+    with torch.no_grad():
+        layer.weight.mul_(2.0)
+    capture[0], before = 1, len(ops.calls)
+    with pytest.raises(RuntimeError, match="alive"):
+        layer(x, r)
+    assert len(ops.calls) == before
+    with torch.no_grad():
+        layer(x, r)  # no gradients, nothing to add up
+    del y
+    layer(x, r)
+    for _ in range(5):
+        layer(x, r)
+    assert len(layer._graphs) == 1  # those that are alive: the last call's, not yet looked for

@@ -50,3 +50,35 @@ def test_what_a_graph_reads_stays(b2):
         torch.cuda.synchronize()
         assert torch.equal(y, want)
         del filler
+
+
+def test_a_capture_beside_a_living_graph_is_refused(b2):
+    layer, x = make()
+    alive = layer(x)  # both results, each of which keeps the graph
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="alive"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            layer(x)
+    alive[0].float().sum().backward()
+    del alive
+    dy, side = torch.randn(40, 512, device="cuda").bfloat16(), torch.cuda.Stream()
+
+    def step():
+        layer.zero_grad()
+        layer.requantise()
+        layer(x)[0].backward(dy)
+
+    step()
+    want = [p.grad.clone() for p in layer.parameters()]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    for p in layer.parameters():
+        p.grad.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p.grad, w) for p, w in zip(layer.parameters(), want)) and b2.b2_device_status() == 0
