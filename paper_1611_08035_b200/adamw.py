@@ -19,8 +19,9 @@ class AdamW(torch.optim.Optimizer):
     """``torch.optim.AdamW``'s update for float32 and bfloat16 parameters on CUDA devices.
 
     state_bits  8 or 32; tensors of fewer than ``least_8bit`` elements keep 32.
-    capturable  keeps the learning rate and the number of the step (a group's, not a parameter's) on the device, where a captured graph of ``step()`` follows them: change
-                ``group["lr"]`` by ``fill_``.  Every parameter's first step is made before the capture; one in it is refused, as is a captured step of a group that is not capturable.
+    capturable  keeps the learning rate and the number of the step on the device, where a captured graph of ``step()`` follows them: change ``group["lr"]`` by ``fill_``.  A number
+                is shared by the parameters whose first step was the same (or who had the same number when ``group["capturable"]`` was set), and counts every step that one of them
+                makes.  A captured step comes after one that was not captured, for every parameter; others are refused, as is one of a group that is not capturable.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=8, least_8bit=4096, capturable=False, seed=0):
@@ -47,14 +48,27 @@ class AdamW(torch.optim.Optimizer):
         ones = lambda: torch.full(((n + 127) // 128,), 127, dtype=torch.uint8, device=p.device).view(E8)  # noqa: E731
         return {"step": 0, "m": zeros(), "v": zeros(), "sm": ones(), "sv": ones()}
 
-    def _device_numbers(self, group, device):
-        """The group's learning rate and step on a device."""
-        if not isinstance(group["lr"], torch.Tensor):
-            group["lr"] = torch.tensor(float(group["lr"]), dtype=torch.float32, device=device)
-        steps = group.setdefault("step_device", {})
-        if device not in steps:
-            steps[device] = torch.zeros(1, dtype=torch.int64, device=device)
-        return (group["lr"] if group["lr"].device == device else group["lr"].to(device)), steps[device]
+    @staticmethod
+    def _device_lr(group, device) -> torch.Tensor:
+        lr = group["lr"]
+        if not isinstance(lr, torch.Tensor) or lr.device.type != device.type:
+            lr = group["lr"] = torch.tensor(float(lr), dtype=torch.float32, device=device)
+        return lr if lr.device == device else lr.to(device)
+
+    def _place_numbers(self, group, params) -> None:
+        """The numbers of the steps that were made, where the group has them: in a capturable one tensors of the device, which those share who come there together with
+        the same number."""
+        shared: dict = {}
+        for p in params:
+            step = self.state[p]["step"]
+            if group["capturable"] and not isinstance(step, torch.Tensor):
+                if (p.device, step) not in shared:
+                    shared[p.device, step] = torch.full((1,), step, dtype=torch.int64, device=p.device)
+                self.state[p]["step"] = shared[p.device, step]
+            elif not group["capturable"] and isinstance(step, torch.Tensor):
+                if id(step) not in shared:
+                    shared[id(step)] = int(step)
+                self.state[p]["step"] = shared[id(step)]
 
     @torch.no_grad()
     def step(self, closure=None, grad_scale: torch.Tensor | None = None):
@@ -64,28 +78,34 @@ class AdamW(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         for number, group in enumerate(self.param_groups):
-            calls: dict = {}  # tensors of one device and one step go together
-            for p in group["params"]:
-                if p.grad is None:
-                    continue
+            params = [p for p in group["params"] if p.grad is not None]
+            for p in params:
                 if p.grad.is_sparse:
                     raise RuntimeError("AdamW does not take sparse gradients")
+                if capturing(p) and not (group["capturable"] and isinstance(self.state[p].get("step"), torch.Tensor) and isinstance(group["lr"], torch.Tensor)
+                                         and group["lr"].device.type == p.device.type):
+                    raise RuntimeError("a captured step is a capturable=True group's that has made one before, without the capture: its states' first values and its numbers would be a replay's")
+                if not self.state[p]:
+                    self.state[p].update(self._new_state(p, group))
+            self._place_numbers(group, params)
+            calls: dict = {}  # tensors of one device and one step go together
+            for p in params:
                 st = self.state[p]
-                if (not st or not group["capturable"]) and capturing(p):
-                    raise RuntimeError("a captured step has capturable=True and was made once before, without the capture: its states' first values and its number would be a replay's")
-                if not st:
-                    st.update(self._new_state(p, group))
-                st["step"] += 1
-                lists = calls.setdefault((p.device, 0 if group["capturable"] else st["step"]), [[] for _ in range(6)])
+                step = st["step"]
+                if group["capturable"]:
+                    lists, _ = calls.setdefault((p.device, id(step)), ([[] for _ in range(6)], step))
+                else:
+                    step = st["step"] = step + 1
+                    lists, _ = calls.setdefault((p.device, step), ([[] for _ in range(6)], step))
                 for to, x in zip(lists, (p, p.grad.contiguous(), *(st.get(k) for k in STATES))):
                     to.append(x)
-            for (device, step), lists in calls.items():
+            for (device, _), (lists, step) in calls.items():
                 lr = group["lr"]
                 if group["capturable"]:
-                    lr, step = self._device_numbers(group, device)
+                    lr = self._device_lr(group, device)
                     step += 1
                 with _device_of(lists[0][0]):
-                    b2.b2_adamw(*lists, lr.to(device) if isinstance(lr, torch.Tensor) and lr.is_cuda else float(lr), *group["betas"], group["eps"], group["weight_decay"], step,
+                    b2.b2_adamw(*lists, lr.to(device) if isinstance(lr, torch.Tensor) and lr.device.type == device.type else float(lr), *group["betas"], group["eps"], group["weight_decay"], step,
                                 group["seed"] + (number << 32), None if grad_scale is None else grad_scale.to(device))
                 torch.autograd.graph.increment_version(lists[0])  # what is made of the parameters (8-bit copies) is made anew
         return loss
