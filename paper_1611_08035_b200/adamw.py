@@ -110,10 +110,27 @@ class AdamW(torch.optim.Optimizer):
                 torch.autograd.graph.increment_version(lists[0])  # what is made of the parameters (8-bit copies) is made anew
         return loss
 
+    def state_dict(self) -> dict:
+        """With plain numbers of steps, wherever they are counted."""
+        d = super().state_dict()
+        known: dict = {}
+        d["state"] = {i: dict(st) for i, st in d["state"].items()}
+        for st in d["state"].values():
+            step = st.get("step")
+            if isinstance(step, torch.Tensor):
+                st["step"] = known[id(step)] if id(step) in known else known.setdefault(id(step), int(step))
+        return d
+
     def load_state_dict(self, state_dict) -> None:
+        """States and numbers of steps go to the parameters' devices, whatever device they were saved from or loaded to.  A graph that was captured before follows the old ones: capture
+        again."""
         super().load_state_dict(state_dict)  # makes every floating state the parameter's type: the saved ones take their places again
         saved = state_dict["state"]
-        names = [i for g in state_dict["param_groups"] for i in g["params"]]
-        for i, p in zip(names, (p for g in self.param_groups for p in g["params"])):
-            if i in saved:
-                self.state[p].update({k: saved[i][k].to(p.device, copy=True) for k in STATES if k in saved[i]})
+        for g, old in zip(self.param_groups, state_dict["param_groups"]):
+            of_group = g.pop("step_device", None)  # where capturable groups once counted, for every parameter
+            for i, p in zip(old["params"], g["params"]):
+                if i in saved:
+                    self.state[p].update({k: saved[i][k].to(p.device, copy=True) for k in STATES if k in saved[i]})
+                    self.state[p]["step"] = max(map(int, of_group.values())) if of_group else int(saved[i].get("step", 0))
+                    if isinstance(g["lr"], torch.Tensor) and g["capturable"]:
+                        g["lr"] = g["lr"].to(p.device)

@@ -65,3 +65,38 @@ def test_set_after_steps_and_taken_back(b2):
     torch.cuda.synchronize()
     alike(a, b, eager, opt, 8)
     assert b2.b2_device_status() == 0
+
+
+@pytest.mark.parametrize("where", ["cpu", "cuda"])
+def test_saved_in_between(b2, where):
+    """A capturable optimiser after a replay, saved, loaded to the host or the device and captured again: as the one that goes on."""
+    import io
+    (a, opt), (b, other) = make(capturable=True), make()
+    for p in a:
+        p.grad.normal_()
+    opt.step()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        opt.step()
+    graph.replay()
+    file = io.BytesIO()
+    torch.save(opt.state_dict(), file)
+    file.seek(0)
+    other.load_state_dict(torch.load(file, map_location=where))
+    with torch.no_grad():
+        for p, q in zip(a, b):
+            q.copy_(p), q.grad.copy_(p.grad)
+    graph.replay()
+    other.step()
+    again = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(again):
+        other.step()
+    for _ in range(2):
+        graph.replay(), again.replay()
+    torch.cuda.synchronize()
+    assert all(int(st["step"]) == 5 for o in (opt, other) for st in o.state.values())
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    for p, q in zip(a, b):
+        assert all(torch.equal(opt.state[p][k].view(torch.uint8), other.state[q][k].view(torch.uint8)) for k in STATES if k in opt.state[p])
