@@ -77,14 +77,16 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        for number, group in enumerate(self.param_groups):
-            params = [p for p in group["params"] if p.grad is not None]
+        with_grads = [[p for p in group["params"] if p.grad is not None] for group in self.param_groups]
+        for group, params in zip(self.param_groups, with_grads):  # what is refused is refused before anything is counted
             for p in params:
                 if p.grad.is_sparse:
                     raise RuntimeError("AdamW does not take sparse gradients")
                 if capturing(p) and not (group["capturable"] and isinstance(self.state[p].get("step"), torch.Tensor) and isinstance(group["lr"], torch.Tensor)
                                          and group["lr"].device.type == p.device.type):
                     raise RuntimeError("a captured step is a capturable=True group's that has made one before, without the capture: its states' first values and its numbers would be a replay's")
+        for number, (group, params) in enumerate(zip(self.param_groups, with_grads)):
+            for p in params:
                 if not self.state[p]:
                     self.state[p].update(self._new_state(p, group))
             self._place_numbers(group, params)
@@ -92,21 +94,22 @@ class AdamW(torch.optim.Optimizer):
             for p in params:
                 st = self.state[p]
                 step = st["step"]
-                if group["capturable"]:
-                    lists, _ = calls.setdefault((p.device, id(step)), ([[] for _ in range(6)], step))
-                else:
-                    step = st["step"] = step + 1
-                    lists, _ = calls.setdefault((p.device, step), ([[] for _ in range(6)], step))
+                lists, _ = calls.setdefault((p.device, id(step) if group["capturable"] else step), ([[] for _ in range(6)], step))
                 for to, x in zip(lists, (p, p.grad.contiguous(), *(st.get(k) for k in STATES))):
                     to.append(x)
             for (device, _), (lists, step) in calls.items():
-                lr = group["lr"]
-                if group["capturable"]:
-                    lr = self._device_lr(group, device)
-                    step += 1
+                lr = self._device_lr(group, device) if group["capturable"] else group["lr"]
+                lr = lr.to(device) if isinstance(lr, torch.Tensor) and lr.device.type == device.type else float(lr)
                 with _device_of(lists[0][0]):
-                    b2.b2_adamw(*lists, lr.to(device) if isinstance(lr, torch.Tensor) and lr.device.type == device.type else float(lr), *group["betas"], group["eps"], group["weight_decay"], step,
-                                group["seed"] + (number << 32), None if grad_scale is None else grad_scale.to(device))
+                    step += 1
+                    try:
+                        b2.b2_adamw(*lists, lr, *group["betas"], group["eps"], group["weight_decay"], step, group["seed"] + (number << 32), None if grad_scale is None else grad_scale.to(device))
+                    except Exception:
+                        step -= 1  # on the device, where it is the parameters' own
+                        raise
+                if not group["capturable"]:
+                    for p in lists[0]:
+                        self.state[p]["step"] = step
                 torch.autograd.graph.increment_version(lists[0])  # what is made of the parameters (8-bit copies) is made anew
         return loss
 

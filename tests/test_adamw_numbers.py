@@ -73,3 +73,34 @@ def test_a_number_that_a_capture_would_make_is_refused(calls, monkeypatch):
     opt.param_groups[0]["lr"] = 1e-4  # a number in place of the tensor that the graph would follow
     with pytest.raises(RuntimeError, match="capture"):
         go(opt, params)
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_refused_steps_do_not_count(calls, capturable, monkeypatch):
+    """Neither those that the optimiser refuses nor those that the binding does."""
+    (a, b), opt = make(capturable=capturable)
+    go(opt, [a, b], 2)
+    a.grad, b.grad = torch.ones(5000), torch.ones(5000).to_sparse()
+    with pytest.raises(RuntimeError, match="sparse"):
+        opt.step()
+    monkeypatch.setattr(adamw, "capturing", lambda x: x is b)
+    b.grad = torch.ones(5000)
+    opt.state[b]["step"] = int(opt.state[b]["step"])  # not the device's
+    with pytest.raises(RuntimeError, match="capture"):
+        opt.step()
+    monkeypatch.setattr(adamw, "capturing", lambda x: False)
+    taken = adamw.b2.b2_adamw
+
+    def refuse(*args):
+        raise TypeError
+
+    monkeypatch.setattr(adamw.b2, "b2_adamw", staticmethod(refuse))
+    versions = a._version, b._version
+    for _ in range(3):
+        with pytest.raises(TypeError):
+            opt.step()
+    monkeypatch.setattr(adamw.b2, "b2_adamw", staticmethod(taken))
+    assert (a._version, b._version) == versions and [int(opt.state[p]["step"]) for p in (a, b)] == [2, 2]
+    calls.clear()
+    go(opt, [a, b])
+    assert [step for _, step in calls] == [3] * len(calls) and sum(n for n, _ in calls) == 2
