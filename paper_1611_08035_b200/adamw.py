@@ -82,6 +82,8 @@ class AdamW(torch.optim.Optimizer):
             for p in params:
                 if p.grad.is_sparse:
                     raise RuntimeError("AdamW does not take sparse gradients")
+                if self.state[p] and any(self.state[p][k].device != p.device for k in STATES if k in self.state[p]):
+                    raise RuntimeError(f"a parameter is on {p.device}, its states are not: load them again after it was moved")
                 if capturing(p) and not (group["capturable"] and isinstance(self.state[p].get("step"), torch.Tensor) and isinstance(group["lr"], torch.Tensor)
                                          and group["lr"].device.type == p.device.type):
                     raise RuntimeError("a captured step is a capturable=True group's that has made one before, without the capture: its states' first values and its numbers would be a replay's")

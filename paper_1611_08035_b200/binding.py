@@ -644,12 +644,15 @@ class _AdamwTensor(ctypes.Structure):  # b2_adamw_tensor
 
 
 def b2_adamw(params, grads, m, v, sm, sv, lr, beta1, beta2, eps, weight_decay, step, seed=0, grad_scale=None, check=True) -> int:
-    """One AdamW step, in place, over lists of contiguous tensors.  params, grads: bfloat16 or float32; m, v: float32, or float8_e4m3fn (v then holds the root of the
+    """One AdamW step, in place, over lists of contiguous tensors of one device, the current one.  params, grads: bfloat16 or float32; m, v: float32, or float8_e4m3fn (v then holds the root of the
     second moment) with float8_e8m0fnu scales sm, sv for 128 elements each.  sm and sv may be None, as may their entries for float32 states.  lr and
     step are numbers, or CUDA tensors of one float32 and one int64 that are read when the call runs; grad_scale: a CUDA tensor of one float32, or None."""
     count = len(params)
     if any(len(x) != count for x in (grads, m, v)) or any(x is not None and len(x) != count for x in (sm, sv)):
         raise ValueError("b2_adamw: the lists have different lengths")
+    devices = {x.device for some in (params, grads, m, v, sm or (), sv or (), (lr, step, grad_scale)) for x in some if getattr(x, "is_cuda", False)}
+    if len(devices) > 1:
+        raise ValueError(f"b2_adamw: the tensors of a call are on one device; these are on {sorted(map(str, devices))}")
     table = (_AdamwTensor * max(count, 1))()
     for i in range(count):
         t = (params[i], grads[i], m[i], v[i], None if sm is None else sm[i], None if sv is None else sv[i])

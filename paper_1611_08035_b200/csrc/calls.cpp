@@ -293,11 +293,13 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
   for (int i = 1; i < 6 && ok; ++i) ok = (i >= 4 && !scales) ? a[i] == Py_None : length(a[i]) == count;
   if (!ok) return hand_over(g_adamw, a, n, names);
   std::vector<b2_adamw_tensor> table(count);
+  int device = -1;  // of all tensors
+  auto here = [&](const at::Tensor* t) { return (device = device < 0 ? t->get_device() : device) == t->get_device(); };
   for (Py_ssize_t i = 0; i < count && ok; ++i) {
     const at::Tensor* t[6] = {};
     for (int j = 0; j < 4 && ok; ++j) {
       t[j] = entry(a[j], i);
-      ok = t[j] && t[j]->numel() == t[0]->numel();
+      ok = t[j] && t[j]->numel() == t[0]->numel() && here(t[j]);
     }
     if (!ok) break;
     const int64_t size = t[0]->numel();
@@ -306,7 +308,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
     ok = type_code(t[0]) && type_code(t[1]) && t[2]->scalar_type() == state && t[3]->scalar_type() == state && (!eight || scales);
     for (int j = 4; j < 6 && eight && ok; ++j) {
       t[j] = entry(a[j], i);
-      ok = t[j] && t[j]->scalar_type() == at::kFloat8_e8m0fnu && t[j]->numel() == (size + 127) / 128;
+      ok = t[j] && t[j]->scalar_type() == at::kFloat8_e8m0fnu && t[j]->numel() == (size + 127) / 128 && here(t[j]);
     }
     if (ok) table[i] = {t[0]->data_ptr(), t[1]->data_ptr(), t[2]->data_ptr(), t[3]->data_ptr(), address(t[4]), address(t[5]), size, type_code(t[0]), type_code(t[1]), eight ? 8 : 32, 0};
   }
@@ -316,7 +318,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
   auto either = [&](at::ScalarType type) -> void* {
     if (!p.ok || p.i >= p.n || !THPVariable_Check(a[p.i])) return nullptr;
     const at::Tensor* t = p.tensor();
-    if (t && (t->scalar_type() != type || t->numel() != 1)) p.ok = false;
+    if (t && (t->scalar_type() != type || t->numel() != 1 || !here(t))) p.ok = false;
     return p.ok ? t->data_ptr() : nullptr;
   };
   void* lr_device = either(at::kFloat);
@@ -324,7 +326,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* names) {
   void* step_device = either(at::kLong);
   const int64_t step = step_device ? 1 : p.integer(), seed = p.i < p.n ? p.integer() : 0;
   const at::Tensor* scale = p.i < p.n ? p.tensor(true) : nullptr;
-  if (!ok || (scale && (scale->scalar_type() != at::kFloat || scale->numel() != 1)) || !p.all_read()) return hand_over(g_adamw, a, n, names);
+  if (!ok || (scale && (scale->scalar_type() != at::kFloat || scale->numel() != 1 || !here(scale))) || !p.all_read()) return hand_over(g_adamw, a, n, names);
   const auto fn = reinterpret_cast<decltype(&b2_adamw)>(g_adamw.fn);
   void *gs = address(scale), *st = stream();
   return result("b2_adamw", [&] {
