@@ -12,8 +12,6 @@
 // eight elements and an addition for each.  m and v are computed by single roundings in a fixed order (no fused multiply-adds), and so is r: then everyone who
 // computes them in fp32 comes to the same bits, and to the same side of a random rounding.
 #include <algorithm>
-#include <memory>
-#include <new>
 
 #include "act.cuh"
 #include "b2gemm.h"
@@ -416,19 +414,35 @@ bool adam_valid(const b2_adamw_tensor& t) {
   const int states = t.state_bits == 8 ? 1 : 4;
   return aligned(t.param, t.type_param == B2_TYPE_BF16 ? 2 : 4) && aligned(t.grad, t.type_grad == B2_TYPE_BF16 ? 2 : 4) && aligned(t.m, states) && aligned(t.v, states);
 }
-// Whether no parameter shares memory with another: a tensor that occurs twice would be updated by two CTAs at once.
+// Whether no parameter shares memory with another: a tensor that occurs twice would be updated by two CTAs at once.  2048 ranges at a time, sorted, on the stack: no call allocates.
 struct AdamRange {
   uintptr_t begin, end;
 };
-bool adam_apart(const b2_adamw_tensor* tensors, int count, AdamRange* r) {
+constexpr int kRanges = 2048;
+int adam_ranges(const b2_adamw_tensor* tensors, int count, AdamRange* r) {
   int n = 0;
-  for (int i = 0; i < count; ++i) {
+  for (int i = 0; i < count && i < kRanges; ++i) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(tensors[i].param);
     if (tensors[i].n > 0) r[n++] = {at, at + (uintptr_t)tensors[i].n * (tensors[i].type_param == B2_TYPE_BF16 ? 2 : 4)};
   }
   std::sort(r, r + n, [](const AdamRange& a, const AdamRange& b) { return a.begin < b.begin; });
-  for (int i = 1; i < n; ++i)
-    if (r[i].begin < r[i - 1].end) return false;
+  return n;
+}
+bool adam_apart(const b2_adamw_tensor* tensors, int count) {
+  AdamRange a[kRanges], b[kRanges];
+  for (int64_t i = 0; i < count; i += kRanges) {
+    const int na = adam_ranges(tensors + i, count - (int)i, a);
+    for (int k = 1; k < na; ++k)
+      if (a[k].begin < a[k - 1].end) return false;
+    for (int64_t j = i + kRanges; j < count; j += kRanges) {
+      const int nb = adam_ranges(tensors + j, count - (int)j, b);
+      for (int x = 0, y = 0; x < na && y < nb;) {
+        if (a[x].begin < b[y].end && b[y].begin < a[x].end) return false;
+        if (a[x].end <= b[y].begin) ++x;
+        else ++y;
+      }
+    }
+  }
   return true;
 }
 int adam_kind(const b2_adamw_tensor& t) { return (t.state_bits == 8 ? 4 : 0) + (t.type_param == B2_TYPE_BF16 ? 2 : 0) + (t.type_grad == B2_TYPE_BF16 ? 1 : 0); }
@@ -485,10 +499,7 @@ extern "C" int b2_adamw(const b2_adamw_tensor* tensors, int count, double lr, do
     if (!adam_valid(tensors[i]) || blocks_of(tensors[i].n, unit(1)) > 0x7fffffffLL) return -1;
     if (tensors[i].n > 0) ++of_kind[adam_kind(tensors[i])], elements[adam_kind(tensors[i])] += (double)tensors[i].n;
   }
-  AdamRange few[32];
-  std::unique_ptr<AdamRange[]> many(count > 32 ? new (std::nothrow) AdamRange[count] : nullptr);
-  if (count > 32 && !many) return B2_ERR_LAUNCH;
-  if (!adam_apart(tensors, count, many ? many.get() : few)) return -1;
+  if (!adam_apart(tensors, count)) return -1;
   AdamStep s = {};
   s.b1 = (float)beta1, s.a1 = (float)(1.0 - beta1), s.b2 = (float)beta2, s.a2 = (float)(1.0 - beta2), s.eps = (float)eps;
   s.seed = seed, s.scale = grad_scale, s.lr_device = lr_device, s.step_device = step_device;
