@@ -70,3 +70,35 @@ class GraphWatch:
 
     def gone(self) -> bool:
         return self._watch is not None and binding.b2_graph_gone(self._watch)
+
+
+DEFAULT_STREAM = 0
+
+
+class AutogradGraphs(list):
+    """The autograd graphs through a module that may be alive, each as a weak reference to its node and the stream that it was made on.
+
+    What reaches a parameter's gradient goes to the stream where the oldest living graph met the parameter first.  A capture can take another stream in, but not the default one: there it ends
+    with an error in the middle of the backward pass, or takes the process with it.  So such a pass is refused before it begins."""
+
+    def elsewhere(self, stream: int) -> list:
+        """The nodes of those that were made on other streams."""
+        return [node for node in (g() for g, s in self if s != stream) if node is not None]
+
+    def add(self, node, stream: int) -> None:
+        self[:] = [g for g in self if g[0]() is not None] + [(weakref.ref(node), stream)]
+
+    def refuse(self, node, stream: int) -> None:
+        """In a captured backward pass through a node."""
+        if stream != DEFAULT_STREAM and any(s == DEFAULT_STREAM and g() is not None for g, s in self) and any(_reached(n) for n, _ in node.next_functions):
+            raise RuntimeError("an autograd graph of this module that was made on the default stream is alive: delete its results, or make it on the stream that captures")
+
+
+def _reached(node) -> bool:
+    """Whether the backward pass that runs now makes the gradient of the parameter whose node this is."""
+    if node is None or not hasattr(node, "variable"):
+        return False
+    try:
+        return torch._C._will_engine_execute_node(node)
+    except RuntimeError:  # it does not say so of what torch.autograd.grad hands out
+        return True

@@ -13,12 +13,11 @@ layer towards a target and times one step of a large one.
 from __future__ import annotations
 
 import contextlib
-import weakref
 
 import torch
 
 from . import binding as b2
-from .capture import GraphWatch, Made, capture_id, capturing, stream_of
+from .capture import AutogradGraphs, GraphWatch, Made, capture_id, capturing, stream_of
 
 F8, E8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
@@ -73,7 +72,7 @@ class _Once(torch.autograd.Function):
 
 class _NormLinear8(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, residual, norm_weight, weight, w8, sw, eps):
+    def forward(ctx, x, residual, norm_weight, weight, w8, sw, eps, graphs):
         ctx.set_materialize_grads(False)  # no gradient for h: nothing to add
         t, d = x.shape
         n = weight.shape[0]
@@ -84,11 +83,14 @@ class _NormLinear8(torch.autograd.Function):
             b2.b2_rmsnorm_f8(d, t, x, d, residual, d, norm_weight, eps, h if residual is not None else None, d, q, d, s, s.shape[1], rstd)
         y = product(w8, sw, 128, "T", q, s, 1, n, t, d)
         ctx.save_for_backward(h, norm_weight, q, s, rstd, w8, sw)
-        ctx.has_residual = residual is not None
+        ctx.has_residual, ctx.graphs = residual is not None, graphs
         return y, h
 
     @staticmethod
     def backward(ctx, dy, dh):
+        given = dh if dy is None else dy
+        if given is not None and capturing(given):
+            ctx.graphs.refuse(ctx, stream_of(given))
         if not torch.is_grad_enabled():
             return _NormLinear8.gradients(ctx, dy, dh)
         with torch.no_grad():  # someone wants to differentiate the gradients: they depend on x and the weights, whatever dy does
@@ -107,7 +109,7 @@ class _NormLinear8(torch.autograd.Function):
                 dnw = torch.zeros_like(norm_weight)
             if wants_weight:
                 dweight = torch.zeros(n, d, dtype=torch.float32, device=device)
-            return dh, dh if ctx.has_residual else None, dnw, dweight, None, None, None
+            return dh, dh if ctx.has_residual else None, dnw, dweight, None, None, None, None
         dy = dy.contiguous()
         with _device_of(h):
             if wants_x or wants_residual or wants_norm:
@@ -122,7 +124,7 @@ class _NormLinear8(torch.autograd.Function):
                 ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), device)
                 b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, None if dh is None else dh.contiguous(), d, dx, d, dnw, ws)
                 dnw = dnw.to(norm_weight.dtype) if wants_norm else None
-        return dx, dx if ctx.has_residual else None, dnw, dweight, None, None, None
+        return dx, dx if ctx.has_residual else None, dnw, dweight, None, None, None, None
 
 
 class NormLinear8(torch.nn.Module):
@@ -131,8 +133,8 @@ class NormLinear8(torch.nn.Module):
     moved; what changes it unseen by autograd (through ``weight.data``, or in a replayed CUDA graph) has to call ``requantise()``.  What a captured graph reads of it is kept while the
     graph lives, and what one makes of it is read by calls of the same capture alone.
 
-    In a CUDA graph that is captured, an eager autograd graph of the same layer must not be alive unless it was made on the capturing stream (its leaves would add up their gradients
-    on the stream that it was made on, outside the capture): such a call is refused."""
+    While a backward pass is captured that makes the parameters' gradients, no autograd graph of the same layer that was made on the default stream may be alive (they would be
+    made there, which cannot be captured): such a pass is refused."""
 
     def __init__(self, features: int, outputs: int, eps: float = 1e-5, device="cuda"):
         super().__init__()
@@ -141,7 +143,7 @@ class NormLinear8(torch.nn.Module):
         self.weight = torch.nn.Parameter(torch.randn(outputs, features, device=device) * features**-0.5)
         self._quantised = None
         self._captured: list = []  # 8-bit weights that captured graphs read, each with a watch of the graph
-        self._graphs: list = []  # autograd graphs through the layer that may be alive, each with its stream
+        self._graphs = AutogradGraphs()
         if self.weight.is_cuda:
             self.requantise()
 
@@ -157,7 +159,7 @@ class NormLinear8(torch.nn.Module):
         self._quantised = (*self._state(self.weight), Made(pair, capture_id(self.weight) if capturing(self.weight) else 0))
 
     def __getstate__(self):
-        return super().__getstate__() | {"_quantised": None, "_captured": [], "_graphs": []}
+        return super().__getstate__() | {"_quantised": None, "_captured": [], "_graphs": AutogradGraphs()}
 
     def _let_go(self) -> None:
         """Of what was kept for graphs that are gone."""
@@ -180,10 +182,6 @@ class NormLinear8(torch.nn.Module):
         if weight.device != device or norm_weight.device != device or (residual is not None and residual.device != device):
             raise ValueError(f"x is on {device}, the weight on {weight.device}, the norm's on {norm_weight.device}, the residual on {None if residual is None else residual.device}")
         of, in_capture = self._quantised, capture_id(x) if capturing(x) else 0
-        stream = stream_of(x)
-        keep = torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or norm_weight.requires_grad or (residual is not None and residual.requires_grad))
-        if keep and in_capture and any(g() is not None and s != stream for g, s in self._graphs):
-            raise RuntimeError("an autograd graph of this layer from another stream is alive: delete its results, or make it on the stream that captures")
         # What a capture made is there when its graph has run: it is for calls of the same capture.
         if of is None or of[0] is not weight or of[1] != self._state(weight)[1] or of[2].capture not in (0, in_capture):
             self.requantise()
@@ -193,9 +191,9 @@ class NormLinear8(torch.nn.Module):
             self._let_go()
             if not any(c[0] is made.tensors and c[1].capture == in_capture for c in self._captured):
                 self._captured.append((made.tensors, GraphWatch(x, in_capture)))
-        y, h = _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), norm_weight.contiguous(), weight, *made.tensors, self.eps)
-        if keep:
-            self._graphs = [g for g in self._graphs if g[0]() is not None] + [(weakref.ref(y.grad_fn), stream)]
+        y, h = _NormLinear8.apply(x.contiguous(), None if residual is None else residual.contiguous(), norm_weight.contiguous(), weight, *made.tensors, self.eps, self._graphs)
+        if y.grad_fn is not None:
+            self._graphs.add(y.grad_fn, stream_of(x))
         return y, h
 
 

@@ -52,21 +52,30 @@ def test_what_a_graph_reads_is_kept_for_it(ops, capture):  # noqa: F811
         assert not layer._captured
 
 
-def test_a_capture_beside_a_living_graph_is_refused(ops, capture):  # noqa: F811
-    """Its leaves would add up their gradients on the other graph's stream, outside the capture."""
+def test_a_captured_backward_pass_beside_a_living_graph_is_refused(ops, capture, monkeypatch):  # noqa: F811
+    """Where it makes the parameters' gradients and the other graph is the default stream's."""
     layer, x, r = make()
-    y = layer(x, r)
-    layer._graphs[0] = (layer._graphs[0][0], 7)  # as if from another stream
-    with torch.no_grad():
-        layer.weight.mul_(2.0)
-    capture[0], before = 1, len(ops.calls)
+    stream = [0]
+    monkeypatch.setattr(layer8, "stream_of", lambda x: stream[0])
+    alive = layer(x, r)
+    stream[0] = capture[0] = 1
+    y, _ = layer(x, r)
+    before = len(ops.calls)
+    for inputs in (None, [layer.weight], [x, layer.norm_weight]):
+        with pytest.raises(RuntimeError, match="alive"):
+            y.float().sum().backward(retain_graph=True, inputs=inputs)
     with pytest.raises(RuntimeError, match="alive"):
-        layer(x, r)
-    assert len(ops.calls) == before
-    with torch.no_grad():
-        layer(x, r)  # no gradients, nothing to add up
-    del y
-    layer(x, r)
+        torch.autograd.grad(y.float().sum(), [layer.weight], retain_graph=True)
+    assert len(ops.calls) == before and layer.weight.grad is None
+    xx = x * 1.0
+    torch.autograd.grad(layer(xx, r.detach())[0].float().sum(), [xx])  # reaches no parameter
+    capture[0] = 0
+    y.float().sum().backward(retain_graph=True)  # not captured
+    del alive
+    capture[0] = 1
+    y.float().sum().backward(retain_graph=True)
+    stream[0] = 2  # made on 1, captured on 2
+    layer(x, r)[0].float().sum().backward()
     for _ in range(5):
         layer(x, r)
-    assert len(layer._graphs) == 1  # those that are alive: the last call's, not yet looked for
+    assert len(layer._graphs) <= 2  # y's, and the last call's, not yet looked for

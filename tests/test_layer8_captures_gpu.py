@@ -52,15 +52,8 @@ def test_what_a_graph_reads_stays(b2):
         del filler
 
 
-def test_a_capture_beside_a_living_graph_is_refused(b2):
+def test_a_captured_training_step(b2):
     layer, x = make()
-    alive = layer(x)  # both results, each of which keeps the graph
-    torch.cuda.synchronize()
-    with pytest.raises(RuntimeError, match="alive"):
-        with torch.cuda.graph(torch.cuda.CUDAGraph()):
-            layer(x)
-    alive[0].float().sum().backward()
-    del alive
     dy, side = torch.randn(40, 512, device="cuda").bfloat16(), torch.cuda.Stream()
 
     def step():
@@ -81,4 +74,56 @@ def test_a_capture_beside_a_living_graph_is_refused(b2):
         p.grad.fill_(float("nan"))
     graph.replay()
     torch.cuda.synchronize()
+    assert all(torch.equal(p.grad, w) for p, w in zip(layer.parameters(), want)) and b2.b2_device_status() == 0
+
+
+def test_graphed_callable(b2):
+    """torch's own way to capture both passes, whose warm-up's graph is alive meanwhile: gradients are handed out, none is added up."""
+    layer, x = make()
+    x.requires_grad_()
+    dy = torch.randn(40, 512, device="cuda").bfloat16()
+
+    def passes(f):
+        x.grad = None
+        layer.zero_grad()
+        y, h = f(x)
+        torch.autograd.backward([y, h], [dy, dy[:, :256].contiguous()])
+        return [y.detach(), h.detach(), x.grad, *(p.grad for p in layer.parameters())]
+
+    want = passes(layer)
+    graphed = torch.cuda.make_graphed_callables(layer, (x.detach().clone().requires_grad_(),))
+    for _ in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(passes(graphed), want))
+    assert b2.b2_device_status() == 0
+
+
+def test_beside_living_graphs(b2):
+    """Of another stream: captured as if it were not there.  Of the default stream: refused, and what was captured of the step ends as any step that failed."""
+    layer, x = make()
+    dy, sides = torch.randn(40, 512, device="cuda").bfloat16(), [torch.cuda.Stream() for _ in range(2)]
+    layer(x)[0].backward(dy)
+    want = [p.grad.clone() for p in layer.parameters()]
+    layer.zero_grad()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(sides[0]):
+        alive = layer(x)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=sides[1]):
+        layer(x)[0].backward(dy)
+    for p in layer.parameters():
+        p.grad.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p.grad, w) for p, w in zip(layer.parameters(), want))
+    del alive, graph
+    layer.zero_grad()
+    alive = layer(x)
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="alive"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=sides[1]):
+            layer(x)[0].backward(dy)
+    assert all(p.grad is None for p in layer.parameters())
+    del alive
+    layer(x)[0].backward(dy)
     assert all(torch.equal(p.grad, w) for p, w in zip(layer.parameters(), want)) and b2.b2_device_status() == 0
