@@ -12,13 +12,11 @@ one step of a large one.
 """
 from __future__ import annotations
 
-import weakref
-
 import torch
 
 from . import binding as b2
 from .adamw import AdamW
-from .capture import GraphWatch, Made, capture_id, capturing, stream_of
+from .capture import AutogradGraphs, GraphWatch, Made, capture_id, capturing, stream_of
 from .layer8 import E8, F8, _blocks, _device_of, _Once, _scratch, product, quantise
 
 ACTIVATIONS = {"none": b2.ACT_NONE, "relu": b2.ACT_RELU, "gelu": b2.ACT_GELU, "gelu_tanh": b2.ACT_GELU_TANH, "silu": b2.ACT_SILU}
@@ -43,7 +41,7 @@ def activation_backward(act, dy, z=None, dz=None, q=None, s=None, db=None) -> No
 
 class _FeedForward8(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, residual, norm_weight, w1, b1, w2, b2_, quantised, act, eps, keep):
+    def forward(ctx, x, residual, norm_weight, w1, b1, w2, b2_, quantised, act, eps, keep, graphs):
         (q1, s1), (q2, s2) = quantised
         (t, d), f, device = x.shape, w1.shape[0], x.device
         b1, b2_ = (None if b is None else b.float() for b in (b1, b2_))
@@ -58,11 +56,14 @@ class _FeedForward8(torch.autograd.Function):
             product_act(q2, s2, "T", aq, as_, d, t, f, b2.ACT_NONE, b2_, residual=h, c=y)
         if keep:
             ctx.save_for_backward(h, norm_weight, rstd, nq, ns, z, aq, as_, q1, s1, q2, s2)
-        ctx.act, ctx.has_residual = act, residual is not None
+        ctx.act, ctx.has_residual, ctx.graphs, ctx.ran = act, residual is not None, graphs, False
         return y
 
     @staticmethod
     def backward(ctx, dy):
+        if capturing(dy):
+            ctx.graphs.refuse(ctx, stream_of(dy))
+        ctx.ran = True
         if not torch.is_grad_enabled():
             return _FeedForward8.gradients(ctx, dy)
         with torch.no_grad():  # someone wants to differentiate the gradients: they depend on x and the weights, whatever dy does
@@ -110,7 +111,7 @@ class _FeedForward8(torch.autograd.Function):
                     ws = _scratch(b2.b2_rmsnorm_backward_workspace_bytes(d, t), device)
                     b2.b2_rmsnorm_backward(d, t, dnorm, d, h, d, rstd, norm_weight, dy, d, dx, d, dnw, ws)
                     dnw = dnw.to(norm_weight.dtype) if need_norm else None
-        return dx if need_x else None, dx if need_r else None, dnw, dw1, db1, dw2, db2, None, None, None, None
+        return dx if need_x else None, dx if need_r else None, dnw, dw1, db1, dw2, db2, None, None, None, None, None
 
 
 class FeedForward8(torch.nn.Module):
@@ -118,8 +119,9 @@ class FeedForward8(torch.nn.Module):
     weight was changed in place, replaced, loaded or moved; what changes it unseen by autograd (a replayed CUDA graph) has to call ``requantise()``, which a captured
     training step does itself, first.  It can be differentiated once.
 
-    In a CUDA graph that is captured, an eager autograd graph of the same block must not be alive unless it was made on the capturing stream (its leaves would add up their gradients
-    on the stream that it was made on, outside the capture): such a call is refused."""
+    In a CUDA graph that is captured, an autograd graph of the same block whose backward pass has yet to come must not be alive unless it was made on the capturing stream: such a call is refused.
+    So is a captured backward pass that makes the parameters' gradients while any graph of the block that was made on the default stream is alive (they would be made there, which cannot be
+    captured)."""
 
     def __init__(self, features: int, hidden: int, activation: str = "gelu", bias: bool = True, eps: float = 1e-5, device="cuda"):
         super().__init__()
@@ -131,10 +133,10 @@ class FeedForward8(torch.nn.Module):
         self.down_bias = torch.nn.Parameter(torch.zeros(features, device=device)) if bias else None
         self._quantised: dict = {}
         self._captured: list = []  # 8-bit weights that captured graphs read, each with a watch of the graph
-        self._graphs: list = []    # autograd graphs through the block that may be alive, each with its stream
+        self._graphs = AutogradGraphs()
 
     def __getstate__(self):
-        return super().__getstate__() | {"_quantised": {}, "_captured": [], "_graphs": []}
+        return super().__getstate__() | {"_quantised": {}, "_captured": [], "_graphs": AutogradGraphs()}
 
     @staticmethod
     def _state(weight):
@@ -175,7 +177,7 @@ class FeedForward8(torch.nn.Module):
         in_capture = capture_id(x) if capturing(x) else 0
         parameters = (self.norm_weight, self.up, self.up_bias, self.down, self.down_bias)
         keep = torch.is_grad_enabled() and any(p is not None and p.requires_grad for p in (x, residual, *parameters))
-        if keep and in_capture and any(g() is not None and s != stream for g, s in self._graphs):
+        if keep and in_capture and not all(node.ran for node in self._graphs.elsewhere(stream)):
             raise RuntimeError("an autograd graph of this block from another stream is alive: delete its results, or make it on the stream that captures")
         for name in ("up", "down"):
             of = self._quantised.get(name)
@@ -192,10 +194,9 @@ class FeedForward8(torch.nn.Module):
             self._let_go()
             if not any(c[0] is up and c[2].capture == in_capture for c in self._captured):
                 self._captured.append((up, down, GraphWatch(x, in_capture)))
-        if not keep:
-            return _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep)
-        y = _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep)
-        self._graphs = [g for g in self._graphs if g[0]() is not None] + [(weakref.ref(y.grad_fn), stream)]
+        y = _FeedForward8.apply(*inputs, quantised, self.act, self.eps, keep, self._graphs)
+        if keep:
+            self._graphs.add(y.grad_fn, stream)
         return y
 
 

@@ -82,3 +82,25 @@ def test_what_is_no_watch_is_refused(b2):
     for watch in (-1, 0, 4096):
         assert b2.lib().b2_graph_gone(watch) == 0 and b2.lib().b2_graph_unwatch(watch) == -1
     assert b2.lib().b2_graph_watch(None, None) == -2
+
+
+def test_a_captured_backward_pass_beside_a_living_graph(ops, capture, monkeypatch):  # noqa: F811
+    """Beside a graph whose backward pass has run, calls are captured; a backward pass is refused where it makes the parameters' gradients and the graph is the default stream's."""
+    block, x, r = make()
+    stream = [0]
+    monkeypatch.setattr(ffn8, "stream_of", lambda x: stream[0])
+    alive = block(x, r)
+    alive.float().sum().backward(retain_graph=True)
+    block.zero_grad()
+    stream[0] = capture[0] = 1
+    y = block(x, r)
+    before = len(ops.calls)
+    with pytest.raises(RuntimeError, match="alive"):
+        y.float().sum().backward(retain_graph=True)
+    with pytest.raises(RuntimeError, match="alive"):
+        torch.autograd.grad(y.float().sum(), [block.down], retain_graph=True)
+    assert len(ops.calls) == before and block.down.grad is None
+    del alive
+    y.float().sum().backward(retain_graph=True)
+    stream[0] = 2  # made and run on 1, captured on 2
+    block(x, r).float().sum().backward()

@@ -62,3 +62,46 @@ def test_a_capture_after_a_refused_one(b2):
     torch.cuda.synchronize()
     with torch.no_grad():
         assert torch.equal(y, block(x))
+
+
+def test_graphed_callable(b2):
+    """torch's own way to capture both passes, whose warm-up's graph is alive meanwhile."""
+    block, x = make()
+    x.requires_grad_()
+    dy = torch.randn(40, 256, device="cuda").bfloat16()
+
+    def passes(f):
+        x.grad = None
+        block.zero_grad()
+        y = f(x)
+        y.backward(dy)
+        return [y.detach(), x.grad, *(p.grad for p in block.parameters())]
+
+    want = passes(block)
+    graphed = torch.cuda.make_graphed_callables(block, (x.detach().clone().requires_grad_(),))
+    for _ in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(passes(graphed), want))
+    assert b2.b2_device_status() == 0
+
+
+def test_a_backward_pass_beside_a_graph_of_the_default_stream(b2):
+    block, x = make()
+    dy, side = torch.randn(40, 256, device="cuda").bfloat16(), torch.cuda.Stream()
+    alive = block(x)
+    alive.backward(dy, retain_graph=True)
+    want = [p.grad for p in block.parameters()]
+    block.zero_grad()
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="alive"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=side):
+            block(x).backward(dy)
+    del alive
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        block(x).backward(dy)
+    for p in block.parameters():
+        p.grad.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p.grad, w) for p, w in zip(block.parameters(), want)) and b2.b2_device_status() == 0
