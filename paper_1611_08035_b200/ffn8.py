@@ -100,7 +100,7 @@ class _FeedForward8(torch.autograd.Function):
                 dz = torch.empty(t, f, dtype=torch.bfloat16, device=device) if need_w1 or need_b1 else None
                 zq, zs = _empty8(t, f, device) if first else (None, None)
                 product_act(q2, s2, "N", dq, ds, f, t, d, ctx.act | b2.ACT_GRADIENT, z=z, c=dz, q=zq, s=zs)
-                if need_b1:
+                if need_b1:  # sums of dz as it was stored: half a step of bf16 in each of t terms, to either side; unrounded ones would have to be added up in the product's epilogue
                     db1 = f32(f)
                     activation_backward(b2.ACT_NONE, dz, db=db1)
                 if need_w1:
