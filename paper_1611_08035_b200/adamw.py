@@ -82,9 +82,10 @@ class AdamW(torch.optim.Optimizer):
             for p in params:
                 if p.grad.is_sparse:
                     raise RuntimeError("AdamW does not take sparse gradients")
-                if self.state[p] and any(self.state[p][k].device != p.device for k in STATES if k in self.state[p]):
+                st = self.state.get(p, {})  # nothing is made of a step that is refused
+                if any(st[k].device != p.device for k in STATES if k in st):
                     raise RuntimeError(f"a parameter is on {p.device}, its states are not: load them again after it was moved")
-                if capturing(p) and not (group["capturable"] and isinstance(self.state[p].get("step"), torch.Tensor) and isinstance(group["lr"], torch.Tensor)
+                if capturing(p) and not (group["capturable"] and isinstance(st.get("step"), torch.Tensor) and isinstance(group["lr"], torch.Tensor)
                                          and group["lr"].device.type == p.device.type):
                     raise RuntimeError("a captured step is a capturable=True group's that has made one before, without the capture: its states' first values and its numbers would be a replay's")
         for number, (group, params) in enumerate(zip(self.param_groups, with_grads)):
@@ -134,7 +135,7 @@ class AdamW(torch.optim.Optimizer):
         for g, old in zip(self.param_groups, state_dict["param_groups"]):
             of_group = g.pop("step_device", None)  # where capturable groups once counted, for every parameter
             for i, p in zip(old["params"], g["params"]):
-                if i in saved:
+                if saved.get(i):
                     self.state[p].update({k: saved[i][k].to(p.device, copy=True) for k in STATES if k in saved[i]})
                     self.state[p]["step"] = max(map(int, of_group.values())) if of_group else int(saved[i].get("step", 0))
                     if isinstance(g["lr"], torch.Tensor) and g["capturable"]:

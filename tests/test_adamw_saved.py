@@ -68,3 +68,18 @@ def test_the_learning_rate_goes_to_the_device(calls, monkeypatch):  # noqa: F811
     monkeypatch.setattr(torch.Tensor, "to", (lambda to: lambda x, *a, **k: (moved.append(a), torch.zeros(()))[1] if x.device.type == "meta" else to(x, *a, **k))(torch.Tensor.to))
     opt.load_state_dict(saved)
     assert moved and opt.param_groups[0]["lr"].device.type == "cpu"
+
+
+def test_a_refused_step_leaves_nothing_to_save(calls):  # noqa: F811
+    params, opt = make()
+    go(opt, params[:1])
+    params[0].grad, params[1].grad = torch.ones(5000), torch.ones(5000).to_sparse()
+    with pytest.raises(RuntimeError):
+        opt.step()
+    saved = opt.state_dict()
+    assert list(saved["state"]) == [0]
+    saved["state"][1] = {}  # as an optimiser that looked at what is not there had it
+    others, other = make()
+    other.load_state_dict(saved)
+    go(other, others)
+    assert sorted(calls[1:]) == [(1, 1), (1, 2)] and set(other.state[others[1]]) == {"step", "m", "v", "sm", "sv"}
