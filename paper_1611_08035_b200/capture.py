@@ -81,12 +81,17 @@ class AutogradGraphs(list):
     What reaches a parameter's gradient goes to the stream where the oldest living graph met the parameter first.  A capture can take another stream in, but not the default one: there it ends
     with an error in the middle of the backward pass, or takes the process with it.  So such a pass is refused before it begins."""
 
+    _most = 32  # entries before those that are gone are dropped
+
     def elsewhere(self, stream: int) -> list:
         """The nodes of those that were made on other streams."""
         return [node for node in (g() for g, s in self if s != stream) if node is not None]
 
     def add(self, node, stream: int) -> None:
-        self[:] = [g for g in self if g[0]() is not None] + [(weakref.ref(node), stream)]
+        if len(self) >= self._most:  # a module that one pass calls a thousand times does not look through all of them every time
+            self[:] = [g for g in self if g[0]() is not None]
+            self._most = max(32, 2 * len(self))
+        self.append((weakref.ref(node), stream))
 
     def refuse(self, node, stream: int) -> None:
         """In a captured backward pass through a node."""

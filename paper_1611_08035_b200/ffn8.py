@@ -138,6 +138,10 @@ class FeedForward8(torch.nn.Module):
     def __getstate__(self):
         return super().__getstate__() | {"_quantised": {}, "_captured": [], "_graphs": AutogradGraphs()}
 
+    def __setstate__(self, state):  # also one that was saved before there were all of these
+        super().__setstate__(state)
+        self._quantised, self._captured, self._graphs = {}, [], AutogradGraphs()
+
     @staticmethod
     def _state(weight):
         return weight, None if weight.is_inference() else weight._version, weight.data_ptr()

@@ -161,6 +161,10 @@ class NormLinear8(torch.nn.Module):
     def __getstate__(self):
         return super().__getstate__() | {"_quantised": None, "_captured": [], "_graphs": AutogradGraphs()}
 
+    def __setstate__(self, state):  # also one that was saved before there were all of these
+        super().__setstate__(state)
+        self._quantised, self._captured, self._graphs = None, [], AutogradGraphs()
+
     def _let_go(self) -> None:
         """Of what was kept for graphs that are gone."""
         self._captured = [c for c in self._captured if not c[1].gone()]
