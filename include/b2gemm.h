@@ -522,12 +522,12 @@ int b2_wgrad_f8(int64_t m, int64_t n, int64_t k, float alpha, const void* Q, int
  *   R        m x n, or NULL.  R may be C (with its leading dimension).  In the gradient form Z may be C, too.
  *   C        m x n: where c is stored, or NULL where Q is given.
  *            No other two of Z, R, C, Q, S and the operands may overlap where one of them is written.
- *   type     of Z, R and C (B2_TYPE_*; it does not matter where there are none).
+ *   type     of Z, R and C (B2_TYPE_*; where there are none, what the sums' accumulation goes by).
  *   Q, S     c as e4m3 numbers m x n with a scale byte for each 128 features of a column (ceil(m/128) x n), by the quantisation rule above: what
  *            b2_gemm_f8 takes as an operand with block 1 and b2_wgrad_f8 as its activation.  Or NULL.
  * Everything is computed in fp32 from the unrounded sum; z and c are rounded once each, when they are stored, and Q is the rounding of the unrounded c.
  * The first eighteen arguments, their numbers, the workspace (b2_gemm_f8_workspace_bytes), limits, and how the sums are accumulated are b2_gemm_f8's,
- * but that they are those of a product in fp32 where Q is wanted: Q does not depend on type, nor on what else is stored.
+ * but that the tensor core sums over at most 4096 of k where Q is wanted and type is bf16 (so that type has its say in Q, in the numbers next to a border of two e4m3 ones).
  * alpha == 0 or k == 0 makes the sum 0 and reads neither A nor B.
  * Arguments: .. 18 as b2_gemm_f8, act 19, bias 20, Z 21, ldz 22, R 23, ldr 24, C 25, ldc 26, type 27, Q 28, ldq 29, S 30, lds 31.  A leading dimension whose
  * matrix is NULL is not looked at.

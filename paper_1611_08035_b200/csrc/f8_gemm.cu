@@ -241,7 +241,7 @@ int f8_run(const F8Product& p, const OUT& out, int type_c, void* workspace, size
   F8ArgsOf<OUT> a = {};
   a.out = out;
   a.kb = (int)blocks_of(k, kF8Block);
-  a.chunk = type_c == B2_TYPE_F32 || f8_whole_blocks(out) ? chunk_blocks<float>() : chunk_blocks<__nv_bfloat16>();
+  a.chunk = type_c == B2_TYPE_F32 ? chunk_blocks<float>() : f8_whole_blocks(out) ? kChunkOfQ : chunk_blocks<__nv_bfloat16>();
   a.status = status_pointer();
   if (!a.status) return B2_ERR_LAUNCH;
   auto scale = [](const void* s, bool blocks_contiguous, int64_t ld, int block, int type) {
