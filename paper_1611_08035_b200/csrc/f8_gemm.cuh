@@ -54,9 +54,10 @@ struct F8Operand {
 // sums over 65536 (6e-5), and without a limit 1.4e-3 at k = 4194304.
 template <typename TC>
 __host__ __device__ constexpr int chunk_blocks() { return sizeof(TC) == 4 ? 16 : 512; }
-// Results in 8 bits beside bf16 ones: a sum that is off by 6e-5 puts one number in a thousand on the other side of a border.  32 blocks (4096) keep it to some 4e-6 for every k; the 16 of
-// fp32 halve that, but a tile's second chunk then waits for the warps that are still busy with the tile before (up projection 16384 x 8192 x 4096 418 -> 482 us, gradient of gelu 490 -> 590), and
-// against 64 bits q is off by 4.7e-5 instead of 4.9e-5 there.
+// Results in 8 bits beside bf16 matrices: a sum that is off by 6e-5 (65536 at once) puts one number in a thousand on the other side of a border of two e4m3 numbers.  32 blocks (4096) bound that for
+// every k: for 16384 x 8192 x 4096 q is 1.3e-4 of its norm from the 64-bit product's (the rounding itself moves it by 2.6e-2); the 16 blocks of fp32 would bring it to the 9e-5 of plain fp32 sums.
+// They cost more than that gives: a tile's second chunk waits for the warps that are still busy with the tile before (up projection, seconds of it, 528 -> 578 us, gradient of gelu 606 -> 660, in a
+// burst 420 -> 490 and 490 -> 600).
 constexpr int kChunkOfQ = 32;
 template <typename TC, typename OUT>
 __host__ __device__ int chunk_blocks_of(const F8ArgsOf<OUT>& a) {
