@@ -202,7 +202,7 @@ __device__ __forceinline__ void adam_pieces(const AdamTensor& t, const AdamStep&
 __device__ __forceinline__ Two sum_rn(Two x, Two y) { return {__fadd_rn(x.a, y.a), __fadd_rn(x.b, y.b)}; }
 // Minus the square roots of -n, n <= 0, rounded to nearest: an approximation of the reciprocal root, and from it one Newton step on the root with the exact remainder (P.
 // Markstein, IBM Journal of Research and Development 34, 1990); all signs turned, so that none is in the way of the packed instructions.  0, and 2^-100 to the largest finite
-// number, give __fsqrt_rn's results: tried for every mantissa and both parities of the exponent.
+// number, give __fsqrt_rn's results: compared once on the GPU, every mantissa with the exponents 0, -2, 20, 98, -50 and -100 and the next ones.
 __device__ __forceinline__ float rsqrt_approx(float x) {
   float y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

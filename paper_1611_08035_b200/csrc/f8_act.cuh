@@ -334,9 +334,9 @@ __device__ __forceinline__ bool act_emit_halves(const F8ActOut& p, int64_t row0,
 // A thread has a whole block, 128 consecutive features of one token.  Two warps a scheduler have little to hide latencies behind, so that what they do is kept short and
 // nothing in it waits for memory: matrices pass through pieces of shared memory, 32 bytes of 32 rows each, swizzled so that the rows' owners read and write them
 // without conflicts.  Results leave by TMA (edges are the tensor maps', for columns of whole 16 bytes); what is read comes by cp.async, a piece ahead; the bias lies in shared memory.
-// Clocks of a tile for a warp, two on a scheduler: alpha and bias 2700, gelu 5500 (4100 of it the unit for exp and 1/x), its slope 8000, a result 3000, what is read 3000, the 8-bit
-// result 2300.  Not kept, all 8192 x 4096 x 256: staged both ways as act_emit_rows does it (with bias, gelu, Z and Q 107 us, now 59); R read by its rows' owners, 64 bytes a row (78 us, now 54); R and
-// Z by TMA, whose small loads wait behind the operands' large ones (1200 clocks a piece; gradient of gelu with C and Q 96 us, now 79); sixteen warps with 64 columns and 96 registers (86; and
+// Clocks of a tile for a warp, two on a scheduler: alpha and bias 2700, gelu 5500 (4100 of it the unit for exp and 1/x), its slope 8000 (measured before it was as exact where it is small, which is 2 % of the kernel's time), a result 3000, what is read 3000, the 8-bit
+// result 2300.  Not kept, all 8192 x 4096 x 256: staged both ways as act_emit_rows does it (with bias, gelu, Z and Q 107 us, now 60); R read by its rows' owners, 64 bytes a row (78 us, now 54); R and
+// Z by TMA, whose small loads wait behind the operands' large ones (1200 clocks a piece; gradient of gelu with C and Q 96 us, now 82); sixteen warps with 64 columns and 96 registers (86; and
 // the scales' and the issuing warps', left with 56 and 40, hold the tensor core up: C alone 16384 x 8192 x 4096 387 -> 481 us).
 constexpr int kActPiece = 32 * 32;
 constexpr int kActBias = kF8Block * 4;
