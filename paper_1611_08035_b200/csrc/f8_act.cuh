@@ -94,7 +94,7 @@ __device__ __forceinline__ void act_rows_out(T* M, int64_t ld, bool vec, int64_t
         }
       }
     }
-  } else {  // columns that start anywhere: neighbouring lanes, neighbouring elements.  Tested one by one everywhere, bf16 4097 x 4096 x 1024 took 228 us, now 103
+  } else {  // columns that start anywhere: neighbouring lanes, neighbouring elements.  Tested one by one everywhere, bf16 4097 x 4096 x 1024 took 228 us, now 108
     const int r0 = lane / L, e0 = lane % L;
     Bits* to = m + (row0 + r0) * ld + col + e0;
     const unsigned char* from = stage + r0 * kEmitPitch + e0 * (int)sizeof(T);
